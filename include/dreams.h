@@ -8,6 +8,8 @@
  *   dreams_tree_accept_sampled  acceptance at temperature tau > 0 (accept-or-resample down the tree)
  *   dreams_tree_accept_lm_head  greedy acceptance from final hidden states (LM head fused with the argmax)
  *   dreams_kv_commit         compaction of the accepted path's K/V into the cache
+ * The cache is one slab of slots per sequence and KV head, or pages of a pool that sequences share ("Paged cache" below:
+ * the attention of a tree and of a prompt over pages, the rows that go into them, and the tables' upkeep).
  *
  * Conventions shared by every entry point
  *   - Pointers named as "device" point to device memory the caller owns (allocated on the current HIP
@@ -453,6 +455,163 @@ dreams_status_t dreams_kv_commit(int32_t num_layers, int64_t layer_stride_elems,
                                  dreams_dtype_t dtype, void* k_cache, void* v_cache, const int32_t* kv_len_in,
                                  const int32_t* accept_path, const int32_t* accept_len, int32_t path_stride,
                                  int32_t* kv_len_out, hipStream_t stream);
+
+/*
+ * Paged cache.  A pool holds num_pages pages of page_size slots; per layer, k_pages and v_pages are
+ * [num_pages, Hkv, page_size, D], the pages page_stride elements apart (so that one buffer may hold a page's K and V side
+ * by side), each page dense.  Slot j of sequence b is row j % page_size of page page_table[b, j / page_size] (table:
+ * device [B, table_width] int32).  A sequence's table need only name the pages of the slots that a call reads or writes;
+ * entries past them may hold anything.  A named page outside [0, num_pages) is never accessed: attention reads another
+ * page of the pool in its place (results unspecified), writes of rows leave it out.
+ *   page_size   a power of two, 16 .. 32768 (DREAMS_ERR_UNSUPPORTED otherwise)
+ *   table_width * page_size <= 2^30 slots
+ * Offsets are 64-bit: a pool may be larger than 4 GiB.
+ */
+
+/*
+ * Attention over pages.
+ *   num_rows     T tree nodes (1..128) or N prompt rows per sequence, <= table_width * page_size
+ *   max_kv_len   host-side upper bound on every kv_len[b], used only to plan the work split; 0 means
+ *                table_width * page_size - num_rows.  0 <= max_kv_len <= table_width * page_size - num_rows.
+ *   num_splits   pieces of the key axis, 0: the library's choice.  Any value gives the same result up to rounding order.
+ *   window       0: every key is in sight.  W >= 1: a key at position p is in sight of a row at position P iff P - p < W
+ *   sinks        or p < sinks (the first tokens of a sequence that stay visible; >= 0, no effect without a window)
+ *   page_stride  elements from a page to the next, >= Hkv * page_size * D; 0 means just that
+ * Other fields as in dreams_attn_desc_t.
+ */
+typedef struct {
+  int32_t batch;
+  int32_t num_q_heads;
+  int32_t num_kv_heads;
+  int32_t head_dim;
+  int32_t num_rows;
+  int32_t num_pages;
+  int32_t page_size;
+  int32_t table_width;
+  int32_t max_kv_len;
+  int32_t num_splits;
+  int32_t window;
+  int32_t sinks;
+  dreams_dtype_t dtype;
+  float scale;
+  int64_t page_stride;
+} dreams_paged_desc_t;
+
+/* Bytes of workspace dreams_paged_verify_attn / dreams_paged_prompt_attn need for `desc` on the current device (0 if
+ * none: then the call accepts a NULL workspace). */
+dreams_status_t dreams_paged_verify_attn_workspace_size(const dreams_paged_desc_t* desc, size_t* bytes);
+dreams_status_t dreams_paged_prompt_attn_workspace_size(const dreams_paged_desc_t* desc, size_t* bytes);
+
+/*
+ * dreams_paged_verify_attn -- dreams_tree_verify_attn over a paged cache, with an optional sliding window: for every
+ * sequence b, query head h and tree node i, softmax attention over the prefix slots 0 .. L_b-1 and the slots L_b + n of
+ * the nodes n that are i or its ancestors (the caller has written the nodes' K/V there, dreams_paged_append), of these
+ * the ones in sight.  The position of prefix slot j is j, that of node n is L_b + depth(n).  T = 1 is a decode step.
+ *   q            device [B, Hq, T, D]
+ *   k_pages, v_pages, page_table: see "Paged cache"
+ *   kv_len       device [B] int32     L_b, clamped into [0, table_width * page_size - T]
+ *   parent       device [B, T] int32  as for dreams_tree_verify_attn (an entry breaking the rules ends that node's walk,
+ *                                     and its depth); may be NULL if tree_mask is given and window is 0
+ *   tree_mask    device [B, T, ceil(T/64)] uint64 or NULL: bit n of row i set <=> node n is visible to node i (if in
+ *                                     sight; the window needs parent for the depths)
+ *   out          device [B, Hq, T, D] same dtype as q;  lse: device [B, Hq, T] float or NULL
+ * A row that sees nothing (a mask without a prefix in sight) gives out = 0 and lse = -inf.  Values in slots that no row
+ * sees do not matter (NaN and infinities included).  Arithmetic and workspace as for dreams_tree_verify_attn.
+ */
+dreams_status_t dreams_paged_verify_attn(const dreams_paged_desc_t* desc, const void* q, const void* k_pages,
+                                         const void* v_pages, const int32_t* page_table, const int32_t* kv_len,
+                                         const int32_t* parent, const uint64_t* tree_mask, void* out, float* lse,
+                                         void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * dreams_paged_prompt_attn -- the attention of a prompt's rows (or of a piece of a prompt behind kv_len[b] cached slots)
+ * over a paged cache that holds their K/V already: row i of sequence b is at position L_b + i and sees the slots
+ * 0 .. L_b + i in sight.
+ *   q          device [B, Hq, N, D]
+ *   kv_len     device [B] int32   L_b, slots before the rows' own; clamped into [0, table_width * page_size - n_b]
+ *   row_len    device [B] int32   n_b, live rows (clamped into [0, N]), or NULL: N each
+ *   out, lse   as above; rows i >= n_b get out = 0 and lse = -inf
+ */
+dreams_status_t dreams_paged_prompt_attn(const dreams_paged_desc_t* desc, const void* q, const void* k_pages,
+                                         const void* v_pages, const int32_t* page_table, const int32_t* kv_len,
+                                         const int32_t* row_len, void* out, float* lse, void* workspace,
+                                         size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * A pool's geometry for the calls that write it or keep its tables.  layer_stride and page_stride are in elements, 0
+ * means dense (page_stride Hkv * page_size * D, layer_stride num_pages * page_stride); both times the element size must be
+ * multiples of 16 bytes, as must head_dim times it (<= 512 bytes).
+ * dreams_pages_reserve and dreams_pages_release read only batch, num_pages, page_size and table_width.
+ */
+typedef struct {
+  int32_t num_layers;
+  int32_t batch;         /* rows of the page table */
+  int32_t num_kv_heads;
+  int32_t head_dim;
+  int32_t num_pages;
+  int32_t page_size;
+  int32_t table_width;
+  dreams_dtype_t dtype;
+  int64_t layer_stride;
+  int64_t page_stride;
+} dreams_page_pool_t;
+
+/*
+ * dreams_paged_append -- new rows into their slots, bit for bit: for every layer, KV head and i < n_b, slot
+ * kv_len[b] + i of sequence b receives K and V row (layer, b, head, i) of k_new and v_new.  kv_len is not changed.  Rows
+ * past the table or on pages outside the pool, and sequences with kv_len[b] < 0, are left out.
+ *   k_new, v_new   device, num_rows rows a sequence; strides[4] (host): elements between layers, sequences, KV heads and
+ *                  rows (so [NL, B, Hkv, N, D] and [NL, B, N, Hkv, D] both serve), multiples of 16 bytes; rows dense
+ *   row_len        device [B] int32 n_b (at most num_rows), or NULL: num_rows each
+ */
+dreams_status_t dreams_paged_append(const dreams_page_pool_t* pool, const void* k_new, const void* v_new,
+                                    int32_t num_rows, const int64_t* strides, const int32_t* page_table,
+                                    const int32_t* kv_len, const int32_t* row_len, void* k_pages, void* v_pages,
+                                    hipStream_t stream);
+
+/* dreams_paged_kv_commit -- dreams_kv_commit over pages: slot kv_len_in[b] + k receives slot kv_len_in[b] +
+ * accept_path[b,k] for k = 0 .. accept_len[b], in every layer and KV head; kv_len_out[b] = kv_len_in[b] + accept_len[b] + 1.
+ * Arguments and skipped entries as there (an entry whose slot the table does not cover is skipped too). */
+dreams_status_t dreams_paged_kv_commit(const dreams_page_pool_t* pool, void* k_pages, void* v_pages,
+                                       const int32_t* page_table, const int32_t* kv_len_in, const int32_t* accept_path,
+                                       const int32_t* accept_len, int32_t path_stride, int32_t* kv_len_out,
+                                       hipStream_t stream);
+
+/*
+ * Page tables.  page_count[b] is the number of pages that sequence b holds, the first entries of its row; refcount[p] the
+ * number of sequences that hold page p, 0 marking it free (device int32 [B] and [num_pages]; a new pool is all zeros).
+ * Pages are taken lowest number first and the calls read nothing but the state before them, so that the same calls
+ * always give the same tables.  Limits: num_pages <= DREAMS_PAGES_MAX, batch and list lengths <=
+ * DREAMS_PAGES_MAX_SEQUENCES, batch * table_width < 2^31 (DREAMS_ERR_UNSUPPORTED otherwise).  Calls on one pool are
+ * ordered by the caller (one stream, or synchronised ones).
+ *
+ * Pages are shared by forks only, and only pages filled to the end are: as long as kv_len[b] is only raised (and lowered by
+ * dreams_pages_release), the slots from kv_len[b] on are the sequence's own.
+ */
+#define DREAMS_PAGES_MAX 524288
+#define DREAMS_PAGES_MAX_SEQUENCES 4096
+
+/* dreams_pages_reserve -- room: every sequence b, in order, that holds fewer than ceil(want_len[b] / page_size) pages takes
+ * as many as it lacks, if that many are free by then (all or none) and its row is wide enough.  granted[b] (out): 1 if the
+ * sequence holds want_len[b] slots, else 0 and nothing of it changes.  want_len[b] <= 0 asks for nothing. */
+dreams_status_t dreams_pages_reserve(const dreams_page_pool_t* pool, int32_t* page_table, int32_t* page_count,
+                                     int32_t* refcount, const int32_t* want_len, int32_t* granted, hipStream_t stream);
+
+/* dreams_pages_fork -- copies of sequences: for i < count, sequence dst[i] becomes a copy of sequence src[i], sharing its
+ * pages filled to the end and taking a page of its own (lowest free, pairs in order) for the copied rows of a partly filled
+ * one; kv_len[dst[i]] = kv_len[src[i]].  granted[i] (out): 1, or 0 and nothing changes: dst[i] holds pages or was named
+ * before in dst, dst[i] = src[i], an index is outside the table, src[i]'s pages do not cover its kv_len, or no page is free.
+ * Sources are read as they are before the call. */
+dreams_status_t dreams_pages_fork(const dreams_page_pool_t* pool, void* k_pages, void* v_pages, int32_t* page_table,
+                                  int32_t* page_count, int32_t* kv_len, int32_t* refcount, int32_t count,
+                                  const int32_t* src, const int32_t* dst, int32_t* granted, hipStream_t stream);
+
+/* dreams_pages_release -- sequences seqs[0 .. count-1] give up their pages: all of them (trim 0; kv_len becomes 0), or those
+ * past the ones that kv_len slots need (trim 1; kv_len stays).  Their entries become -1.  An index outside the table is
+ * skipped, one named again too. */
+dreams_status_t dreams_pages_release(const dreams_page_pool_t* pool, int32_t* page_table, int32_t* page_count,
+                                     int32_t* kv_len, int32_t* refcount, int32_t count, const int32_t* seqs, int32_t trim,
+                                     hipStream_t stream);
 
 /* Static description of a status code. */
 const char* dreams_status_string(dreams_status_t status);

@@ -1160,6 +1160,409 @@ dreams_status_t dreams_kv_commit(int32_t num_layers, int64_t layer_stride_elems,
   return ok();
 }
 
+// ----------------------------------------------------------------------------------------- paged cache
+namespace {
+
+static_assert(kPagesMaxPages == DREAMS_PAGES_MAX && kPagesMaxSeqs == DREAMS_PAGES_MAX_SEQUENCES, "page table limits");
+
+dreams_status_t check_pages(int32_t num_pages, int32_t page_size, int32_t table_width) {
+  if (num_pages < 1) return fail(DREAMS_ERR_INVALID_ARG, "num_pages = %d < 1", num_pages);
+  if (page_size < 1 || table_width < 1)
+    return fail(DREAMS_ERR_INVALID_ARG, "page_size = %d and table_width = %d must be >= 1", page_size, table_width);
+  if (page_size < kPagedMinPage || page_size > kPagedMaxPage || (page_size & (page_size - 1)) != 0)
+    return fail(DREAMS_ERR_UNSUPPORTED, "page_size = %d is not a power of two in [%d, %d]", page_size, kPagedMinPage,
+                kPagedMaxPage);
+  if ((long long)table_width * page_size > kPagedMaxSlots)
+    return fail(DREAMS_ERR_UNSUPPORTED, "table_width * page_size = %lld slots exceed %d",
+                (long long)table_width * page_size, kPagedMaxSlots);
+  return DREAMS_OK;
+}
+
+int page_shift_of(int page_size) { return __builtin_ctz((unsigned)page_size); }
+
+// A page stride (elements; 0: dense) against the page it has to hold and 16-byte alignment.
+dreams_status_t check_page_stride(int64_t stride, int64_t page_elems, int elem, int32_t num_pages) {
+  if (stride == 0) return DREAMS_OK;
+  if (stride < page_elems) return fail(DREAMS_ERR_INVALID_ARG, "page_stride = %lld is smaller than a page (%lld elements)",
+                                       (long long)stride, (long long)page_elems);
+  if (stride > (int64_t)1 << 48 || stride * elem % 16 != 0)
+    return fail(DREAMS_ERR_INVALID_ARG, "page_stride = %lld must be a multiple of 16 bytes", (long long)stride);
+  if (stride > ((int64_t)1 << 60) / num_pages) return fail(DREAMS_ERR_INVALID_ARG, "page_stride = %lld is too large",
+                                                           (long long)stride);
+  return DREAMS_OK;
+}
+
+dreams_status_t check_paged_desc(const dreams_paged_desc_t* d, bool prompt) {
+  if (!d) return fail(DREAMS_ERR_INVALID_ARG, "desc is NULL");
+  if (d->batch < 0) return fail(DREAMS_ERR_INVALID_ARG, "batch = %d < 0", d->batch);
+  if (d->num_q_heads < 1 || d->num_kv_heads < 1 || d->num_q_heads % d->num_kv_heads != 0)
+    return fail(DREAMS_ERR_INVALID_ARG, "num_q_heads = %d must be a positive multiple of num_kv_heads = %d",
+                d->num_q_heads, d->num_kv_heads);
+  if (d->dtype != DREAMS_BF16 && d->dtype != DREAMS_F32)
+    return fail(DREAMS_ERR_INVALID_ARG, "dtype = %d is not DREAMS_BF16 or DREAMS_F32", (int)d->dtype);
+  if (d->head_dim != 64 && d->head_dim != 128)
+    return fail(DREAMS_ERR_UNSUPPORTED, "head_dim = %d (supported: 64, 128)", d->head_dim);
+  dreams_status_t st = check_pages(d->num_pages, d->page_size, d->table_width);
+  if (st != DREAMS_OK) return st;
+  const int slots = d->table_width * d->page_size;
+  if (d->num_rows < 1 || (!prompt && d->num_rows > kMaxNodes) || d->num_rows > slots)
+    return fail(DREAMS_ERR_INVALID_ARG, "num_rows = %d outside [1, %d]", d->num_rows,
+                !prompt && kMaxNodes < slots ? kMaxNodes : slots);
+  if (d->max_kv_len < 0 || d->max_kv_len > slots - d->num_rows)
+    return fail(DREAMS_ERR_INVALID_ARG, "max_kv_len = %d outside [0, table_width * page_size - num_rows = %d]",
+                d->max_kv_len, slots - d->num_rows);
+  if (d->num_splits < 0 || d->num_splits > kMaxSplitsRequest)
+    return fail(DREAMS_ERR_INVALID_ARG, "num_splits = %d outside [0, %d]", d->num_splits, kMaxSplitsRequest);
+  if (d->window < 0 || d->sinks < 0)
+    return fail(DREAMS_ERR_INVALID_ARG, "window = %d and sinks = %d must be >= 0", d->window, d->sinks);
+  if (!isfinite(d->scale)) return fail(DREAMS_ERR_INVALID_ARG, "scale is not finite");
+  const int64_t page = (int64_t)d->num_kv_heads * d->page_size * d->head_dim;
+  st = check_page_stride(d->page_stride, page, d->dtype == DREAMS_BF16 ? 2 : 4, d->num_pages);
+  if (st != DREAMS_OK) return st;
+  if ((long long)d->batch * d->num_q_heads > 0x7fffffffLL / d->num_rows)
+    return fail(DREAMS_ERR_UNSUPPORTED, "problem too large");
+  return DREAMS_OK;
+}
+
+dreams_status_t check_paged_tensors(const dreams_paged_desc_t* d, const void* q, const void* k_pages,
+                                    const void* v_pages, const int32_t* page_table, const int32_t* kv_len, const void* out,
+                                    const float* lse) {
+  if (!q || !k_pages || !v_pages || !page_table || !kv_len || !out)
+    return fail(DREAMS_ERR_INVALID_ARG, "q, k_pages, v_pages, page_table, kv_len and out must not be NULL");
+  if (!aligned(q, 16) || !aligned(k_pages, 16) || !aligned(v_pages, 16) || !aligned(out, 16))
+    return fail(DREAMS_ERR_INVALID_ARG, "q, k_pages, v_pages and out must be 16-byte aligned");
+  if (!aligned(page_table, 4) || !aligned(kv_len, 4) || !aligned(lse, 4))
+    return fail(DREAMS_ERR_INVALID_ARG, "page_table, kv_len or lse is misaligned");
+  return DREAMS_OK;
+}
+
+PagedAttnArgs paged_args(const dreams_paged_desc_t* d, const void* q, const void* k_pages, const void* v_pages,
+                         const int32_t* page_table, const int32_t* kv_len, void* out, float* lse) {
+  PagedAttnArgs a{};
+  const int elem = d->dtype == DREAMS_BF16 ? 2 : 4;
+  a.q = q;
+  a.k = k_pages;
+  a.v = v_pages;
+  a.table = page_table;
+  a.kv_len = kv_len;
+  a.out = out;
+  a.lse = lse;
+  a.bf16 = d->dtype == DREAMS_BF16;
+  a.B = d->batch;
+  a.Hq = d->num_q_heads;
+  a.Hkv = d->num_kv_heads;
+  a.G = d->num_q_heads / d->num_kv_heads;
+  a.T = d->num_rows;
+  a.D = d->head_dim;
+  a.num_pages = d->num_pages;
+  a.page_shift = page_shift_of(d->page_size);
+  a.width = d->table_width;
+  a.capacity = d->table_width * d->page_size;
+  a.page_stride = (d->page_stride ? d->page_stride : (int64_t)d->num_kv_heads * d->page_size * d->head_dim) * elem;
+  a.window = d->window;
+  a.sinks = d->sinks;
+  a.scale_log2 = d->scale * 1.4426950408889634f;
+  return a;
+}
+
+}  // namespace
+
+dreams_status_t dreams_paged_verify_attn_workspace_size(const dreams_paged_desc_t* desc, size_t* bytes) {
+  if (!bytes) return fail(DREAMS_ERR_INVALID_ARG, "bytes is NULL");
+  dreams_status_t st = check_paged_desc(desc, false);
+  if (st != DREAMS_OK) return st;
+  *bytes = 0;
+  return ok();
+}
+
+dreams_status_t dreams_paged_prompt_attn_workspace_size(const dreams_paged_desc_t* desc, size_t* bytes) {
+  if (!bytes) return fail(DREAMS_ERR_INVALID_ARG, "bytes is NULL");
+  dreams_status_t st = check_paged_desc(desc, true);
+  if (st != DREAMS_OK) return st;
+  *bytes = 0;
+  return ok();
+}
+
+dreams_status_t dreams_paged_verify_attn(const dreams_paged_desc_t* desc, const void* q, const void* k_pages,
+                                         const void* v_pages, const int32_t* page_table, const int32_t* kv_len,
+                                         const int32_t* parent, const uint64_t* tree_mask, void* out, float* lse,
+                                         void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  dreams_status_t st = check_paged_desc(desc, false);
+  if (st != DREAMS_OK) return st;
+  if (desc->batch == 0) return ok();
+  st = check_paged_tensors(desc, q, k_pages, v_pages, page_table, kv_len, out, lse);
+  if (st != DREAMS_OK) return st;
+  if (!parent && !tree_mask) return fail(DREAMS_ERR_INVALID_ARG, "either parent or tree_mask must be given");
+  if (!parent && desc->window > 0)
+    return fail(DREAMS_ERR_INVALID_ARG, "a window needs parent: the nodes' positions follow from their depths");
+  if (!aligned(parent, 4) || !aligned(tree_mask, 8))
+    return fail(DREAMS_ERR_INVALID_ARG, "parent or tree_mask is misaligned");
+  PagedAttnArgs a = paged_args(desc, q, k_pages, v_pages, page_table, kv_len, out, lse);
+  a.parent = parent;
+  a.mask = tree_mask;
+  st = device_cus(&a.cus);
+  if (st != DREAMS_OK) return st;
+  hipError_t e = launch_paged_attn_f32(a, stream);
+  if (e != hipSuccess) return hip_fail(e, "paged tree attention launch");
+  return ok();
+}
+
+dreams_status_t dreams_paged_prompt_attn(const dreams_paged_desc_t* desc, const void* q, const void* k_pages,
+                                         const void* v_pages, const int32_t* page_table, const int32_t* kv_len,
+                                         const int32_t* row_len, void* out, float* lse, void* workspace,
+                                         size_t workspace_bytes, hipStream_t stream) {
+  dreams_status_t st = check_paged_desc(desc, true);
+  if (st != DREAMS_OK) return st;
+  if (desc->batch == 0) return ok();
+  st = check_paged_tensors(desc, q, k_pages, v_pages, page_table, kv_len, out, lse);
+  if (st != DREAMS_OK) return st;
+  if (!aligned(row_len, 4)) return fail(DREAMS_ERR_INVALID_ARG, "row_len is misaligned");
+  PagedAttnArgs a = paged_args(desc, q, k_pages, v_pages, page_table, kv_len, out, lse);
+  a.row_len = row_len;
+  a.prompt = 1;
+  st = device_cus(&a.cus);
+  if (st != DREAMS_OK) return st;
+  hipError_t e = launch_paged_attn_f32(a, stream);
+  if (e != hipSuccess) return hip_fail(e, "paged prompt attention launch");
+  return ok();
+}
+
+namespace {
+
+dreams_status_t check_pool(const dreams_page_pool_t* p, int* elem) {
+  if (!p) return fail(DREAMS_ERR_INVALID_ARG, "pool is NULL");
+  if (p->batch < 0) return fail(DREAMS_ERR_INVALID_ARG, "batch = %d < 0", p->batch);
+  if (p->num_layers < 1 || p->num_kv_heads < 1 || p->head_dim < 1)
+    return fail(DREAMS_ERR_INVALID_ARG, "num_layers = %d, num_kv_heads = %d and head_dim = %d must be >= 1",
+                p->num_layers, p->num_kv_heads, p->head_dim);
+  if (p->dtype != DREAMS_BF16 && p->dtype != DREAMS_F32)
+    return fail(DREAMS_ERR_INVALID_ARG, "dtype = %d is not DREAMS_BF16 or DREAMS_F32", (int)p->dtype);
+  dreams_status_t st = check_pages(p->num_pages, p->page_size, p->table_width);
+  if (st != DREAMS_OK) return st;
+  *elem = p->dtype == DREAMS_BF16 ? 2 : 4;
+  const long long row_bytes = (long long)p->head_dim * *elem;
+  if (row_bytes % 16 != 0 || row_bytes > kCommitMaxRowBytes)
+    return fail(DREAMS_ERR_UNSUPPORTED, "head_dim * element size = %lld bytes (must be a multiple of 16, <= %d)",
+                row_bytes, kCommitMaxRowBytes);
+  const int64_t page = (int64_t)p->num_kv_heads * p->page_size * p->head_dim;
+  st = check_page_stride(p->page_stride, page, *elem, p->num_pages);
+  if (st != DREAMS_OK) return st;
+  if (p->layer_stride != 0 && p->num_layers > 1) {
+    const int64_t stride = p->page_stride ? p->page_stride : page;
+    if (p->layer_stride < stride * (p->num_pages - 1) + page || p->layer_stride > (int64_t)1 << 58 ||
+        p->layer_stride * *elem % 16 != 0)
+      return fail(DREAMS_ERR_INVALID_ARG, "layer_stride = %lld must hold a layer's pages and be a multiple of 16 bytes",
+                  (long long)p->layer_stride);
+  }
+  if (p->batch > 65535 || p->num_layers > 65535 ||
+      (long long)p->num_layers * p->num_kv_heads > 0x7fffffffLL / (p->batch > 0 ? p->batch : 1))
+    return fail(DREAMS_ERR_UNSUPPORTED, "problem too large");
+  return DREAMS_OK;
+}
+
+int64_t pool_page_stride(const dreams_page_pool_t* p) {
+  return p->page_stride ? p->page_stride : (int64_t)p->num_kv_heads * p->page_size * p->head_dim;
+}
+int64_t pool_layer_stride(const dreams_page_pool_t* p) {
+  return p->layer_stride ? p->layer_stride : pool_page_stride(p) * p->num_pages;
+}
+
+PagedRowsArgs rows_args(const dreams_page_pool_t* p, int elem, void* k_pages, void* v_pages, const int32_t* page_table,
+                        const int32_t* kv_len) {
+  PagedRowsArgs a{};
+  a.k = (char*)k_pages;
+  a.v = (char*)v_pages;
+  a.table = page_table;
+  a.kv_len = kv_len;
+  a.layer_stride = pool_layer_stride(p) * elem;
+  a.page_stride = pool_page_stride(p) * elem;
+  a.NL = p->num_layers;
+  a.B = p->batch;
+  a.Hkv = p->num_kv_heads;
+  a.num_pages = p->num_pages;
+  a.page_shift = page_shift_of(p->page_size);
+  a.width = p->table_width;
+  a.row_bytes = p->head_dim * elem;
+  return a;
+}
+
+}  // namespace
+
+dreams_status_t dreams_paged_append(const dreams_page_pool_t* pool, const void* k_new, const void* v_new,
+                                    int32_t num_rows, const int64_t* strides, const int32_t* page_table,
+                                    const int32_t* kv_len, const int32_t* row_len, void* k_pages, void* v_pages,
+                                    hipStream_t stream) {
+  int elem = 0;
+  dreams_status_t st = check_pool(pool, &elem);
+  if (st != DREAMS_OK) return st;
+  if (num_rows < 0) return fail(DREAMS_ERR_INVALID_ARG, "num_rows = %d < 0", num_rows);
+  if (!strides) return fail(DREAMS_ERR_INVALID_ARG, "strides is NULL");
+  const int32_t lengths[4] = {pool->num_layers, pool->batch, pool->num_kv_heads, num_rows};
+  for (int i = 0; i < 4; ++i)
+    if (lengths[i] > 1 && (strides[i] < 0 || strides[i] > (int64_t)1 << 48 || strides[i] * elem % 16 != 0))
+      return fail(DREAMS_ERR_INVALID_ARG, "strides[%d] = %lld must be a non-negative multiple of 16 bytes", i,
+                  (long long)strides[i]);
+  if ((long long)num_rows * pool->num_kv_heads / 4 > 0x7fffffffLL / (pool->head_dim * elem / 16))
+    return fail(DREAMS_ERR_UNSUPPORTED, "problem too large");
+  if (pool->batch == 0 || num_rows == 0) return ok();
+  if (!k_new || !v_new || !page_table || !kv_len || !k_pages || !v_pages)
+    return fail(DREAMS_ERR_INVALID_ARG, "k_new, v_new, page_table, kv_len, k_pages and v_pages must not be NULL");
+  if (!aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(k_pages, 16) || !aligned(v_pages, 16))
+    return fail(DREAMS_ERR_INVALID_ARG, "k_new, v_new, k_pages and v_pages must be 16-byte aligned");
+  if (!aligned(page_table, 4) || !aligned(kv_len, 4) || !aligned(row_len, 4))
+    return fail(DREAMS_ERR_INVALID_ARG, "an int32 argument is not 4-byte aligned");
+  PagedRowsArgs a = rows_args(pool, elem, k_pages, v_pages, page_table, kv_len);
+  a.k_new = (const char*)k_new;
+  a.v_new = (const char*)v_new;
+  a.row_len = row_len;
+  a.N = num_rows;
+  // (a stride along an axis of one entry is not used)
+  a.new_layer = lengths[0] > 1 ? strides[0] * elem : 0;
+  a.new_batch = lengths[1] > 1 ? strides[1] * elem : 0;
+  a.new_head = lengths[2] > 1 ? strides[2] * elem : 0;
+  a.new_row = lengths[3] > 1 ? strides[3] * elem : 0;
+  hipError_t e = launch_paged_append(a, stream);
+  if (e != hipSuccess) return hip_fail(e, "paged append launch");
+  return ok();
+}
+
+dreams_status_t dreams_paged_kv_commit(const dreams_page_pool_t* pool, void* k_pages, void* v_pages,
+                                       const int32_t* page_table, const int32_t* kv_len_in, const int32_t* accept_path,
+                                       const int32_t* accept_len, int32_t path_stride, int32_t* kv_len_out,
+                                       hipStream_t stream) {
+  int elem = 0;
+  dreams_status_t st = check_pool(pool, &elem);
+  if (st != DREAMS_OK) return st;
+  if (path_stride < 1) return fail(DREAMS_ERR_INVALID_ARG, "path_stride = %d < 1", path_stride);
+  if (pool->batch == 0) return ok();
+  if (!k_pages || !v_pages || !page_table || !kv_len_in || !accept_path || !accept_len || !kv_len_out)
+    return fail(DREAMS_ERR_INVALID_ARG, "page, table, length and path pointers must not be NULL");
+  if (!aligned(k_pages, 16) || !aligned(v_pages, 16))
+    return fail(DREAMS_ERR_INVALID_ARG, "k_pages and v_pages must be 16-byte aligned");
+  if (!aligned(page_table, 4) || !aligned(kv_len_in, 4) || !aligned(accept_path, 4) || !aligned(accept_len, 4) ||
+      !aligned(kv_len_out, 4))
+    return fail(DREAMS_ERR_INVALID_ARG, "an int32 argument is not 4-byte aligned");
+  if (overlap(kv_len_out, (size_t)pool->batch * 4, kv_len_in, (size_t)pool->batch * 4))
+    return fail(DREAMS_ERR_INVALID_ARG, "kv_len_out must not overlap kv_len_in");
+  PagedRowsArgs a = rows_args(pool, elem, k_pages, v_pages, page_table, kv_len_in);
+  a.path = accept_path;
+  a.accept_len = accept_len;
+  a.kv_len_out = kv_len_out;
+  a.path_stride = path_stride;
+  hipError_t e = launch_paged_commit(a, stream);
+  if (e != hipSuccess) return hip_fail(e, "paged commit launch");
+  return ok();
+}
+
+namespace {
+
+dreams_status_t check_tables(const dreams_page_pool_t* p, const int32_t* table, const int32_t* count,
+                             const int32_t* refcount) {
+  if (!p) return fail(DREAMS_ERR_INVALID_ARG, "pool is NULL");
+  if (p->batch < 0) return fail(DREAMS_ERR_INVALID_ARG, "batch = %d < 0", p->batch);
+  dreams_status_t st = check_pages(p->num_pages, p->page_size, p->table_width);
+  if (st != DREAMS_OK) return st;
+  if (p->num_pages > kPagesMaxPages || p->batch > kPagesMaxSeqs || (long long)p->batch * p->table_width > 0x7fffffffLL)
+    return fail(DREAMS_ERR_UNSUPPORTED, "num_pages = %d, batch = %d, table_width = %d (at most %d pages, %d sequences and "
+                "2^31 - 1 entries)", p->num_pages, p->batch, p->table_width, kPagesMaxPages, kPagesMaxSeqs);
+  if (p->batch == 0) return DREAMS_OK;
+  if (!table || !count || !refcount)
+    return fail(DREAMS_ERR_INVALID_ARG, "page_table, page_count and refcount must not be NULL");
+  if (!aligned(table, 4) || !aligned(count, 4) || !aligned(refcount, 4))
+    return fail(DREAMS_ERR_INVALID_ARG, "an int32 argument is not 4-byte aligned");
+  return DREAMS_OK;
+}
+
+dreams_status_t check_list(int32_t count, const int32_t* a, const int32_t* b) {
+  if (count < 0) return fail(DREAMS_ERR_INVALID_ARG, "count = %d < 0", count);
+  if (count > kPagesMaxSeqs) return fail(DREAMS_ERR_UNSUPPORTED, "count = %d exceeds %d", count, kPagesMaxSeqs);
+  if (count == 0) return DREAMS_OK;
+  if (!a || !b) return fail(DREAMS_ERR_INVALID_ARG, "the list of sequences must not be NULL");
+  if (!aligned(a, 4) || !aligned(b, 4)) return fail(DREAMS_ERR_INVALID_ARG, "an int32 argument is not 4-byte aligned");
+  return DREAMS_OK;
+}
+
+PagesArgs pages_args(const dreams_page_pool_t* p, int32_t* table, int32_t* count, int32_t* kv_len, int32_t* refcount) {
+  PagesArgs a{};
+  a.table = table;
+  a.count = count;
+  a.kv_len = kv_len;
+  a.refcount = refcount;
+  a.B = p->batch;
+  a.width = p->table_width;
+  a.num_pages = p->num_pages;
+  a.page_shift = page_shift_of(p->page_size);
+  return a;
+}
+
+}  // namespace
+
+dreams_status_t dreams_pages_reserve(const dreams_page_pool_t* pool, int32_t* page_table, int32_t* page_count,
+                                     int32_t* refcount, const int32_t* want_len, int32_t* granted, hipStream_t stream) {
+  dreams_status_t st = check_tables(pool, page_table, page_count, refcount);
+  if (st != DREAMS_OK) return st;
+  if (pool->batch == 0) return ok();
+  if (!want_len || !granted) return fail(DREAMS_ERR_INVALID_ARG, "want_len and granted must not be NULL");
+  if (!aligned(want_len, 4) || !aligned(granted, 4))
+    return fail(DREAMS_ERR_INVALID_ARG, "an int32 argument is not 4-byte aligned");
+  PagesArgs a = pages_args(pool, page_table, page_count, nullptr, refcount);
+  a.want = want_len;
+  a.granted = granted;
+  hipError_t e = launch_pages_reserve(a, stream);
+  if (e != hipSuccess) return hip_fail(e, "page reservation launch");
+  return ok();
+}
+
+dreams_status_t dreams_pages_fork(const dreams_page_pool_t* pool, void* k_pages, void* v_pages, int32_t* page_table,
+                                  int32_t* page_count, int32_t* kv_len, int32_t* refcount, int32_t count,
+                                  const int32_t* src, const int32_t* dst, int32_t* granted, hipStream_t stream) {
+  int elem = 0;
+  dreams_status_t st = check_pool(pool, &elem);
+  if (st == DREAMS_OK) st = check_tables(pool, page_table, page_count, refcount);
+  if (st == DREAMS_OK) st = check_list(count, src, dst);
+  if (st != DREAMS_OK) return st;
+  if (pool->batch == 0 || count == 0) return ok();
+  if (!k_pages || !v_pages || !kv_len || !granted)
+    return fail(DREAMS_ERR_INVALID_ARG, "k_pages, v_pages, kv_len and granted must not be NULL");
+  if (!aligned(k_pages, 16) || !aligned(v_pages, 16))
+    return fail(DREAMS_ERR_INVALID_ARG, "k_pages and v_pages must be 16-byte aligned");
+  if (!aligned(kv_len, 4) || !aligned(granted, 4))
+    return fail(DREAMS_ERR_INVALID_ARG, "an int32 argument is not 4-byte aligned");
+  PagesArgs a = pages_args(pool, page_table, page_count, kv_len, refcount);
+  a.src = src;
+  a.dst = dst;
+  a.n = count;
+  a.granted = granted;
+  a.k = (char*)k_pages;
+  a.v = (char*)v_pages;
+  a.layer_stride = pool_layer_stride(pool) * elem;
+  a.page_stride = pool_page_stride(pool) * elem;
+  a.NL = pool->num_layers;
+  a.Hkv = pool->num_kv_heads;
+  a.row_bytes = pool->head_dim * elem;
+  hipError_t e = launch_pages_fork(a, stream);
+  if (e != hipSuccess) return hip_fail(e, "page fork launch");
+  return ok();
+}
+
+dreams_status_t dreams_pages_release(const dreams_page_pool_t* pool, int32_t* page_table, int32_t* page_count,
+                                     int32_t* kv_len, int32_t* refcount, int32_t count, const int32_t* seqs, int32_t trim,
+                                     hipStream_t stream) {
+  dreams_status_t st = check_tables(pool, page_table, page_count, refcount);
+  if (st == DREAMS_OK) st = check_list(count, seqs, seqs);
+  if (st != DREAMS_OK) return st;
+  if (trim != 0 && trim != 1) return fail(DREAMS_ERR_INVALID_ARG, "trim = %d is not 0 or 1", trim);
+  if (pool->batch == 0 || count == 0) return ok();
+  if (!kv_len || !aligned(kv_len, 4)) return fail(DREAMS_ERR_INVALID_ARG, "kv_len must not be NULL, 4-byte aligned");
+  PagesArgs a = pages_args(pool, page_table, page_count, kv_len, refcount);
+  a.dst = seqs;
+  a.n = count;
+  a.trim = trim;
+  hipError_t e = launch_pages_release(a, stream);
+  if (e != hipSuccess) return hip_fail(e, "page release launch");
+  return ok();
+}
+
 const char* dreams_status_string(dreams_status_t status) {
   switch (status) {
     case DREAMS_OK: return "DREAMS_OK";

@@ -294,6 +294,83 @@ struct CommitArgs {
 
 hipError_t launch_kv_commit(const CommitArgs& a, hipStream_t stream);
 
+// ---------------------------------------------------------------------------------------- paged cache
+// A pool of pages holds the slots of every sequence: page p of KV head g is a [page_size, D] slab at
+// p * page_stride + g * page_size * D.  Slot j of sequence b is row j % page_size of page table[b, j / page_size].  Page
+// sizes are powers of two from 16, so that 16 slots from a multiple of 16 on lie in one page.
+constexpr int kPagedMinPage = 16, kPagedMaxPage = 1 << 15;
+constexpr int kPagedMaxSlots = 1 << 30;      // slots that a table row covers, at most
+constexpr int kPagesMaxPages = 1 << 19;      // pages of a pool that pages are taken from, at most (bits and ranks in LDS)
+constexpr int kPagesMaxSeqs = 4096;          // sequences of a table (or pairs of a fork) there, at most
+
+struct PagedAttnArgs {
+  const void* q;             // [B, Hq, T, D]
+  const void* k;             // [pages, Hkv, page_size, D], page_stride bytes a page
+  const void* v;
+  const int32_t* table;      // [B, width]
+  const int32_t* kv_len;     // [B] slots before the rows' own
+  const int32_t* row_len;    // [B] live rows (prompt), or nullptr: T
+  const int32_t* parent;     // [B, T] (tree)
+  const uint64_t* mask;      // [B, T, ceil(T/64)] or nullptr (tree)
+  void* out;                 // [B, Hq, T, D]
+  float* lse;                // [B, Hq, T] or nullptr
+  int prompt;                // 0: the rows are tree nodes (T <= 128); 1: consecutive positions
+  int bf16;
+  int B, Hq, Hkv, G, T, D;
+  int num_pages, page_shift, width;
+  int capacity;              // width << page_shift
+  int64_t page_stride;       // bytes from a page to the next
+  int window, sinks;         // window 0: every key in sight
+  float scale_log2;          // scale * log2(e)
+  int cus;
+};
+hipError_t launch_paged_attn_f32(const PagedAttnArgs& a, hipStream_t stream);
+
+struct PagedRowsArgs {
+  char* k;                   // [NL][pages, Hkv, page_size, row bytes]
+  char* v;
+  const int32_t* table;      // [B, width]
+  const int32_t* kv_len;     // [B]
+  int64_t layer_stride, page_stride;   // bytes
+  int NL, B, Hkv, num_pages, page_shift, width;
+  int row_bytes;             // D * element size, a multiple of 16, <= kCommitMaxRowBytes
+  // append: rows of [NL, B, Hkv, N] at these strides (bytes) go to slots kv_len[b] + 0 .. row_len[b]-1
+  const char* k_new;
+  const char* v_new;
+  const int32_t* row_len;    // [B] or nullptr: N
+  int64_t new_layer, new_batch, new_head, new_row;
+  int N;
+  // commit: slot kv_len[b] + path[b, k] moves to slot kv_len[b] + k, k = 0 .. accept_len[b]
+  const int32_t* path;
+  const int32_t* accept_len;
+  int32_t* kv_len_out;
+  int path_stride;
+};
+hipError_t launch_paged_append(const PagedRowsArgs& a, hipStream_t stream);
+hipError_t launch_paged_commit(const PagedRowsArgs& a, hipStream_t stream);
+
+struct PagesArgs {
+  int32_t* table;            // [B, width]
+  int32_t* count;            // [B] pages that a sequence holds
+  int32_t* kv_len;           // [B]
+  int32_t* refcount;         // [num_pages] sequences that hold a page; 0: free
+  int B, width, num_pages, page_shift;
+  const int32_t* want;       // reserve: [B] slots that a sequence is to hold
+  const int32_t* src;        // fork: [n] sequences ...
+  const int32_t* dst;        //       [n] ... that become copies of them;  release: [n] sequences
+  int n;
+  int trim;                  // release: keep the pages of slots 0 .. kv_len-1
+  int32_t* granted;          // [B] (reserve) or [n] (fork)
+  // fork: the pools
+  char* k;
+  char* v;
+  int64_t layer_stride, page_stride;
+  int NL, Hkv, row_bytes;
+};
+hipError_t launch_pages_reserve(const PagesArgs& a, hipStream_t stream);
+hipError_t launch_pages_fork(const PagesArgs& a, hipStream_t stream);
+hipError_t launch_pages_release(const PagesArgs& a, hipStream_t stream);
+
 // ------------------------------------------------------------------------------- stream read (measurement)
 hipError_t launch_stream_read(const void* src, size_t bytes, uint32_t* sink, hipStream_t stream);
 

@@ -31,6 +31,9 @@ EXPORTS = (
     "dreams_workspace_status", "dreams_tree_verify_attn_splits", "dreams_tree_verify_attn_noalloc",
     "dreams_set_wait_limit", "dreams_prefill_attn_stats", "dreams_prefill_attn_entropy_mean",
     "dreams_prefill_visual_importance", "dreams_prefill_visual_importance_workspace_size",
+    "dreams_paged_verify_attn", "dreams_paged_verify_attn_workspace_size", "dreams_paged_prompt_attn",
+    "dreams_paged_prompt_attn_workspace_size", "dreams_paged_append", "dreams_paged_kv_commit", "dreams_pages_reserve",
+    "dreams_pages_fork", "dreams_pages_release",
 )
 
 
@@ -51,6 +54,18 @@ class PrefillDesc(ctypes.Structure):
     _fields_ = [("batch", ctypes.c_int32), ("num_q_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32),
                 ("head_dim", ctypes.c_int32), ("num_rows", ctypes.c_int32), ("cache_capacity", ctypes.c_int32),
                 ("scale", ctypes.c_float)]
+
+
+class PagedDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "num_q_heads", "num_kv_heads", "head_dim", "num_rows", "num_pages",
+                                              "page_size", "table_width", "max_kv_len", "num_splits", "window", "sinks")]
+    _fields_ += [("dtype", ctypes.c_int), ("scale", ctypes.c_float), ("page_stride", ctypes.c_int64)]
+
+
+class PagePool(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("num_layers", "batch", "num_kv_heads", "head_dim", "num_pages", "page_size",
+                                              "table_width")]
+    _fields_ += [("dtype", ctypes.c_int), ("layer_stride", ctypes.c_int64), ("page_stride", ctypes.c_int64)]
 
 
 _lib = None
@@ -105,6 +120,16 @@ def lib():
                 L.dreams_prefill_attn_entropy_mean.argtypes = [I32, I32, I32, P, P, P, P]
                 L.dreams_prefill_visual_importance.argtypes = [ctypes.POINTER(PrefillDesc), P, P, P, P, I32, I32, P, P,
                                                                SZ, P]
+                PD, PP = ctypes.POINTER(PagedDesc), ctypes.POINTER(PagePool)
+                L.dreams_paged_verify_attn_workspace_size.argtypes = [PD, ctypes.POINTER(SZ)]
+                L.dreams_paged_prompt_attn_workspace_size.argtypes = [PD, ctypes.POINTER(SZ)]
+                L.dreams_paged_verify_attn.argtypes = [PD, P, P, P, P, P, P, P, P, P, P, SZ, P]
+                L.dreams_paged_prompt_attn.argtypes = [PD, P, P, P, P, P, P, P, P, P, SZ, P]
+                L.dreams_paged_append.argtypes = [PP, P, P, I32, ctypes.POINTER(ctypes.c_int64), P, P, P, P, P, P]
+                L.dreams_paged_kv_commit.argtypes = [PP, P, P, P, P, P, P, I32, P, P]
+                L.dreams_pages_reserve.argtypes = [PP, P, P, P, P, P, P]
+                L.dreams_pages_fork.argtypes = [PP, P, P, P, P, P, P, I32, P, P, P, P]
+                L.dreams_pages_release.argtypes = [PP, P, P, P, P, I32, P, I32, P]
                 for f in ("dreams_tree_verify_attn_workspace_size", "dreams_tree_verify_attn",
                           "dreams_tree_accept_workspace_size", "dreams_tree_accept", "dreams_kv_commit",
                           "dreams_check_tree_host", "dreams_stream_read", "dreams_tree_verify_attn_entropy",
@@ -686,3 +711,297 @@ def stream_read(src: torch.Tensor, sink: Optional[torch.Tensor] = None, stream=N
         sink = torch.empty(STREAM_READ_SINK_WORDS, dtype=torch.int32, device=src.device)
     _check(lib().dreams_stream_read(_ptr(src), src.numel() * src.element_size(), _ptr(sink), _stream(stream)))
     return sink
+
+
+# ---------------------------------------------------------------------------------------------------- paged cache
+PAGES_MAX, PAGES_MAX_SEQUENCES = 524288, 4096
+
+
+def _code(dtype) -> int:
+    if dtype is torch.bfloat16:
+        return DREAMS_BF16
+    if dtype is torch.float32:
+        return DREAMS_F32
+    raise TypeError("pages must be bfloat16 or float32")
+
+
+def _need_current(t: torch.Tensor, name: str):
+    """Kernels are launched on the current device: its tensors only."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda):
+        raise ValueError("%s must be a device tensor" % name)
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError("%s is on %s, not on the current device" % (name, t.device))
+
+
+def _need_shape(t: torch.Tensor, name: str, dtype, device, shape):
+    _need(t, name, dtype, device)
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError("%s must be %s, got %s" % (name, list(shape), list(t.shape)))
+
+
+def _page_strides(k_pages: torch.Tensor, v_pages: torch.Tensor):
+    """(layer stride, page stride) in elements of a pool [NL, P, Hkv, page_size, D] or [P, Hkv, page_size, D] whose
+    pages are dense (a page's K and V may lie side by side in one buffer)."""
+    for t, name in ((k_pages, "k_pages"), (v_pages, "v_pages")):
+        if not isinstance(t, torch.Tensor):
+            raise TypeError("%s must be a torch.Tensor" % name)
+        if not t.is_cuda:
+            raise ValueError("%s must be a device tensor" % name)
+        if t.dim() not in (4, 5):
+            raise ValueError("%s must be [NL,] num_pages, Hkv, page_size, D" % name)
+    if k_pages.dtype is not v_pages.dtype:
+        raise TypeError("k_pages and v_pages differ in dtype")
+    if k_pages.device != v_pages.device:
+        raise ValueError("k_pages and v_pages are on different devices")
+    if k_pages.shape != v_pages.shape:
+        raise ValueError("k_pages and v_pages differ in shape")
+    P, H, S, D = k_pages.shape[-4:]
+    st = k_pages.stride()
+
+    def same(axis):    # (a stride along an axis of one entry is not used)
+        return k_pages.shape[axis] == 1 or st[axis] == v_pages.stride()[axis]
+    if not all(same(i) for i in range(k_pages.dim())):
+        raise ValueError("k_pages and v_pages differ in layout")
+    for axis, dense in ((-1, 1), (-2, D), (-3, S * D)):
+        if k_pages.shape[axis] > 1 and st[axis] != dense:
+            raise ValueError("pages must be dense [Hkv, page_size, D]")
+    page = st[-4] if P > 1 else H * S * D
+    layer = st[0] if k_pages.dim() == 5 and k_pages.shape[0] > 1 else 0
+    return layer, page
+
+
+def _pool(k_pages, v_pages, page_table) -> PagePool:
+    layer, page = _page_strides(k_pages, v_pages)
+    _need_current(k_pages, "k_pages")
+    _need(page_table, "page_table", torch.int32, k_pages.device, 2)
+    P, H, S, D = k_pages.shape[-4:]
+    return PagePool(k_pages.shape[0] if k_pages.dim() == 5 else 1, page_table.shape[0], H, D, P, S, page_table.shape[1],
+                    _code(k_pages.dtype), layer, page)
+
+
+def _table_pool(page_table, page_count, refcount, page_size) -> PagePool:
+    _need(page_table, "page_table", torch.int32, None, 2)
+    _need_current(page_table, "page_table")
+    B, width = page_table.shape
+    _need_shape(page_count, "page_count", torch.int32, page_table.device, (B,))
+    _need(refcount, "refcount", torch.int32, page_table.device, 1)
+    return PagePool(1, B, 1, 64, refcount.shape[0], int(page_size), width, DREAMS_BF16, 0, 0)
+
+
+def paged_desc(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor, window: int = 0,
+               sinks: int = 0, max_kv_len: int = 0, num_splits: int = 0, scale: Optional[float] = None) -> PagedDesc:
+    """The description of an attention call over pages; checks the tensors' types, devices and shapes."""
+    layer, page = _page_strides(k_pages, v_pages)
+    if k_pages.dim() != 4:
+        raise ValueError("attention takes one layer's pages: [num_pages, Hkv, page_size, D]")
+    code = _code(k_pages.dtype)
+    _need(q, "q", k_pages.dtype, k_pages.device, 4)
+    _need_current(q, "q")
+    _need(page_table, "page_table", torch.int32, q.device, 2)
+    B, Hq, T, D = q.shape
+    P, H, S, Dk = k_pages.shape
+    if Dk != D or page_table.shape[0] != B:
+        raise ValueError("batch / head_dim mismatch between q, the pages and page_table")
+    return PagedDesc(B, Hq, H, D, T, P, S, page_table.shape[1], max_kv_len, num_splits, window, sinks, code,
+                     1.0 / math.sqrt(D) if scale is None else float(scale), page)
+
+
+def _paged_workspace(kind: str, nbytes: int, device: torch.device, stream, st: int) -> Optional[torch.Tensor]:
+    """The binding's own workspace; under capture one that belongs to the graph (its counters are cleared by every
+    replay), so that no two graphs share one."""
+    if nbytes == 0:
+        return None
+    if not torch.cuda.is_current_stream_capturing():
+        if stream is None:
+            return _workspace(kind, nbytes, device, st)
+        with torch.cuda.stream(stream):
+            return _workspace(kind, nbytes, device, st)
+    if stream is not None and stream.cuda_stream != torch.cuda.current_stream().cuda_stream:
+        raise ValueError("a call captured on another stream than the current one needs a workspace")
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    ws[:WORKSPACE_COUNTER_BYTES].zero_()
+    return ws
+
+
+WORKSPACE_COUNTER_BYTES = 65536
+
+
+def _paged_outputs(q, out, lse, with_lse):
+    if out is None:
+        out = torch.empty_like(q)
+    else:
+        _need_shape(out, "out", q.dtype, q.device, q.shape)
+    if lse is not None:
+        _need_shape(lse, "lse", torch.float32, q.device, q.shape[:3])
+    elif with_lse:
+        lse = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device)
+    return out, lse
+
+
+def paged_verify_attn_workspace_size(desc: PagedDesc) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().dreams_paged_verify_attn_workspace_size(ctypes.byref(desc), ctypes.byref(n)))
+    return n.value
+
+
+def paged_prompt_attn_workspace_size(desc: PagedDesc) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().dreams_paged_prompt_attn_workspace_size(ctypes.byref(desc), ctypes.byref(n)))
+    return n.value
+
+
+def paged_verify_attn(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor,
+                      kv_len: torch.Tensor, parent: Optional[torch.Tensor] = None,
+                      tree_mask: Optional[torch.Tensor] = None, window: int = 0, sinks: int = 0,
+                      scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                      lse: Optional[torch.Tensor] = None, with_lse: bool = True, max_kv_len: int = 0, num_splits: int = 0,
+                      workspace: Optional[torch.Tensor] = None,
+                      stream=None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """dreams_paged_verify_attn.  q [B,Hq,T,D]; k_pages/v_pages [num_pages,Hkv,page_size,D] (bf16 or fp32, same as q;
+    dense pages, any page stride); page_table [B,width] and kv_len [B] int32; parent [B,T] int32 and/or tree_mask
+    [B,T,ceil(T/64)] int64 (bit patterns; a window needs parent).  Keys more than `window` - 1 positions before a node are
+    out of its sight, but for the first `sinks` (window 0: none is).  Returns (out, lse [B,Hq,T] float32 or None)."""
+    desc = paged_desc(q, k_pages, v_pages, page_table, window, sinks, max_kv_len, num_splits, scale)
+    B, _, T, _ = q.shape
+    _need_shape(kv_len, "kv_len", torch.int32, q.device, (B,))
+    if parent is not None:
+        _need_shape(parent, "parent", torch.int32, q.device, (B, T))
+    if tree_mask is not None:
+        _need_shape(tree_mask, "tree_mask", torch.int64, q.device, (B, T, (T + 63) // 64))
+    out, lse = _paged_outputs(q, out, lse, with_lse)
+    st = _stream(stream)
+    if workspace is None:
+        workspace = _paged_workspace("paged", paged_verify_attn_workspace_size(desc), q.device, stream, st)
+    _check(lib().dreams_paged_verify_attn(ctypes.byref(desc), _ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(page_table),
+                                          _ptr(kv_len), _ptr(parent), _ptr(tree_mask), _ptr(out), _ptr(lse),
+                                          _ptr(workspace),
+                                          0 if workspace is None else workspace.numel() * workspace.element_size(), st))
+    return out, lse
+
+
+def paged_prompt_attn(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor,
+                      kv_len: torch.Tensor, row_len: Optional[torch.Tensor] = None, window: int = 0, sinks: int = 0,
+                      scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                      lse: Optional[torch.Tensor] = None, with_lse: bool = True, max_kv_len: int = 0, num_splits: int = 0,
+                      workspace: Optional[torch.Tensor] = None,
+                      stream=None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """dreams_paged_prompt_attn: causal attention of prompt rows at positions kv_len[b] + i, whose K/V the pages hold
+    already.  q [B,Hq,N,D]; row_len [B] int32 live rows (None: N each; the others give 0 and -inf); the rest as for
+    paged_verify_attn.  Returns (out, lse [B,Hq,N] float32 or None)."""
+    desc = paged_desc(q, k_pages, v_pages, page_table, window, sinks, max_kv_len, num_splits, scale)
+    B = q.shape[0]
+    _need_shape(kv_len, "kv_len", torch.int32, q.device, (B,))
+    if row_len is not None:
+        _need_shape(row_len, "row_len", torch.int32, q.device, (B,))
+    out, lse = _paged_outputs(q, out, lse, with_lse)
+    st = _stream(stream)
+    if workspace is None:
+        workspace = _paged_workspace("paged", paged_prompt_attn_workspace_size(desc), q.device, stream, st)
+    _check(lib().dreams_paged_prompt_attn(ctypes.byref(desc), _ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(page_table),
+                                          _ptr(kv_len), _ptr(row_len), _ptr(out), _ptr(lse), _ptr(workspace),
+                                          0 if workspace is None else workspace.numel() * workspace.element_size(), st))
+    return out, lse
+
+
+def paged_append(k_new: torch.Tensor, v_new: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,
+                 page_table: torch.Tensor, kv_len: torch.Tensor, row_len: Optional[torch.Tensor] = None,
+                 stream=None) -> None:
+    """dreams_paged_append, in place on k_pages / v_pages [NL,num_pages,Hkv,page_size,D] (or one layer's, without NL):
+    rows of k_new / v_new [NL,B,Hkv,N,D] (or without NL), of any strides with dense rows (a transposed view of a
+    projection's [B,N,Hkv,D] serves), go to the slots kv_len[b] .. of every sequence; row_len [B] int32 of them (None: N)."""
+    pool = _pool(k_pages, v_pages, page_table)
+    dev, dt = k_pages.device, k_pages.dtype
+    B = page_table.shape[0]
+    for t, name in ((k_new, "k_new"), (v_new, "v_new")):
+        if not isinstance(t, torch.Tensor):
+            raise TypeError("%s must be a torch.Tensor" % name)
+        if t.dtype is not dt:
+            raise TypeError("%s must be %s, got %s" % (name, dt, t.dtype))
+        if t.device != dev:
+            raise ValueError("%s is on %s, expected %s" % (name, t.device, dev))
+        lead = (pool.num_layers, B) if k_pages.dim() == 5 else (B,)
+        if t.dim() != k_pages.dim() or tuple(t.shape[:-2]) != lead + (pool.num_kv_heads,) or t.shape[-1] != pool.head_dim:
+            raise ValueError("%s must be [NL,] B, Hkv, N, D like the pages" % name)
+        if t.shape[-1] > 1 and t.stride(-1) != 1:
+            raise ValueError("the rows of %s must be dense" % name)
+    if k_new.shape != v_new.shape or any(n > 1 and x != y
+                                         for n, x, y in zip(k_new.shape, k_new.stride(), v_new.stride())):
+        raise ValueError("k_new and v_new differ in shape or layout")
+    _need_shape(kv_len, "kv_len", torch.int32, dev, (B,))
+    if row_len is not None:
+        _need_shape(row_len, "row_len", torch.int32, dev, (B,))
+    st = k_new.stride() if k_new.dim() == 5 else (0,) + k_new.stride()
+    strides = (ctypes.c_int64 * 4)(*st[:4])
+    _check(lib().dreams_paged_append(ctypes.byref(pool), _ptr(k_new), _ptr(v_new), k_new.shape[-2], strides,
+                                     _ptr(page_table), _ptr(kv_len), _ptr(row_len), _ptr(k_pages), _ptr(v_pages),
+                                     _stream(stream)))
+
+
+def paged_kv_commit(k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor, kv_len_in: torch.Tensor,
+                    accept_path: torch.Tensor, accept_len: torch.Tensor, kv_len_out: Optional[torch.Tensor] = None,
+                    stream=None) -> torch.Tensor:
+    """dreams_paged_kv_commit, in place on k_pages / v_pages [NL,num_pages,Hkv,page_size,D] (or one layer's).  Returns
+    kv_len_out [B] int32."""
+    pool = _pool(k_pages, v_pages, page_table)
+    dev, B = k_pages.device, page_table.shape[0]
+    _need_shape(kv_len_in, "kv_len_in", torch.int32, dev, (B,))
+    _need(accept_path, "accept_path", torch.int32, dev, 2)
+    if accept_path.shape[0] != B:
+        raise ValueError("accept_path must have page_table's batch size")
+    _need_shape(accept_len, "accept_len", torch.int32, dev, (B,))
+    if kv_len_out is None:
+        kv_len_out = torch.empty(B, dtype=torch.int32, device=dev)
+    _need_shape(kv_len_out, "kv_len_out", torch.int32, dev, (B,))
+    _check(lib().dreams_paged_kv_commit(ctypes.byref(pool), _ptr(k_pages), _ptr(v_pages), _ptr(page_table),
+                                        _ptr(kv_len_in), _ptr(accept_path), _ptr(accept_len), accept_path.shape[1],
+                                        _ptr(kv_len_out), _stream(stream)))
+    return kv_len_out
+
+
+def pages_reserve(page_table: torch.Tensor, page_count: torch.Tensor, refcount: torch.Tensor, want_len: torch.Tensor,
+                  page_size: int, granted: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """dreams_pages_reserve, in place on page_table [B,width], page_count [B] and refcount [num_pages] (int32): every
+    sequence gets pages for want_len[b] slots, lowest free first.  Returns granted [B] int32 (1 or 0)."""
+    pool = _table_pool(page_table, page_count, refcount, page_size)
+    dev, B = page_table.device, page_table.shape[0]
+    _need_shape(want_len, "want_len", torch.int32, dev, (B,))
+    if granted is None:
+        granted = torch.empty(B, dtype=torch.int32, device=dev)
+    _need_shape(granted, "granted", torch.int32, dev, (B,))
+    _check(lib().dreams_pages_reserve(ctypes.byref(pool), _ptr(page_table), _ptr(page_count), _ptr(refcount),
+                                      _ptr(want_len), _ptr(granted), _stream(stream)))
+    return granted
+
+
+def pages_fork(k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor, page_count: torch.Tensor,
+               kv_len: torch.Tensor, refcount: torch.Tensor, src: torch.Tensor, dst: torch.Tensor,
+               granted: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """dreams_pages_fork, in place: sequence dst[i] (without pages) becomes a copy of sequence src[i]; whole pages are
+    shared, the rows of a partly filled one copied in every layer.  Returns granted [n] int32 (1 or 0)."""
+    pool = _pool(k_pages, v_pages, page_table)
+    dev, B = k_pages.device, page_table.shape[0]
+    _need_shape(page_count, "page_count", torch.int32, dev, (B,))
+    _need_shape(kv_len, "kv_len", torch.int32, dev, (B,))
+    _need_shape(refcount, "refcount", torch.int32, dev, (pool.num_pages,))
+    _need(src, "src", torch.int32, dev, 1)
+    n = src.shape[0]
+    _need_shape(dst, "dst", torch.int32, dev, (n,))
+    if granted is None:
+        granted = torch.empty(n, dtype=torch.int32, device=dev)
+    _need_shape(granted, "granted", torch.int32, dev, (n,))
+    _check(lib().dreams_pages_fork(ctypes.byref(pool), _ptr(k_pages), _ptr(v_pages), _ptr(page_table), _ptr(page_count),
+                                   _ptr(kv_len), _ptr(refcount), n, _ptr(src), _ptr(dst), _ptr(granted),
+                                   _stream(stream)))
+    return granted
+
+
+def pages_release(page_table: torch.Tensor, page_count: torch.Tensor, kv_len: torch.Tensor, refcount: torch.Tensor,
+                  seqs: torch.Tensor, page_size: int, trim: bool = False, stream=None) -> None:
+    """dreams_pages_release, in place: the sequences seqs [n] int32 give up all their pages (kv_len becomes 0) or, with
+    trim, those past the ones that their kv_len slots need."""
+    pool = _table_pool(page_table, page_count, refcount, page_size)
+    dev, B = page_table.device, page_table.shape[0]
+    _need_shape(kv_len, "kv_len", torch.int32, dev, (B,))
+    _need(seqs, "seqs", torch.int32, dev, 1)
+    _check(lib().dreams_pages_release(ctypes.byref(pool), _ptr(page_table), _ptr(page_count), _ptr(kv_len),
+                                      _ptr(refcount), seqs.shape[0], _ptr(seqs), 1 if trim else 0, _stream(stream)))
