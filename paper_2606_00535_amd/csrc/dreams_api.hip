@@ -1265,21 +1265,160 @@ PagedAttnArgs paged_args(const dreams_paged_desc_t* d, const void* q, const void
   return a;
 }
 
+// The bf16 kernel's work split over pages.
+struct PagedPlan {
+  AttnPlan p;
+  int groups_per_head, unit_parts;
+};
+
+dreams_status_t plan_paged(const dreams_paged_desc_t* d, bool prompt, PagedPlan* plan) {
+  dreams_status_t st = check_paged_desc(d, prompt);
+  if (st != DREAMS_OK) return st;
+  *plan = PagedPlan{};
+  AttnPlan& p = plan->p;
+  p.splits = 1;
+  if (d->dtype != DREAMS_BF16 || d->batch == 0) return DREAMS_OK;
+  p.G = d->num_q_heads / d->num_kv_heads;
+  const int T = d->num_rows, slots = d->table_width * d->page_size;
+  const long long max_len = d->max_kv_len > 0 ? d->max_kv_len : slots - T;
+  if ((long long)p.G * T > 0x3fffffff || (long long)d->batch * d->num_kv_heads > 0x3fffffff / 8)
+    return fail(DREAMS_ERR_UNSUPPORTED, "problem too large");
+  p.rows_total = p.G * T;
+  p.rows_per_wg = tree_attn_bf16_rows_per_wg(p.rows_total);
+  p.row_groups = (p.rows_total + p.rows_per_wg - 1) / p.rows_per_wg;
+  p.units = d->batch * d->num_kv_heads;
+  int span = T;   // positions that a workgroup's rows can be apart
+  if (prompt && p.row_groups > 1) {
+    // Row groups of one head see only the keys before them; packed ones leave no row of a workgroup empty.
+    const int R = p.rows_per_wg;
+    const long long per_head = (long long)p.G * ((T + R - 1) / R);
+    if (per_head * (max_len + T / 2 + R / 2) <= p.row_groups * (max_len + T)) {
+      plan->groups_per_head = (T + R - 1) / R;
+      p.row_groups = (int)per_head;
+      span = R < T ? R : T;
+    }
+  }
+  long long keys = max_len + T;
+  if (d->window > 0) {
+    const long long seen = ((long long)d->sinks + 31) / 32 * 32 + d->window + span + 31LL;
+    if (seen < keys) keys = seen;
+  }
+  const int n_keys = (int)keys;
+  int parts = 1;
+  while ((long long)p.units * parts % 8 != 0) parts *= 2;
+  plan->unit_parts = parts;
+  const long long groups = (p.row_groups + parts - 1) / parts, xcd_wgs = (long long)p.units * parts / 8 * groups;
+  int splits = d->num_splits;
+  if (splits == 0) {
+    int cus = 0;
+    st = device_cus(&cus);
+    if (st != DREAMS_OK) return st;
+    const int wpc = tree_attn_bf16_wgs_per_cu(p.rows_per_wg);
+    splits = coarse_splits(8 * xcd_wgs, (long long)cus * wpc, n_keys);
+    if (splits > kAttnMaxSplits) splits = kAttnMaxSplits;
+    const long long xcd_cus = cus / 8;
+    if (splits > 1 && xcd_wgs < xcd_cus * wpc) {
+      const int fine = fine_splits(xcd_wgs, xcd_cus, wpc, n_keys);
+      if (fine < splits || 5 * fine >= 7 * splits) splits = fine;
+    }
+  }
+  const int max_splits = (n_keys + kPieceMinKeys - 1) / kPieceMinKeys;
+  if (splits > max_splits) splits = max_splits;
+  if (splits > kAttnMaxSplits) splits = kAttnMaxSplits;
+  const long long sets = (long long)p.units * p.row_groups;
+  if (2 * sets > kMaxSetCounters || splits < 1) splits = 1;
+  p.splits = splits;
+  if (8 * xcd_wgs * splits > 0x7fffffffLL) return fail(DREAMS_ERR_UNSUPPORTED, "problem too large");
+  if (splits > 1) {
+    int stride = 16;
+    while (stride > 2 && sets * stride > kMaxSetCounters) stride >>= 1;
+    p.ctr_stride = stride;
+    p.bytes = attn_partial_bytes(&p, splits, d->head_dim);
+  }
+  return DREAMS_OK;
+}
+
+dreams_status_t run_paged(const dreams_paged_desc_t* desc, bool prompt, const PagedAttnArgs& in, void* workspace,
+                          size_t workspace_bytes, hipStream_t stream) {
+  PagedPlan plan;
+  dreams_status_t st = plan_paged(desc, prompt, &plan);
+  if (st != DREAMS_OK) return st;
+  const AttnPlan& p = plan.p;
+  if (p.bytes > 0) {
+    if (!workspace) return fail(DREAMS_ERR_WORKSPACE, "workspace is NULL but %zu bytes are needed", p.bytes);
+    if (workspace_bytes < p.bytes)
+      return fail(DREAMS_ERR_WORKSPACE, "workspace has %zu bytes, %zu are needed", workspace_bytes, p.bytes);
+    if (!aligned(workspace, 256)) return fail(DREAMS_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+  }
+  if (desc->dtype != DREAMS_BF16) {
+    PagedAttnArgs f = in;
+    st = device_cus(&f.cus);
+    if (st != DREAMS_OK) return st;
+    hipError_t e = launch_paged_attn_f32(f, stream);
+    if (e != hipSuccess) return hip_fail(e, "paged attention launch");
+    return ok();
+  }
+  AttnArgs a{};
+  a.q = in.q;
+  a.k = in.k;
+  a.v = in.v;
+  a.kv_len = in.kv_len;
+  a.parent = in.parent;
+  a.mask = in.mask;
+  a.out = in.out;
+  a.lse = in.lse;
+  char* ws = (char*)workspace;
+  a.part_o = p.bytes ? (__bf16*)(ws + p.o_off) : nullptr;
+  a.part_ml = p.bytes ? (float*)(ws + p.ml_off) : nullptr;
+  a.set_ctr = p.bytes ? (unsigned long long*)ws : nullptr;
+  a.ctr_stride = p.ctr_stride;
+  a.wait_ticks = g_wait_ticks.load(std::memory_order_relaxed);
+  a.err = p.bytes ? (uint32_t*)ws + kErrorWord : nullptr;
+  a.B = in.B;
+  a.Hq = in.Hq;
+  a.Hkv = in.Hkv;
+  a.G = in.G;
+  a.T = in.T;
+  a.D = in.D;
+  a.S_cap = in.capacity;
+  a.units = p.units;
+  a.rows_per_wg = p.rows_per_wg;
+  a.row_groups = p.row_groups;
+  a.splits = p.splits;
+  a.scale_log2 = in.scale_log2;
+  a.table = in.table;
+  a.row_len = in.row_len;
+  a.page_stride = in.page_stride;
+  a.num_pages = in.num_pages;
+  a.page_shift = in.page_shift;
+  a.width = in.width;
+  a.window = in.window;
+  a.sinks = in.sinks;
+  a.chain = in.prompt;
+  a.groups_per_head = plan.groups_per_head;
+  a.unit_parts = plan.unit_parts;
+  hipError_t e = launch_paged_attn_bf16(a, stream);
+  if (e != hipSuccess) return hip_fail(e, "paged attention launch");
+  return ok();
+}
+
 }  // namespace
 
 dreams_status_t dreams_paged_verify_attn_workspace_size(const dreams_paged_desc_t* desc, size_t* bytes) {
   if (!bytes) return fail(DREAMS_ERR_INVALID_ARG, "bytes is NULL");
-  dreams_status_t st = check_paged_desc(desc, false);
+  PagedPlan plan;
+  dreams_status_t st = plan_paged(desc, false, &plan);
   if (st != DREAMS_OK) return st;
-  *bytes = 0;
+  *bytes = plan.p.bytes;
   return ok();
 }
 
 dreams_status_t dreams_paged_prompt_attn_workspace_size(const dreams_paged_desc_t* desc, size_t* bytes) {
   if (!bytes) return fail(DREAMS_ERR_INVALID_ARG, "bytes is NULL");
-  dreams_status_t st = check_paged_desc(desc, true);
+  PagedPlan plan;
+  dreams_status_t st = plan_paged(desc, true, &plan);
   if (st != DREAMS_OK) return st;
-  *bytes = 0;
+  *bytes = plan.p.bytes;
   return ok();
 }
 
@@ -1300,11 +1439,7 @@ dreams_status_t dreams_paged_verify_attn(const dreams_paged_desc_t* desc, const 
   PagedAttnArgs a = paged_args(desc, q, k_pages, v_pages, page_table, kv_len, out, lse);
   a.parent = parent;
   a.mask = tree_mask;
-  st = device_cus(&a.cus);
-  if (st != DREAMS_OK) return st;
-  hipError_t e = launch_paged_attn_f32(a, stream);
-  if (e != hipSuccess) return hip_fail(e, "paged tree attention launch");
-  return ok();
+  return run_paged(desc, false, a, workspace, workspace_bytes, stream);
 }
 
 dreams_status_t dreams_paged_prompt_attn(const dreams_paged_desc_t* desc, const void* q, const void* k_pages,
@@ -1320,11 +1455,7 @@ dreams_status_t dreams_paged_prompt_attn(const dreams_paged_desc_t* desc, const 
   PagedAttnArgs a = paged_args(desc, q, k_pages, v_pages, page_table, kv_len, out, lse);
   a.row_len = row_len;
   a.prompt = 1;
-  st = device_cus(&a.cus);
-  if (st != DREAMS_OK) return st;
-  hipError_t e = launch_paged_attn_f32(a, stream);
-  if (e != hipSuccess) return hip_fail(e, "paged prompt attention launch");
-  return ok();
+  return run_paged(desc, true, a, workspace, workspace_bytes, stream);
 }
 
 namespace {

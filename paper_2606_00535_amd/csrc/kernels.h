@@ -106,6 +106,14 @@ struct AttnArgs {
   int piece_by_len;       // 1: each sequence's pieces are cut from its own L_b + T (read before the first copies)
   float scale_log2;       // scale * log2(e)
   int cus;                // compute units of the device (fp32: rows per workgroup)
+  // A paged cache (launch_paged_attn_bf16; see PagedAttnArgs): S_cap is the slots that a table row covers
+  const int32_t* table;   // [B, width]
+  const int32_t* row_len; // [B] live rows (chain) or nullptr
+  int64_t page_stride;    // bytes
+  int num_pages, page_shift, width, window, sinks;
+  int chain;              // 1: row i of a head is position L_b + i; 0: tree nodes
+  int groups_per_head;    // chain: row groups of a head, or 0: the heads' rows are packed one after another
+  int unit_parts;         // parts of a unit's row groups, each on one XCD; units * unit_parts is a multiple of 8
 };
 
 // Query rows per workgroup the bf16 kernel uses for G*T rows per KV head.
@@ -325,6 +333,7 @@ struct PagedAttnArgs {
   int cus;
 };
 hipError_t launch_paged_attn_f32(const PagedAttnArgs& a, hipStream_t stream);
+hipError_t launch_paged_attn_bf16(const AttnArgs& a, hipStream_t stream);
 
 struct PagedRowsArgs {
   char* k;                   // [NL][pages, Hkv, page_size, row bytes]
