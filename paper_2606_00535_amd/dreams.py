@@ -725,116 +725,145 @@ def _code(dtype) -> int:
     raise TypeError("pages must be bfloat16 or float32")
 
 
-def _need_current(t: torch.Tensor, name: str):
-    """Kernels are launched on the current device: its tensors only."""
-    if not (isinstance(t, torch.Tensor) and t.is_cuda):
+def _current(t: torch.Tensor, name: str, dtype=None) -> int:
+    """The tensor's device index.  Kernels are launched on the current device: its tensors only."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("%s must be a torch.Tensor" % name)
+    if dtype is not None and t.dtype is not dtype:
+        raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
+    at = t.get_device()
+    if at < 0:
         raise ValueError("%s must be a device tensor" % name)
-    if t.device.index != torch.cuda.current_device():
+    if at != torch.cuda.current_device():
         raise ValueError("%s is on %s, not on the current device" % (name, t.device))
+    return at
 
 
-def _need_shape(t: torch.Tensor, name: str, dtype, device, shape):
-    _need(t, name, dtype, device)
-    if tuple(t.shape) != tuple(shape):
-        raise ValueError("%s must be %s, got %s" % (name, list(shape), list(t.shape)))
+def _need_on(t: torch.Tensor, name: str, dtype, at: int, shape=None, ndim=None):
+    """As _need, for a device index, a whole shape or a number of dimensions."""
+    if (isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == at and t.is_contiguous()
+            and (shape is None or t.shape == shape) and (ndim is None or t.dim() == ndim)):
+        return
+    _need(t, name, dtype, torch.device("cuda", at), ndim)
+    raise ValueError("%s must be %s, got %s" % (name, list(shape), list(t.shape)))
 
 
 def _page_strides(k_pages: torch.Tensor, v_pages: torch.Tensor):
-    """(layer stride, page stride) in elements of a pool [NL, P, Hkv, page_size, D] or [P, Hkv, page_size, D] whose
-    pages are dense (a page's K and V may lie side by side in one buffer)."""
+    """(shape, layer stride, page stride) of a pool [NL, P, Hkv, page_size, D] or [P, Hkv, page_size, D] whose pages are
+    dense (a page's K and V may lie side by side in one buffer); strides in elements."""
     for t, name in ((k_pages, "k_pages"), (v_pages, "v_pages")):
         if not isinstance(t, torch.Tensor):
             raise TypeError("%s must be a torch.Tensor" % name)
-        if not t.is_cuda:
-            raise ValueError("%s must be a device tensor" % name)
-        if t.dim() not in (4, 5):
-            raise ValueError("%s must be [NL,] num_pages, Hkv, page_size, D" % name)
+    shape, st, vst = k_pages.shape, k_pages.stride(), v_pages.stride()
     if k_pages.dtype is not v_pages.dtype:
         raise TypeError("k_pages and v_pages differ in dtype")
-    if k_pages.device != v_pages.device:
+    if k_pages.get_device() != v_pages.get_device():
         raise ValueError("k_pages and v_pages are on different devices")
-    if k_pages.shape != v_pages.shape:
+    if shape != v_pages.shape:
         raise ValueError("k_pages and v_pages differ in shape")
-    P, H, S, D = k_pages.shape[-4:]
-    st = k_pages.stride()
-
-    def same(axis):    # (a stride along an axis of one entry is not used)
-        return k_pages.shape[axis] == 1 or st[axis] == v_pages.stride()[axis]
-    if not all(same(i) for i in range(k_pages.dim())):
+    n = len(shape)
+    if n not in (4, 5):
+        raise ValueError("k_pages and v_pages must be [NL,] num_pages, Hkv, page_size, D")
+    P, H, S, D = shape[-4:]
+    # (a stride along an axis of one entry is not used)
+    if st != vst and any(shape[i] > 1 and st[i] != vst[i] for i in range(n)):
         raise ValueError("k_pages and v_pages differ in layout")
-    for axis, dense in ((-1, 1), (-2, D), (-3, S * D)):
-        if k_pages.shape[axis] > 1 and st[axis] != dense:
-            raise ValueError("pages must be dense [Hkv, page_size, D]")
-    page = st[-4] if P > 1 else H * S * D
-    layer = st[0] if k_pages.dim() == 5 and k_pages.shape[0] > 1 else 0
-    return layer, page
+    if st[-3:] != (S * D, D, 1) and any(shape[i] > 1 and st[i] != dense
+                                       for i, dense in ((n - 1, 1), (n - 2, D), (n - 3, S * D))):
+        raise ValueError("pages must be dense [Hkv, page_size, D]")
+    return shape, st[0] if n == 5 and shape[0] > 1 else 0, st[-4] if P > 1 else H * S * D
 
 
-def _pool(k_pages, v_pages, page_table) -> PagePool:
-    layer, page = _page_strides(k_pages, v_pages)
-    _need_current(k_pages, "k_pages")
-    _need(page_table, "page_table", torch.int32, k_pages.device, 2)
-    P, H, S, D = k_pages.shape[-4:]
-    return PagePool(k_pages.shape[0] if k_pages.dim() == 5 else 1, page_table.shape[0], H, D, P, S, page_table.shape[1],
-                    _code(k_pages.dtype), layer, page)
-
-
-def _table_pool(page_table, page_count, refcount, page_size) -> PagePool:
-    _need(page_table, "page_table", torch.int32, None, 2)
-    _need_current(page_table, "page_table")
+def _pool(k_pages, v_pages, page_table):
+    """(PagePool, device index)"""
+    shape, layer, page = _page_strides(k_pages, v_pages)
+    at = _current(k_pages, "k_pages")
+    _need_on(page_table, "page_table", torch.int32, at, None, 2)
+    P, H, S, D = shape[-4:]
     B, width = page_table.shape
-    _need_shape(page_count, "page_count", torch.int32, page_table.device, (B,))
-    _need(refcount, "refcount", torch.int32, page_table.device, 1)
-    return PagePool(1, B, 1, 64, refcount.shape[0], int(page_size), width, DREAMS_BF16, 0, 0)
+    return PagePool(shape[0] if len(shape) == 5 else 1, B, H, D, P, S, width, _code(k_pages.dtype), layer, page), at
+
+
+def _table_pool(page_table, page_count, refcount, page_size):
+    """(PagePool, device index)"""
+    at = _current(page_table, "page_table", torch.int32)
+    _need_on(page_table, "page_table", torch.int32, at, None, 2)
+    B, width = page_table.shape
+    _need_on(page_count, "page_count", torch.int32, at, (B,))
+    _need_on(refcount, "refcount", torch.int32, at, None, 1)
+    return PagePool(1, B, 1, 64, refcount.shape[0], page_size, width, DREAMS_BF16, 0, 0), at
 
 
 def paged_desc(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor, window: int = 0,
                sinks: int = 0, max_kv_len: int = 0, num_splits: int = 0, scale: Optional[float] = None) -> PagedDesc:
     """The description of an attention call over pages; checks the tensors' types, devices and shapes."""
-    layer, page = _page_strides(k_pages, v_pages)
-    if k_pages.dim() != 4:
+    shape, _, page = _page_strides(k_pages, v_pages)
+    if len(shape) != 4:
         raise ValueError("attention takes one layer's pages: [num_pages, Hkv, page_size, D]")
-    code = _code(k_pages.dtype)
-    _need(q, "q", k_pages.dtype, k_pages.device, 4)
-    _need_current(q, "q")
-    _need(page_table, "page_table", torch.int32, q.device, 2)
+    dt = k_pages.dtype
+    code = _code(dt)
+    at = _current(q, "q")
+    if k_pages.get_device() != at:
+        raise ValueError("k_pages is on %s, expected %s" % (k_pages.device, q.device))
+    _need_on(q, "q", dt, at, None, 4)
+    _need_on(page_table, "page_table", torch.int32, at, None, 2)
     B, Hq, T, D = q.shape
-    P, H, S, Dk = k_pages.shape
-    if Dk != D or page_table.shape[0] != B:
+    P, H, S, Dk = shape
+    Bt, width = page_table.shape
+    if Dk != D or Bt != B:
         raise ValueError("batch / head_dim mismatch between q, the pages and page_table")
-    return PagedDesc(B, Hq, H, D, T, P, S, page_table.shape[1], max_kv_len, num_splits, window, sinks, code,
-                     1.0 / math.sqrt(D) if scale is None else float(scale), page)
-
-
-def _paged_workspace(kind: str, nbytes: int, device: torch.device, stream, st: int) -> Optional[torch.Tensor]:
-    """The binding's own workspace; under capture one that belongs to the graph (its counters are cleared by every
-    replay), so that no two graphs share one."""
-    if nbytes == 0:
-        return None
-    if not torch.cuda.is_current_stream_capturing():
-        if stream is None:
-            return _workspace(kind, nbytes, device, st)
-        with torch.cuda.stream(stream):
-            return _workspace(kind, nbytes, device, st)
-    if stream is not None and stream.cuda_stream != torch.cuda.current_stream().cuda_stream:
-        raise ValueError("a call captured on another stream than the current one needs a workspace")
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    ws[:WORKSPACE_COUNTER_BYTES].zero_()
-    return ws
+    return PagedDesc(B, Hq, H, D, T, P, S, width, max_kv_len, num_splits, window, sinks, code,
+                     1.0 / math.sqrt(D) if scale is None else scale, page)
 
 
 WORKSPACE_COUNTER_BYTES = 65536
 
 
+def _call_paged(call, size, desc, tensors, workspace, at, stream):
+    """An attention call with the caller's workspace, or the binding's own (one per device and stream; under capture one
+    that belongs to the graph, its counters cleared by every replay, so that no two graphs share one)."""
+    st = _stream(stream)
+    if workspace is not None:
+        _check(call(desc, *tensors, _ptr(workspace), workspace.numel() * workspace.element_size(), st))
+        return
+    if torch.cuda.is_current_stream_capturing():
+        device = torch.device("cuda", at)
+        if stream is not None and stream.cuda_stream != torch.cuda.current_stream().cuda_stream:
+            raise ValueError("a call captured on another stream than the current one needs a workspace")
+        n = ctypes.c_size_t(0)
+        _check(size(desc, ctypes.byref(n)))
+        ws = None
+        if n.value:
+            ws = torch.empty(n.value, dtype=torch.uint8, device=device)
+            ws[:WORKSPACE_COUNTER_BYTES].zero_()
+        _check(call(desc, *tensors, _ptr(ws), n.value, st))
+        return
+    ws = _ws.get(("paged", at, st))
+    status = call(desc, *tensors, _ptr(ws), 0 if ws is None else ws.numel(), st)
+    if status == DREAMS_ERR_WORKSPACE:      # (nothing was enqueued: the first call, or the first of this size)
+        n = ctypes.c_size_t(0)
+        _check(size(desc, ctypes.byref(n)))
+        device = torch.device("cuda", at)
+        if stream is None:
+            ws = _workspace("paged", n.value, device, st)
+        else:
+            with torch.cuda.stream(stream):
+                ws = _workspace("paged", n.value, device, st)
+        status = call(desc, *tensors, _ptr(ws), ws.numel(), st)
+    _check(status)
+
+
 def _paged_outputs(q, out, lse, with_lse):
+    at = q.get_device()
     if out is None:
         out = torch.empty_like(q)
     else:
-        _need_shape(out, "out", q.dtype, q.device, q.shape)
+        _need_on(out, "out", q.dtype, at, q.shape)
     if lse is not None:
-        _need_shape(lse, "lse", torch.float32, q.device, q.shape[:3])
+        _need_on(lse, "lse", torch.float32, at, q.shape[:3])
     elif with_lse:
-        lse = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device)
+        B, H, T, _ = q.shape
+        lse = q.new_empty((B, H, T), dtype=torch.float32)
     return out, lse
 
 
@@ -862,20 +891,17 @@ def paged_verify_attn(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Ten
     [B,T,ceil(T/64)] int64 (bit patterns; a window needs parent).  Keys more than `window` - 1 positions before a node are
     out of its sight, but for the first `sinks` (window 0: none is).  Returns (out, lse [B,Hq,T] float32 or None)."""
     desc = paged_desc(q, k_pages, v_pages, page_table, window, sinks, max_kv_len, num_splits, scale)
-    B, _, T, _ = q.shape
-    _need_shape(kv_len, "kv_len", torch.int32, q.device, (B,))
+    B, T, at = desc.batch, desc.num_rows, q.get_device()
+    _need_on(kv_len, "kv_len", torch.int32, at, (B,))
     if parent is not None:
-        _need_shape(parent, "parent", torch.int32, q.device, (B, T))
+        _need_on(parent, "parent", torch.int32, at, (B, T))
     if tree_mask is not None:
-        _need_shape(tree_mask, "tree_mask", torch.int64, q.device, (B, T, (T + 63) // 64))
+        _need_on(tree_mask, "tree_mask", torch.int64, at, (B, T, (T + 63) // 64))
     out, lse = _paged_outputs(q, out, lse, with_lse)
-    st = _stream(stream)
-    if workspace is None:
-        workspace = _paged_workspace("paged", paged_verify_attn_workspace_size(desc), q.device, stream, st)
-    _check(lib().dreams_paged_verify_attn(ctypes.byref(desc), _ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(page_table),
-                                          _ptr(kv_len), _ptr(parent), _ptr(tree_mask), _ptr(out), _ptr(lse),
-                                          _ptr(workspace),
-                                          0 if workspace is None else workspace.numel() * workspace.element_size(), st))
+    L = lib()
+    _call_paged(L.dreams_paged_verify_attn, L.dreams_paged_verify_attn_workspace_size, ctypes.byref(desc),
+                (_ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(page_table), _ptr(kv_len), _ptr(parent), _ptr(tree_mask),
+                 _ptr(out), _ptr(lse)), workspace, at, stream)
     return out, lse
 
 
@@ -889,18 +915,19 @@ def paged_prompt_attn(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Ten
     already.  q [B,Hq,N,D]; row_len [B] int32 live rows (None: N each; the others give 0 and -inf); the rest as for
     paged_verify_attn.  Returns (out, lse [B,Hq,N] float32 or None)."""
     desc = paged_desc(q, k_pages, v_pages, page_table, window, sinks, max_kv_len, num_splits, scale)
-    B = q.shape[0]
-    _need_shape(kv_len, "kv_len", torch.int32, q.device, (B,))
+    B, at = desc.batch, q.get_device()
+    _need_on(kv_len, "kv_len", torch.int32, at, (B,))
     if row_len is not None:
-        _need_shape(row_len, "row_len", torch.int32, q.device, (B,))
+        _need_on(row_len, "row_len", torch.int32, at, (B,))
     out, lse = _paged_outputs(q, out, lse, with_lse)
-    st = _stream(stream)
-    if workspace is None:
-        workspace = _paged_workspace("paged", paged_prompt_attn_workspace_size(desc), q.device, stream, st)
-    _check(lib().dreams_paged_prompt_attn(ctypes.byref(desc), _ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(page_table),
-                                          _ptr(kv_len), _ptr(row_len), _ptr(out), _ptr(lse), _ptr(workspace),
-                                          0 if workspace is None else workspace.numel() * workspace.element_size(), st))
+    L = lib()
+    _call_paged(L.dreams_paged_prompt_attn, L.dreams_paged_prompt_attn_workspace_size, ctypes.byref(desc),
+                (_ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(page_table), _ptr(kv_len), _ptr(row_len), _ptr(out),
+                 _ptr(lse)), workspace, at, stream)
     return out, lse
+
+
+_Strides = ctypes.c_int64 * 4
 
 
 def paged_append(k_new: torch.Tensor, v_new: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,
@@ -909,30 +936,28 @@ def paged_append(k_new: torch.Tensor, v_new: torch.Tensor, k_pages: torch.Tensor
     """dreams_paged_append, in place on k_pages / v_pages [NL,num_pages,Hkv,page_size,D] (or one layer's, without NL):
     rows of k_new / v_new [NL,B,Hkv,N,D] (or without NL), of any strides with dense rows (a transposed view of a
     projection's [B,N,Hkv,D] serves), go to the slots kv_len[b] .. of every sequence; row_len [B] int32 of them (None: N)."""
-    pool = _pool(k_pages, v_pages, page_table)
-    dev, dt = k_pages.device, k_pages.dtype
-    B = page_table.shape[0]
+    pool, at = _pool(k_pages, v_pages, page_table)
+    dt, B, n = k_pages.dtype, pool.batch, k_pages.dim()
     for t, name in ((k_new, "k_new"), (v_new, "v_new")):
         if not isinstance(t, torch.Tensor):
             raise TypeError("%s must be a torch.Tensor" % name)
         if t.dtype is not dt:
             raise TypeError("%s must be %s, got %s" % (name, dt, t.dtype))
-        if t.device != dev:
-            raise ValueError("%s is on %s, expected %s" % (name, t.device, dev))
-        lead = (pool.num_layers, B) if k_pages.dim() == 5 else (B,)
-        if t.dim() != k_pages.dim() or tuple(t.shape[:-2]) != lead + (pool.num_kv_heads,) or t.shape[-1] != pool.head_dim:
-            raise ValueError("%s must be [NL,] B, Hkv, N, D like the pages" % name)
-        if t.shape[-1] > 1 and t.stride(-1) != 1:
-            raise ValueError("the rows of %s must be dense" % name)
-    if k_new.shape != v_new.shape or any(n > 1 and x != y
-                                         for n, x, y in zip(k_new.shape, k_new.stride(), v_new.stride())):
+        if t.get_device() != at:
+            raise ValueError("%s is on %s, expected %s" % (name, t.device, k_pages.device))
+    shape, st, vst = k_new.shape, k_new.stride(), v_new.stride()
+    if len(shape) != n or shape[-4:-2] != (B, pool.num_kv_heads) or shape[-1] != pool.head_dim or (
+            n == 5 and shape[0] != pool.num_layers):
+        raise ValueError("k_new must be [NL,] B, Hkv, N, D like the pages")
+    if shape != v_new.shape or (st != vst and any(shape[i] > 1 and st[i] != vst[i] for i in range(n))):
         raise ValueError("k_new and v_new differ in shape or layout")
-    _need_shape(kv_len, "kv_len", torch.int32, dev, (B,))
+    if shape[-1] > 1 and st[-1] != 1:
+        raise ValueError("the rows of k_new and v_new must be dense")
+    _need_on(kv_len, "kv_len", torch.int32, at, (B,))
     if row_len is not None:
-        _need_shape(row_len, "row_len", torch.int32, dev, (B,))
-    st = k_new.stride() if k_new.dim() == 5 else (0,) + k_new.stride()
-    strides = (ctypes.c_int64 * 4)(*st[:4])
-    _check(lib().dreams_paged_append(ctypes.byref(pool), _ptr(k_new), _ptr(v_new), k_new.shape[-2], strides,
+        _need_on(row_len, "row_len", torch.int32, at, (B,))
+    strides = _Strides(*(st[:4] if n == 5 else (0,) + st[:3]))
+    _check(lib().dreams_paged_append(ctypes.byref(pool), _ptr(k_new), _ptr(v_new), shape[-2], strides,
                                      _ptr(page_table), _ptr(kv_len), _ptr(row_len), _ptr(k_pages), _ptr(v_pages),
                                      _stream(stream)))
 
@@ -942,16 +967,17 @@ def paged_kv_commit(k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: to
                     stream=None) -> torch.Tensor:
     """dreams_paged_kv_commit, in place on k_pages / v_pages [NL,num_pages,Hkv,page_size,D] (or one layer's).  Returns
     kv_len_out [B] int32."""
-    pool = _pool(k_pages, v_pages, page_table)
-    dev, B = k_pages.device, page_table.shape[0]
-    _need_shape(kv_len_in, "kv_len_in", torch.int32, dev, (B,))
-    _need(accept_path, "accept_path", torch.int32, dev, 2)
+    pool, at = _pool(k_pages, v_pages, page_table)
+    B = pool.batch
+    _need_on(kv_len_in, "kv_len_in", torch.int32, at, (B,))
+    _need_on(accept_path, "accept_path", torch.int32, at, None, 2)
     if accept_path.shape[0] != B:
         raise ValueError("accept_path must have page_table's batch size")
-    _need_shape(accept_len, "accept_len", torch.int32, dev, (B,))
+    _need_on(accept_len, "accept_len", torch.int32, at, (B,))
     if kv_len_out is None:
-        kv_len_out = torch.empty(B, dtype=torch.int32, device=dev)
-    _need_shape(kv_len_out, "kv_len_out", torch.int32, dev, (B,))
+        kv_len_out = torch.empty_like(kv_len_in)
+    else:
+        _need_on(kv_len_out, "kv_len_out", torch.int32, at, (B,))
     _check(lib().dreams_paged_kv_commit(ctypes.byref(pool), _ptr(k_pages), _ptr(v_pages), _ptr(page_table),
                                         _ptr(kv_len_in), _ptr(accept_path), _ptr(accept_len), accept_path.shape[1],
                                         _ptr(kv_len_out), _stream(stream)))
@@ -962,12 +988,13 @@ def pages_reserve(page_table: torch.Tensor, page_count: torch.Tensor, refcount: 
                   page_size: int, granted: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """dreams_pages_reserve, in place on page_table [B,width], page_count [B] and refcount [num_pages] (int32): every
     sequence gets pages for want_len[b] slots, lowest free first.  Returns granted [B] int32 (1 or 0)."""
-    pool = _table_pool(page_table, page_count, refcount, page_size)
-    dev, B = page_table.device, page_table.shape[0]
-    _need_shape(want_len, "want_len", torch.int32, dev, (B,))
+    pool, at = _table_pool(page_table, page_count, refcount, page_size)
+    B = pool.batch
+    _need_on(want_len, "want_len", torch.int32, at, (B,))
     if granted is None:
-        granted = torch.empty(B, dtype=torch.int32, device=dev)
-    _need_shape(granted, "granted", torch.int32, dev, (B,))
+        granted = torch.empty_like(want_len)
+    else:
+        _need_on(granted, "granted", torch.int32, at, (B,))
     _check(lib().dreams_pages_reserve(ctypes.byref(pool), _ptr(page_table), _ptr(page_count), _ptr(refcount),
                                       _ptr(want_len), _ptr(granted), _stream(stream)))
     return granted
@@ -978,17 +1005,18 @@ def pages_fork(k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.T
                granted: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """dreams_pages_fork, in place: sequence dst[i] (without pages) becomes a copy of sequence src[i]; whole pages are
     shared, the rows of a partly filled one copied in every layer.  Returns granted [n] int32 (1 or 0)."""
-    pool = _pool(k_pages, v_pages, page_table)
-    dev, B = k_pages.device, page_table.shape[0]
-    _need_shape(page_count, "page_count", torch.int32, dev, (B,))
-    _need_shape(kv_len, "kv_len", torch.int32, dev, (B,))
-    _need_shape(refcount, "refcount", torch.int32, dev, (pool.num_pages,))
-    _need(src, "src", torch.int32, dev, 1)
+    pool, at = _pool(k_pages, v_pages, page_table)
+    B = pool.batch
+    _need_on(page_count, "page_count", torch.int32, at, (B,))
+    _need_on(kv_len, "kv_len", torch.int32, at, (B,))
+    _need_on(refcount, "refcount", torch.int32, at, (pool.num_pages,))
+    _need_on(src, "src", torch.int32, at, None, 1)
     n = src.shape[0]
-    _need_shape(dst, "dst", torch.int32, dev, (n,))
+    _need_on(dst, "dst", torch.int32, at, (n,))
     if granted is None:
-        granted = torch.empty(n, dtype=torch.int32, device=dev)
-    _need_shape(granted, "granted", torch.int32, dev, (n,))
+        granted = torch.empty_like(src)
+    else:
+        _need_on(granted, "granted", torch.int32, at, (n,))
     _check(lib().dreams_pages_fork(ctypes.byref(pool), _ptr(k_pages), _ptr(v_pages), _ptr(page_table), _ptr(page_count),
                                    _ptr(kv_len), _ptr(refcount), n, _ptr(src), _ptr(dst), _ptr(granted),
                                    _stream(stream)))
@@ -999,9 +1027,8 @@ def pages_release(page_table: torch.Tensor, page_count: torch.Tensor, kv_len: to
                   seqs: torch.Tensor, page_size: int, trim: bool = False, stream=None) -> None:
     """dreams_pages_release, in place: the sequences seqs [n] int32 give up all their pages (kv_len becomes 0) or, with
     trim, those past the ones that their kv_len slots need."""
-    pool = _table_pool(page_table, page_count, refcount, page_size)
-    dev, B = page_table.device, page_table.shape[0]
-    _need_shape(kv_len, "kv_len", torch.int32, dev, (B,))
-    _need(seqs, "seqs", torch.int32, dev, 1)
+    pool, at = _table_pool(page_table, page_count, refcount, page_size)
+    _need_on(kv_len, "kv_len", torch.int32, at, (pool.batch,))
+    _need_on(seqs, "seqs", torch.int32, at, None, 1)
     _check(lib().dreams_pages_release(ctypes.byref(pool), _ptr(page_table), _ptr(page_count), _ptr(kv_len),
                                       _ptr(refcount), seqs.shape[0], _ptr(seqs), 1 if trim else 0, _stream(stream)))
