@@ -334,6 +334,7 @@ struct PagedAttnArgs {
 };
 hipError_t launch_paged_attn_f32(const PagedAttnArgs& a, hipStream_t stream);
 hipError_t launch_paged_attn_bf16(const AttnArgs& a, hipStream_t stream);
+hipError_t launch_paged_prompt_bf16(const AttnArgs& a, hipStream_t stream);   // chain, groups_per_head > 0, one piece
 
 struct PagedRowsArgs {
   char* k;                   // [NL][pages, Hkv, page_size, row bytes]

@@ -1,0 +1,355 @@
+// Attention of a prompt's rows over a paged cache, bf16 inputs, fp32 accumulation on the matrix cores: row i of a
+// sequence (at position L_b + i) sees the slots up to its own, with a window only those and the sinks in its sight.
+//
+//   * A workgroup of 4 waves owns 128 consecutive rows of one query head, a wave 32 of them; two workgroups share a
+//     compute unit, so the waves of a SIMD belong to different ones and no barrier ties their phases.
+//   * Keys come in tiles of 32.  S^T = K Q^T and O^T += V^T P^T on v_mfma_f32_32x32x16_bf16: a lane holds 16 scores of
+//     one row (lane l and l + 32 share row l % 32), the probabilities are in the value product's operand order as they
+//     come (keys numbered 16 t + 4 (l / 32) + {0..3, 8..11} in both operands), and the values are read transposed
+//     (ds_read_b64_tr_b16).
+//   * A wave's work is pipelined over tiles: the score product of tile k + 1 runs on the matrix cores while the vector
+//     ALU takes the exponentials of tile k, whose value product follows.  So at the time that the wave needs key tile k + 1
+//     it needs value tile k: a stage is two key tiles and the two value tiles one earlier, one barrier a stage (D = 128:
+//     32 KB, two stages; D = 64: 16 KB, four).
+//   * A stage is copied straight into LDS (global_load_lds_dwordx4), each wave a block of 16 key rows and one of 16 value
+//     rows, from the pages that scalar loads of the table name a stage ahead.  Rows in LDS are XOR-swizzled: chunk c of
+//     row r at position c ^ swz(r), so that neither the 32-row key reads nor the 4 x 32 value reads conflict on banks.
+//   * Slots that no row sees are zeroed in LDS, so whatever they hold cannot reach the products.
+#include "kernels.h"
+
+#include <math.h>
+
+namespace dreams {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr float kLn2 = 0.69314718055994530942f;
+constexpr float kLazyLog2 = 8.0f;    // slack of the running maximum, log2 units
+constexpr int kTile = 32;            // keys per tile
+constexpr int kRows = 32;            // rows per wave
+constexpr int kWaves = 4;
+constexpr int kRowsWg = kRows * kWaves;
+
+typedef __attribute__((address_space(3))) void lds_void;
+__device__ __forceinline__ uint32_t lds_addr(const void* p) { return (uint32_t)(uintptr_t)(lds_void*)p; }
+// wave-wide 16-byte copy into LDS: lane l's 16 bytes, from a uniform base plus the lane's offset, land at m0 + 16 l
+__device__ __forceinline__ void copy16_to_lds(uint32_t m0, const void* sbase, uint32_t voff) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(m0), "v"(voff), "s"(sbase)
+               : "memory");
+}
+template <int N>
+__device__ __forceinline__ void wait_vm() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+// workgroup barrier once this wave's LDS accesses are done; copies stay in flight
+__device__ __forceinline__ void barrier_lds() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xC07F);
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// Rows of D bf16 in LDS.  A 256-byte bank line holds one row (D = 128) or two (D = 64).  A key read takes one 16-byte chunk
+// of 32 rows, 16 rows at a time: swz is a bijection over the 16 (8 of a parity) rows.  A value read takes 4 aligned
+// chunks of 4 consecutive rows: the rows differ in swz / 4 (or in their half of the line).
+template <int D>
+struct Rows {
+  static constexpr int ROW = D * 2, CPR = D / 8;
+  static constexpr int BLOCK = 16 * ROW;            // bytes of 16 rows
+  static constexpr int COPIES = BLOCK / 1024;       // wave-wide copies of a block
+  static constexpr int HALF = 2 * kTile * ROW;      // bytes of a stage's keys (or values)
+  static constexpr int STAGE = 2 * HALF;
+  static constexpr int STAGES = 65536 / STAGE;
+  static __device__ __forceinline__ int swz(int r) {
+    if constexpr (D == 128) return (r & 3) * 4 + ((r >> 2) & 3);
+    return ((r >> 1) & 1) * 4 + ((r >> 2) & 3);
+  }
+  static __device__ __forceinline__ int off(int r, int c) { return r * ROW + ((c ^ swz(r)) << 4); }
+};
+
+template <int D>
+__global__ __launch_bounds__(64 * kWaves, 2) void paged_prompt_bf16_kernel(AttnArgs a) {
+  using L = Rows<D>;
+  constexpr int KS = D / 16;        // products of a tile's scores
+  constexpr int DB = D / 32;        // 32-column blocks of the output
+  constexpr int AHEAD = L::STAGES - 1;
+  constexpr int CP = 2 * L::COPIES; // copies a wave issues per stage
+  extern __shared__ __attribute__((aligned(1024))) unsigned char ring[];
+
+  // ---- work item: every (sequence, KV head)'s row groups are dealt to unit_parts parts, a part to an XCD, which takes the
+  // q-th group of all of its parts before the next; groups of 128 rows of a head, the ones with the most keys first
+  const int n = blockIdx.x;
+  const int here = a.units * a.unit_parts / 8;
+  const int q_group = (n >> 3) / here;
+  const int vu = (n & 7) + 8 * ((n >> 3) - q_group * here);
+  const int u = vu / a.unit_parts;
+  const int rg = q_group * a.unit_parts + (vu - u * a.unit_parts);
+  if (rg >= a.row_groups) return;
+  const int b = u / a.Hkv, g = u - b * a.Hkv;
+  const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int T = a.T;
+  const int blk = a.groups_per_head - 1 - rg / a.G, hh = rg - (rg / a.G) * a.G;
+  const int i0 = blk * kRowsWg;                      // the workgroup's first row
+  const int rows_here = min(T - i0, kRowsWg);
+  const size_t row0 = ((size_t)b * a.Hq + (size_t)g * a.G + hh) * T + i0;
+
+  int nb = T;
+  if (a.row_len) nb = min(max(a.row_len[b], 0), T);
+  const int Lp = min(max(a.kv_len[b], 0), a.S_cap - nb);
+  const int i_last = min(i0 + rows_here, nb) - 1;    // the last live row (< i0: none)
+  const int N = i_last >= i0 ? Lp + i_last + 1 : 0;  // slots that some row sees: [0, sink_end) and [low, N)
+  int low = 0, sink_end = 0, sink_tiles = 0, gap = 0;
+  if (a.window > 0 && N > 0) {
+    low = max(Lp + i0 - a.window + 1, 0);
+    sink_end = min(a.sinks, low);
+    sink_tiles = (sink_end + kTile - 1) / kTile * kTile;
+    gap = max(low / kTile * kTile - sink_tiles, 0);
+  }
+  auto slot_of = [&](int key) { return key < sink_tiles ? key : key + gap; };   // (of a tile's keys)
+  const int tiles = (N - gap + kTile - 1) / kTile;
+  const int periods = tiles > 0 ? tiles / 2 + 1 : 0;
+
+  // ---- copies.  Stage j: key blocks of 16 from key 64 j on, value blocks from key 64 j - 32 on; wave w brings block w
+  // of either.  (The value blocks before the first key repeat it, unread; those past the last tile are some page's.)
+  typedef const __attribute__((address_space(4))) int32_t* const_table;
+  const const_table table = (const_table)(uintptr_t)(a.table + (size_t)b * a.width);
+  const int ps1 = (1 << a.page_shift) - 1;
+  const size_t head_off = ((size_t)g << a.page_shift) * L::ROW;
+  const unsigned char* kbase = (const unsigned char*)a.k + head_off;
+  const unsigned char* vbase = (const unsigned char*)a.v + head_off;
+  const uint32_t ring_lds = __builtin_amdgcn_readfirstlane(lds_addr(ring));
+  auto key_slot = [&](int j) { return slot_of(j * 2 * kTile + 16 * wave); };
+  auto value_slot = [&](int j) { return slot_of(max(j * 2 * kTile - kTile + 16 * wave, 0)); };
+  int key_page = 0, value_page = 0;
+  auto look_up = [&](int j) {
+    key_page = table[min(key_slot(j) >> a.page_shift, a.width - 1)];
+    value_page = table[min(value_slot(j) >> a.page_shift, a.width - 1)];
+  };
+  uint32_t coff[L::COPIES];
+#pragma unroll
+  for (int c = 0; c < L::COPIES; ++c) {
+    const int e = c * 64 + lane, r = e / L::CPR, p = e - r * L::CPR;
+    coff[c] = (uint32_t)(r * L::ROW + ((p ^ L::swz(r)) << 4));
+  }
+  auto issue = [&](int j) {
+    const uint32_t dst = ring_lds + (j % L::STAGES) * L::STAGE + wave * L::BLOCK;
+    const int kp = min(max(key_page, 0), a.num_pages - 1), vp = min(max(value_page, 0), a.num_pages - 1);
+    const unsigned char* ks = kbase + (int64_t)kp * a.page_stride + (int64_t)(key_slot(j) & ps1) * L::ROW;
+    const unsigned char* vs = vbase + (int64_t)vp * a.page_stride + (int64_t)(value_slot(j) & ps1) * L::ROW;
+#pragma unroll
+    for (int c = 0; c < L::COPIES; ++c) copy16_to_lds(dst + c * 1024, ks, coff[c]);
+#pragma unroll
+    for (int c = 0; c < L::COPIES; ++c) copy16_to_lds(dst + L::HALF + c * 1024, vs, coff[c]);
+    look_up(j + 1);
+  };
+  // this wave's rows of stage j that no row of the workgroup sees become zeros
+  auto zero_unseen = [&](int j) {
+    unsigned char* at = ring + (j % L::STAGES) * L::STAGE + wave * L::BLOCK;
+#pragma unroll
+    for (int part = 0; part < 2; ++part) {
+      const int s0 = part ? value_slot(j) : key_slot(j);
+      if (s0 + 16 > N || (s0 < low && s0 + 16 > sink_end)) {
+        constexpr int LPR = 4, PER = L::CPR / LPR;     // 4 lanes a row
+        const int s = s0 + lane / LPR;
+        if (s >= N || (s < low && s >= sink_end)) {
+#pragma unroll
+          for (int c = 0; c < PER; ++c)
+            *(u32x4*)(at + part * L::HALF + (lane / LPR) * L::ROW + ((lane % LPR) * PER + c) * 16) = u32x4{0u, 0u, 0u, 0u};
+        }
+      }
+    }
+  };
+
+  // ---- queries: B operand of the score products, row col of the wave, 8 columns from 16 ds + 8 h on
+  const int row = wave * kRows + col;                // this lane's row of the workgroup
+  bf16x8 qf[KS];
+  {
+    const unsigned char* src = (const unsigned char*)a.q + (row0 + min(row, rows_here - 1)) * L::ROW;
+#pragma unroll
+    for (int ds = 0; ds < KS; ++ds) qf[ds] = *(const bf16x8*)(src + (ds * 16 + 8 * h) * 2);
+  }
+  const bool live = row < rows_here && i0 + row < nb;
+  const float c_scale = fmaxf(fabsf(a.scale_log2), 1.17549435e-38f);
+#pragma unroll
+  for (int ds = 0; ds < KS; ++ds) {
+    u32x4 x = __builtin_bit_cast(u32x4, qf[ds]);
+    if (a.scale_log2 < 0.f) x ^= 0x80008000u;        // (a negative scale flips the queries' signs, exact)
+    if (!live) x = u32x4{0u, 0u, 0u, 0u};            // (rows past the sequence's own may hold anything)
+    qf[ds] = __builtin_bit_cast(bf16x8, x);
+  }
+  look_up(0);
+  for (int j = 0; j < AHEAD; ++j)
+    if (j < periods) issue(j);
+
+  // what the rows see
+  const int pos = Lp + i0 + row;
+  const int see_from = a.window > 0 ? pos - a.window + 1 : 0, see_to = live ? pos : -1;
+  const int wave_first = Lp + i0 + wave * kRows;
+  const int wave_last = min(wave_first + kRows - 1, Lp + i_last);
+  const int plain_from = a.window > 0 ? wave_last - a.window + 1 : 0;
+  // tiles of this wave: those up to its last row's slot (in key numbers: the slot less the gap)
+  const int wave_tiles = wave_last < wave_first ? 0 : min(tiles, (wave_last - gap) / kTile + 1);
+
+  f32x16 o[DB];
+  float m = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+
+  const int tr_row = 4 * h + ((lane & 15) >> 2);     // transposed read: this lane's row of 4 and its piece of 16 columns
+  const int tr_c = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1), tr_half = (lane & 1) * 8;
+
+  // scores of tile k (key tile k % 2 of its stage)
+  auto scores = [&](f32x16& s, int k) {
+    const unsigned char* kt = ring + ((k >> 1) % L::STAGES) * L::STAGE + (k & 1) * (kTile * L::ROW);
+    bf16x8 kf[KS];
+#pragma unroll
+    for (int ds = 0; ds < KS; ++ds) kf[ds] = *(const bf16x8*)(kt + L::off(col, ds * 2 + h));
+    const int s0 = slot_of(k * kTile);
+    if (s0 + kTile - 1 > wave_first || (s0 < plain_from && s0 + kTile > a.sinks)) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int key = s0 + 8 * (i >> 2) + 4 * h + (i & 3);
+        const bool vis = (key <= see_to) & ((key >= see_from) | (key < a.sinks));
+        s[i] = vis ? 0.f : -INFINITY;
+      }
+#pragma unroll
+      for (int ds = 0; ds < KS; ++ds) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ds], qf[ds], s, 0, 0, 0);
+    } else {
+      f32x16 z;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) z[i] = 0.f;
+      s = z;
+#pragma unroll
+      for (int ds = 0; ds < KS; ++ds) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ds], qf[ds], s, 0, 0, 0);
+    }
+  };
+  // the reference moves where a score passes it by more than 2^8 (rare after the first tiles)
+  auto move_reference = [&](const f32x16& s) {
+    float x = vmax(vmax(s[0], s[1]), s[2]);
+#pragma unroll
+    for (int i = 3; i < 15; i += 2) x = vmax(vmax(x, s[i]), s[i + 1]);
+    x = vmax(x, s[15]);
+    const float top = c_scale * x;
+    if (__any(top > m + kLazyLog2)) {
+      const float t = fmaxf(top, __shfl_xor(top, 32));
+      if (t > m + kLazyLog2) {
+        const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - t);
+        m = t;
+        l *= alpha;
+#pragma unroll
+        for (int d = 0; d < DB; ++d) o[d] *= alpha;
+      }
+    }
+  };
+  // exponentials of tile k and its value product (value tile of stage (k + 1) / 2)
+  auto values = [&](const f32x16& s, int k) {
+    const unsigned char* vt =
+        ring + (((k + 1) >> 1) % L::STAGES) * L::STAGE + L::HALF + ((k + 1) & 1) * (kTile * L::ROW);
+    const float m_use = m == -INFINITY ? 0.f : m;
+    float sum = 0.f;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      bf16x8 p;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float e = __builtin_amdgcn_exp2f(fmaf(s[8 * t + i], c_scale, -m_use));
+        sum += e;
+        p[i] = (__bf16)e;
+      }
+#pragma unroll
+      for (int d = 0; d < DB; ++d) {
+        const int c = d * 4 + tr_c;
+        bf16x8 va;
+        const bf16x4 lo = __builtin_bit_cast(
+            bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                        (__attribute__((address_space(3))) s16x4*)(vt + L::off(16 * t + tr_row, c) + tr_half)));
+        const bf16x4 hi = __builtin_bit_cast(
+            bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                        (__attribute__((address_space(3))) s16x4*)(vt + L::off(16 * t + 8 + tr_row, c) + tr_half)));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          va[i] = lo[i];
+          va[4 + i] = hi[i];
+        }
+        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, p, o[d], 0, 0, 0);
+      }
+    }
+    l += sum;
+  };
+
+  f32x16 s0, s1;   // of even and odd tiles
+  for (int j = 0; j < periods; ++j) {
+    // this wave's copies of stage j have landed (those of the AHEAD - 1 stages after it may be in flight)
+    if (j + AHEAD <= periods) wait_vm<(AHEAD - 1) * CP>(); else wait_vm<0>();
+    zero_unseen(j);
+    barrier_lds();   // stage j complete for every wave; every wave is past stage j - 1, whose slot is free
+    if (j + AHEAD < periods) issue(j + AHEAD);
+    const int k = 2 * j;
+    if (k < wave_tiles) scores(s0, k);
+    if (k >= 1 && k - 1 < wave_tiles) values(s1, k - 1);
+    if (k < wave_tiles) move_reference(s0);
+    if (k + 1 < wave_tiles) scores(s1, k + 1);
+    if (k < wave_tiles) values(s0, k);
+    if (k + 1 < wave_tiles) move_reference(s1);
+  }
+
+  // ---- the rows' sums (two lanes a row), then the output through LDS in whole rows
+  l += __shfl_xor(l, 32);
+  barrier_lds();   // every wave is done with the ring
+  const float inv = live && l > 0.f ? 1.0f / l : 0.f;
+  unsigned char* mine = ring + wave * (kRows * L::ROW);
+  auto piece = [&](int r, int c) { return mine + r * L::ROW + ((c ^ (r & (L::CPR - 1))) << 4); };
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      bf16x4 x;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = (__bf16)(live ? o[d][i + e] * inv : 0.f);
+      *(bf16x4*)(piece(col, d * 4 + (i >> 2)) + 8 * h) = x;
+    }
+  if (a.lse && h == 0 && row < rows_here) a.lse[row0 + row] = live && l > 0.f ? (m + __log2f(l)) * kLn2 : -INFINITY;
+  __builtin_amdgcn_s_waitcnt(0xC07F);
+  asm volatile("" ::: "memory");
+#pragma unroll
+  for (int x = 0; x < kRows * L::CPR / 64; ++x) {
+    const int e = x * 64 + lane, r = e / L::CPR, c = e - r * L::CPR;
+    if (wave * kRows + r < rows_here)
+      *(u32x4*)((unsigned char*)a.out + (row0 + wave * kRows + r) * L::ROW + c * 16) = *(const u32x4*)piece(r, c);
+  }
+}
+
+template <int D>
+hipError_t launch(const AttnArgs& a, hipStream_t stream) {
+  constexpr int lds = 65536;
+  static bool configured = false;
+  if (!configured) {
+    hipError_t e = hipFuncSetAttribute((const void*)paged_prompt_bf16_kernel<D>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e != hipSuccess) return e;
+    configured = true;
+  }
+  const unsigned groups = (a.row_groups + a.unit_parts - 1) / a.unit_parts;
+  hipLaunchKernelGGL(paged_prompt_bf16_kernel<D>, dim3((unsigned)a.units * a.unit_parts * groups), dim3(64 * kWaves), lds,
+                     stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_paged_prompt_bf16(const AttnArgs& a, hipStream_t stream) {
+  if (a.unit_parts < 1 || a.units * a.unit_parts % 8 != 0 || a.groups_per_head * a.G != a.row_groups)
+    return hipErrorInvalidValue;
+  if (a.D == 128) return launch<128>(a, stream);
+  if (a.D == 64) return launch<64>(a, stream);
+  return hipErrorInvalidValue;
+}
+
+}  // namespace dreams
