@@ -18,6 +18,7 @@
 #include "kernels.h"
 
 #include <math.h>
+#include <type_traits>
 
 namespace dreams {
 namespace {
@@ -131,21 +132,18 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_prompt_bf16_kernel(AttnA
     key_page = table[min(key_slot(j) >> a.page_shift, a.width - 1)];
     value_page = table[min(value_slot(j) >> a.page_shift, a.width - 1)];
   };
-  uint32_t coff[L::COPIES];
-#pragma unroll
-  for (int c = 0; c < L::COPIES; ++c) {
-    const int e = c * 64 + lane, r = e / L::CPR, p = e - r * L::CPR;
-    coff[c] = (uint32_t)(r * L::ROW + ((p ^ L::swz(r)) << 4));
-  }
+  // (lane's offset of copy 0; copy c is 1 KB on, its rows' swizzle differs by swz(first row of c))
+  const uint32_t coff0 = (uint32_t)((lane / L::CPR) * L::ROW + (((lane % L::CPR) ^ L::swz(lane / L::CPR)) << 4));
+  auto coff = [&](int c) { return (coff0 ^ (uint32_t)(L::swz(c * (64 / L::CPR)) << 4)) + c * 1024; };
   auto issue = [&](int j) {
     const uint32_t dst = ring_lds + (j % L::STAGES) * L::STAGE + wave * L::BLOCK;
     const int kp = min(max(key_page, 0), a.num_pages - 1), vp = min(max(value_page, 0), a.num_pages - 1);
     const unsigned char* ks = kbase + (int64_t)kp * a.page_stride + (int64_t)(key_slot(j) & ps1) * L::ROW;
     const unsigned char* vs = vbase + (int64_t)vp * a.page_stride + (int64_t)(value_slot(j) & ps1) * L::ROW;
 #pragma unroll
-    for (int c = 0; c < L::COPIES; ++c) copy16_to_lds(dst + c * 1024, ks, coff[c]);
+    for (int c = 0; c < L::COPIES; ++c) copy16_to_lds(dst + c * 1024, ks, coff(c));
 #pragma unroll
-    for (int c = 0; c < L::COPIES; ++c) copy16_to_lds(dst + L::HALF + c * 1024, vs, coff[c]);
+    for (int c = 0; c < L::COPIES; ++c) copy16_to_lds(dst + L::HALF + c * 1024, vs, coff(c));
     look_up(j + 1);
   };
   // this wave's rows of stage j that no row of the workgroup sees become zeros
@@ -206,29 +204,42 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_prompt_bf16_kernel(AttnA
   const int tr_row = 4 * h + ((lane & 15) >> 2);     // transposed read: this lane's row of 4 and its piece of 16 columns
   const int tr_c = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1), tr_half = (lane & 1) * 8;
 
-  // scores of tile k (key tile k % 2 of its stage)
-  auto scores = [&](f32x16& s, int k) {
-    const unsigned char* kt = ring + ((k >> 1) % L::STAGES) * L::STAGE + (k & 1) * (kTile * L::ROW);
-    bf16x8 kf[KS];
+  // Operand addresses within a tile: the swizzle leaves one offset per 32 (keys: 16) columns, the rest are constants.
+  uint32_t koff[KS], voff[DB][2];
 #pragma unroll
-    for (int ds = 0; ds < KS; ++ds) kf[ds] = *(const bf16x8*)(kt + L::off(col, ds * 2 + h));
-    const int s0 = slot_of(k * kTile);
-    if (s0 + kTile - 1 > wave_first || (s0 < plain_from && s0 + kTile > a.sinks)) {
+  for (int ds = 0; ds < KS; ++ds) koff[ds] = ring_lds + L::off(col, ds * 2 + h);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int key = s0 + 8 * (i >> 2) + 4 * h + (i & 3);
-        const bool vis = (key <= see_to) & ((key >= see_from) | (key < a.sinks));
-        s[i] = vis ? 0.f : -INFINITY;
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int x = 0; x < 2; ++x) voff[d][x] = ring_lds + L::HALF + L::off(8 * x + tr_row, d * 4 + tr_c) + tr_half;
+  typedef __attribute__((address_space(3))) const bf16x8 lds_bf16x8;
+  typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+  // kt, vt: byte offsets of a tile's keys (values) in the ring, constants in the unrolled loop
+  auto read_keys = [&](bf16x8 (&kf)[KS], int kt) {
+#pragma unroll
+    for (int ds = 0; ds < KS; ++ds) kf[ds] = *(lds_bf16x8*)(uintptr_t)(koff[ds] + kt);
+  };
+  auto read_values = [&](bf16x8 (&va)[DB], int vt, int t) {
+#pragma unroll
+    for (int d = 0; d < DB; ++d) {
+      const bf16x4 lo = __builtin_bit_cast(
+          bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)(voff[d][0] + vt + 16 * t * L::ROW)));
+      const bf16x4 hi = __builtin_bit_cast(
+          bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)(voff[d][1] + vt + 16 * t * L::ROW)));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        va[d][i] = lo[i];
+        va[d][4 + i] = hi[i];
       }
+    }
+  };
+  // where the products of a tile start if some key is out of some row's sight: 0 or -inf
+  auto mask = [&](f32x16& s, int s0) {
 #pragma unroll
-      for (int ds = 0; ds < KS; ++ds) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ds], qf[ds], s, 0, 0, 0);
-    } else {
-      f32x16 z;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) z[i] = 0.f;
-      s = z;
-#pragma unroll
-      for (int ds = 0; ds < KS; ++ds) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ds], qf[ds], s, 0, 0, 0);
+    for (int i = 0; i < 16; ++i) {
+      const int key = s0 + 8 * (i >> 2) + 4 * h + (i & 3);
+      const bool vis = (key <= see_to) & ((key >= see_from) | (key < a.sinks));
+      s[i] = vis ? 0.f : -INFINITY;
     }
   };
   // the reference moves where a score passes it by more than 2^8 (rare after the first tiles)
@@ -249,57 +260,121 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_prompt_bf16_kernel(AttnA
       }
     }
   };
-  // exponentials of tile k and its value product (value tile of stage (k + 1) / 2)
-  auto values = [&](const f32x16& s, int k) {
-    const unsigned char* vt =
-        ring + (((k + 1) >> 1) % L::STAGES) * L::STAGE + L::HALF + ((k + 1) & 1) * (kTile * L::ROW);
+  // One basic block, in this order: the scores of the next tile (NEXT; MASKED: starting from its mask in sn) beside the
+  // exponentials of this one (THIS), then its value product.
+  auto block = [&](auto next, auto masked, auto current, f32x16& sn, int kt, const f32x16& sc, int vt) {
+    constexpr bool NEXT = decltype(next)::value, MASKED = decltype(masked)::value, THIS = decltype(current)::value;
+    bf16x8 kf[KS], va[DB], vb[DB];
+    bf16x8 p[2];
     const float m_use = m == -INFINITY ? 0.f : m;
-    float sum = 0.f;
+    float sum0 = 0.f, sum1 = 0.f;
+    auto score = [&](int ds) {
+      if constexpr (NEXT) {
+        f32x16 z;
+        if (ds == 0 && !MASKED) {
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      bf16x8 p;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float e = __builtin_amdgcn_exp2f(fmaf(s[8 * t + i], c_scale, -m_use));
-        sum += e;
-        p[i] = (__bf16)e;
-      }
-#pragma unroll
-      for (int d = 0; d < DB; ++d) {
-        const int c = d * 4 + tr_c;
-        bf16x8 va;
-        const bf16x4 lo = __builtin_bit_cast(
-            bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (__attribute__((address_space(3))) s16x4*)(vt + L::off(16 * t + tr_row, c) + tr_half)));
-        const bf16x4 hi = __builtin_bit_cast(
-            bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (__attribute__((address_space(3))) s16x4*)(vt + L::off(16 * t + 8 + tr_row, c) + tr_half)));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          va[i] = lo[i];
-          va[4 + i] = hi[i];
+          for (int i = 0; i < 16; ++i) z[i] = 0.f;
+        } else {
+          z = sn;
         }
-        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, p, o[d], 0, 0, 0);
+        sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ds], qf[ds], z, 0, 0, 0);
       }
-    }
-    l += sum;
+    };
+    auto weights = [&](int i) {   // of two keys
+      if constexpr (THIS) {
+        const float e0 = __builtin_amdgcn_exp2f(fmaf(sc[i], c_scale, -m_use));
+        const float e1 = __builtin_amdgcn_exp2f(fmaf(sc[i + 1], c_scale, -m_use));
+        sum0 += e0;
+        sum1 += e1;
+        p[i / 8][i % 8] = (__bf16)e0;
+        p[i / 8][i % 8 + 1] = (__bf16)e1;
+      }
+    };
+    auto value = [&](const bf16x8 (&v)[DB], int t, int d) {
+      if constexpr (THIS) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[d], p[t], o[d], 0, 0, 0);
+    };
+#define FENCE __builtin_amdgcn_sched_barrier(0)
+    FENCE;
+    if constexpr (NEXT) read_keys(kf, kt);
+    FENCE;
+    weights(0); weights(2); FENCE;
+    constexpr int Q = KS / 4;   // score products per quarter
+#pragma unroll
+    for (int x = 0; x < Q; ++x) { score(x); }
+    weights(4); FENCE;
+#pragma unroll
+    for (int x = 0; x < Q; ++x) { score(Q + x); }
+    if constexpr (THIS) read_values(va, vt, 0);
+    weights(6); FENCE;
+#pragma unroll
+    for (int x = 0; x < Q; ++x) { score(2 * Q + x); }
+    weights(8); FENCE;
+#pragma unroll
+    for (int x = 0; x < Q; ++x) { score(3 * Q + x); }
+    if constexpr (THIS) read_values(vb, vt, 1);
+    weights(10); FENCE;
+#pragma unroll
+    for (int d = 0; d < DB / 2; ++d) value(va, 0, d);
+    weights(12); FENCE;
+#pragma unroll
+    for (int d = DB / 2; d < DB; ++d) value(va, 0, d);
+    weights(14); FENCE;
+#pragma unroll
+    for (int d = 0; d < DB; ++d) value(vb, 1, d);
+    if constexpr (THIS) l += sum0 + sum1;
+#undef FENCE
   };
-
-  f32x16 s0, s1;   // of even and odd tiles
-  for (int j = 0; j < periods; ++j) {
+  constexpr std::true_type yes{};
+  constexpr std::false_type no{};
+  auto next_stage = [&](int j) {
     // this wave's copies of stage j have landed (those of the AHEAD - 1 stages after it may be in flight)
     if (j + AHEAD <= periods) wait_vm<(AHEAD - 1) * CP>(); else wait_vm<0>();
     zero_unseen(j);
     barrier_lds();   // stage j complete for every wave; every wave is past stage j - 1, whose slot is free
     if (j + AHEAD < periods) issue(j + AHEAD);
-    const int k = 2 * j;
-    if (k < wave_tiles) scores(s0, k);
-    if (k >= 1 && k - 1 < wave_tiles) values(s1, k - 1);
-    if (k < wave_tiles) move_reference(s0);
-    if (k + 1 < wave_tiles) scores(s1, k + 1);
-    if (k < wave_tiles) values(s0, k);
-    if (k + 1 < wave_tiles) move_reference(s1);
+  };
+  f32x16 s0, s1;     // scores of even and odd tiles (tile -1: none)
+#pragma unroll
+  for (int i = 0; i < 16; ++i) s1[i] = -INFINITY;
+  // Periods (stages) [0, plain0) and [plain1, periods) take their tiles masked, those between are in sight of all of the
+  // wave's rows; every wave passes every stage's barrier, in whichever loop.
+  auto edge_step = [&](int k, f32x16& sn, const f32x16& sc, int t) {   // scores of tile k, values of tile k - 1
+    if (k < wave_tiles) {
+      mask(sn, slot_of(k * kTile));
+      block(yes, yes, yes, sn, t, sc, t);
+      move_reference(sn);
+    } else if (k == wave_tiles) {
+      block(no, no, yes, sn, t, sc, t);
+    }
+  };
+  auto edge_periods = [&](int from, int to) {
+    for (int j0 = from; j0 < to; j0 += L::STAGES) {
+#pragma unroll
+      for (int x = 0; x < L::STAGES; ++x) {
+        const int j = j0 + x;
+        if (j >= to) break;
+        next_stage(j);
+        edge_step(2 * j, s0, s1, x * L::STAGE);
+        edge_step(2 * j + 1, s1, s0, x * L::STAGE + kTile * L::ROW);
+      }
+    }
+  };
+  const int first_plain = a.window > 0 ? max((plain_from - gap + kTile - 1) / kTile, 0) : 0;   // tiles
+  const int last_plain = wave_tiles > 0 ? max((wave_first + 1 - gap) / kTile, 0) : 0;
+  const int plain0 = min((first_plain + 2 * L::STAGES - 1) / (2 * L::STAGES) * L::STAGES, periods);
+  const int plain1 = max(last_plain / (2 * L::STAGES) * L::STAGES, plain0);
+  edge_periods(0, plain0);
+  for (int j0 = plain0; j0 < plain1; j0 += L::STAGES) {
+#pragma unroll
+    for (int x = 0; x < L::STAGES; ++x) {
+      next_stage(j0 + x);
+      block(yes, no, yes, s0, x * L::STAGE, s1, x * L::STAGE);
+      move_reference(s0);
+      block(yes, no, yes, s1, x * L::STAGE + kTile * L::ROW, s0, x * L::STAGE + kTile * L::ROW);
+      move_reference(s1);
+    }
   }
+  edge_periods(plain1, periods);
 
   // ---- the rows' sums (two lanes a row), then the output through LDS in whole rows
   l += __shfl_xor(l, 32);
