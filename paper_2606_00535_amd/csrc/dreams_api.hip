@@ -1397,6 +1397,8 @@ dreams_status_t run_paged(const dreams_paged_desc_t* desc, bool prompt, const Pa
   a.chain = in.prompt;
   a.groups_per_head = plan.groups_per_head;
   a.unit_parts = plan.unit_parts;
+  st = device_cus(&a.cus);
+  if (st != DREAMS_OK) return st;
   const bool rows = a.groups_per_head > 0 && a.splits == 1;
   hipError_t e = rows ? launch_paged_prompt_bf16(a, stream) : launch_paged_attn_bf16(a, stream);
   if (e != hipSuccess) return hip_fail(e, "paged attention launch");

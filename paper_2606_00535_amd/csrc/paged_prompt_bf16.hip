@@ -85,9 +85,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_prompt_bf16_kernel(AttnA
   // ---- work item: every (sequence, KV head)'s row groups are dealt to unit_parts parts, a part to an XCD, which takes the
   // q-th group of all of its parts before the next; groups of 128 rows of a head, the ones with the most keys first
   const int n = blockIdx.x;
+  // (Two workgroups to a compute unit: the second ones take their groups in the opposite order, so that the longest run
+  // beside the shortest of the first round.)
   const int here = a.units * a.unit_parts / 8;
-  const int q_group = (n >> 3) / here;
-  const int vu = (n & 7) + 8 * ((n >> 3) - q_group * here);
+  const int on_xcd = n >> 3, slots = a.cus / 4;
+  const int rank = on_xcd >= slots / 2 && on_xcd < slots && (int)(gridDim.x >> 3) >= slots ? slots + slots / 2 - 1 - on_xcd
+                                                                                             : on_xcd;
+  const int q_group = rank / here;
+  const int vu = (n & 7) + 8 * (rank - q_group * here);
   const int u = vu / a.unit_parts;
   const int rg = q_group * a.unit_parts + (vu - u * a.unit_parts);
   if (rg >= a.row_groups) return;
@@ -233,13 +238,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_prompt_bf16_kernel(AttnA
       }
     }
   };
-  // where the products of a tile start if some key is out of some row's sight: 0 or -inf
+  // keys out of a row's sight
   auto mask = [&](f32x16& s, int s0) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const int key = s0 + 8 * (i >> 2) + 4 * h + (i & 3);
       const bool vis = (key <= see_to) & ((key >= see_from) | (key < a.sinks));
-      s[i] = vis ? 0.f : -INFINITY;
+      s[i] = vis ? s[i] : -INFINITY;
     }
   };
   // the reference moves where a score passes it by more than 2^8 (rare after the first tiles)
@@ -260,10 +265,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_prompt_bf16_kernel(AttnA
       }
     }
   };
-  // One basic block, in this order: the scores of the next tile (NEXT; MASKED: starting from its mask in sn) beside the
-  // exponentials of this one (THIS), then its value product.
-  auto block = [&](auto next, auto masked, auto current, f32x16& sn, int kt, const f32x16& sc, int vt) {
-    constexpr bool NEXT = decltype(next)::value, MASKED = decltype(masked)::value, THIS = decltype(current)::value;
+  // One basic block, in this order: the scores of the next tile (NEXT) beside the exponentials of this one, then its value
+  // product.
+  auto block = [&](auto next, f32x16& sn, const f32x16& sc, int kt, int vt) {
+    constexpr bool NEXT = decltype(next)::value;
     bf16x8 kf[KS], va[DB], vb[DB];
     bf16x8 p[2];
     const float m_use = m == -INFINITY ? 0.f : m;
@@ -271,7 +276,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_prompt_bf16_kernel(AttnA
     auto score = [&](int ds) {
       if constexpr (NEXT) {
         f32x16 z;
-        if (ds == 0 && !MASKED) {
+        if (ds == 0) {
 #pragma unroll
           for (int i = 0; i < 16; ++i) z[i] = 0.f;
         } else {
@@ -281,17 +286,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_prompt_bf16_kernel(AttnA
       }
     };
     auto weights = [&](int i) {   // of two keys
-      if constexpr (THIS) {
-        const float e0 = __builtin_amdgcn_exp2f(fmaf(sc[i], c_scale, -m_use));
-        const float e1 = __builtin_amdgcn_exp2f(fmaf(sc[i + 1], c_scale, -m_use));
-        sum0 += e0;
-        sum1 += e1;
-        p[i / 8][i % 8] = (__bf16)e0;
-        p[i / 8][i % 8 + 1] = (__bf16)e1;
-      }
+      const float e0 = __builtin_amdgcn_exp2f(fmaf(sc[i], c_scale, -m_use));
+      const float e1 = __builtin_amdgcn_exp2f(fmaf(sc[i + 1], c_scale, -m_use));
+      sum0 += e0;
+      sum1 += e1;
+      p[i / 8][i % 8] = (__bf16)e0;
+      p[i / 8][i % 8 + 1] = (__bf16)e1;
     };
     auto value = [&](const bf16x8 (&v)[DB], int t, int d) {
-      if constexpr (THIS) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[d], p[t], o[d], 0, 0, 0);
+      o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[d], p[t], o[d], 0, 0, 0);
     };
 #define FENCE __builtin_amdgcn_sched_barrier(0)
     FENCE;
@@ -304,14 +307,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_prompt_bf16_kernel(AttnA
     weights(4); FENCE;
 #pragma unroll
     for (int x = 0; x < Q; ++x) { score(Q + x); }
-    if constexpr (THIS) read_values(va, vt, 0);
+    read_values(va, vt, 0);
     weights(6); FENCE;
 #pragma unroll
     for (int x = 0; x < Q; ++x) { score(2 * Q + x); }
     weights(8); FENCE;
 #pragma unroll
     for (int x = 0; x < Q; ++x) { score(3 * Q + x); }
-    if constexpr (THIS) read_values(vb, vt, 1);
+    read_values(vb, vt, 1);
     weights(10); FENCE;
 #pragma unroll
     for (int d = 0; d < DB / 2; ++d) value(va, 0, d);
@@ -321,7 +324,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_prompt_bf16_kernel(AttnA
     weights(14); FENCE;
 #pragma unroll
     for (int d = 0; d < DB; ++d) value(vb, 1, d);
-    if constexpr (THIS) l += sum0 + sum1;
+    l += sum0 + sum1;
 #undef FENCE
   };
   constexpr std::true_type yes{};
@@ -336,45 +339,36 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_prompt_bf16_kernel(AttnA
   f32x16 s0, s1;     // scores of even and odd tiles (tile -1: none)
 #pragma unroll
   for (int i = 0; i < 16; ++i) s1[i] = -INFINITY;
-  // Periods (stages) [0, plain0) and [plain1, periods) take their tiles masked, those between are in sight of all of the
-  // wave's rows; every wave passes every stage's barrier, in whichever loop.
-  auto edge_step = [&](int k, f32x16& sn, const f32x16& sc, int t) {   // scores of tile k, values of tile k - 1
-    if (k < wave_tiles) {
-      mask(sn, slot_of(k * kTile));
-      block(yes, yes, yes, sn, t, sc, t);
-      move_reference(sn);
-    } else if (k == wave_tiles) {
-      block(no, no, yes, sn, t, sc, t);
-    }
-  };
-  auto edge_periods = [&](int from, int to) {
-    for (int j0 = from; j0 < to; j0 += L::STAGES) {
+  // tiles [far0, far1) that no row of the wave sees: from behind the sinks to its first row's (without a gap, the sinks may
+  // reach into the run)
+  const int far0 = gap > 0 ? sink_tiles / kTile : a.sinks > 0 ? (a.sinks - 1) / kTile + 1 : 0;
+  const int far1 = a.window > 0 ? (wave_first - a.window + 1 - gap) / kTile : 0;
+  auto step = [&](int k, f32x16& sn, const f32x16& sc, int t) {   // scores of tile k, values of tile k - 1
+    if (k >= wave_tiles) return;
+    if (k > far0 && k < far1) {      // (tile far0, too, is all masked: it takes the value product of the one before)
 #pragma unroll
-      for (int x = 0; x < L::STAGES; ++x) {
-        const int j = j0 + x;
-        if (j >= to) break;
-        next_stage(j);
-        edge_step(2 * j, s0, s1, x * L::STAGE);
-        edge_step(2 * j + 1, s1, s0, x * L::STAGE + kTile * L::ROW);
-      }
+      for (int i = 0; i < 16; ++i) sn[i] = -INFINITY;
+      return;
     }
+    block(yes, sn, sc, t, t);
+    const int s0 = slot_of(k * kTile);
+    if (s0 + kTile - 1 > wave_first || (s0 < plain_from && s0 + kTile > a.sinks)) mask(sn, s0);
+    move_reference(sn);
   };
-  const int first_plain = a.window > 0 ? max((plain_from - gap + kTile - 1) / kTile, 0) : 0;   // tiles
-  const int last_plain = wave_tiles > 0 ? max((wave_first + 1 - gap) / kTile, 0) : 0;
-  const int plain0 = min((first_plain + 2 * L::STAGES - 1) / (2 * L::STAGES) * L::STAGES, periods);
-  const int plain1 = max(last_plain / (2 * L::STAGES) * L::STAGES, plain0);
-  edge_periods(0, plain0);
-  for (int j0 = plain0; j0 < plain1; j0 += L::STAGES) {
+  for (int j0 = 0; j0 < periods; j0 += L::STAGES) {
 #pragma unroll
     for (int x = 0; x < L::STAGES; ++x) {
-      next_stage(j0 + x);
-      block(yes, no, yes, s0, x * L::STAGE, s1, x * L::STAGE);
-      move_reference(s0);
-      block(yes, no, yes, s1, x * L::STAGE + kTile * L::ROW, s0, x * L::STAGE + kTile * L::ROW);
-      move_reference(s1);
+      const int j = j0 + x;
+      if (j >= periods) break;
+      next_stage(j);
+      step(2 * j, s0, s1, x * L::STAGE);
+      step(2 * j + 1, s1, s0, x * L::STAGE + kTile * L::ROW);
+      if (wave_tiles >> 1 == j) {   // the value product of the wave's last tile
+        if (wave_tiles & 1) s1 = s0;
+        block(no, s0, s1, 0, x * L::STAGE + (wave_tiles & 1) * (kTile * L::ROW));
+      }
     }
   }
-  edge_periods(plain1, periods);
 
   // ---- the rows' sums (two lanes a row), then the output through LDS in whole rows
   l += __shfl_xor(l, 32);
