@@ -6,6 +6,7 @@
 #include <stdarg.h>
 #include <stdio.h>
 
+#include <algorithm>
 #include <atomic>
 #include <mutex>
 #include <string>
@@ -1269,6 +1270,7 @@ PagedAttnArgs paged_args(const dreams_paged_desc_t* d, const void* q, const void
 struct PagedPlan {
   AttnPlan p;
   int groups_per_head, unit_parts;
+  int longest, shortest;   // keys of a row group, by the host's bound
 };
 
 dreams_status_t plan_paged(const dreams_paged_desc_t* d, bool prompt, PagedPlan* plan) {
@@ -1304,6 +1306,8 @@ dreams_status_t plan_paged(const dreams_paged_desc_t* d, bool prompt, PagedPlan*
     if (seen < keys) keys = seen;
   }
   const int n_keys = (int)keys;
+  plan->longest = n_keys;
+  plan->shortest = plan->groups_per_head > 0 && max_len + span < keys ? (int)(max_len + span) : n_keys;
   int parts = 1;
   while ((long long)p.units * parts % 8 != 0) parts *= 2;
   plan->unit_parts = parts;
@@ -1314,10 +1318,18 @@ dreams_status_t plan_paged(const dreams_paged_desc_t* d, bool prompt, PagedPlan*
     st = device_cus(&cus);
     if (st != DREAMS_OK) return st;
     const int wpc = tree_attn_bf16_wgs_per_cu(p.rows_per_wg);
+    const long long xcd_cus = cus / 8;
     splits = coarse_splits(8 * xcd_wgs, (long long)cus * wpc, n_keys);
     if (splits > kAttnMaxSplits) splits = kAttnMaxSplits;
-    const long long xcd_cus = cus / 8;
-    if (splits > 1 && xcd_wgs < xcd_cus * wpc) {
+    if (p.rows_per_wg == 128) {
+      // Key groups in a workgroup first (paged_key_groups): pieces as far as every workgroup has a compute unit of its own;
+      // or, where that leaves much of the chip idle and the row groups are about as long, workgroups of one key group, two to
+      // a unit.
+      const long long long_enough = n_keys / kPlanPieceKeys;
+      const long long whole = std::min(xcd_cus / xcd_wgs, long_enough), two = std::min(2 * xcd_cus / xcd_wgs, long_enough);
+      const bool level = 10LL * plan->shortest >= 6LL * plan->longest;
+      splits = (int)(level && 5 * two >= 12 * std::max(whole, 1LL) ? two : whole);
+    } else if (splits > 1 && xcd_wgs < xcd_cus * wpc) {
       const int fine = fine_splits(xcd_wgs, xcd_cus, wpc, n_keys);
       if (fine < splits || 5 * fine >= 7 * splits) splits = fine;
     }
@@ -1336,6 +1348,20 @@ dreams_status_t plan_paged(const dreams_paged_desc_t* d, bool prompt, PagedPlan*
     p.bytes = attn_partial_bytes(&p, splits, d->head_dim);
   }
   return DREAMS_OK;
+}
+
+// Key groups of a workgroup of 128 rows: two (8 waves, one workgroup a compute unit) while every workgroup has a unit of its
+// own, where one group would leave half of it idle; else one (two workgroups a unit, not tied by each other's barriers: 896
+// row groups of 8192 rows 478 us, 530 with two groups; 448 of 8320 keys 285, 312).  In between, up to two to a unit, prompts
+// whose row groups differ much in length gain by the finer schedule of whole units: the longest should not share its unit to
+// the end.  The longest then runs beside no other, and the last ones to start, as long as the cus-th, behind the first to end:
+// 273 groups of up to 8990 keys 159 us, 196 with one group; 288 up to 1152 28, 33; but 288 of 4000 to 5152 146, 130.
+int paged_key_groups(const PagedPlan& plan, int cus) {
+  const long long wgs = (long long)plan.p.units * plan.p.row_groups * plan.p.splits;
+  if (wgs <= cus) return 2;
+  if (wgs > 2LL * cus || plan.p.splits > 1) return 1;
+  const double second = plan.shortest + (double)(plan.longest - plan.shortest) * (1.0 - (double)cus / (double)wgs);
+  return 2.0 * second <= 1.3 * plan.longest ? 2 : 1;
 }
 
 dreams_status_t run_paged(const dreams_paged_desc_t* desc, bool prompt, const PagedAttnArgs& in, void* workspace,
@@ -1399,8 +1425,8 @@ dreams_status_t run_paged(const dreams_paged_desc_t* desc, bool prompt, const Pa
   a.unit_parts = plan.unit_parts;
   st = device_cus(&a.cus);
   if (st != DREAMS_OK) return st;
-  const bool rows = a.groups_per_head > 0 && a.splits == 1;
-  hipError_t e = rows ? launch_paged_prompt_bf16(a, stream) : launch_paged_attn_bf16(a, stream);
+  a.key_groups = paged_key_groups(plan, a.cus);
+  hipError_t e = a.rows_per_wg == 128 ? launch_paged_rows_bf16(a, stream) : launch_paged_attn_bf16(a, stream);
   if (e != hipSuccess) return hip_fail(e, "paged attention launch");
   return ok();
 }

@@ -113,6 +113,7 @@ struct AttnArgs {
   int num_pages, page_shift, width, window, sinks;
   int chain;              // 1: row i of a head is position L_b + i; 0: tree nodes
   int groups_per_head;    // chain: row groups of a head, or 0: the heads' rows are packed one after another
+  int key_groups;         // 128 rows: key groups of 4 waves in a workgroup (1 or 2)
   int unit_parts;         // parts of a unit's row groups, each on one XCD; units * unit_parts is a multiple of 8
 };
 
@@ -333,8 +334,8 @@ struct PagedAttnArgs {
   int cus;
 };
 hipError_t launch_paged_attn_f32(const PagedAttnArgs& a, hipStream_t stream);
-hipError_t launch_paged_attn_bf16(const AttnArgs& a, hipStream_t stream);
-hipError_t launch_paged_prompt_bf16(const AttnArgs& a, hipStream_t stream);   // chain, groups_per_head > 0, one piece
+hipError_t launch_paged_attn_bf16(const AttnArgs& a, hipStream_t stream);   // up to 64 rows a KV head
+hipError_t launch_paged_rows_bf16(const AttnArgs& a, hipStream_t stream);   // 128 rows a workgroup
 
 struct PagedRowsArgs {
   char* k;                   // [NL][pages, Hkv, page_size, row bytes]

@@ -1,4 +1,5 @@
-// Attention over a paged cache, bf16: the builds of the kernel in tree_attn_bf16.h that read pages.
+// Attention over a paged cache, bf16, where a KV head has at most 64 rows: the builds of the kernel in tree_attn_bf16.h that
+// read pages.
 #include "tree_attn_bf16.h"
 
 namespace dreams {
@@ -10,7 +11,6 @@ hipError_t launch_for_rows(const AttnArgs& a, hipStream_t stream) {
     case 16: return launch_streaming<D, 1, 4, 4, NST, 1, false, true>(a, stream);
     case 32: return launch_streaming<D, 1, 4, 8, NST, 1, false, true>(a, stream);
     case 64: return launch_streaming<D, 2, 2, 4, NST / 2, 2, false, true>(a, stream);
-    case 128: return launch_streaming<D, 2, 1, 4, NST / 2, 2, false, true>(a, stream);
   }
   return hipErrorInvalidValue;
 }

@@ -15,51 +15,32 @@
 //     rows, from the pages that scalar loads of the table name a stage ahead.  Rows in LDS are XOR-swizzled: chunk c of
 //     row r at position c ^ swz(r), so that neither the 32-row key reads nor the 4 x 32 value reads conflict on banks.
 //   * Slots that no row sees are zeroed in LDS, so whatever they hold cannot reach the products.
-#include "kernels.h"
+#include "tree_attn_bf16.h"
 
-#include <math.h>
 #include <type_traits>
 
 namespace dreams {
 namespace {
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr float kLn2 = 0.69314718055994530942f;
-constexpr float kLazyLog2 = 8.0f;    // slack of the running maximum, log2 units
 constexpr int kTile = 32;            // keys per tile
 constexpr int kRows = 32;            // rows per wave
 constexpr int kWaves = 4;
 constexpr int kRowsWg = kRows * kWaves;
 
-typedef __attribute__((address_space(3))) void lds_void;
-__device__ __forceinline__ uint32_t lds_addr(const void* p) { return (uint32_t)(uintptr_t)(lds_void*)p; }
-// wave-wide 16-byte copy into LDS: lane l's 16 bytes, from a uniform base plus the lane's offset, land at m0 + 16 l
-__device__ __forceinline__ void copy16_to_lds(uint32_t m0, const void* sbase, uint32_t voff) {
+// wave-wide copy into LDS: lane l's 16 bytes, from a uniform base plus the lane's offset, land at m0 + 16 l.  (Without the
+// streaming hint: the query heads of a KV head read the same keys.)
+__device__ __forceinline__ void tile16_to_lds(uint32_t m0, const void* sbase, uint32_t voff) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(m0), "v"(voff), "s"(sbase)
                : "memory");
-}
-template <int N>
-__device__ __forceinline__ void wait_vm() {
-  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
-}
-// workgroup barrier once this wave's LDS accesses are done; copies stay in flight
-__device__ __forceinline__ void barrier_lds() {
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt(0xC07F);
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
 }
 
 // Rows of D bf16 in LDS.  A 256-byte bank line holds one row (D = 128) or two (D = 64).  A key read takes one 16-byte chunk
 // of 32 rows, 16 rows at a time: swz is a bijection over the 16 (8 of a parity) rows.  A value read takes 4 aligned
 // chunks of 4 consecutive rows: the rows differ in swz / 4 (or in their half of the line).
 template <int D>
-struct Rows {
+struct TileRows {
   static constexpr int ROW = D * 2, CPR = D / 8;
   static constexpr int BLOCK = 16 * ROW;            // bytes of 16 rows
   static constexpr int COPIES = BLOCK / 1024;       // wave-wide copies of a block
@@ -73,42 +54,59 @@ struct Rows {
   static __device__ __forceinline__ int off(int r, int c) { return r * ROW + ((c ^ swz(r)) << 4); }
 };
 
-template <int D>
-__global__ __launch_bounds__(64 * kWaves, 2) void paged_prompt_bf16_kernel(AttnArgs a) {
-  using L = Rows<D>;
+// KG: key groups of 4 waves (1 or 2), each on its half of the workgroup's tiles with a ring of its own; their states meet in
+// LDS at the end.  With several pieces of the key axis (workgroups), each takes its run of tiles, and the pieces merge as the
+// tree kernel's do.
+// TREE: tree nodes; else consecutive positions, in groups of one head's rows (groups_per_head > 0) or packed likewise.
+template <int D, int KG, bool TREE>
+__global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(AttnArgs a) {
+  using L = TileRows<D>;
   constexpr int KS = D / 16;        // products of a tile's scores
   constexpr int DB = D / 32;        // 32-column blocks of the output
   constexpr int AHEAD = L::STAGES - 1;
   constexpr int CP = 2 * L::COPIES; // copies a wave issues per stage
-  extern __shared__ __attribute__((aligned(1024))) unsigned char ring[];
+  extern __shared__ __attribute__((aligned(1024))) unsigned char rings[];
+  __shared__ float merge_lds[KG > 1 ? 2 * 64 * kWaves : 1];   // the second key group's maxima and sums
+  __shared__ uint32_t pieces_lds[2];                // (merge_set)
+  __shared__ int par_lds[TREE ? kMaxNodes : 1], depth_lds[TREE ? kMaxNodes : 1];
 
   // ---- work item: every (sequence, KV head)'s row groups are dealt to unit_parts parts, a part to an XCD, which takes the
   // q-th group of all of its parts before the next; groups of 128 rows of a head, the ones with the most keys first
-  const int n = blockIdx.x;
   // (Two workgroups to a compute unit: the second ones take their groups in the opposite order, so that the longest run
   // beside the shortest of the first round.)
+  const int n = blockIdx.x;
   const int here = a.units * a.unit_parts / 8;
-  const int on_xcd = n >> 3, slots = a.cus / 4;
+  const int on_xcd = n >> 3, slots = KG > 1 ? 1 << 30 : a.cus / 4;
   const int rank = on_xcd >= slots / 2 && on_xcd < slots && (int)(gridDim.x >> 3) >= slots ? slots + slots / 2 - 1 - on_xcd
                                                                                              : on_xcd;
-  const int q_group = rank / here;
-  const int vu = (n & 7) + 8 * (rank - q_group * here);
+  const int q_group = rank / (here * a.splits), within = rank - q_group * (here * a.splits);
+  const int vu = (n & 7) + 8 * (within / a.splits), split = within - (within / a.splits) * a.splits;
   const int u = vu / a.unit_parts;
   const int rg = q_group * a.unit_parts + (vu - u * a.unit_parts);
   if (rg >= a.row_groups) return;
   const int b = u / a.Hkv, g = u - b * a.Hkv;
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, h = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wave8 = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wave = wave8 % kWaves, kg = wave8 / kWaves;
+  unsigned char* ring = rings + kg * 65536;
   const int T = a.T;
-  const int blk = a.groups_per_head - 1 - rg / a.G, hh = rg - (rg / a.G) * a.G;
-  const int i0 = blk * kRowsWg;                      // the workgroup's first row
-  const int rows_here = min(T - i0, kRowsWg);
-  const size_t row0 = ((size_t)b * a.Hq + (size_t)g * a.G + hh) * T + i0;
+  // the workgroup's rows: [row_base, row_base + rows_here) of the KV head's G * T
+  int row_base = rg * kRowsWg, rows_here = a.G * T - row_base;
+  if (!TREE && a.groups_per_head > 0) {
+    const int blk = a.groups_per_head - 1 - rg / a.G, hh = rg - (rg / a.G) * a.G;
+    row_base = hh * T + blk * kRowsWg;
+    rows_here = T - blk * kRowsWg;
+  }
+  rows_here = min(rows_here, kRowsWg);
+  // the lowest position of a row, from the prefix on (of a chain's rows in one head: the first's)
+  const bool one_head = !TREE && row_base % T + rows_here <= T;
+  const int i0 = one_head ? row_base % T : 0;
+  const size_t row0 = ((size_t)b * a.Hq + (size_t)g * a.G) * T + row_base;
 
   int nb = T;
-  if (a.row_len) nb = min(max(a.row_len[b], 0), T);
+  if (!TREE && a.row_len) nb = min(max(a.row_len[b], 0), T);
   const int Lp = min(max(a.kv_len[b], 0), a.S_cap - nb);
-  const int i_last = min(i0 + rows_here, nb) - 1;    // the last live row (< i0: none)
+  const int i_last = TREE ? T - 1 : min(one_head ? i0 + rows_here : T, nb) - 1;   // the last live row's (< i0: none)
   const int N = i_last >= i0 ? Lp + i_last + 1 : 0;  // slots that some row sees: [0, sink_end) and [low, N)
   int low = 0, sink_end = 0, sink_tiles = 0, gap = 0;
   if (a.window > 0 && N > 0) {
@@ -118,8 +116,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_prompt_bf16_kernel(AttnA
     gap = max(low / kTile * kTile - sink_tiles, 0);
   }
   auto slot_of = [&](int key) { return key < sink_tiles ? key : key + gap; };   // (of a tile's keys)
-  const int tiles = (N - gap + kTile - 1) / kTile;
-  const int periods = tiles > 0 ? tiles / 2 + 1 : 0;
+  // the piece's tiles, and this key group's of them: [tile0, tile0 + tiles) (the first group's are never fewer: its count
+  // sets the barriers)
+  const int all_tiles = (N - gap + kTile - 1) / kTile, piece = (all_tiles + a.splits - 1) / a.splits;
+  const int begin = min(split * piece, all_tiles), piece_tiles = min(piece, all_tiles - begin);
+  const int half = (piece_tiles + KG - 1) / KG;
+  const int tile0 = begin + kg * half, tiles = min(half, piece_tiles - kg * half);
+  const int periods = half > 0 ? half / 2 + 1 : 0;
 
   // ---- copies.  Stage j: key blocks of 16 from key 64 j on, value blocks from key 64 j - 32 on; wave w brings block w
   // of either.  (The value blocks before the first key repeat it, unread; those past the last tile are some page's.)
@@ -130,8 +133,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_prompt_bf16_kernel(AttnA
   const unsigned char* kbase = (const unsigned char*)a.k + head_off;
   const unsigned char* vbase = (const unsigned char*)a.v + head_off;
   const uint32_t ring_lds = __builtin_amdgcn_readfirstlane(lds_addr(ring));
-  auto key_slot = [&](int j) { return slot_of(j * 2 * kTile + 16 * wave); };
-  auto value_slot = [&](int j) { return slot_of(max(j * 2 * kTile - kTile + 16 * wave, 0)); };
+  auto key_slot = [&](int j) { return slot_of((tile0 + j * 2) * kTile + 16 * wave); };
+  auto value_slot = [&](int j) { return slot_of(max((tile0 + j * 2) * kTile - kTile + 16 * wave, 0)); };
   int key_page = 0, value_page = 0;
   auto look_up = [&](int j) {
     key_page = table[min(key_slot(j) >> a.page_shift, a.width - 1)];
@@ -146,9 +149,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_prompt_bf16_kernel(AttnA
     const unsigned char* ks = kbase + (int64_t)kp * a.page_stride + (int64_t)(key_slot(j) & ps1) * L::ROW;
     const unsigned char* vs = vbase + (int64_t)vp * a.page_stride + (int64_t)(value_slot(j) & ps1) * L::ROW;
 #pragma unroll
-    for (int c = 0; c < L::COPIES; ++c) copy16_to_lds(dst + c * 1024, ks, coff(c));
+    for (int c = 0; c < L::COPIES; ++c) tile16_to_lds(dst + c * 1024, ks, coff(c));
 #pragma unroll
-    for (int c = 0; c < L::COPIES; ++c) copy16_to_lds(dst + L::HALF + c * 1024, vs, coff(c));
+    for (int c = 0; c < L::COPIES; ++c) tile16_to_lds(dst + L::HALF + c * 1024, vs, coff(c));
     look_up(j + 1);
   };
   // this wave's rows of stage j that no row of the workgroup sees become zeros
@@ -177,7 +180,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_prompt_bf16_kernel(AttnA
 #pragma unroll
     for (int ds = 0; ds < KS; ++ds) qf[ds] = *(const bf16x8*)(src + (ds * 16 + 8 * h) * 2);
   }
-  const bool live = row < rows_here && i0 + row < nb;
+  const int node = (row_base + min(row, rows_here - 1)) % T;   // the lane's tree node, or its position behind the prefix
+  const bool live = row < rows_here && (TREE || node < nb);
   const float c_scale = fmaxf(fabsf(a.scale_log2), 1.17549435e-38f);
 #pragma unroll
   for (int ds = 0; ds < KS; ++ds) {
@@ -186,18 +190,78 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_prompt_bf16_kernel(AttnA
     if (!live) x = u32x4{0u, 0u, 0u, 0u};            // (rows past the sequence's own may hold anything)
     qf[ds] = __builtin_bit_cast(bf16x8, x);
   }
+  // (this piece has started: see merge_set)
+  unsigned long long start_old = 0;
+  const size_t pset = (size_t)u * a.row_groups + rg;
+  if (a.splits > 1 && tid == 0) {
+    const unsigned long long x = xcd_id();
+    start_old = __hip_atomic_fetch_add(a.set_ctr + pset * a.ctr_stride,
+                                       1ull | (x << kCtrXcdSum) | ((x * x) << kCtrXcdSq), __ATOMIC_RELAXED,
+                                       __HIP_MEMORY_SCOPE_AGENT);
+  }
+  const bool parents = TREE && (!a.mask || a.window > 0);
+  if (parents && wave8 == 0)
+    for (int c = 0; c * 64 < T; ++c)
+      copy4_to_lds(__builtin_amdgcn_readfirstlane(lds_addr(par_lds)) + c * 256,
+                   a.parent + (size_t)b * T + min(c * 64 + lane, T - 1));
   look_up(0);
   for (int j = 0; j < AHEAD; ++j)
     if (j < periods) issue(j);
 
-  // what the rows see
-  const int pos = Lp + i0 + row;
+  // ---- what the rows see: of a chain the slots [see_from, see_to] and the sinks; of a tree the prefix from see_from on, the
+  // sinks, and the nodes in anc0, anc1
+  int pos = Lp + node, deepest = 0;
+  uint64_t anc0 = 0, anc1 = 0;
+  if constexpr (TREE) {
+    if (a.mask) {
+      const int words = (T + 63) / 64;
+      const uint64_t* bits = a.mask + ((size_t)b * T + node) * words;
+      anc0 = bits[0];
+      anc1 = words > 1 ? bits[1] : 0;
+    }
+    if (parents) {
+      wait_vm<0>();
+      __syncthreads();
+      auto walk = [&](int from, auto visit) {   // from a node to the root, or to an entry that breaks the rules
+        int j = from, d = 0;
+        for (;; ++d) {
+          visit(j);
+          const int p = par_lds[j];
+          if (p < 0 || p >= j) return d;
+          j = p;
+        }
+      };
+      if (a.window > 0) {
+        if (tid < T) depth_lds[tid] = walk(tid, [](int) {});
+        __syncthreads();
+        for (int j = lane; j < T; j += 64) deepest = max(deepest, depth_lds[j]);
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) deepest = max(deepest, __shfl_xor(deepest, off));
+        deepest = __builtin_amdgcn_readfirstlane(deepest);
+      }
+      if (!a.mask) walk(node, [&](int j) { (j < 64 ? anc0 : anc1) |= 1ull << (j & 63); });
+      pos = Lp;
+      if (a.window > 0) {
+        const int depth = depth_lds[node], far = depth - a.window;
+        pos += depth;
+        auto drop_far = [&](uint64_t& word, int first) {   // nodes out of sight
+          for (uint64_t rest = word; rest; rest &= rest - 1) {
+            const int j = __builtin_ctzll(rest), d = first + j < T ? depth_lds[first + j] : 0;
+            if (d <= far && Lp + d >= a.sinks) word &= ~(1ull << j);
+          }
+        };
+        drop_far(anc0, 0);
+        drop_far(anc1, 64);
+      }
+    }
+  }
   const int see_from = a.window > 0 ? pos - a.window + 1 : 0, see_to = live ? pos : -1;
-  const int wave_first = Lp + i0 + wave * kRows;
-  const int wave_last = min(wave_first + kRows - 1, Lp + i_last);
-  const int plain_from = a.window > 0 ? wave_last - a.window + 1 : 0;
+  // the last slot that every row of the wave may see, and the last that one of them does
+  const int wave_first = TREE ? Lp - 1 : one_head ? Lp + i0 + wave * kRows : Lp;
+  const int wave_last = one_head ? min(wave_first + kRows - 1, Lp + i_last) : N - 1;
+  const int plain_from = a.window > 0 ? (TREE ? Lp + deepest : wave_last) - a.window + 1 : 0;
   // tiles of this wave: those up to its last row's slot (in key numbers: the slot less the gap)
-  const int wave_tiles = wave_last < wave_first ? 0 : min(tiles, (wave_last - gap) / kTile + 1);
+  const int wave_tiles = wave_last < wave_first ? 0 : max(min(tiles, (wave_last - gap) / kTile + 1 - tile0), 0);
 
   f32x16 o[DB];
   float m = -INFINITY, l = 0.f;
@@ -243,7 +307,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_prompt_bf16_kernel(AttnA
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const int key = s0 + 8 * (i >> 2) + 4 * h + (i & 3);
-      const bool vis = (key <= see_to) & ((key >= see_from) | (key < a.sinks));
+      const bool near = (key >= see_from) | (key < a.sinks);
+      bool vis = (key <= see_to) & near;
+      if constexpr (TREE) {
+        const int j = key - Lp;
+        const uint64_t word = j < 64 ? anc0 : anc1;
+        vis = j < 0 ? near : (key < N) & (((word >> (j & 63)) & 1ull) != 0);
+      }
       s[i] = vis ? s[i] : -INFINITY;
     }
   };
@@ -341,17 +411,17 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_prompt_bf16_kernel(AttnA
   for (int i = 0; i < 16; ++i) s1[i] = -INFINITY;
   // tiles [far0, far1) that no row of the wave sees: from behind the sinks to its first row's (without a gap, the sinks may
   // reach into the run)
-  const int far0 = gap > 0 ? sink_tiles / kTile : a.sinks > 0 ? (a.sinks - 1) / kTile + 1 : 0;
-  const int far1 = a.window > 0 ? (wave_first - a.window + 1 - gap) / kTile : 0;
+  const int far0 = (gap > 0 ? sink_tiles / kTile : a.sinks > 0 ? (a.sinks - 1) / kTile + 1 : 0) - tile0;
+  const int far1 = !TREE && a.window > 0 ? (wave_first - a.window + 1 - gap) / kTile - tile0 : 0;
   auto step = [&](int k, f32x16& sn, const f32x16& sc, int t) {   // scores of tile k, values of tile k - 1
     if (k >= wave_tiles) return;
-    if (k > far0 && k < far1) {      // (tile far0, too, is all masked: it takes the value product of the one before)
+    if (k > far0 && k > 0 && k < far1) {      // (tile far0, too, is all masked: it takes the value product of the one before)
 #pragma unroll
       for (int i = 0; i < 16; ++i) sn[i] = -INFINITY;
       return;
     }
     block(yes, sn, sc, t, t);
-    const int s0 = slot_of(k * kTile);
+    const int s0 = slot_of((tile0 + k) * kTile);
     if (s0 + kTile - 1 > wave_first || (s0 < plain_from && s0 + kTile > a.sinks)) mask(sn, s0);
     move_reference(sn);
   };
@@ -370,54 +440,105 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_prompt_bf16_kernel(AttnA
     }
   }
 
-  // ---- the rows' sums (two lanes a row), then the output through LDS in whole rows
+  // ---- the rows' sums (two lanes a row); the second key group's states through LDS
   l += __shfl_xor(l, 32);
-  barrier_lds();   // every wave is done with the ring
-  const float inv = live && l > 0.f ? 1.0f / l : 0.f;
-  unsigned char* mine = ring + wave * (kRows * L::ROW);
-  auto piece = [&](int r, int c) { return mine + r * L::ROW + ((c ^ (r & (L::CPR - 1))) << 4); };
+  barrier_lds();   // every wave is done with the rings
+  if constexpr (KG > 1) {
+    float* const far = (float*)(rings + 65536) + wave * (16 * DB * 64) + lane;
+    float* const ml = merge_lds + wave * 128 + lane;
+    if (kg == 1) {
 #pragma unroll
-  for (int d = 0; d < DB; ++d)
+      for (int d = 0; d < DB; ++d)
 #pragma unroll
-    for (int i = 0; i < 16; i += 4) {
-      bf16x4 x;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = (__bf16)(live ? o[d][i + e] * inv : 0.f);
-      *(bf16x4*)(piece(col, d * 4 + (i >> 2)) + 8 * h) = x;
+        for (int i = 0; i < 16; ++i) far[(d * 16 + i) * 64] = o[d][i];
+      ml[0] = m;
+      ml[64] = l;
     }
-  if (a.lse && h == 0 && row < rows_here) a.lse[row0 + row] = live && l > 0.f ? (m + __log2f(l)) * kLn2 : -INFINITY;
-  __builtin_amdgcn_s_waitcnt(0xC07F);
-  asm volatile("" ::: "memory");
+    __syncthreads();
+    if (kg == 0) {
+      const float mo = ml[0], M = fmaxf(m, mo);
+      const float w = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M);
+      const float wo = mo == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mo - M);
 #pragma unroll
-  for (int x = 0; x < kRows * L::CPR / 64; ++x) {
-    const int e = x * 64 + lane, r = e / L::CPR, c = e - r * L::CPR;
-    if (wave * kRows + r < rows_here)
-      *(u32x4*)((unsigned char*)a.out + (row0 + wave * kRows + r) * L::ROW + c * 16) = *(const u32x4*)piece(r, c);
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] = o[d][i] * w + far[(d * 16 + i) * 64] * wo;
+      l = l * w + ml[64] * wo;
+      m = M;
+    }
   }
+  // ---- the output (or the piece's rows) through LDS, in whole rows
+  const int S = a.splits;
+  if (kg == 0) {
+    const float inv = live && l > 0.f ? 1.0f / l : 0.f;
+    unsigned char* mine = ring + wave * (kRows * L::ROW);
+    auto row_piece = [&](int r, int c) { return mine + r * L::ROW + ((c ^ (r & (L::CPR - 1))) << 4); };
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4) {
+        bf16x4 x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = (__bf16)(live ? o[d][i + e] * inv : 0.f);
+        *(bf16x4*)(row_piece(col, d * 4 + (i >> 2)) + 8 * h) = x;
+      }
+    const size_t prow = (pset * S + split) * kRowsWg;   // the piece's row 0 among the pieces
+    if (h == 0 && row < rows_here) {
+      if (S == 1) {
+        if (a.lse) a.lse[row0 + row] = live && l > 0.f ? (m + __log2f(l)) * kLn2 : -INFINITY;
+      } else {
+        *(float2*)(a.part_ml + 2 * (prow + row)) = live ? make_float2(m, l) : make_float2(-INFINITY, 0.f);
+      }
+    }
+    __builtin_amdgcn_s_waitcnt(0xC07F);
+    asm volatile("" ::: "memory");
+    unsigned char* dst = S == 1 ? (unsigned char*)a.out + row0 * L::ROW : (unsigned char*)a.part_o + prow * L::ROW;
+#pragma unroll
+    for (int x = 0; x < kRows * L::CPR / 64; ++x) {
+      const int e = x * 64 + lane, r = e / L::CPR, c = e - r * L::CPR;
+      if (wave * kRows + r < rows_here)
+        *(u32x4*)(dst + (size_t)(wave * kRows + r) * L::ROW + c * 16) = *(const u32x4*)row_piece(r, c);
+    }
+  }
+  if (S == 1) return;
+  merge_set<D, kWaves * KG, false>(a, pset, kRowsWg, split, start_old, row0, rows_here, &pieces_lds[0], &pieces_lds[1]);
+}
+
+template <int D, int KG, bool TREE>
+hipError_t launch(const AttnArgs& a, hipStream_t stream) {
+  constexpr int lds = KG * 65536;
+  static bool configured[64] = {};
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  if (dev < 0 || dev >= 64) return hipErrorInvalidDevice;
+  if (!configured[dev]) {
+    e = hipFuncSetAttribute((const void*)paged_rows_bf16_kernel<D, KG, TREE>,
+                            hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e != hipSuccess) return e;
+    configured[dev] = true;
+  }
+  const unsigned groups = (a.row_groups + a.unit_parts - 1) / a.unit_parts;
+  hipLaunchKernelGGL((paged_rows_bf16_kernel<D, KG, TREE>), dim3((unsigned)a.units * a.unit_parts * groups * a.splits),
+                     dim3(64 * kWaves * KG), lds, stream, a);
+  return hipGetLastError();
 }
 
 template <int D>
-hipError_t launch(const AttnArgs& a, hipStream_t stream) {
-  constexpr int lds = 65536;
-  static bool configured = false;
-  if (!configured) {
-    hipError_t e = hipFuncSetAttribute((const void*)paged_prompt_bf16_kernel<D>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-    if (e != hipSuccess) return e;
-    configured = true;
-  }
-  const unsigned groups = (a.row_groups + a.unit_parts - 1) / a.unit_parts;
-  hipLaunchKernelGGL(paged_prompt_bf16_kernel<D>, dim3((unsigned)a.units * a.unit_parts * groups), dim3(64 * kWaves), lds,
-                     stream, a);
-  return hipGetLastError();
+hipError_t launch_rows(const AttnArgs& a, hipStream_t stream) {
+  if (!a.chain) return a.key_groups == 2 ? launch<D, 2, true>(a, stream) : launch<D, 1, true>(a, stream);
+  return a.key_groups == 2 ? launch<D, 2, false>(a, stream) : launch<D, 1, false>(a, stream);
 }
 
 }  // namespace
 
-hipError_t launch_paged_prompt_bf16(const AttnArgs& a, hipStream_t stream) {
-  if (a.unit_parts < 1 || a.units * a.unit_parts % 8 != 0 || a.groups_per_head * a.G != a.row_groups)
+hipError_t launch_paged_rows_bf16(const AttnArgs& a, hipStream_t stream) {
+  if (a.unit_parts < 1 || a.units * a.unit_parts % 8 != 0 || a.rows_per_wg != kRowsWg ||
+      (a.groups_per_head > 0 && a.groups_per_head * a.G != a.row_groups))
     return hipErrorInvalidValue;
-  if (a.D == 128) return launch<128>(a, stream);
-  if (a.D == 64) return launch<64>(a, stream);
+  if (a.splits > 1 && (!a.part_o || !a.part_ml || !a.set_ctr || a.ctr_stride < 2)) return hipErrorInvalidValue;
+  if (a.D == 128) return launch_rows<128>(a, stream);
+  if (a.D == 64) return launch_rows<64>(a, stream);
   return hipErrorInvalidValue;
 }
 

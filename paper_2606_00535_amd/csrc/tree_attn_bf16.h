@@ -216,6 +216,75 @@ __device__ __forceinline__ void merge_pieces(const AttnArgs& a, size_t prow0, in
   }
 }
 
+// The set's merge, spread over its pieces.  One 64-bit counter word per set (fields at the kCtr*
+// shifts): pieces started, pieces arrived, a bit per arrived piece, and the sum and the sum of squares of the
+// started pieces' XCD ids.  A piece that arrives when its whole set has started waits for every arrival and
+// merges its own slice of the rows: every piece it waits for is running and arrives without waiting for
+// anything.  A piece that arrives earlier leaves; the piece whose start completed the set saw it among the
+// arrived bits then, and merges its slice too (that piece arrives after the set is complete, so it never
+// leaves).  So every wait ends, and each slice is merged once.  The last arrival puts the word back to zero
+// for the next call; a waiting piece takes either the full count or that zero as the end of its wait.  The
+// pieces' rows are read from this XCD's L2: all pieces of a set share blockIdx % 8, and consecutive
+// workgroups of a dispatch go to consecutive XCDs (which XCD takes workgroup 0 differs, e.g. between direct
+// and graph launches).  A merging piece checks that: S ids whose sum is S x and sum of squares S x^2 all
+// equal x, this piece's own.
+template <int D, int W, bool ENT>
+__device__ __forceinline__ void merge_set(const AttnArgs& a, size_t pset, int R, int split, unsigned long long start_old,
+                                          size_t orow0, int rows_valid, uint32_t* merge_lds, uint32_t* good_lds) {
+  const int S = a.splits, tid = threadIdx.x;
+  const size_t prow0 = pset * S * R;   // the set's piece 0, row 0
+  unsigned long long* ctr = a.set_ctr + pset * a.ctr_stride;
+  wait_vector_memory();   // this piece's rows have reached the L2
+  __syncthreads();
+  if (tid == 0) {
+    const unsigned long long old = __hip_atomic_fetch_add(
+        ctr, (1ull << kCtrArrived) | (1ull << (kCtrMask + split)), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const unsigned long long cnt = (1ull << kCtrCountBits) - 1;
+    const bool coop = (old & cnt) == (unsigned long long)S;
+    const bool last = ((old >> kCtrArrived) & cnt) == (unsigned long long)(S - 1);
+    bool good = true;
+    if (coop) {
+      const unsigned long long x = xcd_id();
+      const unsigned long long sum = (old >> kCtrXcdSum) & ((1ull << (kCtrXcdSq - kCtrXcdSum)) - 1);
+      const unsigned long long sq = old >> kCtrXcdSq;
+      if (sum != S * x || sq != S * x * x) {
+        raise_device_error(a.err, kErrXcdSplit);
+        good = false;
+      }
+    }
+    if (last) {
+      __hip_atomic_store(ctr, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    } else if (coop) {
+      const uint64_t t0 = __builtin_amdgcn_s_memrealtime();
+      for (;;) {
+        const unsigned long long now = __hip_atomic_load(ctr, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (((now >> kCtrArrived) & cnt) == (unsigned long long)S || (now & cnt) == 0ull) break;
+        if (__builtin_amdgcn_s_memrealtime() - t0 > a.wait_ticks) {
+          raise_device_error(a.err, kErrWaitTimeout);
+          good = false;
+          break;
+        }
+        __builtin_amdgcn_s_sleep(1);
+      }
+    }
+    // slices this workgroup merges: its own (when it waited), and those of the pieces that left before this
+    // piece's start completed the set
+    uint32_t slices = coop ? 1u << split : 0u;
+    if ((start_old & cnt) == (unsigned long long)(S - 1))
+      slices |= (uint32_t)(start_old >> kCtrMask) & (uint32_t)((1ull << S) - 1);
+    *merge_lds = slices;
+    *good_lds = good ? 1u : 0u;
+  }
+  __syncthreads();
+  const uint32_t slices = *merge_lds;
+  for (int k = 0; k < S; ++k) {
+    if (!((slices >> k) & 1u)) continue;
+    const int r0 = k * R / S, r1 = (k + 1) * R / S;
+    merge_pieces<D, W, ENT>(a, prow0, R, (__bf16*)a.out + orow0 * D, a.lse ? a.lse + orow0 : nullptr,
+                            ENT ? a.entropy + orow0 : nullptr, rows_valid, r0, r1 - r0, *good_lds == 1u);
+  }
+}
+
 // LDS of a workgroup: the ring, the query rows when they sit beside it, the ancestor sets and the tree as
 // copied (static), and a few words; WPC workgroups share a compute unit's 160 KB.
 template <int D, int NST, int WPC>
@@ -298,12 +367,6 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
   int Lp_paged = 0, N_paged = 0, low = 0, sink_end = 0, sink_steps = 0, gap = 0, nb = T;
   int i_first = 0, i_last = 0;   // chain: the first and last position of the workgroup's rows
   if constexpr (PAGED) {
-    if (a.chain && a.groups_per_head > 0) {
-      // a head's rows in groups of their own, the ones with the most keys first
-      const int blk = a.groups_per_head - 1 - rg / a.G, hh = rg - (rg / a.G) * a.G;
-      row_base = hh * T + blk * R;
-      rows_here = T - blk * R;
-    }
     rows_here = min(rows_here, R);
     if (a.chain && a.row_len) nb = min(max(a.row_len[b], 0), T);
     Lp_paged = min(max(kv_len_b, 0), a.S_cap - nb);
@@ -567,16 +630,11 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
         for (int ds = 0; ds < DS; ++ds) qf[rb][ds] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
       }
     }
-    int first = i_first, last = i_last;
-    if (a.chain && a.groups_per_head > 0) {
-      first = i_first + rh * RW;
-      last = min(first + RW - 1, i_last);
-    }
     if (a.chain) {
-      plain_to = Lp + first + 1;
-      wave_to = Lp + last;
+      plain_to = Lp + i_first + 1;
+      wave_to = Lp + i_last;
     }
-    if (a.window > 0) plain_from = Lp + (a.chain ? last : deepest) - a.window + 1;
+    if (a.window > 0) plain_from = Lp + (a.chain ? i_last : deepest) - a.window + 1;
   }
   // Ring depth: the pipelined loop frees a super-step's slots at the barrier that follows its operand reads,
   // so every slot can hold a copy in flight; the plain loop keeps one slot for the super-step being read.
@@ -996,69 +1054,7 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
   }
   if (S == 1) return;
 
-  // ---- the set's merge, spread over its pieces.  One 64-bit counter word per set (fields at the kCtr*
-  // shifts): pieces started, pieces arrived, a bit per arrived piece, and the sum and the sum of squares of the
-  // started pieces' XCD ids.  A piece that arrives when its whole set has started waits for every arrival and
-  // merges its own slice of the rows: every piece it waits for is running and arrives without waiting for
-  // anything.  A piece that arrives earlier leaves; the piece whose start completed the set saw it among the
-  // arrived bits then, and merges its slice too (that piece arrives after the set is complete, so it never
-  // leaves).  So every wait ends, and each slice is merged once.  The last arrival puts the word back to zero
-  // for the next call; a waiting piece takes either the full count or that zero as the end of its wait.  The
-  // pieces' rows are read from this XCD's L2: all pieces of a set share blockIdx % 8, and consecutive
-  // workgroups of a dispatch go to consecutive XCDs (which XCD takes workgroup 0 differs, e.g. between direct
-  // and graph launches).  A merging piece checks that: S ids whose sum is S x and sum of squares S x^2 all
-  // equal x, this piece's own.
-  unsigned long long* ctr = a.set_ctr + pset * a.ctr_stride;
-  wait_vector_memory();   // this piece's rows have reached the L2
-  __syncthreads();
-  if (tid == 0) {
-    const unsigned long long old = __hip_atomic_fetch_add(
-        ctr, (1ull << kCtrArrived) | (1ull << (kCtrMask + split)), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    const unsigned long long cnt = (1ull << kCtrCountBits) - 1;
-    const bool coop = (old & cnt) == (unsigned long long)S;
-    const bool last = ((old >> kCtrArrived) & cnt) == (unsigned long long)(S - 1);
-    bool good = true;
-    if (coop) {
-      const unsigned long long x = xcd_id();
-      const unsigned long long sum = (old >> kCtrXcdSum) & ((1ull << (kCtrXcdSq - kCtrXcdSum)) - 1);
-      const unsigned long long sq = old >> kCtrXcdSq;
-      if (sum != S * x || sq != S * x * x) {
-        raise_device_error(a.err, kErrXcdSplit);
-        good = false;
-      }
-    }
-    if (last) {
-      __hip_atomic_store(ctr, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    } else if (coop) {
-      const uint64_t t0 = __builtin_amdgcn_s_memrealtime();
-      for (;;) {
-        const unsigned long long now = __hip_atomic_load(ctr, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        if (((now >> kCtrArrived) & cnt) == (unsigned long long)S || (now & cnt) == 0ull) break;
-        if (__builtin_amdgcn_s_memrealtime() - t0 > a.wait_ticks) {
-          raise_device_error(a.err, kErrWaitTimeout);
-          good = false;
-          break;
-        }
-        __builtin_amdgcn_s_sleep(1);
-      }
-    }
-    // slices this workgroup merges: its own (when it waited), and those of the pieces that left before this
-    // piece's start completed the set
-    uint32_t slices = coop ? 1u << split : 0u;
-    if ((start_old & cnt) == (unsigned long long)(S - 1))
-      slices |= (uint32_t)(start_old >> kCtrMask) & (uint32_t)((1ull << S) - 1);
-    merge_lds = slices;
-    good_lds = good ? 1u : 0u;
-  }
-  __syncthreads();
-  const uint32_t slices = merge_lds;
-  const size_t orow0 = qrow0 + (size_t)row_base;
-  for (int k = 0; k < S; ++k) {
-    if (!((slices >> k) & 1u)) continue;
-    const int r0 = k * R / S, r1 = (k + 1) * R / S;
-    merge_pieces<D, W, ENT>(a, prow0, R, (__bf16*)a.out + orow0 * D, a.lse ? a.lse + orow0 : nullptr,
-                            ENT ? a.entropy + orow0 : nullptr, rows_valid, r0, r1 - r0, good_lds == 1u);
-  }
+  merge_set<D, W, ENT>(a, pset, R, split, start_old, qrow0 + (size_t)row_base, rows_valid, &merge_lds, &good_lds);
 }
 
 template <int D, int RB, int KW, int W, int NST, int WPC, bool ENT, bool PAGED>
