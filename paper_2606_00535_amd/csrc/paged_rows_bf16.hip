@@ -264,7 +264,7 @@ __global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(At
   const int wave_tiles = wave_last < wave_first ? 0 : max(min(tiles, (wave_last - gap) / kTile + 1 - tile0), 0);
 
   f32x16 o[DB];
-  float m = -INFINITY, l = 0.f;
+  float m = -3.402823466e38f, l = 0.f;   // (finite: no score, -inf, less the reference is NaN)
 #pragma unroll
   for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -317,17 +317,19 @@ __global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(At
       s[i] = vis ? s[i] : -INFINITY;
     }
   };
-  // the reference moves where a score passes it by more than 2^8 (rare after the first tiles)
-  auto move_reference = [&](const f32x16& s) {
+  auto row_max = [&](const f32x16& s) {
     float x = vmax(vmax(s[0], s[1]), s[2]);
 #pragma unroll
     for (int i = 3; i < 15; i += 2) x = vmax(vmax(x, s[i]), s[i + 1]);
-    x = vmax(x, s[15]);
+    return vmax(x, s[15]);
+  };
+  // the reference moves where a score passes it by more than 2^8 (rare after the first tiles)
+  auto move_reference = [&](float x) {
     const float top = c_scale * x;
     if (__any(top > m + kLazyLog2)) {
       const float t = fmaxf(top, __shfl_xor(top, 32));
       if (t > m + kLazyLog2) {
-        const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - t);
+        const float alpha = __builtin_amdgcn_exp2f(m - t);
         m = t;
         l *= alpha;
 #pragma unroll
@@ -335,14 +337,16 @@ __global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(At
       }
     }
   };
-  // One basic block, in this order: the scores of the next tile (NEXT) beside the exponentials of this one, then its value
-  // product.
+  // One basic block in a fixed order, a matrix instruction and what the vector ALU does in its shadow at a time: the scores
+  // of the next tile (NEXT) beside the exponentials of this one, then its value product beside the next tile's maximum,
+  // which is returned.
   auto block = [&](auto next, f32x16& sn, const f32x16& sc, int kt, int vt) {
     constexpr bool NEXT = decltype(next)::value;
+    constexpr int FIRST = 4, PER = (16 - FIRST) / (KS + DB);   // exponentials ahead of the products, and beside each
+    static_assert(FIRST + PER * (KS + DB) == 16 && FIRST + PER * KS >= 8, "the first 8 keys' weights precede their product");
     bf16x8 kf[KS], va[DB], vb[DB];
     bf16x8 p[2];
-    const float m_use = m == -INFINITY ? 0.f : m;
-    float sum0 = 0.f, sum1 = 0.f;
+    float sum[2] = {0.f, 0.f}, e[2], x = 0.f;
     auto score = [&](int ds) {
       if constexpr (NEXT) {
         f32x16 z;
@@ -355,47 +359,48 @@ __global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(At
         sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ds], qf[ds], z, 0, 0, 0);
       }
     };
-    auto weights = [&](int i) {   // of two keys
-      const float e0 = __builtin_amdgcn_exp2f(fmaf(sc[i], c_scale, -m_use));
-      const float e1 = __builtin_amdgcn_exp2f(fmaf(sc[i + 1], c_scale, -m_use));
-      sum0 += e0;
-      sum1 += e1;
-      p[i / 8][i % 8] = (__bf16)e0;
-      p[i / 8][i % 8 + 1] = (__bf16)e1;
-    };
-    auto value = [&](const bf16x8 (&v)[DB], int t, int d) {
-      o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[d], p[t], o[d], 0, 0, 0);
+    auto weight = [&](int i) {
+      e[i & 1] = __builtin_amdgcn_exp2f(fmaf(sc[i], c_scale, -m));
+      sum[i & 1] += e[i & 1];
+      if (i & 1) {
+        p[i / 8][i % 8 - 1] = (__bf16)e[0];
+        p[i / 8][i % 8] = (__bf16)e[1];
+      }
     };
 #define FENCE __builtin_amdgcn_sched_barrier(0)
     FENCE;
     if constexpr (NEXT) read_keys(kf, kt);
     FENCE;
-    weights(0); weights(2); FENCE;
-    constexpr int Q = KS / 4;   // score products per quarter
 #pragma unroll
-    for (int x = 0; x < Q; ++x) { score(x); }
-    weights(4); FENCE;
+    for (int i = 0; i < FIRST; ++i) weight(i);
+    FENCE;
 #pragma unroll
-    for (int x = 0; x < Q; ++x) { score(Q + x); }
-    read_values(va, vt, 0);
-    weights(6); FENCE;
+    for (int ds = 0; ds < KS; ++ds) {
+      score(ds);
+      if (ds == KS / 2 - 1) read_values(va, vt, 0);
+      if (ds == KS - 1) read_values(vb, vt, 1);
 #pragma unroll
-    for (int x = 0; x < Q; ++x) { score(2 * Q + x); }
-    weights(8); FENCE;
+      for (int i = 0; i < PER; ++i) weight(FIRST + ds * PER + i);
+      FENCE;
+    }
 #pragma unroll
-    for (int x = 0; x < Q; ++x) { score(3 * Q + x); }
-    read_values(vb, vt, 1);
-    weights(10); FENCE;
+    for (int d = 0; d < DB; ++d) {
+      o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[d], p[0], o[d], 0, 0, 0);
 #pragma unroll
-    for (int d = 0; d < DB / 2; ++d) value(va, 0, d);
-    weights(12); FENCE;
+      for (int i = 0; i < PER; ++i) weight(FIRST + (KS + d) * PER + i);
+      FENCE;
+    }
 #pragma unroll
-    for (int d = DB / 2; d < DB; ++d) value(va, 0, d);
-    weights(14); FENCE;
-#pragma unroll
-    for (int d = 0; d < DB; ++d) value(vb, 1, d);
-    l += sum0 + sum1;
+    for (int d = 0; d < DB; ++d) {
+      o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vb[d], p[1], o[d], 0, 0, 0);
+      if constexpr (NEXT) {
+        if (d == 0) x = row_max(sn);
+      }
+    }
+    l += sum[0] + sum[1];
+    FENCE;
 #undef FENCE
+    return x;
   };
   constexpr std::true_type yes{};
   constexpr std::false_type no{};
@@ -420,10 +425,13 @@ __global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(At
       for (int i = 0; i < 16; ++i) sn[i] = -INFINITY;
       return;
     }
-    block(yes, sn, sc, t, t);
+    float x = block(yes, sn, sc, t, t);
     const int s0 = slot_of((tile0 + k) * kTile);
-    if (s0 + kTile - 1 > wave_first || (s0 < plain_from && s0 + kTile > a.sinks)) mask(sn, s0);
-    move_reference(sn);
+    if (s0 + kTile - 1 > wave_first || (s0 < plain_from && s0 + kTile > a.sinks)) {
+      mask(sn, s0);
+      x = row_max(sn);
+    }
+    move_reference(x);
   };
   for (int j0 = 0; j0 < periods; j0 += L::STAGES) {
 #pragma unroll
@@ -457,8 +465,7 @@ __global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(At
     __syncthreads();
     if (kg == 0) {
       const float mo = ml[0], M = fmaxf(m, mo);
-      const float w = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M);
-      const float wo = mo == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mo - M);
+      const float w = __builtin_amdgcn_exp2f(m - M), wo = __builtin_amdgcn_exp2f(mo - M);
 #pragma unroll
       for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -487,7 +494,7 @@ __global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(At
       if (S == 1) {
         if (a.lse) a.lse[row0 + row] = live && l > 0.f ? (m + __log2f(l)) * kLn2 : -INFINITY;
       } else {
-        *(float2*)(a.part_ml + 2 * (prow + row)) = live ? make_float2(m, l) : make_float2(-INFINITY, 0.f);
+        *(float2*)(a.part_ml + 2 * (prow + row)) = live && l > 0.f ? make_float2(m, l) : make_float2(-INFINITY, 0.f);
       }
     }
     __builtin_amdgcn_s_waitcnt(0xC07F);
