@@ -42,47 +42,50 @@ __global__ __launch_bounds__(kAppendThreads) void paged_append_kernel(PagedRowsA
 }
 
 // A node at depth k has k ancestors with smaller indices, so path[k] >= k: sources lie at or behind their
-// destinations, and a destination can be a later row's source.  Passes over k run in increasing order, each gathers all
-// of its rows into LDS before it scatters them.  Rows with path[k] == k stay.  One workgroup per (layer, sequence, KV head).
+// destinations, and a destination can be a later row's source.  Passes over k run in increasing order, each with all of its
+// rows in registers before it writes one.  Rows with path[k] == k stay.  A wave per (layer, sequence, KV head), a lane per 16
+// bytes of a row; a pass has kCommitLoads times as many rows as a wave holds at once.  Latency bounds it (the lengths and
+// the path, the table, the rows, one after another): waves that need no LDS and no barrier, four to a workgroup.
+constexpr int kCommitLoads = 4;
+
 __global__ __launch_bounds__(kCommitThreads) void paged_commit_kernel(PagedRowsArgs a) {
-  constexpr int RW = kCommitRowsPerPass;
-  constexpr int MAXW = kCommitMaxRowBytes / 16;
-  __shared__ u32x4 kbuf[RW * MAXW];
-  __shared__ u32x4 vbuf[RW * MAXW];
-  const int n = blockIdx.x;                  // (layer * B + b) * Hkv + g
-  const int g = n % a.Hkv, lb = n / a.Hkv;
+  const int lane = threadIdx.x & 63;
+  const long long n = (long long)blockIdx.x * (kCommitThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (n >= (long long)a.NL * a.B * a.Hkv) return;       // (layer * B + b) * Hkv + g
+  const int g = (int)(n % a.Hkv), lb = (int)(n / a.Hkv);
   const int b = lb % a.B, layer = lb / a.B;
+  const int words = a.row_bytes / 16, at_once = 64 / words;   // rows of a wave
+  const int r = lane / words, w = lane - r * words;
+  const int32_t* path = a.path + (size_t)b * a.path_stride;
   const int L = a.kv_len[b];
   int A = a.accept_len[b];
   A = A < 0 ? 0 : (A > a.path_stride - 1 ? a.path_stride - 1 : A);
-  if (layer == 0 && g == 0 && threadIdx.x == 0) a.kv_len_out[b] = L + A + 1;
+  if (layer == 0 && g == 0 && lane == 0) a.kv_len_out[b] = L + A + 1;
   if (L < 0) return;
-  const int words = a.row_bytes / 16;
-  char* kc = a.k + layer * a.layer_stride;
-  char* vc = a.v + layer * a.layer_stride;
+  char* kc = a.k + layer * a.layer_stride + w * 16;
+  char* vc = a.v + layer * a.layer_stride + w * 16;
   const int32_t* table = a.table + (size_t)b * a.width;
-  const int32_t* path = a.path + (size_t)b * a.path_stride;
-  for (int k0 = 0; k0 <= A; k0 += RW) {
-    const int items = min(RW, A + 1 - k0) * words;
-    for (int e = threadIdx.x; e < items; e += kCommitThreads) {
-      const int r = e / words, w = e - r * words, k = k0 + r, src = path[k];
+  for (int k0 = 0; k0 <= A; k0 += kCommitLoads * at_once) {
+    u32x4 kr[kCommitLoads], vr[kCommitLoads];
+    int64_t to[kCommitLoads];
+#pragma unroll
+    for (int t = 0; t < kCommitLoads; ++t) {
+      const int k = k0 + t * at_once + r;
+      const int src = r < at_once && k <= A ? path[k] : 0;
       const int64_t from = src > k ? slot_offset(a, table, g, (long long)L + src) : -1;
-      if (from >= 0) {
-        kbuf[r * MAXW + w] = *(const u32x4*)(kc + from + w * 16);
-        vbuf[r * MAXW + w] = *(const u32x4*)(vc + from + w * 16);
+      to[t] = from >= 0 ? slot_offset(a, table, g, (long long)L + k) : -1;
+      if (to[t] >= 0) {
+        kr[t] = *(const u32x4*)(kc + from);
+        vr[t] = *(const u32x4*)(vc + from);
       }
     }
-    __syncthreads();
-    for (int e = threadIdx.x; e < items; e += kCommitThreads) {
-      const int r = e / words, w = e - r * words, k = k0 + r, src = path[k];
-      const int64_t from = src > k ? slot_offset(a, table, g, (long long)L + src) : -1;
-      const int64_t to = from >= 0 ? slot_offset(a, table, g, (long long)L + k) : -1;
-      if (to >= 0) {
-        *(u32x4*)(kc + to + w * 16) = kbuf[r * MAXW + w];
-        *(u32x4*)(vc + to + w * 16) = vbuf[r * MAXW + w];
+    wait_vector_memory();   // (every lane's rows are in registers)
+#pragma unroll
+    for (int t = 0; t < kCommitLoads; ++t)
+      if (to[t] >= 0) {
+        *(u32x4*)(kc + to[t]) = kr[t];
+        *(u32x4*)(vc + to[t]) = vr[t];
       }
-    }
-    __syncthreads();
   }
 }
 
@@ -97,7 +100,7 @@ hipError_t launch_paged_append(const PagedRowsArgs& a, hipStream_t stream) {
 }
 
 hipError_t launch_paged_commit(const PagedRowsArgs& a, hipStream_t stream) {
-  const long long grid = (long long)a.NL * a.B * a.Hkv;
+  const long long waves = (long long)a.NL * a.B * a.Hkv, grid = (waves + kCommitThreads / 64 - 1) / (kCommitThreads / 64);
   if (grid <= 0) return hipSuccess;
   hipLaunchKernelGGL(paged_commit_kernel, dim3((unsigned)grid), dim3(kCommitThreads), 0, stream, a);
   return hipGetLastError();
