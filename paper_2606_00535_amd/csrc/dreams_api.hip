@@ -146,10 +146,10 @@ int fine_splits(long long wgs, long long cus, int wpc, int n_keys) {
   return s > 1 ? (int)s : 1;
 }
 
-size_t attn_partial_bytes(AttnPlan* p, int splits, int head_dim) {
+size_t attn_partial_bytes(AttnPlan* p, int splits, int head_dim, int elem = 2) {
   const size_t rows = (size_t)p->units * p->row_groups * splits * p->rows_per_wg;
   p->o_off = kCounterBytes;
-  p->ml_off = p->o_off + align_up(rows * head_dim * 2, 256);
+  p->ml_off = p->o_off + align_up(rows * head_dim * elem, 256);
   p->e_off = p->ml_off + align_up(rows * 2 * sizeof(float), 256);
   return p->e_off + align_up(rows * sizeof(float), 256);
 }
@@ -1345,7 +1345,7 @@ dreams_status_t plan_paged(const dreams_paged_desc_t* d, bool prompt, PagedPlan*
     int stride = 16;
     while (stride > 2 && sets * stride > kMaxSetCounters) stride >>= 1;
     p.ctr_stride = stride;
-    p.bytes = attn_partial_bytes(&p, splits, d->head_dim);
+    p.bytes = attn_partial_bytes(&p, splits, d->head_dim, 4);
   }
   return DREAMS_OK;
 }

@@ -88,7 +88,7 @@ struct AttnArgs {
   float* entropy;         // [B, Hq, T] attention entropy of every row (nats), or nullptr
   // Several pieces per (sequence, KV head, row group) -- a "set": each piece stores its rows' normalised output
   // (bf16) and softmax state, and the set's pieces merge them, each a slice of the rows.
-  __bf16* part_o;         // [sets, splits, rows_per_wg, D]   accumulator / sum, rounded to bf16
+  __bf16* part_o;         // [sets, splits, rows_per_wg, D]   accumulator / sum, rounded to bf16 (paged: fp32)
   float* part_ml;         // [sets, splits, rows_per_wg, 2]   (max in log2 units, sum)
   float* part_e;          // [sets, splits, rows_per_wg]      entropy terms (with entropy only)
   // The 64-bit counter word of set s at set_ctr[s * ctr_stride]: pieces started, pieces arrived, a bit per

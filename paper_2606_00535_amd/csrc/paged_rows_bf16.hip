@@ -474,41 +474,48 @@ __global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(At
       m = M;
     }
   }
-  // ---- the output (or the piece's rows) through LDS, in whole rows
-  const int S = a.splits;
-  if (kg == 0) {
-    const float inv = live && l > 0.f ? 1.0f / l : 0.f;
-    unsigned char* mine = ring + wave * (kRows * L::ROW);
-    auto row_piece = [&](int r, int c) { return mine + r * L::ROW + ((c ^ (r & (L::CPR - 1))) << 4); };
+  const float inv = live && l > 0.f ? 1.0f / l : 0.f;
+  if (a.splits > 1) {   // the piece's rows, in fp32
+    const size_t prow = (pset * a.splits + split) * kRowsWg + row;
+    if (kg == 0 && row < rows_here) {
+      float* const dst = (float*)a.part_o + prow * D + 4 * h;
 #pragma unroll
-    for (int d = 0; d < DB; ++d)
+      for (int d = 0; d < DB; ++d)
 #pragma unroll
-      for (int i = 0; i < 16; i += 4) {
-        bf16x4 x;
+        for (int i = 0; i < 16; i += 4) {
+          f32x4 x;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = (__bf16)(live ? o[d][i + e] * inv : 0.f);
-        *(bf16x4*)(row_piece(col, d * 4 + (i >> 2)) + 8 * h) = x;
-      }
-    const size_t prow = (pset * S + split) * kRowsWg;   // the piece's row 0 among the pieces
-    if (h == 0 && row < rows_here) {
-      if (S == 1) {
-        if (a.lse) a.lse[row0 + row] = live && l > 0.f ? (m + __log2f(l)) * kLn2 : -INFINITY;
-      } else {
-        *(float2*)(a.part_ml + 2 * (prow + row)) = live && l > 0.f ? make_float2(m, l) : make_float2(-INFINITY, 0.f);
-      }
+          for (int e = 0; e < 4; ++e) x[e] = live ? o[d][i + e] * inv : 0.f;
+          *(f32x4*)(dst + d * 32 + 2 * i) = x;
+        }
+      if (h == 0) *(float2*)(a.part_ml + 2 * prow) = live && l > 0.f ? make_float2(m, l) : make_float2(-INFINITY, 0.f);
     }
-    __builtin_amdgcn_s_waitcnt(0xC07F);
-    asm volatile("" ::: "memory");
-    unsigned char* dst = S == 1 ? (unsigned char*)a.out + row0 * L::ROW : (unsigned char*)a.part_o + prow * L::ROW;
-#pragma unroll
-    for (int x = 0; x < kRows * L::CPR / 64; ++x) {
-      const int e = x * 64 + lane, r = e / L::CPR, c = e - r * L::CPR;
-      if (wave * kRows + r < rows_here)
-        *(u32x4*)(dst + (size_t)(wave * kRows + r) * L::ROW + c * 16) = *(const u32x4*)row_piece(r, c);
-    }
+    merge_set<D, kWaves * KG, false, float>(a, pset, kRowsWg, split, start_old, row0, rows_here, &pieces_lds[0],
+                                            &pieces_lds[1]);
+    return;
   }
-  if (S == 1) return;
-  merge_set<D, kWaves * KG, false>(a, pset, kRowsWg, split, start_old, row0, rows_here, &pieces_lds[0], &pieces_lds[1]);
+  if (kg == 1) return;
+  // ---- the output through LDS, in whole rows
+  unsigned char* mine = ring + wave * (kRows * L::ROW);
+  auto row_piece = [&](int r, int c) { return mine + r * L::ROW + ((c ^ (r & (L::CPR - 1))) << 4); };
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      bf16x4 x;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = (__bf16)(live ? o[d][i + e] * inv : 0.f);
+      *(bf16x4*)(row_piece(col, d * 4 + (i >> 2)) + 8 * h) = x;
+    }
+  if (a.lse && h == 0 && row < rows_here) a.lse[row0 + row] = live && l > 0.f ? (m + __log2f(l)) * kLn2 : -INFINITY;
+  __builtin_amdgcn_s_waitcnt(0xC07F);
+  asm volatile("" ::: "memory");
+#pragma unroll
+  for (int x = 0; x < kRows * L::CPR / 64; ++x) {
+    const int e = x * 64 + lane, r = e / L::CPR, c = e - r * L::CPR;
+    if (wave * kRows + r < rows_here)
+      *(u32x4*)((unsigned char*)a.out + (row0 + wave * kRows + r) * L::ROW + c * 16) = *(const u32x4*)row_piece(r, c);
+  }
 }
 
 template <int D, int KG, bool TREE>

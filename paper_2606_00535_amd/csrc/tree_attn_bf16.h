@@ -152,13 +152,16 @@ struct Rows {
 // non-temporal 16-byte loads, a row's pieces side by side, whole 128-byte lines.  The loads are issued
 // unconditionally (addresses clamped into the set), so that all of them are in flight together (loads under a
 // branch are each waited for before the branch joins); waves with no row of the slice skip it.  Rows at or
-// past rows_valid are not written.  good = false writes NaN rows (a failed wait).
-template <int D, int W, bool ENT>
+// past rows_valid are not written.  good = false writes NaN rows (a failed wait).  PT: type of the pieces' rows (paged calls
+// keep them in fp32: 64 rows of 32 heads in 8 pieces are 8 MB in L2 instead of 4, and the output is rounded once less).
+template <int D, int W, bool ENT, typename PT>
 __device__ __forceinline__ void merge_pieces(const AttnArgs& a, size_t prow0, int R, __bf16* out_rows, float* lse_rows,
                                              float* ent_rows, int rows_valid, int r0, int nrows, bool good) {
   constexpr int CPR = D / 8;
   constexpr int PCH = 8;    // pieces per batch of loads
   typedef __bf16 bf16x8m __attribute__((ext_vector_type(8)));
+  typedef PT ptx8 __attribute__((ext_vector_type(8)));
+  const PT* const part_o = (const PT*)a.part_o;
   const int S = a.splits;
   const int items = nrows * CPR;
   const int wave = (int)threadIdx.x >> 6;
@@ -175,13 +178,13 @@ __device__ __forceinline__ void merge_pieces(const AttnArgs& a, size_t prow0, in
     for (int s0 = 0; s0 < S; s0 += PCH) {
       f32x2 ml[PCH];
       float ev[PCH];
-      bf16x8m x[PCH];
+      ptx8 x[PCH];
 #pragma unroll
       for (int k = 0; k < PCH; ++k) {
         const size_t pr = prow0 + (size_t)min(s0 + k, S - 1) * R + rl;
         ml[k] = __builtin_nontemporal_load((const f32x2*)(a.part_ml + 2 * pr));
         ev[k] = ENT ? __builtin_nontemporal_load(a.part_e + pr) : 0.f;
-        x[k] = __builtin_nontemporal_load((const bf16x8m*)(a.part_o + pr * D + ch * 8));
+        x[k] = __builtin_nontemporal_load((const ptx8*)(part_o + pr * D + ch * 8));
       }
       float Mn = M;
 #pragma unroll
@@ -228,7 +231,7 @@ __device__ __forceinline__ void merge_pieces(const AttnArgs& a, size_t prow0, in
 // workgroups of a dispatch go to consecutive XCDs (which XCD takes workgroup 0 differs, e.g. between direct
 // and graph launches).  A merging piece checks that: S ids whose sum is S x and sum of squares S x^2 all
 // equal x, this piece's own.
-template <int D, int W, bool ENT>
+template <int D, int W, bool ENT, typename PT>
 __device__ __forceinline__ void merge_set(const AttnArgs& a, size_t pset, int R, int split, unsigned long long start_old,
                                           size_t orow0, int rows_valid, uint32_t* merge_lds, uint32_t* good_lds) {
   const int S = a.splits, tid = threadIdx.x;
@@ -280,7 +283,7 @@ __device__ __forceinline__ void merge_set(const AttnArgs& a, size_t pset, int R,
   for (int k = 0; k < S; ++k) {
     if (!((slices >> k) & 1u)) continue;
     const int r0 = k * R / S, r1 = (k + 1) * R / S;
-    merge_pieces<D, W, ENT>(a, prow0, R, (__bf16*)a.out + orow0 * D, a.lse ? a.lse + orow0 : nullptr,
+    merge_pieces<D, W, ENT, PT>(a, prow0, R, (__bf16*)a.out + orow0 * D, a.lse ? a.lse + orow0 : nullptr,
                             ENT ? a.entropy + orow0 : nullptr, rows_valid, r0, r1 - r0, *good_lds == 1u);
   }
 }
@@ -996,6 +999,28 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
   // exchange area; 16-byte pieces of a row XOR-swizzled by the row, so neither the matrix-core-layout writes
   // nor the row reads conflict on banks), with each row's (max, sum) and entropy term; they are then written
   // out as whole 16-byte pieces of rows.
+  const int S = a.splits;
+  const size_t pset = (size_t)u * a.row_groups + rg;
+  const size_t prow0 = pset * S * R;   // the set's piece 0, row 0
+  const int rows_valid = min(R, rows_here);
+  if constexpr (PAGED) {
+    if (S > 1) {   // (a piece's rows go to the workspace in fp32, straight from the registers)
+      float* const dst = (float*)a.part_o + (prow0 + (size_t)split * R) * D;
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        const int rl = rh * RW + rb * 16 + col;
+        if (rl >= rows_valid) continue;
+        const float inv = l_run[rb] > 0.f ? 1.0f / l_run[rb] : 0.f;
+#pragma unroll
+        for (int dd = 0; dd < DBK; ++dd) *(f32x4*)(dst + (size_t)rl * D + c0 + dd * 16) = fin[rb][dd] * inv;
+        if (kw == 0 && quad == 0)
+          *(float2*)(a.part_ml + 2 * (prow0 + (size_t)split * R + rl)) = make_float2(m_run[rb], l_run[rb]);
+      }
+      merge_set<D, W, ENT, float>(a, pset, R, split, start_old, qrow0 + (size_t)row_base, rows_valid, &merge_lds,
+                                &good_lds);
+      return;
+    }
+  }
   constexpr int CPR = D / 8;                  // 16-byte pieces per row
   constexpr size_t XBYTES = KW > 1 ? ((size_t)(KW - 1) * R * D * 4 + (size_t)KW * R * 12 + 1023) / 1024 * 1024 : 0;
   static_assert(XBYTES + (size_t)R * D * 2 + (size_t)R * 12 <= (size_t)NST * L::SLOT, "row staging fits the ring");
@@ -1025,10 +1050,6 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
 
   // (row, 16-byte piece) items of the workgroup's rows, dealt to the threads
   constexpr int ITEMS = (R * CPR + 64 * W - 1) / (64 * W);   // items per thread
-  const int S = a.splits;
-  const size_t pset = (size_t)u * a.row_groups + rg;
-  const size_t prow0 = pset * S * R;   // the set's piece 0, row 0
-  const int rows_valid = min(R, rows_here);
   // One piece writes the output; with several, every piece stores its rows (normalised, bf16), their (max,
   // sum) and entropy terms as piece `split` of its set.  Rows of one KV head are consecutive in memory.
   {
@@ -1052,9 +1073,9 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
       }
     }
   }
-  if (S == 1) return;
+  if (PAGED || S == 1) return;
 
-  merge_set<D, W, ENT>(a, pset, R, split, start_old, qrow0 + (size_t)row_base, rows_valid, &merge_lds, &good_lds);
+  merge_set<D, W, ENT, __bf16>(a, pset, R, split, start_old, qrow0 + (size_t)row_base, rows_valid, &merge_lds, &good_lds);
 }
 
 template <int D, int RB, int KW, int W, int NST, int WPC, bool ENT, bool PAGED>

@@ -4,8 +4,8 @@ Attention tolerances.  Let A[d] = sum_j p_j |v_j[d]| of a row, n its keys, and d
 the error of an fp32 score (products of bf16 values are exact in fp32; D sums, the scale and the reference add one rounding
 each), in the exponent a relative error of a probability.  Sums of n terms in fp32 in any order add n 2^-24, the
 exponential, the division and the merges a few 2^-24 more (16 here).  fp32: |out - ref| <= A (2 ds + (n + 16) 2^-24).  bf16
-adds half steps of 2^-8 (torch.finfo(bfloat16).eps / 2): the probabilities' rounding before the value product (A), a piece's
-partial output (A again) and the result's (|ref|).  lse: ds + (n + 16) 2^-24 + |lse| 2^-22."""
+adds half steps of 2^-8 (torch.finfo(bfloat16).eps / 2): the probabilities' rounding before the value product (A) and the
+result's (|ref|).  lse: ds + (n + 16) 2^-24 + |lse| 2^-22."""
 import numpy as np
 import torch
 
@@ -120,7 +120,7 @@ def check(out, lse, ref, bf16, label):
     sums = 2 * ds + (n + 16) * 2.0 ** -24
     tol = size * sums[..., None]
     if bf16:
-        tol = tol * (1 + 2.0 ** -7) + 2.0 ** -8 * (2 * size + np.abs(want)) * (1 + 2.0 ** -7)
+        tol = tol * (1 + 2.0 ** -7) + 2.0 ** -8 * (size + np.abs(want)) * (1 + 2.0 ** -7)
     err = np.abs(got - want)
     worst = np.unravel_index(np.argmax(err - tol), err.shape)
     assert (err <= tol + 1e-30).all(), (label, "out", worst, got[worst], want[worst], tol[worst])
