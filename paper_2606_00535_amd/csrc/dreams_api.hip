@@ -1248,7 +1248,6 @@ PagedAttnArgs paged_args(const dreams_paged_desc_t* d, const void* q, const void
   a.kv_len = kv_len;
   a.out = out;
   a.lse = lse;
-  a.bf16 = d->dtype == DREAMS_BF16;
   a.B = d->batch;
   a.Hq = d->num_q_heads;
   a.Hkv = d->num_kv_heads;

@@ -312,7 +312,7 @@ constexpr int kPagedMaxSlots = 1 << 30;      // slots that a table row covers, a
 constexpr int kPagesMaxPages = 1 << 19;      // pages of a pool that pages are taken from, at most (bits and ranks in LDS)
 constexpr int kPagesMaxSeqs = 4096;          // sequences of a table (or pairs of a fork) there, at most
 
-struct PagedAttnArgs {
+struct PagedAttnArgs {       // fp32 (the bf16 kernels' AttnArgs have the same)
   const void* q;             // [B, Hq, T, D]
   const void* k;             // [pages, Hkv, page_size, D], page_stride bytes a page
   const void* v;
@@ -324,7 +324,6 @@ struct PagedAttnArgs {
   void* out;                 // [B, Hq, T, D]
   float* lse;                // [B, Hq, T] or nullptr
   int prompt;                // 0: the rows are tree nodes (T <= 128); 1: consecutive positions
-  int bf16;
   int B, Hq, Hkv, G, T, D;
   int num_pages, page_shift, width;
   int capacity;              // width << page_shift

@@ -1,4 +1,4 @@
-// Attention over a paged cache on the vector ALU: rows that are tree nodes (every node sees the prefix and its
+// Attention over a paged cache, fp32, on the vector ALU: rows that are tree nodes (every node sees the prefix and its
 // ancestors-or-self) or consecutive positions of a prompt (row i sees the slots up to its own), in either case only
 // keys within `window` positions, or among the first `sinks`.
 //
@@ -10,6 +10,7 @@
 #include "kernels.h"
 
 #include <math.h>
+#include <type_traits>
 
 namespace dreams {
 namespace {
@@ -18,7 +19,6 @@ constexpr float kLn2 = 0.69314718055994530942f;
 constexpr int kWaves = 16;
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
 template <int CTRL>
 __device__ __forceinline__ float add_rotated(float x) {
@@ -36,12 +36,7 @@ __device__ __forceinline__ float sum_lanes(float x) {
   return x;
 }
 
-__device__ __forceinline__ f32x4 load4(const float* p) { return *(const f32x4*)p; }
-__device__ __forceinline__ f32x4 load4(const __bf16* p) { return __builtin_convertvector(*(const bf16x4*)p, f32x4); }
-__device__ __forceinline__ void store1(float* p, float x) { *p = x; }
-__device__ __forceinline__ void store1(__bf16* p, float x) { *p = (__bf16)x; }
-
-template <typename E, int D, int R, bool PROMPT>
+template <int D, int R, bool PROMPT>
 __global__ __launch_bounds__(64 * kWaves) void paged_attn_f32_kernel(PagedAttnArgs a) {
   constexpr int NW = kWaves;
   constexpr int LPK = D / 4;          // lanes per key
@@ -74,11 +69,10 @@ __global__ __launch_bounds__(64 * kWaves) void paged_attn_f32_kernel(PagedAttnAr
   auto at = [&](int slot) {   // this lane's piece of a slot's row, in elements
     int id = table[slot >> a.page_shift];
     id = id < 0 ? 0 : (id >= a.num_pages ? a.num_pages - 1 : id);
-    return (int64_t)id * (a.page_stride / (int)sizeof(E)) +
-           ((int64_t)(g << a.page_shift) + (slot & ps1)) * D + 4 * c;
+    return (int64_t)id * (a.page_stride / 4) + (((int64_t)g << a.page_shift) + (slot & ps1)) * D + 4 * c;
   };
-  const E* kp = (const E*)a.k;
-  const E* vp = (const E*)a.v;
+  const float* kp = (const float*)a.k;
+  const float* vp = (const float*)a.v;
 
   // depths and ancestor sets of the tree's rows
   if constexpr (!PROMPT) {
@@ -132,7 +126,7 @@ __global__ __launch_bounds__(64 * kWaves) void paged_attn_f32_kernel(PagedAttnAr
   for (int r = 0; r < R; ++r) {
     const long long row = min(r0 + r, rows_u - 1);
     const int i = (int)(row % T);
-    q[r] = load4((const E*)a.q + (row0 + row) * D + 4 * c);
+    q[r] = *(const f32x4*)((const float*)a.q + (row0 + row) * D + 4 * c);
     acc[r] = f32x4{0.f, 0.f, 0.f, 0.f};
     m[r] = -INFINITY;
     l[r] = 0.f;
@@ -151,9 +145,10 @@ __global__ __launch_bounds__(64 * kWaves) void paged_attn_f32_kernel(PagedAttnAr
   const int total = first + (end_max - lo_min);
   auto slot_of = [&](int n) { return n < first ? n : n - first + lo_min; };
 
-  // NK groups of keys into every row's state; only the keys that see(r, t), whose values alone count
-  auto update = [&](auto nk, const f32x4* kk, const f32x4* vv, auto see) {
+  // NK groups of keys into every row's state; masked: only the keys that see(r, t), whose values alone count
+  auto update = [&](auto nk, auto masked, const f32x4* kk, const f32x4* vv, auto see) {
     constexpr int NK = decltype(nk)::value;
+    constexpr bool MASKED = decltype(masked)::value;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       float x[NK], mx = m[r];
@@ -164,7 +159,7 @@ __global__ __launch_bounds__(64 * kWaves) void paged_attn_f32_kernel(PagedAttnAr
         s = fmaf(q[r][2], kk[t][2], s);
         s = fmaf(q[r][3], kk[t][3], s);
         x[t] = sum_lanes<LPK>(s);
-        if (see(r, t)) mx = fmaxf(mx, x[t] * a.scale_log2);
+        if (!MASKED || see(r, t)) mx = fmaxf(mx, x[t] * a.scale_log2);
       }
       const float ref = mx == -INFINITY ? 0.f : mx;   // (nothing seen yet: every weight below is 2^-inf = 0)
       const float alpha = __builtin_amdgcn_exp2f(m[r] - ref);
@@ -172,7 +167,7 @@ __global__ __launch_bounds__(64 * kWaves) void paged_attn_f32_kernel(PagedAttnAr
       f32x4 pv = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int t = 0; t < NK; ++t) {
-        const bool s = see(r, t);
+        const bool s = !MASKED || see(r, t);
         const float p = s ? __builtin_amdgcn_exp2f(fmaf(x[t], a.scale_log2, -ref)) : 0.f;
         psum += p;
 #pragma unroll
@@ -195,19 +190,23 @@ __global__ __launch_bounds__(64 * kWaves) void paged_attn_f32_kernel(PagedAttnAr
       e[t] = at(slot[t]);
     }
 #pragma unroll
-    for (int t = 0; t < U; ++t) kk[t] = load4(kp + e[t]);
+    for (int t = 0; t < U; ++t) kk[t] = *(const f32x4*)(kp + e[t]);
 #pragma unroll
-    for (int t = 0; t < U; ++t) vv[t] = load4(vp + e[t]);
-    update(std::integral_constant<int, U>{}, kk, vv, [&](int r, int t) {
-      return n0 + t * KPI + kg < total && slot[t] < end[r] && (slot[t] >= lo[r] || slot[t] < a.sinks);
-    });
+    for (int t = 0; t < U; ++t) vv[t] = *(const f32x4*)(vp + e[t]);
+    const int first_slot = slot_of(n0), last_slot = slot_of(n0 + KPI * U - 1);   // (a pass in sight of every row)
+    if (n0 + KPI * U <= total && last_slot < end_min && first_slot >= lo_max)
+      update(std::integral_constant<int, U>{}, std::false_type{}, kk, vv, [](int, int) { return true; });
+    else
+      update(std::integral_constant<int, U>{}, std::true_type{}, kk, vv, [&](int r, int t) {
+        return n0 + t * KPI + kg < total && slot[t] < end[r] && (slot[t] >= lo[r] || slot[t] < a.sinks);
+      });
   }
   if constexpr (!PROMPT) {
     for (int j0 = wave * KPI; j0 < T; j0 += NW * KPI) {
       const int j = min(j0 + kg, T - 1);
       const int64_t e = at(L + j);
-      const f32x4 kt = load4(kp + e), vt = load4(vp + e);
-      update(std::integral_constant<int, 1>{}, &kt, &vt,
+      const f32x4 kt = *(const f32x4*)(kp + e), vt = *(const f32x4*)(vp + e);
+      update(std::integral_constant<int, 1>{}, std::true_type{}, &kt, &vt,
              [&](int r, int) { return j0 + kg < T && ((anc_lds[r][j >> 6] >> (j & 63)) & 1ull) != 0; });
     }
   }
@@ -248,36 +247,31 @@ __global__ __launch_bounds__(64 * kWaves) void paged_attn_f32_kernel(PagedAttnAr
   }
   const float lt = (l4[0] + l4[1]) + (l4[2] + l4[3]), o = (o4[0] + o4[1]) + (o4[2] + o4[3]);
   const size_t row = row0 + r0 + r;
-  store1((E*)a.out + row * D + d, lt > 0.f ? o / lt : 0.f);
+  ((float*)a.out)[row * D + d] = lt > 0.f ? o / lt : 0.f;
   if (a.lse && d == 0) a.lse[row] = lt > 0.f ? (M + log2f(lt)) * kLn2 : -INFINITY;
 }
 
-template <typename E, int D, bool PROMPT, int R>
+template <int D, bool PROMPT, int R>
 hipError_t launch_rows(const PagedAttnArgs& a, hipStream_t stream) {
   const long long grid = (long long)a.B * a.Hkv * (((long long)a.G * a.T + R - 1) / R);
-  hipLaunchKernelGGL((paged_attn_f32_kernel<E, D, R, PROMPT>), dim3((unsigned)grid), dim3(64 * kWaves), 0, stream, a);
+  hipLaunchKernelGGL((paged_attn_f32_kernel<D, R, PROMPT>), dim3((unsigned)grid), dim3(64 * kWaves), 0, stream, a);
   return hipGetLastError();
 }
 
-template <typename E, int D, bool PROMPT>
+template <int D, bool PROMPT>
 hipError_t launch(const PagedAttnArgs& a, hipStream_t stream) {
   const long long rows = (long long)a.B * a.Hq * a.T;
-  if (rows <= a.cus) return launch_rows<E, D, PROMPT, 1>(a, stream);
-  if (rows <= 2LL * a.cus) return launch_rows<E, D, PROMPT, 2>(a, stream);
-  return launch_rows<E, D, PROMPT, 4>(a, stream);
-}
-
-template <typename E>
-hipError_t launch_type(const PagedAttnArgs& a, hipStream_t stream) {
-  if (a.D == 64) return a.prompt ? launch<E, 64, true>(a, stream) : launch<E, 64, false>(a, stream);
-  if (a.D == 128) return a.prompt ? launch<E, 128, true>(a, stream) : launch<E, 128, false>(a, stream);
-  return hipErrorInvalidValue;
+  if (rows <= a.cus) return launch_rows<D, PROMPT, 1>(a, stream);
+  if (rows <= 2LL * a.cus) return launch_rows<D, PROMPT, 2>(a, stream);
+  return launch_rows<D, PROMPT, 4>(a, stream);
 }
 
 }  // namespace
 
 hipError_t launch_paged_attn_f32(const PagedAttnArgs& a, hipStream_t stream) {
-  return a.bf16 ? launch_type<__bf16>(a, stream) : launch_type<float>(a, stream);
+  if (a.D == 64) return a.prompt ? launch<64, true>(a, stream) : launch<64, false>(a, stream);
+  if (a.D == 128) return a.prompt ? launch<128, true>(a, stream) : launch<128, false>(a, stream);
+  return hipErrorInvalidValue;
 }
 
 }  // namespace dreams

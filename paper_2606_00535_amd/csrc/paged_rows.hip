@@ -14,7 +14,7 @@ __device__ __forceinline__ int64_t slot_offset(const PagedRowsArgs& a, const int
   const int id = table[slot >> a.page_shift];
   if (id < 0 || id >= a.num_pages) return -1;
   const int row = (int)slot & ((1 << a.page_shift) - 1);
-  return (int64_t)id * a.page_stride + ((int64_t)(g << a.page_shift) + row) * a.row_bytes;
+  return (int64_t)id * a.page_stride + (((int64_t)g << a.page_shift) + row) * a.row_bytes;
 }
 
 constexpr int kAppendThreads = 256;

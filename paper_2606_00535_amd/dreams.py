@@ -787,6 +787,8 @@ def _pool(k_pages, v_pages, page_table):
 def _table_pool(page_table, page_count, refcount, page_size):
     """(PagePool, device index)"""
     at = _current(page_table, "page_table", torch.int32)
+    if not 0 < page_size < 2 ** 31:
+        raise ValueError("page_size must be in [1, 2^31)")
     _need_on(page_table, "page_table", torch.int32, at, None, 2)
     B, width = page_table.shape
     _need_on(page_count, "page_count", torch.int32, at, (B,))
@@ -807,6 +809,8 @@ def paged_desc(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, pa
         raise ValueError("k_pages is on %s, expected %s" % (k_pages.device, q.device))
     _need_on(q, "q", dt, at, None, 4)
     _need_on(page_table, "page_table", torch.int32, at, None, 2)
+    if not (-1 < window < 2 ** 31 and -1 < sinks < 2 ** 31 and -1 < max_kv_len < 2 ** 31 and -1 < num_splits < 2 ** 31):
+        raise ValueError("window, sinks, max_kv_len and num_splits must be in [0, 2^31)")
     B, Hq, T, D = q.shape
     P, H, S, Dk = shape
     Bt, width = page_table.shape

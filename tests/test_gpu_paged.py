@@ -481,3 +481,252 @@ def test_prompts_steps_and_forks(dev, dt, window, sinks):
     assert count.cpu().numpy().tolist() == held.tolist()
     dreams.pages_release(table, count, kv_len, ref, R.ints([3, 2, 1, 0, 0], dev), ps)
     assert int(ref.abs().sum()) == 0 and int(count.sum()) == 0 and int(kv_len.sum()) == 0 and int((table != -1).sum()) == 0
+
+
+# -------------------------------------------------------------------------------- graphs, streams, workspaces, waits
+def attention_case(rng, dev, dt, kind):
+    bf16 = dt == torch.bfloat16
+    Hq, Hkv, D, ps, lens = 8, 2, 128, 16, [2100, 700]
+    T = 60 if kind == "verify" else 20 if kind == "verify16" else 200
+    c = R.Cache(rng, dev, np.array(lens) + T, Hkv, ps, D, bf16)
+    q, _ = R.rounded(rng, (2, Hq, T, D), bf16, dev)
+    kv = R.ints(lens, dev)
+    if kind == "prompt":
+        rows = R.ints([200, 77], dev)
+        return lambda **kw: dreams.paged_prompt_attn(q, c.kd, c.vd, c.tabled, kv, rows, window=900, sinks=3, **kw)
+    par = R.ints(R.tree(rng, 2, T), dev)
+    return lambda **kw: dreams.paged_verify_attn(q, c.kd, c.vd, c.tabled, kv, par, **kw)
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("kind", ["verify", "verify16", "prompt"])
+def test_attention_replayed(dev, dt, kind):
+    """Captured calls without a workspace of the caller's have their own: two graphs and eager calls do not share one."""
+    call = attention_case(np.random.default_rng(11), dev, dt, kind)
+    eager = [bits(t) for t in call(num_splits=4)]
+    graphs, outs = [], []
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(call(num_splits=4))
+        graphs.append(g)
+    side = [torch.cuda.Stream() for _ in range(2)]
+    filler = torch.zeros(333, device=dev)
+    for rep in range(4):
+        for pair in outs:
+            for t in pair:
+                t.fill_(float("nan"))
+        torch.cuda.synchronize()
+        for g, s in zip(graphs, side):       # both at once
+            with torch.cuda.stream(s):
+                g.replay()
+        filler.add_(1.0)
+        other = call(num_splits=4)           # and an eager one
+        torch.cuda.synchronize()
+        for pair in outs + [other]:
+            for t, want in zip(pair, eager):
+                assert np.array_equal(bits(t), want), (kind, rep)
+
+
+@pytest.mark.parametrize("kind", ["verify", "prompt"])
+def test_attention_on_other_streams(dev, kind):
+    call = attention_case(np.random.default_rng(12), dev, torch.bfloat16, kind)
+    want = [bits(t) for t in call(num_splits=3)]
+    torch.cuda.synchronize()
+    side = [torch.cuda.Stream() for _ in range(3)]
+    results = []
+    for s in side:                           # as the current stream, one workspace each
+        with torch.cuda.stream(s):
+            results.append(call(num_splits=3))
+    for s in side:                           # and given
+        results.append(call(num_splits=3, stream=s))
+    torch.cuda.synchronize()
+    for r in results:
+        for t, w in zip(r, want):
+            assert np.array_equal(bits(t), w)
+    outs = [torch.empty_like(results[0][0]), torch.empty_like(results[0][1])]
+    with pytest.raises(ValueError, match="out must be"):
+        call(out=outs[0][:, :1].contiguous())
+    with pytest.raises(ValueError, match="workspace"):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            call(num_splits=3, stream=side[0])
+
+
+def test_workspaces(dev):
+    """A caller's workspace: too small is refused, left zero, free of flags; a wait that gives up is reported."""
+    rng = np.random.default_rng(13)
+    D, T, lens = 128, 60, [2000, 1900]
+    for Hq, Hkv in ((4, 2), (16, 2)):        # 128 and 480 rows a KV head
+        c = R.Cache(rng, dev, np.array(lens) + T, Hkv, 32, D, True)
+        q, qh = R.rounded(rng, (2, Hq, T, D), True, dev)
+        par = R.tree(rng, 2, T)
+        desc = dreams.paged_desc(q, c.kd, c.vd, c.tabled, num_splits=8)
+        n = dreams.paged_verify_attn_workspace_size(desc)
+        assert n > 65536
+        ws = torch.zeros(n, dtype=torch.uint8, device=dev)
+
+        def call():
+            return dreams.paged_verify_attn(q, c.kd, c.vd, c.tabled, R.ints(lens, dev), R.ints(par, dev), num_splits=8,
+                                            workspace=ws)
+        ref = R.verify(qh, c.k, c.v, c.table, lens, par, R.ancestors(par), 0, 0, 1 / np.sqrt(D))
+        for _ in range(2):
+            R.check(*call(), ref, True, "workspace")
+            dreams.workspace_status(ws)
+            assert not ws[:65536].any()
+        with pytest.raises(dreams.DreamsError) as e:
+            dreams.paged_verify_attn(q, c.kd, c.vd, c.tabled, R.ints(lens, dev), R.ints(par, dev), num_splits=8,
+                                     workspace=ws[:n - 256])
+        assert e.value.status == dreams.DREAMS_ERR_WORKSPACE
+        try:
+            dreams.set_wait_limit(0.0)
+            call()
+            torch.cuda.synchronize()
+            with pytest.raises(dreams.DreamsError) as e:
+                dreams.workspace_status(ws)
+            assert e.value.status == dreams.DREAMS_ERR_DEVICE
+        finally:
+            dreams.set_wait_limit(0.2)
+        ws[:65536].zero_()
+        R.check(*call(), ref, True, "after a wait that gave up")
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+def test_upkeep_replayed(dev, dt):
+    """Release, fork, reserve, append and commit in one graph: every replay does what the definition does."""
+    rng = np.random.default_rng(14)
+    B, width, P, ps, NL, Hkv, D, N = 5, 12, 70, 16, 2, 2, 64, 6
+    t = R.Tables(B, width, P, ps)
+    lens = np.array([70, 33, 0, 48, 100], np.int32)
+    t.reserve(lens)
+    t.kv_len[:] = lens
+    on = t.on(dev)
+    table, count, kv_len, ref = on
+    k, v = random_bits(rng, (NL, P, Hkv, ps, D), dt, dev), random_bits(rng, (NL, P, Hkv, ps, D), dt, dev)
+    new = [random_bits(rng, (NL, B, Hkv, N, D), dt, dev) for _ in range(2)]
+    src, dst = R.ints([0, 1], dev), R.ints([2, 4], dev)
+    path, alen = R.ints([[0, 2, 5, -1, -1, -1]] * B, dev), R.ints([2, 1, 0, 2, 2], dev)
+    outs = dict(forked=torch.zeros(2, dtype=torch.int32, device=dev), room=torch.zeros(B, dtype=torch.int32, device=dev),
+                after=torch.zeros(B, dtype=torch.int32, device=dev))
+
+    def chain():
+        dreams.pages_release(table, count, kv_len, ref, dst, ps)
+        dreams.pages_fork(k, v, table, count, kv_len, ref, src, dst, granted=outs["forked"])
+        dreams.pages_reserve(table, count, ref, kv_len + N, ps, granted=outs["room"])
+        dreams.paged_append(new[0], new[1], k, v, table, kv_len)
+        dreams.paged_kv_commit(k, v, table, kv_len, path, alen, kv_len_out=outs["after"])
+        kv_len.copy_(outs["after"])
+
+    start = [x.clone() for x in on + [k, v]]
+    side = torch.cuda.Stream()               # every kernel once before the capture
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        chain()
+    torch.cuda.synchronize()
+    for x, y in zip(on + [k, v], start):
+        x.copy_(y)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        chain()
+    pools = [bits(k).copy(), bits(v).copy()]
+    for rep in range(4):
+        g.replay()
+        torch.cuda.synchronize()
+        t.release([2, 4])
+        granted, copies = t.fork([0, 1], [2, 4])
+        assert outs["forked"].tolist() == granted == [1, 1]
+        room = t.reserve(t.kv_len + N)
+        assert outs["room"].tolist() == room == [1] * B, rep
+        for w, x in zip(pools, new):
+            xb = bits(x)
+            for a, b, n in copies:
+                w[:, b, :, :n] = w[:, a, :, :n]
+            for b in range(B):
+                for i in range(N):
+                    j = int(t.kv_len[b]) + i
+                    w[:, t.table[b, j // ps], :, j % ps] = xb[:, b, :, i]
+                for n in range(int(alen[b]) + 1):
+                    s, d = int(t.kv_len[b]) + [0, 2, 5][n], int(t.kv_len[b]) + n
+                    w[:, t.table[b, d // ps], :, d % ps] = w[:, t.table[b, s // ps], :, s % ps]
+        t.kv_len += alen.cpu().numpy() + 1
+        assert outs["after"].tolist() == t.kv_len.tolist()
+        t.same(on)
+        assert np.array_equal(bits(k), pools[0]) and np.array_equal(bits(v), pools[1])
+
+
+def test_empty_batches(dev):
+    z = lambda *s: torch.zeros(s, dtype=torch.int32, device=dev)
+    pages = torch.zeros((3, 2, 16, 64), dtype=torch.bfloat16, device=dev)
+    q = torch.zeros((0, 4, 5, 64), dtype=torch.bfloat16, device=dev)
+    out, lse = dreams.paged_verify_attn(q, pages, pages, z(0, 4), z(0), z(0, 5))
+    assert out.shape == q.shape and lse.shape == (0, 4, 5)
+    dreams.paged_prompt_attn(q, pages, pages, z(0, 4), z(0))
+    dreams.paged_append(torch.zeros((0, 2, 5, 64), dtype=torch.bfloat16, device=dev),
+                        torch.zeros((0, 2, 5, 64), dtype=torch.bfloat16, device=dev), pages, pages, z(0, 4), z(0))
+    dreams.paged_append(torch.zeros((2, 2, 0, 64), dtype=torch.bfloat16, device=dev),
+                        torch.zeros((2, 2, 0, 64), dtype=torch.bfloat16, device=dev), pages, pages, z(2, 4), z(2))
+    assert dreams.paged_kv_commit(pages, pages, z(0, 4), z(0), z(0, 5), z(0)).shape == (0,)
+    assert dreams.pages_reserve(z(0, 4), z(0), z(3), z(0), 16).shape == (0,)
+    table, count, kv, ref = z(2, 4), z(2), z(2), z(3)
+    assert dreams.pages_fork(pages, pages, table, count, kv, ref, z(0), z(0)).shape == (0,)
+    dreams.pages_release(table, count, kv, ref, z(0), 16)
+    torch.cuda.synchronize()
+
+
+def test_refusals_on_the_device(dev):
+    """What only device tensors reach: shapes, layouts, ranges."""
+    z = lambda *s: torch.zeros(s, dtype=torch.int32, device=dev)
+    pages = torch.zeros((3, 2, 16, 64), dtype=torch.bfloat16, device=dev)
+    q = torch.zeros((2, 4, 5, 64), dtype=torch.bfloat16, device=dev)
+    ok = dict(q=q, k_pages=pages, v_pages=pages, page_table=z(2, 4), kv_len=z(2))
+
+    def bad(exception, match, **kw):
+        for f, more in ((dreams.paged_verify_attn, dict(parent=z(2, 5))), (dreams.paged_prompt_attn, {})):
+            with pytest.raises(exception, match=match):
+                f(**{**ok, **more, **kw})
+    bad(TypeError, "q must be", q=q.float())
+    bad(ValueError, "contiguous", q=q.transpose(1, 2))
+    bad(ValueError, "device tensor", q=q.cpu())
+    bad(ValueError, "mismatch", page_table=z(3, 4))
+    bad(ValueError, "kv_len must be", kv_len=z(3))
+    bad(TypeError, "kv_len must be", kv_len=z(2).long())
+    bad(ValueError, "differ in shape", v_pages=pages[:2])
+    bad(ValueError, "dense", k_pages=torch.zeros((3, 2, 16, 128), dtype=torch.bfloat16, device=dev)[..., :64],
+        v_pages=torch.zeros((3, 2, 16, 128), dtype=torch.bfloat16, device=dev)[..., :64])
+    bad(ValueError, "layout", k_pages=torch.zeros((3, 2, 2, 16, 64), dtype=torch.bfloat16, device=dev)[:, 0])
+    bad(ValueError, "window", window=2 ** 32)
+    bad(ValueError, "window", sinks=-1)
+    bad(dreams.DreamsError, "max_kv_len", max_kv_len=60)
+    bad(dreams.DreamsError, "scale", scale=float("inf"))
+    bad(ValueError, "lse must be", lse=torch.zeros((2, 4, 4), device=dev))
+    with pytest.raises(ValueError, match="parent must be"):
+        dreams.paged_verify_attn(**ok, parent=z(2, 4))
+    with pytest.raises(dreams.DreamsError, match="parent or tree_mask"):
+        dreams.paged_verify_attn(**ok)
+    with pytest.raises(dreams.DreamsError, match="depths"):
+        dreams.paged_verify_attn(**ok, window=4, tree_mask=torch.ones((2, 5, 1), dtype=torch.int64, device=dev))
+    with pytest.raises(ValueError, match="row_len must be"):
+        dreams.paged_prompt_attn(**ok, row_len=z(1))
+    odd = torch.zeros((3, 2, 24, 64), dtype=torch.bfloat16, device=dev)
+    bad(dreams.DreamsError, "page_size", k_pages=odd, v_pages=odd)
+    new = torch.zeros((2, 2, 5, 64), dtype=torch.bfloat16, device=dev)
+    for wrong in (new[:1], new[:, :1], new[..., :32], new.float(), new[None]):
+        with pytest.raises((ValueError, TypeError)):
+            dreams.paged_append(wrong, wrong, pages, pages, z(2, 4), z(2))
+    with pytest.raises(ValueError, match="dense"):
+        dreams.paged_append(new.transpose(2, 3).contiguous().transpose(2, 3), new.transpose(2, 3).contiguous().transpose(2, 3),
+                            pages, pages, z(2, 4), z(2))
+    with pytest.raises(dreams.DreamsError, match="strides"):
+        wide = torch.zeros((2, 2, 5, 66), dtype=torch.bfloat16, device=dev)[..., :64]
+        dreams.paged_append(wide, wide, pages, pages, z(2, 4), z(2))
+    with pytest.raises(ValueError, match="refcount must be"):
+        dreams.pages_fork(pages, pages, z(2, 4), z(2), z(2), z(4), z(1), z(1))
+    with pytest.raises(ValueError, match="dst must be"):
+        dreams.pages_fork(pages, pages, z(2, 4), z(2), z(2), z(3), z(1), z(2))
+    with pytest.raises(ValueError, match="page_size"):
+        dreams.pages_reserve(z(2, 4), z(2), z(3), z(2), 2 ** 32 + 16)
+    with pytest.raises(dreams.DreamsError, match="page_size"):
+        dreams.pages_reserve(z(2, 4), z(2), z(3), z(2), 48)
+    kv = z(2)
+    with pytest.raises(dreams.DreamsError, match="overlap"):
+        dreams.paged_kv_commit(pages, pages, z(2, 4), kv, z(2, 5), z(2), kv_len_out=kv)
