@@ -1324,7 +1324,8 @@ dreams_status_t plan_paged(const dreams_paged_desc_t* d, bool prompt, PagedPlan*
       // Key groups in a workgroup first (paged_key_groups): pieces as far as every workgroup has a compute unit of its own;
       // or, where that leaves much of the chip idle and the row groups are about as long, workgroups of one key group, two to
       // a unit.
-      const long long long_enough = n_keys / kPlanPieceKeys;
+      // (8 heads on 2 x 300 rows behind 500: pieces of at least 384 keys 22.9 us, of 160 16.9, of 128 16.9, of 64 16.5)
+      const long long long_enough = n_keys / kPieceMinKeys;
       const long long whole = std::min(xcd_cus / xcd_wgs, long_enough), two = std::min(2 * xcd_cus / xcd_wgs, long_enough);
       const bool level = 10LL * plan->shortest >= 6LL * plan->longest;
       splits = (int)(level && 5 * two >= 12 * std::max(whole, 1LL) ? two : whole);

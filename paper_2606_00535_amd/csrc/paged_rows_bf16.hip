@@ -103,6 +103,16 @@ __global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(At
   const int i0 = one_head ? row_base % T : 0;
   const size_t row0 = ((size_t)b * a.Hq + (size_t)g * a.G) * T + row_base;
 
+  // ---- queries: B operand of the score products, row col of the wave, 8 columns from 16 ds + 8 h on.  (Loaded ahead of the
+  // lengths and the table, used once the first copies are out.)
+  const int row = wave * kRows + col;                // this lane's row of the workgroup
+  bf16x8 qf[KS];
+  {
+    const unsigned char* src = (const unsigned char*)a.q + (row0 + min(row, rows_here - 1)) * L::ROW;
+#pragma unroll
+    for (int ds = 0; ds < KS; ++ds) qf[ds] = *(const bf16x8*)(src + (ds * 16 + 8 * h) * 2);
+  }
+
   int nb = T;
   if (!TREE && a.row_len) nb = min(max(a.row_len[b], 0), T);
   const int Lp = min(max(a.kv_len[b], 0), a.S_cap - nb);
@@ -172,24 +182,6 @@ __global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(At
     }
   };
 
-  // ---- queries: B operand of the score products, row col of the wave, 8 columns from 16 ds + 8 h on
-  const int row = wave * kRows + col;                // this lane's row of the workgroup
-  bf16x8 qf[KS];
-  {
-    const unsigned char* src = (const unsigned char*)a.q + (row0 + min(row, rows_here - 1)) * L::ROW;
-#pragma unroll
-    for (int ds = 0; ds < KS; ++ds) qf[ds] = *(const bf16x8*)(src + (ds * 16 + 8 * h) * 2);
-  }
-  const int node = (row_base + min(row, rows_here - 1)) % T;   // the lane's tree node, or its position behind the prefix
-  const bool live = row < rows_here && (TREE || node < nb);
-  const float c_scale = fmaxf(fabsf(a.scale_log2), 1.17549435e-38f);
-#pragma unroll
-  for (int ds = 0; ds < KS; ++ds) {
-    u32x4 x = __builtin_bit_cast(u32x4, qf[ds]);
-    if (a.scale_log2 < 0.f) x ^= 0x80008000u;        // (a negative scale flips the queries' signs, exact)
-    if (!live) x = u32x4{0u, 0u, 0u, 0u};            // (rows past the sequence's own may hold anything)
-    qf[ds] = __builtin_bit_cast(bf16x8, x);
-  }
   // (this piece has started: see merge_set)
   unsigned long long start_old = 0;
   const size_t pset = (size_t)u * a.row_groups + rg;
@@ -208,6 +200,16 @@ __global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(At
   for (int j = 0; j < AHEAD; ++j)
     if (j < periods) issue(j);
 
+  const int node = (row_base + min(row, rows_here - 1)) % T;   // the lane's tree node, or its position behind the prefix
+  const bool live = row < rows_here && (TREE || node < nb);
+  const float c_scale = fmaxf(fabsf(a.scale_log2), 1.17549435e-38f);
+#pragma unroll
+  for (int ds = 0; ds < KS; ++ds) {
+    u32x4 x = __builtin_bit_cast(u32x4, qf[ds]);
+    if (a.scale_log2 < 0.f) x ^= 0x80008000u;        // (a negative scale flips the queries' signs, exact)
+    if (!live) x = u32x4{0u, 0u, 0u, 0u};            // (rows past the sequence's own may hold anything)
+    qf[ds] = __builtin_bit_cast(bf16x8, x);
+  }
   // ---- what the rows see: of a chain the slots [see_from, see_to] and the sinks; of a tree the prefix from see_from on, the
   // sinks, and the nodes in anc0, anc1
   int pos = Lp + node, deepest = 0;
