@@ -516,8 +516,9 @@ dreams_status_t dreams_paged_prompt_attn_workspace_size(const dreams_paged_desc_
  *                                     sight; the window needs parent for the depths)
  *   out          device [B, Hq, T, D] same dtype as q;  lse: device [B, Hq, T] float or NULL
  * A row that sees nothing (a mask without a prefix in sight) gives out = 0 and lse = -inf.  Values in slots that no row
- * sees do not matter (NaN and infinities included); those of the tree's own slots are to be finite.  Arithmetic and
- * workspace as for dreams_tree_verify_attn, but for the pieces' rows, which are merged in fp32 unrounded.
+ * sees do not matter (NaN and infinities included).  Values (V) in slots that only some of a sequence's rows see (the
+ * rows' own, and those that a window ends in) are to be finite: elsewhere than in the rows that see it, a V that is not may
+ * leave NaN too.  K may hold anything where a row does not see it.  Arithmetic and workspace as for dreams_tree_verify_attn, but for the pieces' rows, which are merged in fp32 unrounded.
  */
 dreams_status_t dreams_paged_verify_attn(const dreams_paged_desc_t* desc, const void* q, const void* k_pages,
                                          const void* v_pages, const int32_t* page_table, const int32_t* kv_len,
@@ -531,7 +532,8 @@ dreams_status_t dreams_paged_verify_attn(const dreams_paged_desc_t* desc, const 
  *   q          device [B, Hq, N, D]
  *   kv_len     device [B] int32   L_b, slots before the rows' own; clamped into [0, table_width * page_size - n_b]
  *   row_len    device [B] int32   n_b, live rows (clamped into [0, N]), or NULL: N each
- *   out, lse   as above; rows i >= n_b get out = 0 and lse = -inf
+ *   out, lse   as above; rows i >= n_b get out = 0 and lse = -inf (their q, and the slots from
+ *              L_b + n_b on, may hold anything)
  */
 dreams_status_t dreams_paged_prompt_attn(const dreams_paged_desc_t* desc, const void* q, const void* k_pages,
                                          const void* v_pages, const int32_t* page_table, const int32_t* kv_len,

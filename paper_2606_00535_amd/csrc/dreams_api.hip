@@ -1179,6 +1179,9 @@ dreams_status_t check_pages(int32_t num_pages, int32_t page_size, int32_t table_
   return DREAMS_OK;
 }
 
+// (a launch has at most 2^32 - 1 threads along its first axis)
+bool fits_grid(long long workgroups, int threads) { return workgroups <= 0xffffffffLL / threads; }
+
 int page_shift_of(int page_size) { return __builtin_ctz((unsigned)page_size); }
 
 // A page stride (elements; 0: dense) against the page it has to hold and 16-byte alignment.
@@ -1220,7 +1223,11 @@ dreams_status_t check_paged_desc(const dreams_paged_desc_t* d, bool prompt) {
   const int64_t page = (int64_t)d->num_kv_heads * d->page_size * d->head_dim;
   st = check_page_stride(d->page_stride, page, d->dtype == DREAMS_BF16 ? 2 : 4, d->num_pages);
   if (st != DREAMS_OK) return st;
-  if ((long long)d->batch * d->num_q_heads > 0x7fffffffLL / d->num_rows)
+  const long long rows = (long long)d->batch * d->num_q_heads;
+  if (rows > 0x7fffffffLL / d->num_rows ||
+      (d->dtype == DREAMS_F32 && !fits_grid(paged_attn_f32_workgroups(d->batch * d->num_kv_heads,
+                                                                      d->num_q_heads / d->num_kv_heads, d->num_rows),
+                                            kPagedF32Threads)))
     return fail(DREAMS_ERR_UNSUPPORTED, "problem too large");
   return DREAMS_OK;
 }
@@ -1340,7 +1347,7 @@ dreams_status_t plan_paged(const dreams_paged_desc_t* d, bool prompt, PagedPlan*
   const long long sets = (long long)p.units * p.row_groups;
   if (2 * sets > kMaxSetCounters || splits < 1) splits = 1;
   p.splits = splits;
-  if (8 * xcd_wgs * splits > 0x7fffffffLL) return fail(DREAMS_ERR_UNSUPPORTED, "problem too large");
+  if (!fits_grid(8 * xcd_wgs * splits, 512)) return fail(DREAMS_ERR_UNSUPPORTED, "problem too large");
   if (splits > 1) {
     int stride = 16;
     while (stride > 2 && sets * stride > kMaxSetCounters) stride >>= 1;
@@ -1515,7 +1522,8 @@ dreams_status_t check_pool(const dreams_page_pool_t* p, int* elem) {
                   (long long)p->layer_stride);
   }
   if (p->batch > 65535 || p->num_layers > 65535 ||
-      (long long)p->num_layers * p->num_kv_heads > 0x7fffffffLL / (p->batch > 0 ? p->batch : 1))
+      !fits_grid((long long)p->num_layers * p->num_kv_heads, 256) ||
+      !fits_grid((long long)p->num_layers * p->num_kv_heads * p->batch, 64))
     return fail(DREAMS_ERR_UNSUPPORTED, "problem too large");
   return DREAMS_OK;
 }
@@ -1562,7 +1570,7 @@ dreams_status_t dreams_paged_append(const dreams_page_pool_t* pool, const void* 
     if (lengths[i] > 1 && (strides[i] < 0 || strides[i] > (int64_t)1 << 48 || strides[i] * elem % 16 != 0))
       return fail(DREAMS_ERR_INVALID_ARG, "strides[%d] = %lld must be a non-negative multiple of 16 bytes", i,
                   (long long)strides[i]);
-  if ((long long)num_rows * pool->num_kv_heads / 4 > 0x7fffffffLL / (pool->head_dim * elem / 16))
+  if ((long long)num_rows * pool->num_kv_heads > (0xffffffffLL - 255) / (pool->head_dim * elem / 16))
     return fail(DREAMS_ERR_UNSUPPORTED, "problem too large");
   if (pool->batch == 0 || num_rows == 0) return ok();
   if (!k_new || !v_new || !page_table || !kv_len || !k_pages || !v_pages)

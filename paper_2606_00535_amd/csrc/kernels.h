@@ -332,6 +332,10 @@ struct PagedAttnArgs {       // fp32 (the bf16 kernels' AttnArgs have the same)
   float scale_log2;          // scale * log2(e)
   int cus;
 };
+constexpr int kPagedF32Threads = 1024;
+inline long long paged_attn_f32_workgroups(int units, int G, int T) {   // of a large call: 4 rows each
+  return (long long)units * (((long long)G * T + 3) / 4);
+}
 hipError_t launch_paged_attn_f32(const PagedAttnArgs& a, hipStream_t stream);
 hipError_t launch_paged_attn_bf16(const AttnArgs& a, hipStream_t stream);   // up to 64 rows a KV head
 hipError_t launch_paged_rows_bf16(const AttnArgs& a, hipStream_t stream);   // 128 rows a workgroup

@@ -16,7 +16,7 @@ namespace dreams {
 namespace {
 
 constexpr float kLn2 = 0.69314718055994530942f;
-constexpr int kWaves = 16;
+constexpr int kWaves = kPagedF32Threads / 64;
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 

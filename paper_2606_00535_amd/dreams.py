@@ -771,6 +771,8 @@ def _page_strides(k_pages: torch.Tensor, v_pages: torch.Tensor):
     if st[-3:] != (S * D, D, 1) and any(shape[i] > 1 and st[i] != dense
                                        for i, dense in ((n - 1, 1), (n - 2, D), (n - 3, S * D))):
         raise ValueError("pages must be dense [Hkv, page_size, D]")
+    if (P > 1 and st[-4] == 0) or (n == 5 and shape[0] > 1 and st[0] == 0):   # (0 means dense below)
+        raise ValueError("pages or layers share memory (expanded views)")
     return shape, st[0] if n == 5 and shape[0] > 1 else 0, st[-4] if P > 1 else H * S * D
 
 
@@ -828,12 +830,18 @@ def _call_paged(call, size, desc, tensors, workspace, at, stream):
     that belongs to the graph, its counters cleared by every replay, so that no two graphs share one)."""
     st = _stream(stream)
     if workspace is not None:
+        if workspace.get_device() != at or not workspace.is_contiguous():
+            raise ValueError("workspace must be a contiguous tensor on the call's device")
         _check(call(desc, *tensors, _ptr(workspace), workspace.numel() * workspace.element_size(), st))
         return
-    if torch.cuda.is_current_stream_capturing():
-        device = torch.device("cuda", at)
-        if stream is not None and stream.cuda_stream != torch.cuda.current_stream().cuda_stream:
+    capturing = torch.cuda.is_current_stream_capturing()
+    if stream is not None and stream.cuda_stream != torch.cuda.current_stream().cuda_stream:
+        with torch.cuda.stream(stream):
+            capturing |= torch.cuda.is_current_stream_capturing()
+        if capturing:
             raise ValueError("a call captured on another stream than the current one needs a workspace")
+    if capturing:
+        device = torch.device("cuda", at)
         n = ctypes.c_size_t(0)
         _check(size(desc, ctypes.byref(n)))
         ws = None

@@ -730,3 +730,27 @@ def test_refusals_on_the_device(dev):
     kv = z(2)
     with pytest.raises(dreams.DreamsError, match="overlap"):
         dreams.paged_kv_commit(pages, pages, z(2, 4), kv, z(2, 5), z(2), kv_len_out=kv)
+
+
+def test_workspaces_that_are_refused(dev):
+    call = attention_case(np.random.default_rng(12), dev, torch.bfloat16, "verify")
+    with pytest.raises(ValueError, match="workspace"):
+        call(num_splits=3, workspace=torch.zeros(1 << 22, dtype=torch.uint8))
+    with pytest.raises(ValueError, match="workspace"):
+        call(num_splits=3, workspace=torch.zeros((1 << 22, 2), dtype=torch.uint8, device=dev)[:, 0])
+    out, lse = call(num_splits=3)
+    want = [bits(out), bits(lse)]
+    # captured on a stream that is not the current one
+    side, other = torch.cuda.Stream(), torch.cuda.Stream()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        outs = call(num_splits=3)
+        with torch.cuda.stream(other):
+            with pytest.raises(ValueError, match="workspace"):
+                call(num_splits=3, stream=side, out=out, lse=lse)
+    for _ in range(3):
+        g.replay()
+        torch.cuda.synchronize()
+        for t, w in zip(outs, want):
+            assert np.array_equal(bits(t), w)
+        call(num_splits=3)

@@ -175,3 +175,41 @@ def test_bindings(D):
         D.pages_fork(pages, pages, table, one, one, torch.zeros(4, dtype=torch.int32), one, one)
     with pytest.raises(ValueError, match="device tensor"):
         D.pages_release(table, one, one, torch.zeros(4, dtype=torch.int32), one, 16)
+
+
+def test_limits_of_a_launch(D):
+    """Calls with more threads than a launch can have are refused by name."""
+    n = ctypes.c_size_t(0)
+    big = dict(batch=1 << 10, num_q_heads=32, num_kv_heads=8, page_size=1024, table_width=1024)
+    size = D.lib().dreams_paged_prompt_attn_workspace_size
+    # 2^15 heads of 4096 rows: 2^25 workgroups of 1024 threads in fp32, 2^20 of 128 rows in bf16
+    assert size(ctypes.byref(desc(D, num_rows=4096, dtype=D.DREAMS_F32, **big)), ctypes.byref(n)) == -2
+    assert size(ctypes.byref(desc(D, num_rows=4096, **big)), ctypes.byref(n)) == 0
+    assert size(ctypes.byref(desc(D, num_rows=511, dtype=D.DREAMS_F32, **big)), ctypes.byref(n)) == 0
+    # 2^27 units of one row group
+    assert size(ctypes.byref(desc(D, batch=1 << 24, num_q_heads=8, num_kv_heads=8, num_rows=1)), ctypes.byref(n)) == -2
+    pool = D.PagePool(1, 1, 8, 128, 4, 16, 4, D.DREAMS_BF16, 0, 0)
+    strides = (ctypes.c_int64 * 4)(0, 0, 128, 1024)
+    append = lambda rows: D.lib().dreams_paged_append(ctypes.byref(pool), None, None, rows, strides, FAKE, FAKE, None,
+                                                      FAKE, FAKE, None)
+    assert append(1 << 25) == -2             # 2^25 rows of 8 heads, 16 words each: 2^32 threads
+    assert append((1 << 25) - 2) == -1       # (it fits: the next check, of k_new, refuses it)
+    wide = D.PagePool(60000, 60000, 8, 64, 4, 16, 4, D.DREAMS_BF16, 0, 0)
+    assert D.lib().dreams_paged_kv_commit(ctypes.byref(wide), *[FAKE] * 6, 5, FAKE, None) == -2
+
+
+def test_views_whose_pages_share_memory(D):
+    """An expanded view has no stride between its pages (or layers): refused, not taken for a dense pool."""
+    table, one = torch.zeros((1, 3), dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
+    page, layer = torch.zeros((1, 2, 16, 64)), torch.zeros((1, 4, 2, 16, 64))
+    for pages in (page.expand(4, 2, 16, 64), layer.expand(3, 4, 2, 16, 64)):
+        with pytest.raises(ValueError, match="share memory"):
+            D.paged_append(pages, pages, pages, pages, table, one)
+        with pytest.raises(ValueError, match="share memory"):
+            D.paged_kv_commit(pages, pages, table, one, table, one)
+        with pytest.raises(ValueError, match="share memory"):
+            D.pages_fork(pages, pages, table, one, one, torch.zeros(4, dtype=torch.int32), one, one)
+    with pytest.raises(ValueError, match="share memory"):
+        D.paged_prompt_attn(torch.zeros((1, 2, 3, 64)), page.expand(4, 2, 16, 64), page.expand(4, 2, 16, 64), table, one)
+    with pytest.raises(ValueError, match="device tensor"):    # (one page, one layer: no stride is used)
+        D.paged_append(page, page, page.expand(1, 2, 16, 64), page, table, one)
