@@ -1279,6 +1279,28 @@ struct PagedPlan {
   int longest, shortest;   // keys of a row group, by the host's bound
 };
 
+// Pieces of the key axis for workgroups of 128 rows, xcd_wgs on each XCD: the number that takes the least time, in keys that a
+// compute unit takes for 128 rows (16.6 ns each at D = 128).  A workgroup alone on its unit has two key groups and takes its
+// keys at the unit's rate, two share it.  Pieces cost their rows' way to memory and back: 300 keys and 1.25 for each.
+// (level: the row groups are about as long.  Else pieces only as far as every workgroup has a unit of its own.)
+// 32 heads on 8 x 4 x 140 rows behind 1000 keys, 160 workgroups: 28 us whole, 41, 37 and 46 in 2, 3 and 4 pieces; on 140 x 2
+// rows: 27, 28, 25, 27; 28 heads on 4 x 6 x 219 rows of 64 columns behind 5228: 125, 116, 104, 104.
+int paged_pieces(int n_keys, long long xcd_wgs, long long xcd_cus, bool level) {
+  long long best = 0;
+  int pieces = 1;
+  for (int s = 1; s <= kAttnMaxSplits && (s == 1 || s <= n_keys / kPieceMinKeys); ++s) {
+    const long long wgs = xcd_wgs * s, rest = wgs % (2 * xcd_cus);
+    if (s > 1 && !level && wgs > xcd_cus) break;
+    const long long turns = wgs / (2 * xcd_cus) * 2 + (rest == 0 ? 0 : rest <= xcd_cus ? 1 : 2);
+    const long long time = turns * ((n_keys + s - 1) / s) + (s > 1 ? 300 + 10 * wgs : 0);
+    if (s == 1 || time < best) {
+      best = time;
+      pieces = s;
+    }
+  }
+  return pieces;
+}
+
 dreams_status_t plan_paged(const dreams_paged_desc_t* d, bool prompt, PagedPlan* plan) {
   dreams_status_t st = check_paged_desc(d, prompt);
   if (st != DREAMS_OK) return st;
@@ -1297,7 +1319,9 @@ dreams_status_t plan_paged(const dreams_paged_desc_t* d, bool prompt, PagedPlan*
   p.units = d->batch * d->num_kv_heads;
   int span = T;   // positions that a workgroup's rows can be apart
   if (prompt && p.row_groups > 1) {
-    // Row groups of one head see only the keys before them; packed ones leave no row of a workgroup empty.
+    // Row groups of one head see only the keys before them; packed ones leave no row of a workgroup empty.  The fewer keys
+    // decide (32 heads, 8 KV heads: 2000 rows 84 us packed, 51 by heads; 28 heads, 4 KV heads, 16 x 140 rows behind 1000 keys
+    // 49 packed, 72 by heads).
     const int R = p.rows_per_wg;
     const long long per_head = (long long)p.G * ((T + R - 1) / R);
     if (per_head * (max_len + T / 2 + R / 2) <= p.row_groups * (max_len + T)) {
@@ -1328,14 +1352,7 @@ dreams_status_t plan_paged(const dreams_paged_desc_t* d, bool prompt, PagedPlan*
     splits = coarse_splits(8 * xcd_wgs, (long long)cus * wpc, n_keys);
     if (splits > kAttnMaxSplits) splits = kAttnMaxSplits;
     if (p.rows_per_wg == 128) {
-      // Key groups in a workgroup first (paged_key_groups): pieces as far as every workgroup has a compute unit of its own;
-      // or, where that leaves much of the chip idle and the row groups are about as long, workgroups of one key group, two to
-      // a unit.
-      // (8 heads on 2 x 300 rows behind 500: pieces of at least 384 keys 22.9 us, of 160 16.9, of 128 16.9, of 64 16.5)
-      const long long long_enough = n_keys / kPieceMinKeys;
-      const long long whole = std::min(xcd_cus / xcd_wgs, long_enough), two = std::min(2 * xcd_cus / xcd_wgs, long_enough);
-      const bool level = 10LL * plan->shortest >= 6LL * plan->longest;
-      splits = (int)(level && 5 * two >= 12 * std::max(whole, 1LL) ? two : whole);
+      splits = paged_pieces(n_keys, xcd_wgs, xcd_cus, 10LL * plan->shortest >= 6LL * plan->longest);
     } else if (splits > 1 && xcd_wgs < xcd_cus * wpc) {
       const int fine = fine_splits(xcd_wgs, xcd_cus, wpc, n_keys);
       if (fine < splits || 5 * fine >= 7 * splits) splits = fine;
