@@ -31,9 +31,18 @@ constexpr int kRowsWg = kRows * kWaves;
 
 // wave-wide copy into LDS: lane l's 16 bytes, from a uniform base plus the lane's offset, land at m0 + 16 l.  (Without the
 // streaming hint: the query heads of a KV head read the same keys.)
-__device__ __forceinline__ void tile16_to_lds(uint32_t m0, const void* sbase, uint32_t voff) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(m0), "v"(voff), "s"(sbase)
-               : "memory");
+template <int N>
+__device__ __forceinline__ void tile16_to_lds(uint32_t m0, const void* sbase, const uint32_t (&voff)[N]) {
+  static_assert(N == 2 || N == 4);
+  if constexpr (N == 2)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3\n\t"
+                 "global_load_lds_dwordx4 %2, %3 offset:%4" ::"s"(m0), "v"(voff[0]), "v"(voff[1]), "s"(sbase), "n"(1024)
+                 : "memory");
+  else
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5\n\t"
+                 "global_load_lds_dwordx4 %2, %5 offset:%6\n\tglobal_load_lds_dwordx4 %3, %5 offset:%7\n\t"
+                 "global_load_lds_dwordx4 %4, %5 offset:%8" ::"s"(m0), "v"(voff[0]), "v"(voff[1]), "v"(voff[2]),
+                 "v"(voff[3]), "s"(sbase), "n"(1024), "n"(2 * 1024), "n"(3 * 1024) : "memory");
 }
 
 // Rows of D bf16 in LDS.  A 256-byte bank line holds one row (D = 128) or two (D = 64).  A key read takes one 16-byte chunk
@@ -147,24 +156,28 @@ __global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(At
   auto value_slot = [&](int j) { return slot_of(max((tile0 + j * 2) * kTile - kTile + 16 * wave, 0)); };
   int key_page = 0, value_page = 0;
   auto look_up = [&](int j) {
-    key_page = table[min(key_slot(j) >> a.page_shift, a.width - 1)];
-    value_page = table[min(value_slot(j) >> a.page_shift, a.width - 1)];
+    key_page = table[min((uint32_t)key_slot(j) >> a.page_shift, (uint32_t)a.width - 1)];
+    value_page = table[min((uint32_t)value_slot(j) >> a.page_shift, (uint32_t)a.width - 1)];
+  };
+  // (unsigned 32-bit parts of the offsets: scalar instructions cost a wave as much as others)
+  auto block_at = [&](const unsigned char* base, int page, int slot) {
+    const uint32_t p = min(max(page, 0), a.num_pages - 1);
+    return base + (uint64_t)p * (uint64_t)a.page_stride + (uint32_t)(slot & ps1) * (uint32_t)L::ROW;
   };
   // (lane's offset of copy 0; copy c is 1 KB on, its rows' swizzle differs by swz(first row of c))
   const uint32_t coff0 = (uint32_t)((lane / L::CPR) * L::ROW + (((lane % L::CPR) ^ L::swz(lane / L::CPR)) << 4));
-  auto coff = [&](int c) { return (coff0 ^ (uint32_t)(L::swz(c * (64 / L::CPR)) << 4)) + c * 1024; };
+  uint32_t coff[L::COPIES];
+#pragma unroll
+  for (int c = 0; c < L::COPIES; ++c) coff[c] = coff0 ^ (uint32_t)(L::swz(c * (64 / L::CPR)) << 4);
   auto issue = [&](int j) {
     const uint32_t dst = ring_lds + (j % L::STAGES) * L::STAGE + wave * L::BLOCK;
-    const int kp = min(max(key_page, 0), a.num_pages - 1), vp = min(max(value_page, 0), a.num_pages - 1);
-    const unsigned char* ks = kbase + (int64_t)kp * a.page_stride + (int64_t)(key_slot(j) & ps1) * L::ROW;
-    const unsigned char* vs = vbase + (int64_t)vp * a.page_stride + (int64_t)(value_slot(j) & ps1) * L::ROW;
-#pragma unroll
-    for (int c = 0; c < L::COPIES; ++c) tile16_to_lds(dst + c * 1024, ks, coff(c));
-#pragma unroll
-    for (int c = 0; c < L::COPIES; ++c) tile16_to_lds(dst + L::HALF + c * 1024, vs, coff(c));
+    tile16_to_lds(dst, block_at(kbase, key_page, key_slot(j)), coff);
+    tile16_to_lds(dst + L::HALF, block_at(vbase, value_page, value_slot(j)), coff);
     look_up(j + 1);
   };
-  // this wave's rows of stage j that no row of the workgroup sees become zeros
+  // this wave's rows of stage j that no row of the workgroup sees become zeros (of stages [whole0, whole1) all are seen)
+  const int first_seen = a.window > 0 ? max(sink_tiles, low - gap) + kTile - tile0 * kTile : 0;
+  const int whole0 = max((first_seen + 63) / 64, 0), whole1 = (N - gap - tile0 * kTile) / 64;
   auto zero_unseen = [&](int j) {
     unsigned char* at = ring + (j % L::STAGES) * L::STAGE + wave * L::BLOCK;
 #pragma unroll
@@ -278,7 +291,10 @@ __global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(At
   // Operand addresses within a tile: the swizzle leaves one offset per 32 (keys: 16) columns, the rest are constants.
   uint32_t koff[KS], voff[DB][2];
 #pragma unroll
-  for (int ds = 0; ds < KS; ++ds) koff[ds] = ring_lds + L::off(col, ds * 2 + h);
+  for (int ds = 0; ds < KS; ++ds) {
+    koff[ds] = ring_lds + L::off(col, ds * 2 + h);
+    asm("" : "+v"(koff[ds]));     // (whole, not to be put together at every read)
+  }
 #pragma unroll
   for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -326,13 +342,14 @@ __global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(At
     return vmax(x, s[15]);
   };
   // the reference moves where a score passes it by more than 2^8 (rare after the first tiles)
+  float limit = -INFINITY;     // (before scaling)
   auto move_reference = [&](float x) {
-    const float top = c_scale * x;
-    if (__any(top > m + kLazyLog2)) {
-      const float t = fmaxf(top, __shfl_xor(top, 32));
+    if (__any(x > limit)) {
+      const float t = c_scale * fmaxf(x, __shfl_xor(x, 32));
       if (t > m + kLazyLog2) {
         const float alpha = __builtin_amdgcn_exp2f(m - t);
         m = t;
+        limit = (t + kLazyLog2) / c_scale;
         l *= alpha;
 #pragma unroll
         for (int d = 0; d < DB; ++d) o[d] *= alpha;
@@ -348,7 +365,7 @@ __global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(At
     static_assert(FIRST + PER * (KS + DB) == 16 && FIRST + PER * KS >= 8, "the first 8 keys' weights precede their product");
     bf16x8 kf[KS], va[DB], vb[DB];
     bf16x8 p[2];
-    float sum[2] = {0.f, 0.f}, e[2], x = 0.f;
+    float sum[2], e[2], x = 0.f;
     auto score = [&](int ds) {
       if constexpr (NEXT) {
         f32x16 z;
@@ -363,7 +380,7 @@ __global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(At
     };
     auto weight = [&](int i) {
       e[i & 1] = __builtin_amdgcn_exp2f(fmaf(sc[i], c_scale, -m));
-      sum[i & 1] += e[i & 1];
+      sum[i & 1] = i < 2 ? e[i & 1] : sum[i & 1] + e[i & 1];
       if (i & 1) {
         p[i / 8][i % 8 - 1] = (__bf16)e[0];
         p[i / 8][i % 8] = (__bf16)e[1];
@@ -396,7 +413,10 @@ __global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(At
     for (int d = 0; d < DB; ++d) {
       o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vb[d], p[1], o[d], 0, 0, 0);
       if constexpr (NEXT) {
-        if (d == 0) x = row_max(sn);
+        if (d == 0) {
+          x = row_max(sn);
+          asm volatile("" : "+v"(x));   // (here, not behind the products)
+        }
       }
     }
     l += sum[0] + sum[1];
@@ -409,7 +429,7 @@ __global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(At
   auto next_stage = [&](int j) {
     // this wave's copies of stage j have landed (those of the AHEAD - 1 stages after it may be in flight)
     if (j + AHEAD <= periods) wait_vm<(AHEAD - 1) * CP>(); else wait_vm<0>();
-    zero_unseen(j);
+    if (j < whole0 || j >= whole1) zero_unseen(j);
     barrier_lds();   // stage j complete for every wave; every wave is past stage j - 1, whose slot is free
     if (j + AHEAD < periods) issue(j + AHEAD);
   };
@@ -420,17 +440,22 @@ __global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(At
   // reach into the run)
   const int far0 = (gap > 0 ? sink_tiles / kTile : a.sinks > 0 ? (a.sinks - 1) / kTile + 1 : 0) - tile0;
   const int far1 = !TREE && a.window > 0 ? (wave_first - a.window + 1 - gap) / kTile - tile0 : 0;
+  // plain tiles, in sight of every row of the wave
+  const int plain0 = max((max(plain_from - gap, 0) + kTile - 1) / kTile, sink_tiles / kTile) - tile0;
+  const uint32_t plain_tiles = max(min(max(wave_first + 1 - gap, 0) / kTile - tile0, wave_tiles) - plain0, 0);
   auto step = [&](int k, f32x16& sn, const f32x16& sc, int t) {   // scores of tile k, values of tile k - 1
-    if (k >= wave_tiles) return;
-    if (k > far0 && k > 0 && k < far1) {      // (tile far0, too, is all masked: it takes the value product of the one before)
+    const bool plain = (uint32_t)(k - plain0) < plain_tiles;
+    if (!plain) {
+      if (k >= wave_tiles) return;
+      if (k > far0 && k > 0 && k < far1) {    // (tile far0, too, is all masked: it takes the value product of the one before)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) sn[i] = -INFINITY;
-      return;
+        for (int i = 0; i < 16; ++i) sn[i] = -INFINITY;
+        return;
+      }
     }
     float x = block(yes, sn, sc, t, t);
-    const int s0 = slot_of((tile0 + k) * kTile);
-    if (s0 + kTile - 1 > wave_first || (s0 < plain_from && s0 + kTile > a.sinks)) {
-      mask(sn, s0);
+    if (!plain) {
+      mask(sn, slot_of((tile0 + k) * kTile));
       x = row_max(sn);
     }
     move_reference(x);
