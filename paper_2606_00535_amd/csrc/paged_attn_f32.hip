@@ -7,6 +7,10 @@
 // lanes look their key's page up in the table.  Every lane group keeps its own online softmax (running maximum, running
 // sum, accumulator) in fp32; the states are merged within the wave, then across the waves in wave order through LDS,
 // so results are reproducible.
+//
+// Latency bounds small calls: 8 heads on 2 x 16 nodes and 300 keys in sight take 7.5 us, a chain of lengths, tree, table,
+// rows and merge.  Large ones are bound by the vector ALU, which pays a reduction over D/4 lanes for each score (32
+// heads on 60 nodes and 3136 keys, D = 128: 164 us, 19 TFLOP/s).
 #include "kernels.h"
 
 #include <math.h>
@@ -260,6 +264,8 @@ hipError_t launch_rows(const PagedAttnArgs& a, hipStream_t stream) {
 
 template <int D, bool PROMPT>
 hipError_t launch(const PagedAttnArgs& a, hipStream_t stream) {
+  // (More rows a workgroup read a key for all of them; fewer leave no compute unit idle.  With 1, 2 and 4 rows: 32 rows in all,
+  // 2000 keys 23, 31, 51 us; 256: 27, 32, 53; 512: 50, 33, 52; 640 x 3136 keys 113, 97, 80; 1920: 305, 198, 164.)
   const long long rows = (long long)a.B * a.Hq * a.T;
   if (rows <= a.cus) return launch_rows<D, PROMPT, 1>(a, stream);
   if (rows <= 2LL * a.cus) return launch_rows<D, PROMPT, 2>(a, stream);

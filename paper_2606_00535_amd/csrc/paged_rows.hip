@@ -19,7 +19,8 @@ __device__ __forceinline__ int64_t slot_offset(const PagedRowsArgs& a, const int
 
 constexpr int kAppendThreads = 256;
 
-// A thread per 16 bytes of a new row (K and V).
+// A thread per 16 bytes of a new row (K and V).  Memory bounds it: 32 layers x 4 x 60 rows of 32 heads, D = 128 (252 MB read and
+// written) take 47-51 us from HBM, 5.0-5.4 TB/s, a large copy's rate; a few rows 2.5 us.
 __global__ __launch_bounds__(kAppendThreads) void paged_append_kernel(PagedRowsArgs a) {
   const int b = blockIdx.y, layer = blockIdx.z;
   const int words = a.row_bytes / 16;
@@ -45,7 +46,8 @@ __global__ __launch_bounds__(kAppendThreads) void paged_append_kernel(PagedRowsA
 // destinations, and a destination can be a later row's source.  Passes over k run in increasing order, each with all of its
 // rows in registers before it writes one.  Rows with path[k] == k stay.  A wave per (layer, sequence, KV head), a lane per 16
 // bytes of a row; a pass has kCommitLoads times as many rows as a wave holds at once.  Latency bounds it (the lengths and
-// the path, the table, the rows, one after another): waves that need no LDS and no barrier, four to a workgroup.
+// the path, the table, the rows, one after another): waves that need no LDS and no barrier, four to a workgroup (32 layers
+// x 4 sequences x 32 heads, up to 6 rows each: 7.5 us; through LDS, a workgroup a head, 12.6; one sequence's 4 heads 3.6).
 constexpr int kCommitLoads = 4;
 
 __global__ __launch_bounds__(kCommitThreads) void paged_commit_kernel(PagedRowsArgs a) {

@@ -1,8 +1,10 @@
-// Attention of a prompt's rows over a paged cache, bf16 inputs, fp32 accumulation on the matrix cores: row i of a
-// sequence (at position L_b + i) sees the slots up to its own, with a window only those and the sinks in its sight.
+// Attention over a paged cache, bf16 inputs, fp32 accumulation on the matrix cores, for KV heads of more than 64 rows (heads
+// x positions): the rows of a prompt, where row i (at position L_b + i) sees the slots up to its own, and large trees; with
+// a window only those and the sinks in sight.
 //
-//   * A workgroup of 4 waves owns 128 consecutive rows of one query head, a wave 32 of them; two workgroups share a
-//     compute unit, so the waves of a SIMD belong to different ones and no barrier ties their phases.
+//   * A workgroup of 4 waves owns 128 rows, a wave 32 of them; two workgroups share a compute unit, so the waves of a SIMD
+//     belong to different ones and no barrier ties their phases.  A prompt's rows are 128 consecutive ones of one query head
+//     (which end at different keys) or the heads' rows one after another, as are a tree's.
 //   * Keys come in tiles of 32.  S^T = K Q^T and O^T += V^T P^T on v_mfma_f32_32x32x16_bf16: a lane holds 16 scores of
 //     one row (lane l and l + 32 share row l % 32), the probabilities are in the value product's operand order as they
 //     come (keys numbered 16 t + 4 (l / 32) + {0..3, 8..11} in both operands), and the values are read transposed
@@ -15,6 +17,18 @@
 //     rows, from the pages that scalar loads of the table name a stage ahead.  Rows in LDS are XOR-swizzled: chunk c of
 //     row r at position c ^ swz(r), so that neither the 32-row key reads nor the 4 x 32 value reads conflict on banks.
 //   * Slots that no row sees are zeroed in LDS, so whatever they hold cannot reach the products.
+//   * Few workgroups: two key groups in each (a ring each, one workgroup to a compute unit), then pieces of the key axis over
+//     several, merged as the tree kernel's are, in fp32.
+//
+// What bounds it, at 28 heads on 4 x 8192 rows, D = 128 (458 us: 1050 TFLOP/s, where a library product of 16384^3 makes 1360):
+// power and issue.  The matrix cores work 54 % of the cycles at a clock of 1.6 GHz (inputs of zeros, which cost less power,
+// take 15 % less time).  A wave issues in order: a tile's 16 products, 72 vector, 24 LDS and 48 scalar instructions leave it
+// waiting to issue for 36 % of its time, and barriers and copies for 20 %.  Without the waits for copies the time is the
+// same, without the barriers 3 % less (10 % for 1000 rows with a window of 1024), without the key or value reads 2-5 % each.
+// Scalar instructions count like others: with 80 to 100 a tile it was 482 us.
+// Tried: 64 rows a wave (half the LDS reads, but one wave a SIMD: 640 us, 442 instead of 285 for trees of 896 x 8320), 8 waves on
+// one ring of 128 KB (level at 8192 rows, 20 % slower at 6000), the next tile's keys fetched ahead of the barrier and the
+// last value products put off to the next tile (2-3 % slower), the copies' addresses beside the products (level).
 #include "tree_attn_bf16.h"
 
 #include <type_traits>

@@ -44,6 +44,9 @@
 //     scalar load each, one super-step ahead.  The rows are tree nodes, or (chain) consecutive positions of a prompt.
 //     With a window, the keys of a workgroup are its sinks and one run of slots; both start at multiples of 32 and are
 //     numbered through, so pieces, steps and the ring do not know of the gap.
+//     (32 heads on 60 nodes behind 3136 slots: 20.9 us, 18.1 from one slab, of which the pieces' rows in fp32 are 1.1; one
+//     token of 32 heads on 4 sequences with 1028 keys in sight 13.0 us from HBM, nearly all of it latency: lengths, table,
+//     ring, exchange, merge.)
 #pragma once
 
 #include "kernels.h"
