@@ -81,7 +81,7 @@ def kernel_source_hash() -> str:
     changes with the code, not with its comments)."""
     import re
     h = hashlib.sha256()
-    for f in sorted(glob.glob(os.path.join(ROOT, "paper_2606_00535_amd", "csrc", "tree_attn_bf16.hip"))):
+    for f in sorted(glob.glob(os.path.join(ROOT, "paper_2606_00535_amd", "csrc", "tree_attn_bf16.h*"))):
         src = open(f).read()
         src = re.sub(r"/\*.*?\*/", "", src, flags=re.S)
         src = re.sub(r"//[^\n]*", "", src)
