@@ -716,6 +716,15 @@ def stream_read(src: torch.Tensor, sink: Optional[torch.Tensor] = None, stream=N
 # ---------------------------------------------------------------------------------------------------- paged cache
 PAGES_MAX, PAGES_MAX_SEQUENCES = 524288, 4096
 
+# (small calls take as long as the host does: torch's calls without their wrappers, where it has them)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_capturing = getattr(torch._C, "_cuda_isCurrentStreamCapturing", torch.cuda.is_current_stream_capturing)
+
+
+def _stream_on(stream, at) -> int:
+    """_stream, where `at` is the current device."""
+    return _raw_stream(at) if stream is None and _raw_stream is not None else _stream(stream)
+
 
 def _code(dtype) -> int:
     if dtype is torch.bfloat16:
@@ -734,7 +743,7 @@ def _current(t: torch.Tensor, name: str, dtype=None) -> int:
     at = t.get_device()
     if at < 0:
         raise ValueError("%s must be a device tensor" % name)
-    if at != torch.cuda.current_device():
+    if at != _current_device():
         raise ValueError("%s is on %s, not on the current device" % (name, t.device))
     return at
 
@@ -828,16 +837,16 @@ WORKSPACE_COUNTER_BYTES = 65536
 def _call_paged(call, size, desc, tensors, workspace, at, stream):
     """An attention call with the caller's workspace, or the binding's own (one per device and stream; under capture one
     that belongs to the graph, its counters cleared by every replay, so that no two graphs share one)."""
-    st = _stream(stream)
+    st = _stream_on(stream, at)
     if workspace is not None:
         if workspace.get_device() != at or not workspace.is_contiguous():
             raise ValueError("workspace must be a contiguous tensor on the call's device")
         _check(call(desc, *tensors, _ptr(workspace), workspace.numel() * workspace.element_size(), st))
         return
-    capturing = torch.cuda.is_current_stream_capturing()
+    capturing = _capturing()
     if stream is not None and stream.cuda_stream != torch.cuda.current_stream().cuda_stream:
         with torch.cuda.stream(stream):
-            capturing |= torch.cuda.is_current_stream_capturing()
+            capturing |= _capturing()
         if capturing:
             raise ValueError("a call captured on another stream than the current one needs a workspace")
     if capturing:
@@ -875,7 +884,7 @@ def _paged_outputs(q, out, lse, with_lse):
         _need_on(lse, "lse", torch.float32, at, q.shape[:3])
     elif with_lse:
         B, H, T, _ = q.shape
-        lse = q.new_empty((B, H, T), dtype=torch.float32)
+        lse = q.new_empty(B, H, T, dtype=torch.float32)
     return out, lse
 
 
@@ -912,8 +921,8 @@ def paged_verify_attn(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Ten
     out, lse = _paged_outputs(q, out, lse, with_lse)
     L = lib()
     _call_paged(L.dreams_paged_verify_attn, L.dreams_paged_verify_attn_workspace_size, ctypes.byref(desc),
-                (_ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(page_table), _ptr(kv_len), _ptr(parent), _ptr(tree_mask),
-                 _ptr(out), _ptr(lse)), workspace, at, stream)
+                (q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(), kv_len.data_ptr(),
+                 _ptr(parent), _ptr(tree_mask), out.data_ptr(), _ptr(lse)), workspace, at, stream)
     return out, lse
 
 
@@ -934,8 +943,8 @@ def paged_prompt_attn(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Ten
     out, lse = _paged_outputs(q, out, lse, with_lse)
     L = lib()
     _call_paged(L.dreams_paged_prompt_attn, L.dreams_paged_prompt_attn_workspace_size, ctypes.byref(desc),
-                (_ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(page_table), _ptr(kv_len), _ptr(row_len), _ptr(out),
-                 _ptr(lse)), workspace, at, stream)
+                (q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(), kv_len.data_ptr(),
+                 _ptr(row_len), out.data_ptr(), _ptr(lse)), workspace, at, stream)
     return out, lse
 
 
@@ -969,9 +978,9 @@ def paged_append(k_new: torch.Tensor, v_new: torch.Tensor, k_pages: torch.Tensor
     if row_len is not None:
         _need_on(row_len, "row_len", torch.int32, at, (B,))
     strides = _Strides(*(st[:4] if n == 5 else (0,) + st[:3]))
-    _check(lib().dreams_paged_append(ctypes.byref(pool), _ptr(k_new), _ptr(v_new), shape[-2], strides,
-                                     _ptr(page_table), _ptr(kv_len), _ptr(row_len), _ptr(k_pages), _ptr(v_pages),
-                                     _stream(stream)))
+    _check(lib().dreams_paged_append(ctypes.byref(pool), k_new.data_ptr(), v_new.data_ptr(), shape[-2], strides,
+                                     page_table.data_ptr(), kv_len.data_ptr(), _ptr(row_len), k_pages.data_ptr(),
+                                     v_pages.data_ptr(), _stream_on(stream, at)))
 
 
 def paged_kv_commit(k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor, kv_len_in: torch.Tensor,
@@ -990,9 +999,10 @@ def paged_kv_commit(k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: to
         kv_len_out = torch.empty_like(kv_len_in)
     else:
         _need_on(kv_len_out, "kv_len_out", torch.int32, at, (B,))
-    _check(lib().dreams_paged_kv_commit(ctypes.byref(pool), _ptr(k_pages), _ptr(v_pages), _ptr(page_table),
-                                        _ptr(kv_len_in), _ptr(accept_path), _ptr(accept_len), accept_path.shape[1],
-                                        _ptr(kv_len_out), _stream(stream)))
+    _check(lib().dreams_paged_kv_commit(ctypes.byref(pool), k_pages.data_ptr(), v_pages.data_ptr(),
+                                        page_table.data_ptr(), kv_len_in.data_ptr(), accept_path.data_ptr(),
+                                        accept_len.data_ptr(), accept_path.shape[1],
+                                        kv_len_out.data_ptr(), _stream_on(stream, at)))
     return kv_len_out
 
 
@@ -1007,8 +1017,8 @@ def pages_reserve(page_table: torch.Tensor, page_count: torch.Tensor, refcount: 
         granted = torch.empty_like(want_len)
     else:
         _need_on(granted, "granted", torch.int32, at, (B,))
-    _check(lib().dreams_pages_reserve(ctypes.byref(pool), _ptr(page_table), _ptr(page_count), _ptr(refcount),
-                                      _ptr(want_len), _ptr(granted), _stream(stream)))
+    _check(lib().dreams_pages_reserve(ctypes.byref(pool), page_table.data_ptr(), page_count.data_ptr(),
+                                      refcount.data_ptr(), want_len.data_ptr(), granted.data_ptr(), _stream_on(stream, at)))
     return granted
 
 
@@ -1029,9 +1039,9 @@ def pages_fork(k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.T
         granted = torch.empty_like(src)
     else:
         _need_on(granted, "granted", torch.int32, at, (n,))
-    _check(lib().dreams_pages_fork(ctypes.byref(pool), _ptr(k_pages), _ptr(v_pages), _ptr(page_table), _ptr(page_count),
-                                   _ptr(kv_len), _ptr(refcount), n, _ptr(src), _ptr(dst), _ptr(granted),
-                                   _stream(stream)))
+    _check(lib().dreams_pages_fork(ctypes.byref(pool), k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(),
+                                   page_count.data_ptr(), kv_len.data_ptr(), refcount.data_ptr(), n, src.data_ptr(),
+                                   dst.data_ptr(), granted.data_ptr(), _stream_on(stream, at)))
     return granted
 
 
@@ -1042,5 +1052,6 @@ def pages_release(page_table: torch.Tensor, page_count: torch.Tensor, kv_len: to
     pool, at = _table_pool(page_table, page_count, refcount, page_size)
     _need_on(kv_len, "kv_len", torch.int32, at, (pool.batch,))
     _need_on(seqs, "seqs", torch.int32, at, None, 1)
-    _check(lib().dreams_pages_release(ctypes.byref(pool), _ptr(page_table), _ptr(page_count), _ptr(kv_len),
-                                      _ptr(refcount), seqs.shape[0], _ptr(seqs), 1 if trim else 0, _stream(stream)))
+    _check(lib().dreams_pages_release(ctypes.byref(pool), page_table.data_ptr(), page_count.data_ptr(),
+                                      kv_len.data_ptr(), refcount.data_ptr(), seqs.shape[0], seqs.data_ptr(),
+                                      1 if trim else 0, _stream_on(stream, at)))
