@@ -22,7 +22,7 @@
 //
 // What bounds it, at 28 heads on 4 x 8192 rows, D = 128 (458 us: 1050 TFLOP/s, where a library product of 16384^3 makes 1360):
 // power and issue.  The matrix cores work 54 % of the cycles at a clock of 1.6 GHz (inputs of zeros, which cost less power,
-// take 15 % less time).  A wave issues in order: a tile's 16 products, 72 vector, 24 LDS and 48 scalar instructions leave it
+// take 15 % less time).  A wave issues in order: a tile's 16 products, 72 vector, 24 LDS and 36 scalar instructions leave it
 // waiting to issue for 36 % of its time, and barriers and copies for 20 %.  Without the waits for copies the time is the
 // same, without the barriers 3 % less (10 % for 1000 rows with a window of 1024), without the key or value reads 2-5 % each.
 // Scalar instructions count like others: with 80 to 100 a tile it was 482 us.
@@ -157,8 +157,9 @@ __global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(At
   const int tile0 = begin + kg * half, tiles = min(half, piece_tiles - kg * half);
   const int periods = half > 0 ? half / 2 + 1 : 0;
 
-  // ---- copies.  Stage j: key blocks of 16 from key 64 j on, value blocks from key 64 j - 32 on; wave w brings block w
-  // of either.  (The value blocks before the first key repeat it, unread; those past the last tile are some page's.)
+  // ---- copies.  Stage j: key blocks of 16 from key 64 j on, value blocks from key 64 j - 32 on.  Wave w brings key block w and
+  // value block (w + 2) % 4, the same slots' values (waves 0 and 1) or those of its keys a stage earlier: one look-up and one
+  // offset a stage.  (The value blocks before the first key repeat it, unread; those past the last tile are some page's.)
   typedef const __attribute__((address_space(4))) int32_t* const_table;
   const const_table table = (const_table)(uintptr_t)(a.table + (size_t)b * a.width);
   const int ps1 = (1 << a.page_shift) - 1;
@@ -167,35 +168,38 @@ __global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(At
   const unsigned char* vbase = (const unsigned char*)a.v + head_off;
   const uint32_t ring_lds = __builtin_amdgcn_readfirstlane(lds_addr(ring));
   auto key_slot = [&](int j) { return slot_of((tile0 + j * 2) * kTile + 16 * wave); };
-  auto value_slot = [&](int j) { return slot_of(max((tile0 + j * 2) * kTile - kTile + 16 * wave, 0)); };
-  int key_page = 0, value_page = 0;
-  auto look_up = [&](int j) {
-    key_page = table[min((uint32_t)key_slot(j) >> a.page_shift, (uint32_t)a.width - 1)];
-    value_page = table[min((uint32_t)value_slot(j) >> a.page_shift, (uint32_t)a.width - 1)];
-  };
-  // (unsigned 32-bit parts of the offsets: scalar instructions cost a wave as much as others)
-  auto block_at = [&](const unsigned char* base, int page, int slot) {
+  const int slot_before = slot_of(max((tile0 - 2) * kTile + 16 * wave, 0));   // of stage -1
+  auto value_slot = [&](int j) { return wave < 2 ? key_slot(j) : j > 0 ? key_slot(j - 1) : slot_before; };
+  auto look_up = [&](int slot) { return table[min((uint32_t)slot >> a.page_shift, (uint32_t)a.width - 1)]; };
+  // (unsigned 32-bit parts: scalar instructions cost a wave as much as others)
+  auto offset = [&](int page, int slot) {
     const uint32_t p = min(max(page, 0), a.num_pages - 1);
-    return base + (uint64_t)p * (uint64_t)a.page_stride + (uint32_t)(slot & ps1) * (uint32_t)L::ROW;
+    return (uint64_t)p * (uint64_t)a.page_stride + (uint32_t)(slot & ps1) * (uint32_t)L::ROW;
   };
   // (lane's offset of copy 0; copy c is 1 KB on, its rows' swizzle differs by swz(first row of c))
   const uint32_t coff0 = (uint32_t)((lane / L::CPR) * L::ROW + (((lane % L::CPR) ^ L::swz(lane / L::CPR)) << 4));
   uint32_t coff[L::COPIES];
 #pragma unroll
   for (int c = 0; c < L::COPIES; ++c) coff[c] = coff0 ^ (uint32_t)(L::swz(c * (64 / L::CPR)) << 4);
+  const uint32_t value_at = L::HALF + ((wave + 2) & 3) * L::BLOCK;
+  int page = 0;                    // of the next stage to copy
+  uint64_t before = 0;             // the offset of the stage before
   auto issue = [&](int j) {
-    const uint32_t dst = ring_lds + (j % L::STAGES) * L::STAGE + wave * L::BLOCK;
-    tile16_to_lds(dst, block_at(kbase, key_page, key_slot(j)), coff);
-    tile16_to_lds(dst + L::HALF, block_at(vbase, value_page, value_slot(j)), coff);
-    look_up(j + 1);
+    const uint32_t dst = ring_lds + (j % L::STAGES) * L::STAGE;
+    const uint64_t at = offset(page, key_slot(j));
+    tile16_to_lds(dst + wave * L::BLOCK, kbase + at, coff);
+    tile16_to_lds(dst + value_at, vbase + (wave < 2 ? at : before), coff);
+    before = at;
+    page = look_up(key_slot(j + 1));
   };
   // this wave's rows of stage j that no row of the workgroup sees become zeros (of stages [whole0, whole1) all are seen)
   const int first_seen = a.window > 0 ? max(sink_tiles, low - gap) + kTile - tile0 * kTile : 0;
   const int whole0 = max((first_seen + 63) / 64, 0), whole1 = (N - gap - tile0 * kTile) / 64;
   auto zero_unseen = [&](int j) {
-    unsigned char* at = ring + (j % L::STAGES) * L::STAGE + wave * L::BLOCK;
+    unsigned char* stage = ring + (j % L::STAGES) * L::STAGE;
 #pragma unroll
     for (int part = 0; part < 2; ++part) {
+      unsigned char* at = stage + (part ? value_at : wave * L::BLOCK);
       const int s0 = part ? value_slot(j) : key_slot(j);
       if (s0 + 16 > N || (s0 < low && s0 + 16 > sink_end)) {
         constexpr int LPR = 4, PER = L::CPR / LPR;     // 4 lanes a row
@@ -203,7 +207,7 @@ __global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(At
         if (s >= N || (s < low && s >= sink_end)) {
 #pragma unroll
           for (int c = 0; c < PER; ++c)
-            *(u32x4*)(at + part * L::HALF + (lane / LPR) * L::ROW + ((lane % LPR) * PER + c) * 16) = u32x4{0u, 0u, 0u, 0u};
+            *(u32x4*)(at + (lane / LPR) * L::ROW + ((lane % LPR) * PER + c) * 16) = u32x4{0u, 0u, 0u, 0u};
         }
       }
     }
@@ -223,7 +227,9 @@ __global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(At
     for (int c = 0; c * 64 < T; ++c)
       copy4_to_lds(__builtin_amdgcn_readfirstlane(lds_addr(par_lds)) + c * 256,
                    a.parent + (size_t)b * T + min(c * 64 + lane, T - 1));
-  look_up(0);
+  const int page_before = look_up(slot_before);
+  page = look_up(key_slot(0));
+  before = offset(page_before, slot_before);
   for (int j = 0; j < AHEAD; ++j)
     if (j < periods) issue(j);
 
