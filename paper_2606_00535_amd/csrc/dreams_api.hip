@@ -1186,6 +1186,7 @@ int page_shift_of(int page_size) { return __builtin_ctz((unsigned)page_size); }
 
 // A page stride (elements; 0: dense) against the page it has to hold and 16-byte alignment.
 dreams_status_t check_page_stride(int64_t stride, int64_t page_elems, int elem, int32_t num_pages) {
+  if (page_elems > ((int64_t)1 << 56) / num_pages) return fail(DREAMS_ERR_UNSUPPORTED, "problem too large");
   if (stride == 0) return DREAMS_OK;
   if (stride < page_elems) return fail(DREAMS_ERR_INVALID_ARG, "page_stride = %lld is smaller than a page (%lld elements)",
                                        (long long)stride, (long long)page_elems);
@@ -1348,7 +1349,7 @@ dreams_status_t plan_paged(const dreams_paged_desc_t* d, bool prompt, PagedPlan*
     st = device_cus(&cus);
     if (st != DREAMS_OK) return st;
     const int wpc = tree_attn_bf16_wgs_per_cu(p.rows_per_wg);
-    const long long xcd_cus = cus / 8;
+    const long long xcd_cus = std::max(cus / 8, 1);
     splits = coarse_splits(8 * xcd_wgs, (long long)cus * wpc, n_keys);
     if (splits > kAttnMaxSplits) splits = kAttnMaxSplits;
     if (p.rows_per_wg == 128) {
