@@ -1,6 +1,6 @@
-// Attention over a paged cache, fp32, on the vector ALU: rows that are tree nodes (every node sees the prefix and its
-// ancestors-or-self) or consecutive positions of a prompt (row i sees the slots up to its own), in either case only
-// keys within `window` positions, or among the first `sinks`.
+// Attention over a paged cache, fp32: rows that are tree nodes (every node sees the prefix and its ancestors-or-self) or
+// consecutive positions of a prompt (row i sees the slots up to its own), in either case only keys within `window`
+// positions, or among the first `sinks`.  Few rows on the vector ALU, many in tiles on the matrix cores (below).
 //
 // A workgroup of 16 waves owns R rows (1, 2 or 4) of one KV head and every key that one of them sees: the sinks and one
 // run of slots.  A key's K (or V) row is held by D/4 neighbouring lanes, so a wave reads 64 / (D/4) rows per load; its
@@ -9,7 +9,7 @@
 // so results are reproducible.
 //
 // Latency bounds small calls: 8 heads on 2 x 16 nodes and 300 keys in sight take 7.5 us, a chain of lengths, tree, table,
-// rows and merge.  Large ones are bound by the vector ALU, which pays a reduction over D/4 lanes for each score (32
+// rows and merge.  Larger ones are bound by the vector ALU, which pays a reduction over D/4 lanes for each score (32
 // heads on 60 nodes and 3136 keys, D = 128: 164 us, 19 TFLOP/s).
 #include "kernels.h"
 
@@ -255,6 +255,216 @@ __global__ __launch_bounds__(64 * kWaves) void paged_attn_f32_kernel(PagedAttnAr
   if (a.lse && d == 0) a.lse[row] = lt > 0.f ? (M + log2f(lt)) * kLn2 : -INFINITY;
 }
 
+// Many rows: the same on the matrix cores, fp32 in and out.  A workgroup of 4 waves owns 64 consecutive
+// rows of a KV head's G * T, a wave 16 of them; keys go through LDS in tiles of 32, two buffers, the next tile's rows in
+// registers meanwhile.  S^T = K Q^T and O^T += V^T P^T on v_mfma_f32_16x16x4_f32: lane (g, n) = (lane / 16, lane % 16) holds
+// the scores of row n with keys 4 g + 0..3 of 16, just the operand that the value product takes if its step i is over keys
+// 4 g + i.  Sums run over any order of a row's D, so four steps share a 16-byte read of K (columns 16 t + 4 g + 0..3) and four
+// output blocks one of V (block jb: columns 64 c + 4 m + jb).  Bound by the matrix cores' fp32 rate and, with one or two waves a
+// SIMD, by the chain from table to LDS: 5 x 32 heads on 310 rows, D = 128, 88 us, 45 TFLOP/s of what the rows see (the
+// matrix cores' fp32 rate is 157).
+constexpr int kTile = 32, kTileRows = 64, kTileWaves = 4;
+
+template <int D, bool PROMPT>
+__global__ __launch_bounds__(64 * kTileWaves, 2) void paged_tiles_f32_kernel(PagedAttnArgs a) {
+  constexpr int KS = D / 16, KROW = D + 4;           // a K row's padding: 16 rows' reads fall on different banks
+  constexpr int C4 = D / 4, PER = kTile * C4 / 256;  // 16-byte pieces of a row, and of a tile per thread
+  extern __shared__ __attribute__((aligned(16))) float kv_lds[];   // two buffers of a tile's K rows and V rows
+  __shared__ int par_lds[PROMPT ? 1 : kMaxNodes], depth_lds[PROMPT ? 1 : kMaxNodes];
+  __shared__ int range_lds[kTileWaves][2];
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, n = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int T = a.T, rows_u = a.G * T, units = a.B * a.Hkv;
+  const int u = (int)(blockIdx.x % (unsigned)units), r0 = (int)(blockIdx.x / (unsigned)units) * kTileRows;
+  const int b = u / a.Hkv, head = u - b * a.Hkv;
+  int nb = T;
+  if (PROMPT && a.row_len) nb = min(max(a.row_len[b], 0), T);
+  const int L = min(max(a.kv_len[b], 0), a.capacity - nb);
+  const size_t row0 = (size_t)u * rows_u;
+  const int row = r0 + wave * 16 + n, i = min(row, rows_u - 1) % T;
+  const bool live = row < rows_u && (!PROMPT || i < nb);
+
+  // the row's slots: [0, min(sinks, lo)), [lo, end), and of a tree the ancestors'
+  int pos = L + i;
+  uint64_t anc0 = 0, anc1 = 0;
+  if constexpr (!PROMPT) {
+    if (tid < T) par_lds[tid] = a.parent ? a.parent[(size_t)b * T + tid] : -1;
+    __syncthreads();
+    auto walk = [&](int from, auto visit) {   // from a node to the root, or to an entry that breaks the rules
+      int j = from, d = 0;
+      for (;; ++d) {
+        visit(j);
+        const int p = par_lds[j];
+        if (p < 0 || p >= j) return d;
+        j = p;
+      }
+    };
+    if (tid < T) depth_lds[tid] = walk(tid, [](int) {});
+    __syncthreads();
+    pos = L + depth_lds[i];
+    if (a.mask) {
+      const int words = (T + 63) / 64;
+      const uint64_t* bits = a.mask + ((size_t)b * T + i) * words;
+      anc0 = bits[0];
+      anc1 = words > 1 ? bits[1] : 0;
+    } else {
+      walk(i, [&](int j) { (j < 64 ? anc0 : anc1) |= 1ull << (j & 63); });
+    }
+    if (a.window > 0)
+      for (int j = 0; j < T; ++j)
+        if (depth_lds[i] - depth_lds[j] >= a.window && L + depth_lds[j] >= a.sinks) (j < 64 ? anc0 : anc1) &= ~(1ull << (j & 63));
+  }
+  const int end = live ? (PROMPT ? pos + 1 : L) : 0;
+  const int lo = min(a.window > 0 && pos >= a.window ? pos - a.window + 1 : 0, end);
+  auto over_rows = [&](int x, auto op) {   // of the wave's 16 rows
+#pragma unroll
+    for (int off = 1; off < 16; off <<= 1) x = op(x, __shfl_xor(x, off));
+    return __builtin_amdgcn_readfirstlane(x);
+  };
+  auto lower = [](int x, int y) { return min(x, y); };
+  auto upper = [](int x, int y) { return max(x, y); };
+  const int w_lo = over_rows(live ? lo : 0x7fffffff, lower);             // some row's
+  const int w_end = over_rows(live ? (PROMPT ? end : L + T) : 0, upper);
+  const int plain_lo = over_rows(live ? lo : 0, upper), plain_end = over_rows(live ? end : 0x7fffffff, lower);   // every live row's
+  if (lane == 0) {
+    range_lds[wave][0] = w_lo;
+    range_lds[wave][1] = w_end;
+  }
+  __syncthreads();
+  int lo_all = range_lds[0][0], end_all = range_lds[0][1];
+#pragma unroll
+  for (int w = 1; w < kTileWaves; ++w) {
+    lo_all = min(lo_all, range_lds[w][0]);
+    end_all = max(end_all, range_lds[w][1]);
+  }
+  lo_all = min(lo_all, end_all);
+  const int first = min(a.sinks, lo_all);            // sinks before the run
+  const int total = first + (end_all - lo_all), tiles = (total + kTile - 1) / kTile;
+  auto slot_of = [&](int key) { return key < first ? key : key - first + lo_all; };
+
+  f32x4 q[KS], o[D / 16];
+#pragma unroll
+  for (int t = 0; t < KS; ++t) {
+    q[t] = *(const f32x4*)((const float*)a.q + (row0 + min(row, rows_u - 1)) * D + 16 * t + 4 * g);
+    if (!live) q[t] = f32x4{0.f, 0.f, 0.f, 0.f};     // (may hold anything)
+  }
+#pragma unroll
+  for (int t = 0; t < D / 16; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;
+
+  // a tile's rows: thread tid takes piece tid % C4 of rows tid / C4 + (256 / C4) x
+  const int32_t* table = a.table + (size_t)b * a.width;
+  const int ps1 = (1 << a.page_shift) - 1, piece = tid % C4;
+  int page[PER];
+  f32x4 kr[PER], vr[PER];
+  auto key_of = [&](int tile, int x) { return tile * kTile + tid / C4 + (256 / C4) * x; };
+  auto look_up = [&](int tile) {
+#pragma unroll
+    for (int x = 0; x < PER; ++x) page[x] = table[slot_of(min(key_of(tile, x), total - 1)) >> a.page_shift];
+  };
+  auto load = [&](int tile) {
+#pragma unroll
+    for (int x = 0; x < PER; ++x) {
+      const int key = key_of(tile, x), slot = slot_of(min(key, total - 1));
+      const int id = min(max(page[x], 0), a.num_pages - 1);
+      const int64_t at = (int64_t)id * (a.page_stride / 4) + (((int64_t)head << a.page_shift) + (slot & ps1)) * D + 4 * piece;
+      kr[x] = *(const f32x4*)((const float*)a.k + at);
+      vr[x] = *(const f32x4*)((const float*)a.v + at);
+      if (key >= total) kr[x] = vr[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  };
+  if (tiles > 0) {
+    look_up(0);
+    load(0);
+    if (tiles > 1) look_up(1);
+  }
+  for (int k = 0; k < tiles; ++k) {
+    float* const kt = kv_lds + (k & 1) * (kTile * (KROW + D));
+    float* const vt = kt + kTile * KROW;
+#pragma unroll
+    for (int x = 0; x < PER; ++x) {
+      const int r = tid / C4 + (256 / C4) * x;
+      *(f32x4*)(kt + r * KROW + 4 * piece) = kr[x];
+      *(f32x4*)(vt + r * D + 4 * piece) = vr[x];
+    }
+    __syncthreads();   // (the tile before last is behind every wave, so its buffer is free at the next turn)
+    if (k + 1 < tiles) load(k + 1);
+    if (k + 2 < tiles) look_up(k + 2);
+    const int s_first = slot_of(k * kTile), s_last = slot_of(min(k * kTile + kTile, total) - 1);
+    if (s_first >= w_end || (s_last < w_lo && s_first >= a.sinks)) continue;   // no row of the wave sees it
+    f32x4 s[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+    for (int t = 0; t < KS; ++t) {
+      const f32x4 k0 = *(const f32x4*)(kt + n * KROW + 16 * t + 4 * g);
+      const f32x4 k1 = *(const f32x4*)(kt + (16 + n) * KROW + 16 * t + 4 * g);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        s[0] = __builtin_amdgcn_mfma_f32_16x16x4f32(k0[j], q[t][j], s[0], 0, 0, 0);
+        s[1] = __builtin_amdgcn_mfma_f32_16x16x4f32(k1[j], q[t][j], s[1], 0, 0, 0);
+      }
+    }
+    const bool plain = k * kTile + kTile <= total && s_last < plain_end && s_first >= plain_lo;
+    float top = m;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float x = s[kb][e] * a.scale_log2;
+        if (!plain) {
+          const int key = k * kTile + 16 * kb + 4 * g + e, slot = slot_of(key), j = slot - L;
+          bool vis = slot < end && (slot >= lo || slot < a.sinks);
+          if constexpr (!PROMPT) vis |= j >= 0 && j < T && (((j < 64 ? anc0 : anc1) >> (j & 63)) & 1ull) != 0;
+          if (!vis || !live || key >= total) x = -INFINITY;
+        }
+        s[kb][e] = x;
+        top = fmaxf(top, x);
+      }
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    if (__any(top > m)) {
+      const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+      l *= alpha;
+#pragma unroll
+      for (int t = 0; t < D / 16; ++t) o[t] *= alpha;
+      m = top;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;      // (nothing seen yet: every weight below is 2^-inf = 0)
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        s[kb][e] = __builtin_amdgcn_exp2f(s[kb][e] - ref);
+        l += s[kb][e];
+      }
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c) {
+          const f32x4 v = *(const f32x4*)(vt + (16 * kb + 4 * g + e) * D + 64 * c + 4 * n);
+#pragma unroll
+          for (int jb = 0; jb < 4; ++jb)
+            o[4 * c + jb] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[jb], s[kb][e], o[4 * c + jb], 0, 0, 0);
+        }
+  }
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+  if (row >= rows_u) return;
+  const bool any = live && l > 0.f;
+  float* const out = (float*)a.out + (row0 + row) * D;
+#pragma unroll
+  for (int c = 0; c < D / 64; ++c)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      f32x4 x;
+#pragma unroll
+      for (int jb = 0; jb < 4; ++jb) x[jb] = any ? o[4 * c + jb][e] / l : 0.f;
+      *(f32x4*)(out + 64 * c + 16 * g + 4 * e) = x;
+    }
+  if (a.lse && g == 0) a.lse[row0 + row] = any ? (m + log2f(l)) * kLn2 : -INFINITY;
+}
+
 template <int D, bool PROMPT, int R>
 hipError_t launch_rows(const PagedAttnArgs& a, hipStream_t stream) {
   const long long grid = (long long)a.B * a.Hkv * (((long long)a.G * a.T + R - 1) / R);
@@ -263,10 +473,32 @@ hipError_t launch_rows(const PagedAttnArgs& a, hipStream_t stream) {
 }
 
 template <int D, bool PROMPT>
+hipError_t launch_tiles(const PagedAttnArgs& a, hipStream_t stream) {
+  constexpr int lds = 2 * kTile * (2 * D + 4) * (int)sizeof(float);
+  static bool configured[64] = {};
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  if (dev < 0 || dev >= 64) return hipErrorInvalidDevice;
+  if (!configured[dev]) {
+    e = hipFuncSetAttribute((const void*)paged_tiles_f32_kernel<D, PROMPT>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e != hipSuccess) return e;
+    configured[dev] = true;
+  }
+  const long long grid = (long long)a.B * a.Hkv * (((long long)a.G * a.T + kTileRows - 1) / kTileRows);
+  hipLaunchKernelGGL((paged_tiles_f32_kernel<D, PROMPT>), dim3((unsigned)grid), dim3(64 * kTileWaves), lds, stream, a);
+  return hipGetLastError();
+}
+
+template <int D, bool PROMPT>
 hipError_t launch(const PagedAttnArgs& a, hipStream_t stream) {
+  const long long rows = (long long)a.B * a.Hq * a.T;
+  // The tiles want rows for every unit's matrix cores, and enough of one KV head to fill a wave's 16 by half (by rows in all:
+  // 7 x 24 heads on 171 rows, D = 64: 154 us on the vector ALU, 23 in tiles; 5 x 32 on 310, D = 128: 383, 88; 4096 behind 1000
+  // keys 76, 68; 3840 behind 3136 325, 334; 2048 behind 300 18, 30; 4096 rows, 8 a KV head, behind 300: 63, 42; 4 a head 72, 88).
+  if (rows >= 16LL * a.cus && (long long)a.G * a.T >= 8) return launch_tiles<D, PROMPT>(a, stream);
   // (More rows a workgroup read a key for all of them; fewer leave no compute unit idle.  With 1, 2 and 4 rows: 32 rows in all,
   // 2000 keys 23, 31, 51 us; 256: 27, 32, 53; 512: 50, 33, 52; 640 x 3136 keys 113, 97, 80; 1920: 305, 198, 164.)
-  const long long rows = (long long)a.B * a.Hq * a.T;
   if (rows <= a.cus) return launch_rows<D, PROMPT, 1>(a, stream);
   if (rows <= 2LL * a.cus) return launch_rows<D, PROMPT, 2>(a, stream);
   return launch_rows<D, PROMPT, 4>(a, stream);

@@ -754,3 +754,51 @@ def test_workspaces_that_are_refused(dev):
         for t, w in zip(outs, want):
             assert np.array_equal(bits(t), w)
         call(num_splits=3)
+
+
+# heads, D, page, lengths, rows or nodes, window, sinks, mask
+MANY_F32 = [
+    ((16, 4), 64, 16, [50, 300, 0, 131], 70, 0, 0, False),
+    ((16, 4), 128, 32, [50, 300, 0, 131], 70, 0, 0, True),               # masks that leave rows empty
+    ((16, 4), 64, 16, [500, 33, 0, 131], 70, 40, 5, False),
+    ((16, 2), 128, 64, [200, 33, 7, 600], 65, 3, 0, True),               # a window shorter than the tree is deep
+    ((16, 16), 64, 16, [9 * i for i in range(29)], 9, 0, 0, False),      # 9 rows a KV head
+    ((5, 5), 128, 16, [90] * 14, 60, 64, 33, False),
+]
+
+
+@pytest.mark.parametrize("kind", ["verify", "prompt"])
+@pytest.mark.parametrize("heads,D,ps,lens,N,window,sinks,masked", MANY_F32)
+def test_many_rows_f32(dev, heads, D, ps, lens, N, window, sinks, masked, kind):
+    """fp32 calls of more than 4096 rows (16 a compute unit), at least 8 of a KV head."""
+    rng = np.random.default_rng(15)
+    Hq, Hkv = heads
+    B = len(lens)
+    assert B * Hq * N >= 4096 and Hq // Hkv * N >= 8
+    note(kind, heads, D, ps, lens, N, window, sinks, masked)
+    q, qh = R.rounded(rng, (B, Hq, N, D), False, dev)
+    if kind == "verify":
+        c = R.Cache(rng, dev, np.array(lens) + N, Hkv, ps, D, False)
+        par = R.tree(rng, B, N)
+        see = R.ancestors(par)
+        if masked:
+            see &= rng.random(see.shape) < 0.5
+            see[:, 0] = False
+        out, lse = dreams.paged_verify_attn(q, c.kd, c.vd, c.tabled, R.ints(lens, dev), parent=R.ints(par, dev),
+                                            tree_mask=torch.from_numpy(R.mask_bits(see)).to(dev) if masked else None,
+                                            window=window, sinks=sinks)
+        torch.cuda.synchronize()
+        ref = R.verify(qh, c.k, c.v, c.table, lens, par, see, window, sinks, 1 / np.sqrt(D))
+    else:
+        rows = [int(x) for x in rng.integers(0, N + 1, size=B)]
+        rows[0], rows[-1] = N, 0
+        width = -(-(max(lens) + N) // ps)
+        c = R.Cache(rng, dev, np.array(lens) + np.array(rows), Hkv, ps, D, False, width=width)
+        for b in range(B):
+            q[b, :, rows[b]:] = float("nan")
+            qh[b, :, rows[b]:] = 0
+        out, lse = dreams.paged_prompt_attn(q, c.kd, c.vd, c.tabled, R.ints(lens, dev), R.ints(rows, dev), window=window,
+                                            sinks=sinks)
+        torch.cuda.synchronize()
+        ref = R.prompt(qh, c.k, c.v, c.table, lens, rows, window, sinks, 1 / np.sqrt(D))
+    R.check(out, lse, ref, False, kind)
