@@ -290,7 +290,7 @@ __global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(At
       }
     }
   }
-  const int see_from = a.window > 0 ? pos - a.window + 1 : 0, see_to = live ? pos : -1;
+  const int see_from = a.window > 0 ? max(pos - a.window + 1, 0) : 0, see_to = live ? pos : -1;
   // the last slot that every row of the wave may see, and the last that one of them does
   const int wave_first = TREE ? Lp - 1 : one_head ? Lp + i0 + wave * kRows : Lp;
   const int wave_last = one_head ? min(wave_first + kRows - 1, Lp + i_last) : N - 1;
@@ -340,19 +340,27 @@ __global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(At
       }
     }
   };
-  // keys out of a row's sight
+  // keys out of a row's sight.  (Lane's score i is key at + c(i), c a constant: the row's limits move instead of the keys.)
   auto mask = [&](f32x16& s, int s0) {
+    const int at = s0 + 4 * h;
+    auto c = [](int i) { return 8 * (i >> 2) + (i & 3); };
+    if constexpr (TREE) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int key = s0 + 8 * (i >> 2) + 4 * h + (i & 3);
-      const bool near = (key >= see_from) | (key < a.sinks);
-      bool vis = (key <= see_to) & near;
-      if constexpr (TREE) {
-        const int j = key - Lp;
+      for (int i = 0; i < 16; ++i) {
+        const int key = at + c(i), j = key - Lp;
         const uint64_t word = j < 64 ? anc0 : anc1;
-        vis = j < 0 ? near : (key < N) & (((word >> (j & 63)) & 1ull) != 0);
+        const bool vis = j < 0 ? (key >= see_from) | (key < a.sinks) : (key < N) & (((word >> (j & 63)) & 1ull) != 0);
+        s[i] = vis ? s[i] : -INFINITY;
       }
-      s[i] = vis ? s[i] : -INFINITY;
+    } else if (s0 >= a.sinks || a.window == 0) {
+      const int from = see_from - at;
+      const uint32_t seen = max(see_to - see_from + 1, 0);     // (none of a dead row's)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = (uint32_t)(c(i) - from) < seen ? s[i] : -INFINITY;
+    } else {
+      const int from = see_from - at, to = see_to - at, sinks = a.sinks - at;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = (c(i) <= to) & ((c(i) >= from) | (c(i) < sinks)) ? s[i] : -INFINITY;
     }
   };
   auto row_max = [&](const f32x16& s) {
