@@ -345,13 +345,21 @@ __global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(At
     const int at = s0 + 4 * h;
     auto c = [](int i) { return 8 * (i >> 2) + (i & 3); };
     if constexpr (TREE) {
+      // a bit a key of the tile: the prefix's in sight and the nodes in anc0, anc1
+      auto range = [](int lo, int hi) {     // keys [lo, hi) of the tile
+        auto below = [](int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u; };
+        return below(hi) & ~below(lo);
+      };
+      const int first = Lp - s0;            // the first node's key
+      const uint32_t prefix = (range(see_from - s0, first) | range(0, a.sinks - s0)) & range(0, first);
+      const uint64_t nodes = first >= 32    ? 0
+                             : first >= 0   ? anc0 << first
+                             : first > -64  ? anc0 >> -first | anc1 << (64 + first)
+                             : first > -128 ? anc1 >> (-64 - first)
+                                            : 0;
+      const uint32_t bits = (prefix | ((uint32_t)nodes & range(first, N - s0))) >> (4 * h);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int key = at + c(i), j = key - Lp;
-        const uint64_t word = j < 64 ? anc0 : anc1;
-        const bool vis = j < 0 ? (key >= see_from) | (key < a.sinks) : (key < N) & (((word >> (j & 63)) & 1ull) != 0);
-        s[i] = vis ? s[i] : -INFINITY;
-      }
+      for (int i = 0; i < 16; ++i) s[i] = bits & (1u << c(i)) ? s[i] : -INFINITY;
     } else if (s0 >= a.sinks || a.window == 0) {
       const int from = see_from - at;
       const uint32_t seen = max(see_to - see_from + 1, 0);     // (none of a dead row's)
