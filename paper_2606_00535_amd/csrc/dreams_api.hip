@@ -1281,11 +1281,11 @@ struct PagedPlan {
 };
 
 // Pieces of the key axis for workgroups of 128 rows, xcd_wgs on each XCD: the number that takes the least time, in keys that a
-// compute unit takes for 128 rows (16.6 ns each at D = 128).  A workgroup alone on its unit has two key groups and takes its
+// compute unit takes for 128 rows (16 ns each at D = 128).  A workgroup alone on its unit has two key groups and takes its
 // keys at the unit's rate, two share it.  Pieces cost their rows' way to memory and back: 300 keys and 1.25 for each.
 // (level: the row groups are about as long.  Else pieces only as far as every workgroup has a unit of its own.)
-// 32 heads on 8 x 4 x 140 rows behind 1000 keys, 160 workgroups: 28 us whole, 41, 37 and 46 in 2, 3 and 4 pieces; on 140 x 2
-// rows: 27, 28, 25, 27; 28 heads on 4 x 6 x 219 rows of 64 columns behind 5228: 125, 116, 104, 104.
+// 32 heads on 8 x 4 x 140 rows behind 1000 keys, 160 workgroups: 26 us whole, 38, 35 and 43 in 2, 3 and 4 pieces; on 140 x 2
+// rows: 24, 26, 23, 26; 28 heads on 4 x 6 x 219 rows of 64 columns behind 5228: 99, 98, 88, 88.
 int paged_pieces(int n_keys, long long xcd_wgs, long long xcd_cus, bool level) {
   long long best = 0;
   int pieces = 1;
@@ -1321,8 +1321,8 @@ dreams_status_t plan_paged(const dreams_paged_desc_t* d, bool prompt, PagedPlan*
   int span = T;   // positions that a workgroup's rows can be apart
   if (prompt && p.row_groups > 1) {
     // Row groups of one head see only the keys before them; packed ones leave no row of a workgroup empty.  The fewer keys
-    // decide (32 heads, 8 KV heads: 2000 rows 84 us packed, 51 by heads; 28 heads, 4 KV heads, 16 x 140 rows behind 1000 keys
-    // 49 packed, 72 by heads).
+    // decide (32 heads, 8 KV heads: 2000 rows 69 us packed, 48 by heads; 28 heads, 4 KV heads, 16 x 140 rows behind 1000 keys
+    // 45 packed, 63 by heads).
     const int R = p.rows_per_wg;
     const long long per_head = (long long)p.G * ((T + R - 1) / R);
     if (per_head * (max_len + T / 2 + R / 2) <= p.row_groups * (max_len + T)) {
@@ -1376,11 +1376,11 @@ dreams_status_t plan_paged(const dreams_paged_desc_t* d, bool prompt, PagedPlan*
 }
 
 // Key groups of a workgroup of 128 rows: two (8 waves, one workgroup a compute unit) while every workgroup has a unit of its
-// own, where one group would leave half of it idle; else one (two workgroups a unit, not tied by each other's barriers: 896
-// row groups of 8192 rows 478 us, 530 with two groups; 448 of 8320 keys 285, 312).  In between, up to two to a unit, prompts
+// own, where one group would leave half of it idle; else one (two workgroups a unit, not tied by each other's barriers: 1792
+// row groups of 8192 rows 451 us, 489 with two groups; 448 of 8320 keys 248, 265).  In between, up to two to a unit, prompts
 // whose row groups differ much in length gain by the finer schedule of whole units: the longest should not share its unit to
 // the end.  The longest then runs beside no other, and the last ones to start, as long as the cus-th, behind the first to end:
-// 273 groups of up to 8990 keys 159 us, 196 with one group; 288 up to 1152 28, 33; but 288 of 4000 to 5152 146, 130.
+// 280 groups of up to 8990 keys 143 us, 162 with one group; 288 up to 1152 24, 28; but 288 of 4000 to 5152 145, 120.
 int paged_key_groups(const PagedPlan& plan, int cus) {
   const long long wgs = (long long)plan.p.units * plan.p.row_groups * plan.p.splits;
   if (wgs <= cus) return 2;

@@ -20,12 +20,14 @@
 //   * Few workgroups: two key groups in each (a ring each, one workgroup to a compute unit), then pieces of the key axis over
 //     several, merged as the tree kernel's are, in fp32.
 //
-// What bounds it, at 28 heads on 4 x 8192 rows, D = 128 (458 us: 1050 TFLOP/s, where a library product of 16384^3 makes 1360):
+// What bounds it, at 28 heads on 4 x 8192 rows, D = 128 (450 us: 1070 TFLOP/s, where a library product of 16384^3 makes 1360):
 // power and issue.  The matrix cores work 54 % of the cycles at a clock of 1.6 GHz (inputs of zeros, which cost less power,
 // take 15 % less time).  A wave issues in order: a tile's 16 products, 72 vector, 24 LDS and 36 scalar instructions leave it
 // waiting to issue for 36 % of its time, and barriers and copies for 20 %.  Without the waits for copies the time is the
 // same, without the barriers 3 % less (10 % for 1000 rows with a window of 1024), without the key or value reads 2-5 % each.
-// Scalar instructions count like others: with 80 to 100 a tile it was 482 us.
+// Scalar instructions count like others: with 80 to 100 a tile it was 482 us.  Short calls are bound by their masked tiles and
+// the epilogue: 24 heads on 8 x 8 x 187 rows, D = 64, 10.0 us, 3.1 of them until the first stage has landed, 1.5 behind the
+// last; with a mask of several compares a score 11.0 (trees, 28 heads on 4 x 60 nodes behind 500: 19.4 and 17.1).
 // Tried: 64 rows a wave (half the LDS reads, but one wave a SIMD: 640 us, 442 instead of 285 for trees of 896 x 8320), 8 waves on
 // one ring of 128 KB (level at 8192 rows, 20 % slower at 6000), the next tile's keys fetched ahead of the barrier and the
 // last value products put off to the next tile (2-3 % slower), the copies' addresses beside the products (level).
