@@ -722,9 +722,11 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
     if constexpr (PAGED) {
       if (key0 > wave_to) return;
     }
-    // S^T blocks kb = 0, 1: element e of a lane in quad q is key kb*16 + e*4 + q, row col.  The mask enters
+    // S^T blocks kb = 0, 1: element e of a lane in quad q is key kb*16 + e*4 + q, row col.  One slab: the mask enters
     // as the products' starting value (0 or -inf), so nothing rewrites the scores after the matrix cores
-    // have written them; only steps that reach the tree slots or the piece end need it.
+    // have written them.  Paged: it replaces the scores, since a key that this row does not see may hold anything where
+    // another row sees it, or a mask hides it (-inf plus the product of a NaN or an infinity would be NaN).  Only steps that
+    // reach the tree slots or the piece end need it.
     f32x4 s[RB][2];
     auto products = [&](bool from_zero) {
       // (the products are issued at a raised wave priority, so that the SIMD's other wave -- in its softmax --
@@ -742,6 +744,7 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
     };
     bool edge = key0 + kStep > Lp || key0 + kStep > k_end;
     if constexpr (PAGED) edge = key0 + kStep > plain_to || (key0 < plain_from && key0 + kStep > a.sinks);
+    if (PAGED || !edge) products(true);   // (the first products start from an inline zero: no accumulator to clear)
     if (edge) {
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
@@ -758,13 +761,11 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
               const bool near = (key >= see_from[rb]) | (key < a.sinks);
               vis = a.chain ? (key <= see_to[rb]) & near : (key < N) & ((key < Lp) ? near : anc);
             }
-            s[rb][kb][e] = vis ? 0.f : -INFINITY;
+            s[rb][kb][e] = vis ? (PAGED ? s[rb][kb][e] : 0.f) : -INFINITY;
           }
         }
       }
-      products(false);
-    } else {
-      products(true);   // the first products start from an inline zero (no accumulator to clear)
+      if (!PAGED) products(false);
     }
 
     // this lane's maximum over its 8 keys of each row, in scaled log2 units (c > 0 keeps the order)
@@ -773,7 +774,7 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
       // (NaN-propagating maximum: three-input instructions, no canonicalising of the products' results; a
-      // score is never NaN, the rows past a sequence's end being zeroed)
+      // score is NaN only of a key that the row sees, the rows past a sequence's end being zeroed)
       // Two row blocks: a chain, so that every step is one three-input maximum (four instructions instead of six:
       // head_dim 64 with entropies 18.05 -> 17.65 us); one row block: a tree, which is shorter (18.8 against 18.9 us).
       float x;

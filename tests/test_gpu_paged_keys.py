@@ -1,0 +1,129 @@
+"""Keys that are not finite, in a paged cache: a row that does not see such a key is as without it (whatever the rows beside
+it see), a row that sees a NaN is NaN.  Their values are finite, as a slot's have to be that some row sees."""
+import numpy as np
+import pytest
+import torch
+
+import paged_ref as R
+from gpu_util import device, note
+from paper_2606_00535_amd import dreams
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def dev():
+    d = device()
+    dreams.lib()
+    return d
+
+
+def poison(rng, c, dev, b, slots, values):
+    """Keys of a sequence's slots become `values`, one drawn for each element; the definition's copy has zeros there."""
+    ps = c.k.shape[2]
+    for j in slots:
+        page = int(c.table[b, j // ps])
+        bad = rng.choice(np.array(values), size=c.k[page, :, j % ps].shape)
+        c.kd[page, :, j % ps] = torch.from_numpy(bad).to(c.kd.dtype).to(dev)
+        c.k[page, :, j % ps] = 0
+
+
+def check_rows(out, lse, ref, bf16, blind, label):
+    """The rows [B, T] that see no such key against the definition."""
+    keep = np.repeat(blind[:, None], out.shape[1], axis=1)
+    assert keep.any()
+    at = torch.from_numpy(keep).to(out.device)
+    R.check(out[at], lse[at], [x[keep] for x in ref], bf16, label)
+
+
+NOT_FINITE = (np.nan, np.inf, -np.inf, 3e38)
+
+# heads, D, lengths, T, window, sinks, splits: 16, 32, 64 and more rows a KV head
+TREES = [
+    ((4, 4), 128, [70, 0], 16, 0, 0, 0),
+    ((4, 1), 64, [45, 300], 4, 0, 0, 0),
+    ((8, 2), 64, [130, 33], 8, 20, 3, 0),
+    ((4, 2), 128, [900, 31], 16, 100, 4, 3),
+    ((3, 3), 128, [64, 5], 60, 0, 0, 0),
+    ((8, 2), 64, [250, 7], 16, 0, 0, 0),
+    ((4, 4), 128, [1100, 40], 60, 64, 5, 4),
+    ((4, 2), 128, [77, 200], 33, 0, 0, 0),
+    ((7, 1), 64, [500, 20], 60, 40, 2, 0),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads,D,lens,T,window,sinks,splits", TREES)
+def test_nodes_out_of_sight(dev, heads, D, lens, T, window, sinks, splits, dtype):
+    """Keys of nodes that a mask hides from every row, of siblings, and of slots that a window leaves to some rows."""
+    rng = np.random.default_rng(31)
+    bf16, B, ps = dtype == "bf16", len(lens), 16
+    note("nodes", dtype, heads, D, lens, T, window, sinks, splits)
+    par = R.tree(rng, B, T, 4, 3)
+    dep = R.depths(par)
+    for how in ("masked", "sibling", "window"):
+        if how == "window" and not window:
+            continue
+        c = R.Cache(rng, dev, np.array(lens) + T, heads[1], ps, D, bf16)
+        q, qh = R.rounded(rng, (B, heads[0], T, D), bf16, dev)
+        see = R.ancestors(par)
+        blind = np.ones((B, T), bool)
+        for b, L in enumerate(lens):
+            if how == "window":      # seen by the nodes up to depth 1 alone
+                bad = [j for j in (L - window + 2,) if sinks <= j < L]
+            else:
+                nodes = rng.choice(np.arange(1, T), size=max(1, T // 6), replace=False)
+                if how == "masked":
+                    see[b, :, nodes] = False
+                bad = [L + int(n) for n in nodes]
+            poison(rng, c, dev, b, bad, NOT_FINITE)
+            for j in bad:
+                seen = see[b, :, j - L] if j >= L else np.ones(T, bool)
+                at = L + dep[b, j - L] if j >= L else j
+                if window:
+                    seen = seen & ((L + dep[b] - at < window) | (at < sinks))
+                blind[b] &= ~seen
+        masked = how == "masked"
+        out, lse = dreams.paged_verify_attn(q, c.kd, c.vd, c.tabled, R.ints(lens, dev), parent=R.ints(par, dev),
+                                            tree_mask=torch.from_numpy(R.mask_bits(see)).to(dev) if masked else None,
+                                            window=window, sinks=sinks, num_splits=splits)
+        torch.cuda.synchronize()
+        ref = R.verify(qh, c.k, c.v, c.table, lens, par, see, window, sinks, 1 / np.sqrt(D))
+        assert not masked or blind.all()
+        check_rows(out, lse, ref, bf16, blind, how)
+
+
+# heads, D, lengths, N, window, sinks, splits
+PROMPTS = [
+    ((4, 4), 128, [0, 9], 16, 0, 0, 0),
+    ((4, 1), 64, [40, 0], 8, 0, 0, 0),
+    ((4, 4), 128, [30, 0], 64, 0, 0, 0),
+    ((8, 2), 64, [500, 100], 16, 9, 2, 0),
+    ((2, 2), 128, [1500, 20], 50, 20, 0, 3),
+    ((4, 4), 128, [30, 0], 65, 0, 0, 0),
+    ((4, 2), 64, [100, 3], 200, 50, 4, 0),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads,D,lens,N,window,sinks,splits", PROMPTS)
+def test_later_rows_and_keys_behind_a_window(dev, heads, D, lens, N, window, sinks, splits, dtype):
+    rng = np.random.default_rng(32)
+    bf16, B, ps = dtype == "bf16", len(lens), 16
+    note("prompt", dtype, heads, D, lens, N, window, sinks, splits)
+    c = R.Cache(rng, dev, np.array(lens) + N, heads[1], ps, D, bf16)
+    q, qh = R.rounded(rng, (B, heads[0], N, D), bf16, dev)
+    blind = np.ones((B, N), bool)
+    for b, L in enumerate(lens):
+        bad = [L + N - 1, L + N - 2, L + 3 * N // 4]
+        if window and L > window:
+            bad.append(L - window + 2)           # the first row's alone, and the second's
+        poison(rng, c, dev, b, bad, NOT_FINITE)
+        for j in bad:
+            at = L + np.arange(N)
+            blind[b] &= ~((at >= j) & ((at - j < window) if window else True))
+    out, lse = dreams.paged_prompt_attn(q, c.kd, c.vd, c.tabled, R.ints(lens, dev), window=window, sinks=sinks,
+                                        num_splits=splits)
+    torch.cuda.synchronize()
+    ref = R.prompt(qh, c.k, c.v, c.table, lens, [N] * B, window, sinks, 1 / np.sqrt(D))
+    check_rows(out, lse, ref, bf16, blind, "prompt")
