@@ -515,10 +515,12 @@ dreams_status_t dreams_paged_prompt_attn_workspace_size(const dreams_paged_desc_
  *   tree_mask    device [B, T, ceil(T/64)] uint64 or NULL: bit n of row i set <=> node n is visible to node i (if in
  *                                     sight; the window needs parent for the depths)
  *   out          device [B, Hq, T, D] same dtype as q;  lse: device [B, Hq, T] float or NULL
- * A row that sees nothing (a mask without a prefix in sight) gives out = 0 and lse = -inf.  Values in slots that no row
- * sees do not matter (NaN and infinities included), but for the rows' own slots: their V, and that of slots which a window
- * leaves to some of a sequence's rows only, is to be finite.  Where it is not, rows that do not see it may be NaN too.  K may
- * hold anything where a row does not see it.  Arithmetic and workspace as for dreams_tree_verify_attn, but for the pieces' rows, which are merged in fp32 unrounded.
+ * A row that sees nothing (a mask without a prefix in sight) gives out = 0 and lse = -inf, as does one whose scores are all
+ * -inf; a score of NaN or +inf makes its row's out and lse NaN.  Values in slots that no row sees do not matter (NaN and
+ * infinities included), but for the rows' own slots: their V, and that of slots which a window leaves to some of a
+ * sequence's rows only, is to be finite.  Where it is not, rows that do not see it may be NaN too.  K may hold anything
+ * where a row does not see it.  Arithmetic and workspace as for dreams_tree_verify_attn, but for the pieces' rows, which are
+ * merged in fp32 unrounded.
  */
 dreams_status_t dreams_paged_verify_attn(const dreams_paged_desc_t* desc, const void* q, const void* k_pages,
                                          const void* v_pages, const int32_t* page_table, const int32_t* kv_len,

@@ -251,8 +251,9 @@ __global__ __launch_bounds__(64 * kWaves) void paged_attn_f32_kernel(PagedAttnAr
   }
   const float lt = (l4[0] + l4[1]) + (l4[2] + l4[3]), o = (o4[0] + o4[1]) + (o4[2] + o4[3]);
   const size_t row = row0 + r0 + r;
-  ((float*)a.out)[row * D + d] = lt > 0.f ? o / lt : 0.f;
-  if (a.lse && d == 0) a.lse[row] = lt > 0.f ? (M + log2f(lt)) * kLn2 : -INFINITY;
+  const bool some = lt != 0.f;   // (a row that sees a NaN has a NaN sum, and is NaN)
+  ((float*)a.out)[row * D + d] = some ? o / lt : 0.f;
+  if (a.lse && d == 0) a.lse[row] = some ? (M + log2f(lt)) * kLn2 : -INFINITY;
 }
 
 // Many rows: the same on the matrix cores, fp32 in and out.  A workgroup of 4 waves owns 64 consecutive
@@ -451,7 +452,7 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void paged_tiles_f32_kernel(Pag
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
   if (row >= rows_u) return;
-  const bool any = live && l > 0.f;
+  const bool any = live && l != 0.f;   // (a NaN sum gives a NaN)
   float* const out = (float*)a.out + (row0 + row) * D;
 #pragma unroll
   for (int c = 0; c < D / 64; ++c)

@@ -539,7 +539,8 @@ __global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(At
       m = M;
     }
   }
-  const float inv = live && l > 0.f ? 1.0f / l : 0.f;
+  const bool some = live && l != 0.f;    // (a row that sees a NaN has a NaN sum, and is NaN)
+  const float inv = some ? 1.0f / l : 0.f;
   if (a.splits > 1) {   // the piece's rows, in fp32
     const size_t prow = (pset * a.splits + split) * kRowsWg + row;
     if (kg == 0 && row < rows_here) {
@@ -553,7 +554,7 @@ __global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(At
           for (int e = 0; e < 4; ++e) x[e] = live ? o[d][i + e] * inv : 0.f;
           *(f32x4*)(dst + d * 32 + 2 * i) = x;
         }
-      if (h == 0) *(float2*)(a.part_ml + 2 * prow) = live && l > 0.f ? make_float2(m, l) : make_float2(-INFINITY, 0.f);
+      if (h == 0) *(float2*)(a.part_ml + 2 * prow) = some ? make_float2(m, l) : make_float2(-INFINITY, 0.f);
     }
     merge_set<D, kWaves * KG, false, float>(a, pset, kRowsWg, split, start_old, row0, rows_here, &pieces_lds[0],
                                             &pieces_lds[1]);
@@ -572,7 +573,7 @@ __global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(At
       for (int e = 0; e < 4; ++e) x[e] = (__bf16)(live ? o[d][i + e] * inv : 0.f);
       *(bf16x4*)(row_piece(col, d * 4 + (i >> 2)) + 8 * h) = x;
     }
-  if (a.lse && h == 0 && row < rows_here) a.lse[row0 + row] = live && l > 0.f ? (m + __log2f(l)) * kLn2 : -INFINITY;
+  if (a.lse && h == 0 && row < rows_here) a.lse[row0 + row] = some ? (m + __log2f(l)) * kLn2 : -INFINITY;
   __builtin_amdgcn_s_waitcnt(0xC07F);
   asm volatile("" ::: "memory");
 #pragma unroll

@@ -216,7 +216,8 @@ __device__ __forceinline__ void merge_pieces(const AttnArgs& a, size_t prow0, in
     for (int e = 0; e < 8; ++e) res[e] = (__bf16)(acc[e] * inv);
     *(bf16x8m*)(out_rows + (size_t)rl * D + ch * 8) = res;
     if (ch == 0) {
-      if (lse_rows) lse_rows[rl] = !good ? NAN : lsum > 0.f ? (M + __log2f(lsum)) * kLn2 : -INFINITY;
+      const bool some = sizeof(PT) == 4 ? lsum != 0.f : lsum > 0.f;   // (paged: a NaN sum gives a NaN)
+      if (lse_rows) lse_rows[rl] = !good ? NAN : some ? (M + __log2f(lsum)) * kLn2 : -INFINITY;
       if (ENT) ent_rows[rl] = !good ? NAN : row_entropy(lsum, esum);
     }
   }
@@ -1068,7 +1069,8 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
       const float2 ml = ml_lds[tid];
       if (S == 1) {
         const size_t orow = qrow0 + row_base + tid;
-        if (a.lse) a.lse[orow] = ml.y > 0.f ? (ml.x + __log2f(ml.y)) * kLn2 : -INFINITY;
+        const bool some = PAGED ? ml.y != 0.f : ml.y > 0.f;   // (paged: a NaN sum gives a NaN)
+        if (a.lse) a.lse[orow] = some ? (ml.x + __log2f(ml.y)) * kLn2 : -INFINITY;
         if (ENT) a.entropy[orow] = row_entropy(ml.y, e_lds[tid]);
       } else {
         const size_t pr = prow0 + (size_t)split * R + tid;

@@ -127,3 +127,61 @@ def test_later_rows_and_keys_behind_a_window(dev, heads, D, lens, N, window, sin
     torch.cuda.synchronize()
     ref = R.prompt(qh, c.k, c.v, c.table, lens, [N] * B, window, sinks, 1 / np.sqrt(D))
     check_rows(out, lse, ref, bf16, blind, "prompt")
+
+
+# kind, heads, D, length, T or N, splits: every kernel, whole and in pieces
+SEEN = [
+    ("verify", (4, 4), 128, 90, 16, 0),
+    ("verify", (4, 1), 64, 900, 8, 4),
+    ("verify", (2, 2), 128, 900, 60, 4),
+    ("verify", (4, 2), 64, 300, 60, 0),
+    ("verify", (4, 1), 128, 1200, 60, 3),
+    ("prompt", (4, 4), 128, 0, 20, 0),
+    ("prompt", (4, 2), 64, 30, 150, 0),
+    ("prompt", (2, 1), 128, 1500, 150, 4),
+    ("prompt", (64, 8), 64, 30, 70, 0),      # (fp32: 4480 rows, in tiles)
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("what", ["nan", "inf"])
+@pytest.mark.parametrize("kind,heads,D,L,T,splits", SEEN)
+def test_seen_keys_that_are_not_finite(dev, kind, heads, D, L, T, splits, what, dtype):
+    """By the definition: a score of NaN or +inf makes its row's output and log-sum-exp NaN, one of -inf has no weight."""
+    rng = np.random.default_rng(33)
+    bf16, ps = dtype == "bf16", 16
+    note("seen", kind, dtype, heads, D, L, T, splits, what)
+    c = R.Cache(rng, dev, [L + T], heads[1], ps, D, bf16)
+    q, qh = R.rounded(rng, (1, heads[0], T, D), bf16, dev)
+    par = R.tree(rng, 1, T, 4, 3)
+    node = T // 2 if kind == "verify" else T - 9
+    see = R.ancestors(par) if kind == "verify" else np.tril(np.ones((T, T), bool))[None]
+    page, at = int(c.table[0, (L + node) // ps]), (L + node) % ps
+    c.kd[page, :, at, 5] = float(what)                  # one element: the score's sign is the query element's
+    rows = see[0, :, node]
+    if what == "nan":
+        c.k[page, :, at] = 0
+        lost, none = np.broadcast_to(rows, (heads[0], T)), np.zeros((heads[0], T), bool)
+    else:
+        lost, none = rows & (qh[0, :, :, 5] > 0), rows & (qh[0, :, :, 5] < 0)
+        c.k[page, :, at] = 0
+    if kind == "verify":
+        call = lambda: dreams.paged_verify_attn(q, c.kd, c.vd, c.tabled, R.ints([L], dev), R.ints(par, dev), num_splits=splits)
+        ref = lambda s: R.verify(qh, c.k, c.v, c.table, [L], par, s, 0, 0, 1 / np.sqrt(D))
+    else:
+        call = lambda: dreams.paged_prompt_attn(q, c.kd, c.vd, c.tabled, R.ints([L], dev), num_splits=splits)
+        ref = lambda s: [x[None] for x in R.attend(qh[0], R.slots_of(c.k, c.table[0], L + T), R.slots_of(c.v, c.table[0], L + T),
+                                                   np.concatenate((np.ones((T, L), bool), s[0]), axis=1), 1 / np.sqrt(D))]
+    out, lse = call()
+    torch.cuda.synchronize()
+    lost, none = lost[None], none[None]
+    assert lost.any() and (what == "nan" or none.any()) and not (lost | none).all()
+    on = torch.from_numpy(np.ascontiguousarray(lost)).to(dev)
+    assert torch.isnan(out[on]).all() and torch.isnan(lse[on]).all()
+    kept = ~lost & ~none
+    R.check(out[torch.from_numpy(kept).to(dev)], lse[torch.from_numpy(kept).to(dev)], [x[kept] for x in ref(see)], bf16, "others")
+    if none.any():                                      # the key out of sight
+        blind = see.copy()
+        blind[:, :, node] = False
+        some = torch.from_numpy(none).to(dev)
+        R.check(out[some], lse[some], [x[none] for x in ref(blind)], bf16, "no weight")
