@@ -726,6 +726,17 @@ def _stream_on(stream, at) -> int:
     return _raw_stream(at) if stream is None and _raw_stream is not None else _stream(stream)
 
 
+def _new(t: torch.Tensor, stream, shape=None, dtype=None) -> torch.Tensor:
+    """An output like t, allocated on the stream that writes it: memory of the current stream's may still be in use there."""
+    if stream is None:
+        return torch.empty_like(t) if shape is None else t.new_empty(shape, dtype=dtype)
+    captured = _capturing()
+    with torch.cuda.stream(stream):
+        if captured and not _capturing():
+            raise ValueError("a call on another stream than the captured one needs a workspace and its outputs given")
+        return _new(t, None, shape, dtype)
+
+
 def _code(dtype) -> int:
     if dtype is torch.bfloat16:
         return DREAMS_BF16
@@ -874,17 +885,17 @@ def _call_paged(call, size, desc, tensors, workspace, at, stream):
     _check(status)
 
 
-def _paged_outputs(q, out, lse, with_lse):
+def _paged_outputs(q, out, lse, with_lse, stream):
     at = q.get_device()
     if out is None:
-        out = torch.empty_like(q)
+        out = torch.empty_like(q) if stream is None else _new(q, stream)
     else:
         _need_on(out, "out", q.dtype, at, q.shape)
     if lse is not None:
         _need_on(lse, "lse", torch.float32, at, q.shape[:3])
     elif with_lse:
         B, H, T, _ = q.shape
-        lse = q.new_empty(B, H, T, dtype=torch.float32)
+        lse = q.new_empty(B, H, T, dtype=torch.float32) if stream is None else _new(q, stream, (B, H, T), torch.float32)
     return out, lse
 
 
@@ -910,7 +921,8 @@ def paged_verify_attn(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Ten
     """dreams_paged_verify_attn.  q [B,Hq,T,D]; k_pages/v_pages [num_pages,Hkv,page_size,D] (bf16 or fp32, same as q;
     dense pages, any page stride); page_table [B,width] and kv_len [B] int32; parent [B,T] int32 and/or tree_mask
     [B,T,ceil(T/64)] int64 (bit patterns; a window needs parent).  Keys more than `window` - 1 positions before a node are
-    out of its sight, but for the first `sinks` (window 0: none is).  Returns (out, lse [B,Hq,T] float32 or None)."""
+    out of its sight, but for the first `sinks` (window 0: none is).  Returns (out, lse [B,Hq,T] float32 or None); what a
+    call over pages allocates belongs to the stream it runs on."""
     desc = paged_desc(q, k_pages, v_pages, page_table, window, sinks, max_kv_len, num_splits, scale)
     B, T, at = desc.batch, desc.num_rows, q.get_device()
     _need_on(kv_len, "kv_len", torch.int32, at, (B,))
@@ -918,7 +930,7 @@ def paged_verify_attn(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Ten
         _need_on(parent, "parent", torch.int32, at, (B, T))
     if tree_mask is not None:
         _need_on(tree_mask, "tree_mask", torch.int64, at, (B, T, (T + 63) // 64))
-    out, lse = _paged_outputs(q, out, lse, with_lse)
+    out, lse = _paged_outputs(q, out, lse, with_lse, stream)
     L = lib()
     _call_paged(L.dreams_paged_verify_attn, L.dreams_paged_verify_attn_workspace_size, ctypes.byref(desc),
                 (q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(), kv_len.data_ptr(),
@@ -940,7 +952,7 @@ def paged_prompt_attn(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Ten
     _need_on(kv_len, "kv_len", torch.int32, at, (B,))
     if row_len is not None:
         _need_on(row_len, "row_len", torch.int32, at, (B,))
-    out, lse = _paged_outputs(q, out, lse, with_lse)
+    out, lse = _paged_outputs(q, out, lse, with_lse, stream)
     L = lib()
     _call_paged(L.dreams_paged_prompt_attn, L.dreams_paged_prompt_attn_workspace_size, ctypes.byref(desc),
                 (q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(), kv_len.data_ptr(),
@@ -996,7 +1008,7 @@ def paged_kv_commit(k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: to
         raise ValueError("accept_path must have page_table's batch size")
     _need_on(accept_len, "accept_len", torch.int32, at, (B,))
     if kv_len_out is None:
-        kv_len_out = torch.empty_like(kv_len_in)
+        kv_len_out = _new(kv_len_in, stream)
     else:
         _need_on(kv_len_out, "kv_len_out", torch.int32, at, (B,))
     _check(lib().dreams_paged_kv_commit(ctypes.byref(pool), k_pages.data_ptr(), v_pages.data_ptr(),
@@ -1014,7 +1026,7 @@ def pages_reserve(page_table: torch.Tensor, page_count: torch.Tensor, refcount: 
     B = pool.batch
     _need_on(want_len, "want_len", torch.int32, at, (B,))
     if granted is None:
-        granted = torch.empty_like(want_len)
+        granted = _new(want_len, stream)
     else:
         _need_on(granted, "granted", torch.int32, at, (B,))
     _check(lib().dreams_pages_reserve(ctypes.byref(pool), page_table.data_ptr(), page_count.data_ptr(),
@@ -1036,7 +1048,7 @@ def pages_fork(k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.T
     n = src.shape[0]
     _need_on(dst, "dst", torch.int32, at, (n,))
     if granted is None:
-        granted = torch.empty_like(src)
+        granted = _new(src, stream)
     else:
         _need_on(granted, "granted", torch.int32, at, (n,))
     _check(lib().dreams_pages_fork(ctypes.byref(pool), k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(),
