@@ -186,6 +186,8 @@ def _need(t: torch.Tensor, name: str, dtype, device=None, ndim=None):
         raise ValueError("%s must have %d dimensions" % (name, ndim))
 
 
+# A call on a given stream runs with it as the current one, so that its outputs and its workspace (and that one's first
+# fill) belong to the stream that uses them.
 # Workspaces: one per (device, stream, verb), zero-filled when created and left zero by every call.
 _ws = {}
 _ws_lock = threading.Lock()
@@ -252,6 +254,10 @@ def tree_verify_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
     """dreams_tree_verify_attn.  q [B,Hq,T,D]; k_cache/v_cache [B,Hkv,S_cap,D] (bf16 or fp32, same as q);
     kv_len [B] int32; parent [B,T] int32 or tree_mask [B,T,ceil(T/64)] int64 (bit patterns).
     Returns (out [B,Hq,T,D], lse [B,Hq,T] float32 or None)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return tree_verify_attn(q, k_cache, v_cache, kv_len, parent, tree_mask, scale, out, lse, with_lse,
+                                    max_kv_len, num_splits, workspace)
     out, lse, _ = _verify_attn(q, k_cache, v_cache, kv_len, parent, tree_mask, scale, out, lse, with_lse,
                                max_kv_len, num_splits, workspace, stream, None)
     return out, lse
@@ -265,6 +271,10 @@ def tree_verify_attn_entropy(q: torch.Tensor, k_cache: torch.Tensor, v_cache: to
                              workspace: Optional[torch.Tensor] = None, stream=None):
     """dreams_tree_verify_attn_entropy: as tree_verify_attn, plus every row's attention entropy (nats).
     Returns (out, lse or None, entropy [B,Hq,T] float32)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return tree_verify_attn_entropy(q, k_cache, v_cache, kv_len, parent, tree_mask, scale, out, lse, with_lse,
+                                            entropy, max_kv_len, num_splits, workspace)
     B, Hq, T, _ = q.shape
     if entropy is None:
         entropy = torch.empty((B, Hq, T), dtype=torch.float32, device=q.device)
@@ -278,6 +288,9 @@ def tree_verify_attn_entropy(q: torch.Tensor, k_cache: torch.Tensor, v_cache: to
 
 def attn_entropy_mean(entropy: torch.Tensor, ae: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """dreams_attn_entropy_mean: AE of one layer from its row entropies (any shape).  Returns a [1] float32."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return attn_entropy_mean(entropy, ae)
     _need(entropy, "entropy", torch.float32, entropy.device)
     if ae is None:
         ae = torch.empty(1, dtype=torch.float32, device=entropy.device)
@@ -287,6 +300,9 @@ def attn_entropy_mean(entropy: torch.Tensor, ae: Optional[torch.Tensor] = None, 
 
 def attn_entropy_select(ae: torch.Tensor, best: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """dreams_attn_entropy_select: the distillation layer from per-layer AE [NL].  Returns a [1] int32."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return attn_entropy_select(ae, best)
     _need(ae, "ae", torch.float32, ae.device, 1)
     if best is None:
         best = torch.empty(1, dtype=torch.int32, device=ae.device)
@@ -309,6 +325,9 @@ def visual_importance(q: torch.Tensor, k_cache: torch.Tensor, kv_len: torch.Tens
                       stream=None) -> torch.Tensor:
     """dreams_visual_importance (Eq. 2): q [B,Hq,T,D] and k_cache [B,Hkv,S_cap,D] bf16, kv_len [B] int32, lse
     [B,Hq,T] float32 from the attention call on the same rows.  Returns importance [B, vis_count] float32."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return visual_importance(q, k_cache, kv_len, lse, vis_begin, vis_count, scale, importance, workspace)
     dev = q.device
     _need(q, "q", torch.bfloat16, dev, 4)
     _need(k_cache, "k_cache", torch.bfloat16, dev, 4)
@@ -343,6 +362,9 @@ def prefill_attn_stats(q: torch.Tensor, k_cache: torch.Tensor, prompt_len: torch
     """dreams_prefill_attn_stats: the causal attention of a prompt's own rows (row i sees slots 0..i).  q
     [B,Hq,N,D] and k_cache [B,Hkv,S_cap,D] bf16, prompt_len [B] int32.  Returns (lse, entropy), each [B,Hq,N]
     float32 or None."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return prefill_attn_stats(q, k_cache, prompt_len, scale, lse, entropy, with_lse, with_entropy)
     dev = q.device
     _need(q, "q", torch.bfloat16, dev, 4)
     _need(k_cache, "k_cache", torch.bfloat16, dev, 4)
@@ -364,6 +386,9 @@ def prefill_attn_stats(q: torch.Tensor, k_cache: torch.Tensor, prompt_len: torch
 def prefill_attn_entropy_mean(entropy: torch.Tensor, prompt_len: torch.Tensor, ae: Optional[torch.Tensor] = None,
                               stream=None) -> torch.Tensor:
     """dreams_prefill_attn_entropy_mean: AE of one layer over prompts from entropy [B,Hq,N].  Returns [1] float32."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return prefill_attn_entropy_mean(entropy, prompt_len, ae)
     _need(entropy, "entropy", torch.float32, entropy.device, 3)
     _need(prompt_len, "prompt_len", torch.int32, entropy.device, 1)
     if ae is None:
@@ -388,6 +413,10 @@ def prefill_visual_importance(q: torch.Tensor, k_cache: torch.Tensor, prompt_len
                               stream=None) -> torch.Tensor:
     """dreams_prefill_visual_importance (Eq. 2 over the prompt's causal attention): lse [B,Hq,N] from
     prefill_attn_stats.  Returns importance [B, vis_count] float32."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return prefill_visual_importance(q, k_cache, prompt_len, lse, vis_begin, vis_count, scale, importance,
+                                             workspace)
     dev = q.device
     _need(q, "q", torch.bfloat16, dev, 4)
     _need(k_cache, "k_cache", torch.bfloat16, dev, 4)
@@ -412,6 +441,9 @@ def prefill_visual_importance(q: torch.Tensor, k_cache: torch.Tensor, prompt_len
 def visual_topk(importance: torch.Tensor, keep_count: int, keep: Optional[torch.Tensor] = None,
                 stream=None) -> torch.Tensor:
     """dreams_visual_topk: importance [B, n] float32 -> keep [B, keep_count] int32 (increasing token order)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return visual_topk(importance, keep_count, keep)
     _need(importance, "importance", torch.float32, importance.device, 2)
     B, n = importance.shape
     if keep is None:
@@ -425,6 +457,9 @@ def visual_topk(importance: torch.Tensor, keep_count: int, keep: Optional[torch.
 def visual_gather(k_cache: torch.Tensor, v_cache: torch.Tensor, vis_begin: int, keep: torch.Tensor,
                   k_out: Optional[torch.Tensor] = None, v_out: Optional[torch.Tensor] = None, stream=None):
     """dreams_visual_gather: the kept visual tokens' K/V rows -> (k_out, v_out) [B, Hkv, keep_count, D]."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return visual_gather(k_cache, v_cache, vis_begin, keep, k_out, v_out)
     dt = k_cache.dtype
     dev = k_cache.device
     _need(k_cache, "k_cache", dt, dev, 4)
@@ -501,6 +536,10 @@ def tree_verify_attn_noalloc(q: torch.Tensor, k_cache: torch.Tensor, v_cache: to
                              num_splits: int = 0, stream=None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
     """dreams_tree_verify_attn_noalloc: tree_verify_attn without a workspace (the library's fixed scratch array
     instead).  `out` and `lse` may be passed in so that nothing is allocated here either."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return tree_verify_attn_noalloc(q, k_cache, v_cache, kv_len, parent, tree_mask, scale, out, lse, with_lse,
+                                            max_kv_len, num_splits)
     dt = q.dtype
     if dt not in (torch.bfloat16, torch.float32):
         raise TypeError("q must be bfloat16 or float32")
@@ -543,6 +582,9 @@ def tree_accept(target_logits: torch.Tensor, draft_tokens: torch.Tensor, parent:
     """dreams_tree_accept.  target_logits [B,T,V] float32, draft_tokens / parent [B,T] int32.
     Returns (accept_len [B], accept_path [B,T], next_token [B], target_argmax [B,T] or None), all int32.
     `outputs` may pass preallocated (accept_len, accept_path, next_token, target_argmax-or-None)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return tree_accept(target_logits, draft_tokens, parent, want_target_argmax, outputs, workspace)
     dev = target_logits.device
     _need(target_logits, "target_logits", torch.float32, dev, 3)
     B, T, V = target_logits.shape
@@ -585,6 +627,10 @@ def tree_accept_sampled(target_logits: torch.Tensor, draft_logits: torch.Tensor,
     """dreams_tree_accept_sampled.  target_logits / draft_logits [B,T,V] float32, draft_tokens / parent [B,T]
     int32, uniforms [B,T] float32 in [0, 1).  Returns (accept_len [B], accept_path [B,T], next_token [B]), int32.
     `outputs` may pass preallocated (accept_len, accept_path, next_token)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return tree_accept_sampled(target_logits, draft_logits, draft_tokens, parent, uniforms, temperature,
+                                       outputs, workspace)
     dev = target_logits.device
     _need(target_logits, "target_logits", torch.float32, dev, 3)
     B, T, V = target_logits.shape
@@ -629,6 +675,10 @@ def tree_accept_lm_head(hidden_states: torch.Tensor, lm_weight: torch.Tensor, dr
     """dreams_tree_accept_lm_head.  hidden_states [B,T,H] bfloat16, lm_weight [V,H] bfloat16, draft_tokens /
     parent [B,T] int32.  Returns (accept_len [B], accept_path [B,T], next_token [B], target_argmax [B,T] or
     None), all int32.  `outputs` may pass preallocated (accept_len, accept_path, next_token, target_argmax)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return tree_accept_lm_head(hidden_states, lm_weight, draft_tokens, parent, want_target_argmax, outputs,
+                                       workspace)
     dev = hidden_states.device
     _need(hidden_states, "hidden_states", torch.bfloat16, dev, 3)
     B, T, H = hidden_states.shape
@@ -667,6 +717,9 @@ def kv_commit(k_cache: torch.Tensor, v_cache: torch.Tensor, kv_len_in: torch.Ten
               accept_len: torch.Tensor, kv_len_out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """dreams_kv_commit, in place on k_cache / v_cache of shape [NL, B, Hkv, S_cap, D] (or [B, Hkv, S_cap, D]
     for one layer).  Returns kv_len_out [B] int32."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return kv_commit(k_cache, v_cache, kv_len_in, accept_path, accept_len, kv_len_out)
     dt = k_cache.dtype
     if dt not in (torch.bfloat16, torch.float32):
         raise TypeError("caches must be bfloat16 or float32")
@@ -705,6 +758,9 @@ STREAM_READ_SINK_WORDS = 2048
 def stream_read(src: torch.Tensor, sink: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """dreams_stream_read: one plain read of every byte of `src` (a contiguous device tensor whose size is a
     multiple of 16 bytes), for measuring read bandwidth.  Returns the sink words."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return stream_read(src, sink)
     if not src.is_contiguous():
         raise ValueError("src must be contiguous")
     if sink is None:
