@@ -778,8 +778,12 @@ _capturing = getattr(torch._C, "_cuda_isCurrentStreamCapturing", torch.cuda.is_c
 
 
 def _stream_on(stream, at) -> int:
-    """_stream, where `at` is the current device."""
-    return _raw_stream(at) if stream is None and _raw_stream is not None else _stream(stream)
+    """_stream, where `at` is the current device: a stream of another one would run the kernels there."""
+    if stream is None:
+        return _raw_stream(at) if _raw_stream is not None else _stream(None)
+    if stream.device.index != at:
+        raise ValueError("stream is on %s, not on the current device" % (stream.device,))
+    return stream.cuda_stream
 
 
 def _new(t: torch.Tensor, stream, shape=None, dtype=None) -> torch.Tensor:
