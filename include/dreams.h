@@ -606,7 +606,8 @@ dreams_status_t dreams_pages_reserve(const dreams_page_pool_t* pool, int32_t* pa
  * pages filled to the end and taking a page of its own (lowest free, pairs in order) for the copied rows of a partly filled
  * one; kv_len[dst[i]] = kv_len[src[i]].  granted[i] (out): 1, or 0 and nothing changes: dst[i] holds pages or was named
  * before in dst, dst[i] = src[i], an index is outside the table, src[i]'s pages do not cover its kv_len, or no page is free.
- * Sources are read as they are before the call. */
+ * Sources are read as they are before the call.  A table of no sequences (batch 0) enqueues nothing: granted is not
+ * written. */
 dreams_status_t dreams_pages_fork(const dreams_page_pool_t* pool, void* k_pages, void* v_pages, int32_t* page_table,
                                   int32_t* page_count, int32_t* kv_len, int32_t* refcount, int32_t count,
                                   const int32_t* src, const int32_t* dst, int32_t* granted, hipStream_t stream);

@@ -1114,6 +1114,9 @@ def pages_fork(k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.T
     _check(lib().dreams_pages_fork(ctypes.byref(pool), k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(),
                                    page_count.data_ptr(), kv_len.data_ptr(), refcount.data_ptr(), n, src.data_ptr(),
                                    dst.data_ptr(), granted.data_ptr(), _stream_on(stream, at)))
+    if B == 0:      # (no sequence to copy: the library has not written granted)
+        with torch.cuda.stream(stream):
+            granted.zero_()
     return granted
 
 
