@@ -1213,7 +1213,7 @@ dreams_status_t check_paged_desc(const dreams_paged_desc_t* d, bool prompt) {
   if (d->num_rows < 1 || (!prompt && d->num_rows > kMaxNodes) || d->num_rows > slots)
     return fail(DREAMS_ERR_INVALID_ARG, "num_rows = %d outside [1, %d]", d->num_rows,
                 !prompt && kMaxNodes < slots ? kMaxNodes : slots);
-  if (d->max_kv_len < 0 || d->max_kv_len > slots - d->num_rows)
+  if (d->max_kv_len < 0 || d->max_kv_len > std::max(slots - d->num_rows, 1))   // (1: no prefix, also where rows fill the table)
     return fail(DREAMS_ERR_INVALID_ARG, "max_kv_len = %d outside [0, table_width * page_size - num_rows = %d]",
                 d->max_kv_len, slots - d->num_rows);
   if (d->num_splits < 0 || d->num_splits > kMaxSplitsRequest)
