@@ -522,8 +522,8 @@ dreams_status_t dreams_paged_prompt_attn_workspace_size(const dreams_paged_desc_
  * -inf; a score of NaN or +inf makes its row's out and lse NaN.  Values in slots that no row sees do not matter (NaN and
  * infinities included), but for the rows' own slots: their V, and that of slots which a window leaves to some of a
  * sequence's rows only, is to be finite.  Where it is not, rows that do not see it may be NaN too.  K may hold anything
- * where a row does not see it.  Arithmetic and workspace as for dreams_tree_verify_attn, but for the pieces' rows, which are
- * merged in fp32 unrounded.
+ * where a row does not see it.  Arithmetic as for dreams_tree_verify_attn, but for the pieces' rows, which are merged in fp32
+ * unrounded.  The workspace is dreams_paged_verify_attn_workspace_size bytes at least (fewer: DREAMS_ERR_WORKSPACE).
  */
 dreams_status_t dreams_paged_verify_attn(const dreams_paged_desc_t* desc, const void* q, const void* k_pages,
                                          const void* v_pages, const int32_t* page_table, const int32_t* kv_len,
@@ -567,7 +567,8 @@ typedef struct {
 /*
  * dreams_paged_append -- new rows into their slots, bit for bit: for every layer, KV head and i < n_b, slot
  * kv_len[b] + i of sequence b receives K and V row (layer, b, head, i) of k_new and v_new.  kv_len is not changed.  Rows
- * past the table or on pages outside the pool, and sequences with kv_len[b] < 0, are left out.
+ * past the table or on pages outside the pool, and sequences with kv_len[b] < 0, are left out.  k_new and v_new are no rows
+ * that the call writes.
  *   k_new, v_new   device, num_rows rows a sequence; strides[4] (host): elements between layers, sequences, KV heads and
  *                  rows (so [NL, B, Hkv, N, D] and [NL, B, N, Hkv, D] both serve), multiples of 16 bytes; rows dense
  *   row_len        device [B] int32 n_b (at most num_rows), or NULL: num_rows each

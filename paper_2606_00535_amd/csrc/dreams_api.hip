@@ -1283,7 +1283,9 @@ struct PagedPlan {
 // Pieces of the key axis for workgroups of 128 rows, xcd_wgs on each XCD: the number that takes the least time, in keys that a
 // compute unit takes for 128 rows (16 ns each at D = 128).  A workgroup alone on its unit has two key groups and takes its
 // keys at the unit's rate, two share it.  Pieces cost their rows' way to memory and back: 300 keys and 1.25 for each.
-// (level: the row groups are about as long.  Else pieces only as far as every workgroup has a unit of its own.)
+// (level: the shortest row group is at least 0.6 of the longest, so that they are about as long.  Else pieces only as far as
+// every workgroup has a unit of its own: 7 heads on 4990 rows without a prefix 74 us, 84 with pieces as for level ones.  Of 11
+// more shapes, 8 to 32 heads on 640 to 2000 rows behind 0 to 600 slots, none differs by more than 2 % either way.)
 // 32 heads on 8 x 4 x 140 rows behind 1000 keys, 160 workgroups: 26 us whole, 38, 35 and 43 in 2, 3 and 4 pieces; on 140 x 2
 // rows: 24, 26, 23, 26; 28 heads on 4 x 6 x 219 rows of 64 columns behind 5228: 99, 98, 88, 88.
 int paged_pieces(int n_keys, long long xcd_wgs, long long xcd_cus, bool level) {
@@ -1315,6 +1317,10 @@ dreams_status_t plan_paged(const dreams_paged_desc_t* d, bool prompt, PagedPlan*
   if ((long long)p.G * T > 0x3fffffff || (long long)d->batch * d->num_kv_heads > 0x3fffffff / 8)
     return fail(DREAMS_ERR_UNSUPPORTED, "problem too large");
   p.rows_total = p.G * T;
+  // Up to 64 rows on the tree kernel, whose waves share the keys of the same rows; more on 128-row workgroups.  (Graphs of calls;
+  // the same rows on 128-row workgroups behind it: 32 heads x 60 nodes behind 3136 slots 22.5 us, 26.0; 4 x 8 heads x 64
+  // rows behind 2000 18.8, 22.2; 8 x 16 heads x 48 of 64 columns behind 1500 23.8, 25.8.  Where short keys meet many heads it is
+  // the other way round: 16 x 8 heads x 64 rows of 64 columns behind 500 16.0, 13.5; 4 x 32 heads x 40 behind 1000 26.7, 23.1.)
   p.rows_per_wg = tree_attn_bf16_rows_per_wg(p.rows_total);
   p.row_groups = (p.rows_total + p.rows_per_wg - 1) / p.rows_per_wg;
   p.units = d->batch * d->num_kv_heads;

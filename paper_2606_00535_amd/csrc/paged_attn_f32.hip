@@ -10,7 +10,8 @@
 //
 // Latency bounds small calls: 8 heads on 2 x 16 nodes and 300 keys in sight take 7.5 us, a chain of lengths, tree, table,
 // rows and merge.  Larger ones are bound by the vector ALU, which pays a reduction over D/4 lanes for each score (32
-// heads on 60 nodes and 3136 keys, D = 128: 164 us, 19 TFLOP/s).
+// heads on 60 nodes and 3136 keys, D = 128: 164 us, 19 TFLOP/s).  With 4 rows a workgroup's 16 waves leave 128 registers each,
+// and three of the four builds spill 3 or 4 of them, with one access inside a loop.
 #include "kernels.h"
 
 #include <math.h>
@@ -261,9 +262,9 @@ __global__ __launch_bounds__(64 * kWaves) void paged_attn_f32_kernel(PagedAttnAr
 // registers meanwhile.  S^T = K Q^T and O^T += V^T P^T on v_mfma_f32_16x16x4_f32: lane (g, n) = (lane / 16, lane % 16) holds
 // the scores of row n with keys 4 g + 0..3 of 16, just the operand that the value product takes if its step i is over keys
 // 4 g + i.  Sums run over any order of a row's D, so four steps share a 16-byte read of K (columns 16 t + 4 g + 0..3) and four
-// output blocks one of V (block jb: columns 64 c + 4 m + jb).  Bound by the matrix cores' fp32 rate and, with one or two waves a
-// SIMD, by the chain from table to LDS: 5 x 32 heads on 310 rows, D = 128, 88 us, 45 TFLOP/s of what the rows see (the
-// matrix cores' fp32 rate is 157).
+// output blocks one of V (block jb: columns 64 c + 4 m + jb).  Bound by latency: with one or two waves a SIMD, a tile's loads,
+// score products, exponentials and value products follow one another.  5 x 32 heads on 310 rows, D = 128, 88 us, 45 TFLOP/s of
+// what the rows see, 29 % of the matrix cores' fp32 rate (157).
 constexpr int kTile = 32, kTileRows = 64, kTileWaves = 4;
 
 template <int D, bool PROMPT>

@@ -20,10 +20,11 @@
 //   * Few workgroups: two key groups in each (a ring each, one workgroup to a compute unit), then pieces of the key axis over
 //     several, merged as the tree kernel's are, in fp32.
 //
-// What bounds it, at 28 heads on 4 x 8192 rows, D = 128 (450 us: 1070 TFLOP/s, where a library product of 16384^3 makes 1360):
-// power and issue.  The matrix cores work 54 % of the cycles at a clock of 1.6 GHz (inputs of zeros, which cost less power,
+// What bounds it, at 28 heads on 4 x 8192 rows, D = 128 (440 to 490 us by the device, 980 to 1090 TFLOP/s, where a library
+// product of 16384^3 makes 1360):
+// power and issue.  The matrix cores work 54 % of the cycles at a clock of 1.5 to 1.6 GHz (inputs of zeros, which cost less power,
 // take 15 % less time).  A wave issues in order: a tile's 16 products, 72 vector, 24 LDS and 36 scalar instructions leave it
-// waiting to issue for 36 % of its time, and barriers and copies for 20 %.  Without the waits for copies the time is the
+// waiting to issue for 38 % of its time, and barriers and copies for 19 %.  Without the waits for copies the time is the
 // same, without the barriers 3 % less (10 % for 1000 rows with a window of 1024), without the key or value reads 2-5 % each.
 // Scalar instructions count like others: with 80 to 100 a tile it was 482 us.  Short calls are bound by their masked tiles and
 // the epilogue: 24 heads on 8 x 8 x 187 rows, D = 64, 10.0 us, 3.1 of them until the first stage has landed, 1.5 behind the

@@ -10,10 +10,12 @@
 //   * fork_copy_kernel: the partly filled pages of forked sequences, in every layer.
 //   * pages_release_kernel: a workgroup per released sequence.
 //
-// All are bound by latency, a chain of a few loads and barriers in one launch each: on 8 sequences of up to 91 pages of 32
-// slots, taking pages 4.4 us, a fork of 6 sequences 6.8 and 4.8 for the copied rows of 32 layers (12 MB read and
-// written), a release 3.6.  A launch from a host program costs more than that (8 us), so one workgroup that needs no second
-// launch is the split taken.
+// Over small pools all are bound by latency, a chain of a few loads and barriers in one launch each: on 8 sequences of up to
+// 91 pages of 32 slots, taking pages 4.4 us, a fork of 6 sequences 6.8 and 4.8 for the copied rows of 32 layers (12 MB read
+// and written), a release 3.6.  A launch from a host program costs more than that (8 us), so one workgroup that needs no
+// second launch is the split taken.  Its scan reads every count of the pool, one load in flight a wave, so that reserve and
+// fork grow with the pool (in a graph, 8 sequences: 600 pages 4.3 and 7.3 us, 8192 6.2 and 9.1, 131072 39 and 42, 524288 143
+// and 147); a release does not.
 #include "kernels.h"
 
 namespace dreams {

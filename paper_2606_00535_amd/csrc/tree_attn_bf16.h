@@ -46,7 +46,8 @@
 //     numbered through, so pieces, steps and the ring do not know of the gap.
 //     (32 heads on 60 nodes behind 3136 slots: 20.9 us, 18.1 from one slab, of which the pieces' rows in fp32 are 1.1; one
 //     token of 32 heads on 4 sequences with 1028 keys in sight 13.0 us from HBM, nearly all of it latency: lengths, table,
-//     ring, exchange, merge.)
+//     ring, exchange, merge.  10 to 42 scalar registers spill to lanes of vector registers, with up to
+//     16 accesses in the loop over steps.)
 #pragma once
 
 #include "kernels.h"

@@ -982,8 +982,8 @@ def paged_verify_attn(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Ten
     dense pages, any page stride); page_table [B,width] and kv_len [B] int32; parent [B,T] int32 and/or tree_mask
     [B,T,ceil(T/64)] int64 (bit patterns; a window needs parent).  Keys more than `window` - 1 positions before a node are
     out of its sight, but for the first `sinks` (window 0: none is).  max_kv_len bounds kv_len for the plan (0: the table's
-    width; max(1, longest) where it is known, 1 without a prefix).  Returns (out, lse [B,Hq,T] float32 or None); what a
-    call over pages allocates belongs to the stream it runs on."""
+    width; max(1, longest) where it is known, 1 without a prefix).  A row's own slots hold finite values.  Returns (out, lse
+    [B,Hq,T] float32 or None); what a call over pages allocates belongs to the stream it runs on."""
     desc = paged_desc(q, k_pages, v_pages, page_table, window, sinks, max_kv_len, num_splits, scale)
     B, T, at = desc.batch, desc.num_rows, q.get_device()
     _need_on(kv_len, "kv_len", torch.int32, at, (B,))
