@@ -9,7 +9,9 @@
  *   dreams_tree_accept_lm_head  greedy acceptance from final hidden states (LM head fused with the argmax)
  *   dreams_kv_commit         compaction of the accepted path's K/V into the cache
  * The cache is one slab of slots per sequence and KV head, or pages of a pool that sequences share ("Paged cache" below:
- * the attention of a tree and of a prompt over pages, the rows that go into them, and the tables' upkeep).
+ * the attention of a tree and of a prompt over pages, the rows that go into them, and the tables' upkeep), in 16 or 32 bits
+ * or in 8 ("Pages of 8 bits").  Queries and keys get their positions by rotation ("Rotary positions"), on their way into
+ * pages or by themselves.
  *
  * Conventions shared by every entry point
  *   - Pointers named as "device" point to device memory the caller owns (allocated on the current HIP
@@ -25,7 +27,7 @@
  *     and the results for such entries are unspecified.
  *   - A HIP launch error returns DREAMS_ERR_HIP.
  *   - Element types: DREAMS_BF16 tensors hold bfloat16 bit patterns (round-to-nearest-even); DREAMS_F32
- *     tensors hold IEEE binary32.
+ *     tensors hold IEEE binary32; DREAMS_E4M3 pages hold 8-bit codes with a scale for each 16 slots of a head.
  */
 #ifndef DREAMS_H
 #define DREAMS_H
@@ -48,7 +50,8 @@ typedef enum {
   DREAMS_ERR_DEVICE = -5        /* a kernel of an earlier call flagged a failure (dreams_workspace_status) */
 } dreams_status_t;
 
-typedef enum { DREAMS_F32 = 0, DREAMS_BF16 = 1 } dreams_dtype_t;
+/* (DREAMS_E4M3: pages of 8 bits, in the calls named *_e4m3 only) */
+typedef enum { DREAMS_F32 = 0, DREAMS_BF16 = 1, DREAMS_E4M3 = 2 } dreams_dtype_t;
 
 /*
  * Workspaces.  Every workspace (of either verb that takes one) begins with DREAMS_WORKSPACE_COUNTER_BYTES
@@ -622,6 +625,129 @@ dreams_status_t dreams_pages_fork(const dreams_page_pool_t* pool, void* k_pages,
 dreams_status_t dreams_pages_release(const dreams_page_pool_t* pool, int32_t* page_table, int32_t* page_count,
                                      int32_t* kv_len, int32_t* refcount, int32_t count, const int32_t* seqs, int32_t trim,
                                      hipStream_t stream);
+
+/*
+ * Rotary positions.  A head's first rotary_dim columns are rotary_dim / 2 pairs, of which pair i of a row at position p is
+ * turned by the angle p * frequencies[i] (radians):
+ *     (x, y)  becomes  (amplitude * (x cos - y sin), amplitude * (y cos + x sin))
+ * The other columns stay as they are.  Angles are reduced in 64 bits, sines and products are 32-bit, the result is rounded
+ * once to the type of the output.
+ *   rotary_dim    R, a multiple of 16, 16 .. head_dim
+ *   interleaved   0: pair i is columns i and i + R/2;  1: columns 2i and 2i + 1
+ *   frequencies   device [R/2] double (dreams_rope_frequencies, or any others), 8-byte aligned
+ *   positions     device [B, N] int32 or NULL: every row's position (a negative one turns back)
+ *   parent        device [B, N] int32 or NULL: rows are tree nodes (N <= 128), as for dreams_tree_verify_attn
+ *                 Without positions, row i of sequence b is at kv_len[b] + depth(i) (parent) or kv_len[b] + i.
+ *   amplitude     finite factor of the rotated columns (stretched contexts; normally 1)
+ */
+typedef struct {
+  int32_t rotary_dim;
+  int32_t interleaved;
+  const double* frequencies;
+  const int32_t* positions;
+  const int32_t* parent;
+  float amplitude;
+} dreams_rope_t;
+
+/* Scalings of the frequencies f_i = base^(-2i/R) for contexts beyond the trained one:
+ *   DREAMS_ROPE_PLAIN    none
+ *   DREAMS_ROPE_LINEAR   f_i / factor
+ *   DREAMS_ROPE_PARTS    by parts: f_i (g + (1 - g) / factor), where g rises from 0 to 1 as the turns that the pair makes
+ *                        within the trained context, trained_len * f_i / (2 pi), go from `low` to `high` */
+typedef enum { DREAMS_ROPE_PLAIN = 0, DREAMS_ROPE_LINEAR = 1, DREAMS_ROPE_PARTS = 2 } dreams_rope_scaling_t;
+
+/* dreams_rope_frequencies -- fills frequencies (HOST memory, rotary_dim / 2 doubles; rotary_dim even and >= 2).  base > 0 and
+ * factor > 0 finite; trained_len > 0 and 0 <= low < high finite (read for DREAMS_ROPE_PARTS only). */
+dreams_status_t dreams_rope_frequencies(int32_t rotary_dim, double base, dreams_rope_scaling_t scaling, double factor,
+                                        double trained_len, double low, double high, double* frequencies);
+
+/*
+ * dreams_rope -- rows rotated by their positions: out[b,h,i,:] = rotation of x[b,h,i,:] for every sequence b < batch, head h
+ * < num_heads and row i < num_rows.
+ *   head_dim      D, a multiple of 8, <= 512; dtype DREAMS_BF16 or DREAMS_F32
+ *   x, out        device; x_strides[3], out_strides[3] (host): elements between sequences, heads and rows, multiples of 16
+ *                 bytes (so [B, H, N, D] and [B, N, H, D] both serve); rows dense.  out = x with the same strides works in
+ *                 place; else they must not overlap.
+ *   kv_len        device [B] int32, the position of row 0 (of the root); may be NULL where rope->positions is given
+ */
+dreams_status_t dreams_rope(const dreams_rope_t* rope, int32_t batch, int32_t num_heads, int32_t num_rows, int32_t head_dim,
+                            dreams_dtype_t dtype, const void* x, const int64_t* x_strides, const int32_t* kv_len,
+                            void* out, const int64_t* out_strides, hipStream_t stream);
+
+/*
+ * The queries that go with new rows.  q: device [B, num_q_heads, N, D] of the new rows' type at strides[3] (elements between
+ * sequences, heads and rows, multiples of 16 bytes, rows dense); out: device, dense [B, num_q_heads, N, D], the layout that the
+ * attention calls take; must not overlap q.  Rows i >= row_len[b] of out become 0.
+ */
+typedef struct {
+  const void* q;
+  void* out;
+  int32_t num_q_heads;
+  int64_t strides[3];
+} dreams_rope_queries_t;
+
+/* dreams_paged_append_rope -- dreams_paged_append with k_new rotated on its way into the pages, and, where queries is not
+ * NULL (num_layers 1), the rows' queries rotated in the same launch.  Other arguments as there. */
+dreams_status_t dreams_paged_append_rope(const dreams_page_pool_t* pool, const dreams_rope_t* rope,
+                                         const dreams_rope_queries_t* queries, const void* k_new, const void* v_new,
+                                         int32_t num_rows, const int64_t* strides, const int32_t* page_table,
+                                         const int32_t* kv_len, const int32_t* row_len, void* k_pages, void* v_pages,
+                                         hipStream_t stream);
+
+/*
+ * Pages of 8 bits.  Pages as above in the codes of e4m3 (OCP: 1 sign, 4 exponent and 3 fraction bits, bias 7, largest 448, no
+ * infinity, 0x7f and 0xff NaN), pool dtype DREAMS_E4M3, and for each block of 16 slots of a head (slots 16 j .. 16 j + 15 of
+ * its page) one scale byte s of K and one of V, in e8m0: a row's values are its codes times 2^(s - 127).  head_dim is a
+ * multiple of 16, <= 512 (attention: 64 or 128).
+ * A block takes the least scale (s >= 1) at which the largest finite magnitude in it is at most 448 times it.  Powers of two
+ * lose nothing here: codes have an exponent of their own, and rows that move to a larger scale change only where they
+ * fall below the codes' normal range (2^-14 of the block's largest value and less).  The bytes that these calls write are 1 ..
+ * 247; 0 and 255 give unspecified values.  An infinity or NaN becomes NaN.
+ *   k, v           device uint8 [NL][num_pages, Hkv, page_size / 16]
+ *   layer_stride, page_stride   bytes, 0 means dense (page_stride Hkv * page_size / 16)
+ */
+typedef struct {
+  uint8_t* k;
+  uint8_t* v;
+  int64_t layer_stride;
+  int64_t page_stride;
+} dreams_page_scales_t;
+
+/*
+ * dreams_paged_append_e4m3 -- dreams_paged_append (rope NULL) or dreams_paged_append_rope into pages of 8 bits: every
+ * block that new rows go into takes the larger of its rows' scale and, where it holds slots before kv_len[b], the one it has;
+ * their codes are then moved to it.  A block's later slots are dead: their values may change.
+ *   new_dtype   type of k_new, v_new and the queries: DREAMS_BF16 or DREAMS_F32 (strides in its elements)
+ *   queries     needs rope
+ */
+dreams_status_t dreams_paged_append_e4m3(const dreams_page_pool_t* pool, const dreams_page_scales_t* scales,
+                                         const dreams_rope_t* rope, const dreams_rope_queries_t* queries,
+                                         dreams_dtype_t new_dtype, const void* k_new, const void* v_new, int32_t num_rows,
+                                         const int64_t* strides, const int32_t* page_table, const int32_t* kv_len,
+                                         const int32_t* row_len, void* k_pages, void* v_pages, hipStream_t stream);
+
+/* dreams_paged_kv_commit_e4m3 -- dreams_paged_kv_commit over pages of 8 bits.  A block that rows move into takes the largest
+ * scale of the rows it keeps (slots before kv_len_in[b], path entries that stay where they are or are skipped) and of those
+ * that come, and their codes are moved to it.  A block's slots past the path are dead: their values may change. */
+dreams_status_t dreams_paged_kv_commit_e4m3(const dreams_page_pool_t* pool, const dreams_page_scales_t* scales, void* k_pages,
+                                            void* v_pages, const int32_t* page_table, const int32_t* kv_len_in,
+                                            const int32_t* accept_path, const int32_t* accept_len, int32_t path_stride,
+                                            int32_t* kv_len_out, hipStream_t stream);
+
+/* dreams_paged_read_e4m3 -- the cached rows as values: k_out, v_out device bfloat16 [NL, B, Hkv, num_slots, D] (16-byte
+ * aligned): slot j < kv_len[b] of sequence b, exactly; 0 from kv_len[b] on, past the table, and for a page outside the pool.
+ * (Values below bfloat16's normal range may be flushed.)  What reads a cache as one slab (the visual-token statistics, a pool
+ * of another type) takes it from there. */
+dreams_status_t dreams_paged_read_e4m3(const dreams_page_pool_t* pool, const dreams_page_scales_t* scales,
+                                       const void* k_pages, const void* v_pages, const int32_t* page_table,
+                                       const int32_t* kv_len, int32_t num_slots, void* k_out, void* v_out,
+                                       hipStream_t stream);
+
+/* dreams_pages_fork_e4m3 -- dreams_pages_fork over pages of 8 bits: the copied rows' scales go with them. */
+dreams_status_t dreams_pages_fork_e4m3(const dreams_page_pool_t* pool, const dreams_page_scales_t* scales, void* k_pages,
+                                       void* v_pages, int32_t* page_table, int32_t* page_count, int32_t* kv_len,
+                                       int32_t* refcount, int32_t count, const int32_t* src, const int32_t* dst,
+                                       int32_t* granted, hipStream_t stream);
 
 /* Static description of a status code. */
 const char* dreams_status_string(dreams_status_t status);

@@ -1520,17 +1520,20 @@ dreams_status_t dreams_paged_prompt_attn(const dreams_paged_desc_t* desc, const 
 
 namespace {
 
-dreams_status_t check_pool(const dreams_page_pool_t* p, int* elem) {
+// (e4m3: a pool of 8 bits, else one of another type)
+dreams_status_t check_pool(const dreams_page_pool_t* p, int* elem, bool e4m3 = false) {
   if (!p) return fail(DREAMS_ERR_INVALID_ARG, "pool is NULL");
   if (p->batch < 0) return fail(DREAMS_ERR_INVALID_ARG, "batch = %d < 0", p->batch);
   if (p->num_layers < 1 || p->num_kv_heads < 1 || p->head_dim < 1)
     return fail(DREAMS_ERR_INVALID_ARG, "num_layers = %d, num_kv_heads = %d and head_dim = %d must be >= 1",
                 p->num_layers, p->num_kv_heads, p->head_dim);
-  if (p->dtype != DREAMS_BF16 && p->dtype != DREAMS_F32)
+  if (e4m3 && p->dtype != DREAMS_E4M3)
+    return fail(DREAMS_ERR_INVALID_ARG, "dtype = %d is not DREAMS_E4M3", (int)p->dtype);
+  if (!e4m3 && p->dtype != DREAMS_BF16 && p->dtype != DREAMS_F32)
     return fail(DREAMS_ERR_INVALID_ARG, "dtype = %d is not DREAMS_BF16 or DREAMS_F32", (int)p->dtype);
   dreams_status_t st = check_pages(p->num_pages, p->page_size, p->table_width);
   if (st != DREAMS_OK) return st;
-  *elem = p->dtype == DREAMS_BF16 ? 2 : 4;
+  *elem = e4m3 ? 1 : p->dtype == DREAMS_BF16 ? 2 : 4;
   const long long row_bytes = (long long)p->head_dim * *elem;
   if (row_bytes % 16 != 0 || row_bytes > kCommitMaxRowBytes)
     return fail(DREAMS_ERR_UNSUPPORTED, "head_dim * element size = %lld bytes (must be a multiple of 16, <= %d)",
@@ -1580,13 +1583,10 @@ PagedRowsArgs rows_args(const dreams_page_pool_t* p, int elem, void* k_pages, vo
 
 }  // namespace
 
-dreams_status_t dreams_paged_append(const dreams_page_pool_t* pool, const void* k_new, const void* v_new,
-                                    int32_t num_rows, const int64_t* strides, const int32_t* page_table,
-                                    const int32_t* kv_len, const int32_t* row_len, void* k_pages, void* v_pages,
-                                    hipStream_t stream) {
-  int elem = 0;
-  dreams_status_t st = check_pool(pool, &elem);
-  if (st != DREAMS_OK) return st;
+namespace {
+
+// The new rows of an append: strides (elements of `elem` bytes) against the pool, and pointers.
+dreams_status_t check_append(const dreams_page_pool_t* pool, int elem, int32_t num_rows, const int64_t* strides) {
   if (num_rows < 0) return fail(DREAMS_ERR_INVALID_ARG, "num_rows = %d < 0", num_rows);
   if (!strides) return fail(DREAMS_ERR_INVALID_ARG, "strides is NULL");
   const int32_t lengths[4] = {pool->num_layers, pool->batch, pool->num_kv_heads, num_rows};
@@ -1596,27 +1596,71 @@ dreams_status_t dreams_paged_append(const dreams_page_pool_t* pool, const void* 
                   (long long)strides[i]);
   if ((long long)num_rows * pool->num_kv_heads > (0xffffffffLL - 255) / (pool->head_dim * elem / 16))
     return fail(DREAMS_ERR_UNSUPPORTED, "problem too large");
-  if (pool->batch == 0 || num_rows == 0) return ok();
+  return DREAMS_OK;
+}
+
+dreams_status_t check_append_pointers(const void* k_new, const void* v_new, const int32_t* page_table, const int32_t* kv_len,
+                                      const int32_t* row_len, const void* k_pages, const void* v_pages) {
   if (!k_new || !v_new || !page_table || !kv_len || !k_pages || !v_pages)
     return fail(DREAMS_ERR_INVALID_ARG, "k_new, v_new, page_table, kv_len, k_pages and v_pages must not be NULL");
   if (!aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(k_pages, 16) || !aligned(v_pages, 16))
     return fail(DREAMS_ERR_INVALID_ARG, "k_new, v_new, k_pages and v_pages must be 16-byte aligned");
   if (!aligned(page_table, 4) || !aligned(kv_len, 4) || !aligned(row_len, 4))
     return fail(DREAMS_ERR_INVALID_ARG, "an int32 argument is not 4-byte aligned");
+  return DREAMS_OK;
+}
+
+// (a stride along an axis of one entry is not used)
+void set_new_rows(PagedRowsArgs* a, const dreams_page_pool_t* pool, int elem, const void* k_new, const void* v_new,
+                  int32_t num_rows, const int64_t* strides, const int32_t* row_len) {
+  a->k_new = (const char*)k_new;
+  a->v_new = (const char*)v_new;
+  a->row_len = row_len;
+  a->N = num_rows;
+  a->new_layer = pool->num_layers > 1 ? strides[0] * elem : 0;
+  a->new_batch = pool->batch > 1 ? strides[1] * elem : 0;
+  a->new_head = pool->num_kv_heads > 1 ? strides[2] * elem : 0;
+  a->new_row = num_rows > 1 ? strides[3] * elem : 0;
+}
+
+}  // namespace
+
+dreams_status_t dreams_paged_append(const dreams_page_pool_t* pool, const void* k_new, const void* v_new,
+                                    int32_t num_rows, const int64_t* strides, const int32_t* page_table,
+                                    const int32_t* kv_len, const int32_t* row_len, void* k_pages, void* v_pages,
+                                    hipStream_t stream) {
+  int elem = 0;
+  dreams_status_t st = check_pool(pool, &elem);
+  if (st == DREAMS_OK) st = check_append(pool, elem, num_rows, strides);
+  if (st != DREAMS_OK) return st;
+  if (pool->batch == 0 || num_rows == 0) return ok();
+  st = check_append_pointers(k_new, v_new, page_table, kv_len, row_len, k_pages, v_pages);
+  if (st != DREAMS_OK) return st;
   PagedRowsArgs a = rows_args(pool, elem, k_pages, v_pages, page_table, kv_len);
-  a.k_new = (const char*)k_new;
-  a.v_new = (const char*)v_new;
-  a.row_len = row_len;
-  a.N = num_rows;
-  // (a stride along an axis of one entry is not used)
-  a.new_layer = lengths[0] > 1 ? strides[0] * elem : 0;
-  a.new_batch = lengths[1] > 1 ? strides[1] * elem : 0;
-  a.new_head = lengths[2] > 1 ? strides[2] * elem : 0;
-  a.new_row = lengths[3] > 1 ? strides[3] * elem : 0;
+  set_new_rows(&a, pool, elem, k_new, v_new, num_rows, strides, row_len);
   hipError_t e = launch_paged_append(a, stream);
   if (e != hipSuccess) return hip_fail(e, "paged append launch");
   return ok();
 }
+
+namespace {
+
+dreams_status_t check_commit(const dreams_page_pool_t* pool, const void* k_pages, const void* v_pages,
+                             const int32_t* page_table, const int32_t* kv_len_in, const int32_t* accept_path,
+                             const int32_t* accept_len, const int32_t* kv_len_out) {
+  if (!k_pages || !v_pages || !page_table || !kv_len_in || !accept_path || !accept_len || !kv_len_out)
+    return fail(DREAMS_ERR_INVALID_ARG, "page, table, length and path pointers must not be NULL");
+  if (!aligned(k_pages, 16) || !aligned(v_pages, 16))
+    return fail(DREAMS_ERR_INVALID_ARG, "k_pages and v_pages must be 16-byte aligned");
+  if (!aligned(page_table, 4) || !aligned(kv_len_in, 4) || !aligned(accept_path, 4) || !aligned(accept_len, 4) ||
+      !aligned(kv_len_out, 4))
+    return fail(DREAMS_ERR_INVALID_ARG, "an int32 argument is not 4-byte aligned");
+  if (overlap(kv_len_out, (size_t)pool->batch * 4, kv_len_in, (size_t)pool->batch * 4))
+    return fail(DREAMS_ERR_INVALID_ARG, "kv_len_out must not overlap kv_len_in");
+  return DREAMS_OK;
+}
+
+}  // namespace
 
 dreams_status_t dreams_paged_kv_commit(const dreams_page_pool_t* pool, void* k_pages, void* v_pages,
                                        const int32_t* page_table, const int32_t* kv_len_in, const int32_t* accept_path,
@@ -1627,15 +1671,8 @@ dreams_status_t dreams_paged_kv_commit(const dreams_page_pool_t* pool, void* k_p
   if (st != DREAMS_OK) return st;
   if (path_stride < 1) return fail(DREAMS_ERR_INVALID_ARG, "path_stride = %d < 1", path_stride);
   if (pool->batch == 0) return ok();
-  if (!k_pages || !v_pages || !page_table || !kv_len_in || !accept_path || !accept_len || !kv_len_out)
-    return fail(DREAMS_ERR_INVALID_ARG, "page, table, length and path pointers must not be NULL");
-  if (!aligned(k_pages, 16) || !aligned(v_pages, 16))
-    return fail(DREAMS_ERR_INVALID_ARG, "k_pages and v_pages must be 16-byte aligned");
-  if (!aligned(page_table, 4) || !aligned(kv_len_in, 4) || !aligned(accept_path, 4) || !aligned(accept_len, 4) ||
-      !aligned(kv_len_out, 4))
-    return fail(DREAMS_ERR_INVALID_ARG, "an int32 argument is not 4-byte aligned");
-  if (overlap(kv_len_out, (size_t)pool->batch * 4, kv_len_in, (size_t)pool->batch * 4))
-    return fail(DREAMS_ERR_INVALID_ARG, "kv_len_out must not overlap kv_len_in");
+  st = check_commit(pool, k_pages, v_pages, page_table, kv_len_in, accept_path, accept_len, kv_len_out);
+  if (st != DREAMS_OK) return st;
   PagedRowsArgs a = rows_args(pool, elem, k_pages, v_pages, page_table, kv_len_in);
   a.path = accept_path;
   a.accept_len = accept_len;
@@ -1643,6 +1680,304 @@ dreams_status_t dreams_paged_kv_commit(const dreams_page_pool_t* pool, void* k_p
   a.path_stride = path_stride;
   hipError_t e = launch_paged_commit(a, stream);
   if (e != hipSuccess) return hip_fail(e, "paged commit launch");
+  return ok();
+}
+
+// ------------------------------------------------------------------------------- rotary positions, pages of 8 bits
+namespace {
+
+dreams_status_t check_rope(const dreams_rope_t* r, int32_t head_dim, int32_t num_rows) {
+  if (!r) return fail(DREAMS_ERR_INVALID_ARG, "rope is NULL");
+  if (r->rotary_dim < 1 || r->rotary_dim > head_dim)
+    return fail(DREAMS_ERR_INVALID_ARG, "rotary_dim = %d outside [1, head_dim = %d]", r->rotary_dim, head_dim);
+  if (r->rotary_dim % 16 != 0)
+    return fail(DREAMS_ERR_UNSUPPORTED, "rotary_dim = %d is not a multiple of 16", r->rotary_dim);
+  if (head_dim % 8 != 0) return fail(DREAMS_ERR_UNSUPPORTED, "head_dim = %d is not a multiple of 8", head_dim);
+  if (r->interleaved != 0 && r->interleaved != 1)
+    return fail(DREAMS_ERR_INVALID_ARG, "interleaved = %d is not 0 or 1", r->interleaved);
+  if (!isfinite(r->amplitude)) return fail(DREAMS_ERR_INVALID_ARG, "amplitude is not finite");
+  if (r->parent && !r->positions && num_rows > kMaxNodes)
+    return fail(DREAMS_ERR_INVALID_ARG, "num_rows = %d tree nodes exceed %d", num_rows, kMaxNodes);
+  return DREAMS_OK;
+}
+dreams_status_t check_rope_pointers(const dreams_rope_t* r, const int32_t* kv_len) {
+  if (!r->frequencies) return fail(DREAMS_ERR_INVALID_ARG, "frequencies is NULL");
+  if (!r->positions && !kv_len) return fail(DREAMS_ERR_INVALID_ARG, "either positions or kv_len must be given");
+  if (!aligned(r->frequencies, 8)) return fail(DREAMS_ERR_INVALID_ARG, "frequencies is not 8-byte aligned");
+  if (!aligned(r->positions, 4) || !aligned(r->parent, 4) || !aligned(kv_len, 4))
+    return fail(DREAMS_ERR_INVALID_ARG, "an int32 argument is not 4-byte aligned");
+  return DREAMS_OK;
+}
+
+RopeArgs rope_args(const dreams_rope_t* r, const int32_t* kv_len) {
+  RopeArgs a{};
+  if (!r) return a;
+  a.freq = r->frequencies;
+  a.positions = r->positions;
+  a.parent = r->parent;
+  a.kv_len = kv_len;
+  a.gain = r->amplitude;
+  a.R = r->rotary_dim;
+  a.interleaved = r->interleaved;
+  return a;
+}
+
+// Strides (elements) of [B, heads, rows] rows of head_dim elements.
+dreams_status_t check_row_strides(const char* name, const int64_t* strides, int32_t batch, int32_t heads, int32_t rows,
+                                  int elem) {
+  const int32_t lengths[3] = {batch, heads, rows};
+  for (int i = 0; i < 3; ++i)
+    if (lengths[i] > 1 && (strides[i] < 0 || strides[i] > (int64_t)1 << 48 || strides[i] * elem % 16 != 0))
+      return fail(DREAMS_ERR_INVALID_ARG, "%s[%d] = %lld must be a non-negative multiple of 16 bytes", name, i,
+                  (long long)strides[i]);
+  return DREAMS_OK;
+}
+
+dreams_status_t check_queries(const dreams_rope_queries_t* q, const dreams_page_pool_t* pool, int32_t num_rows, int elem) {
+  if (!q) return DREAMS_OK;
+  if (pool->num_layers != 1)
+    return fail(DREAMS_ERR_INVALID_ARG, "queries go with one layer's rows, num_layers = %d", pool->num_layers);
+  if (q->num_q_heads < 1) return fail(DREAMS_ERR_INVALID_ARG, "num_q_heads = %d < 1", q->num_q_heads);
+  return check_row_strides("queries->strides", q->strides, pool->batch, q->num_q_heads, num_rows, elem);
+}
+dreams_status_t check_query_pointers(const dreams_rope_queries_t* q) {
+  if (!q) return DREAMS_OK;
+  if (!q->q || !q->out) return fail(DREAMS_ERR_INVALID_ARG, "queries->q and queries->out must not be NULL");
+  if (!aligned(q->q, 16) || !aligned(q->out, 16))
+    return fail(DREAMS_ERR_INVALID_ARG, "queries->q and queries->out must be 16-byte aligned");
+  return DREAMS_OK;
+}
+RopeQueryArgs query_args(const dreams_rope_queries_t* q, const dreams_page_pool_t* pool, int32_t num_rows, int elem) {
+  RopeQueryArgs a{};
+  if (!q) return a;
+  a.q = (const char*)q->q;
+  a.out = (char*)q->out;
+  a.Hq = q->num_q_heads;
+  a.batch = pool->batch > 1 ? q->strides[0] * elem : 0;
+  a.head = q->num_q_heads > 1 ? q->strides[1] * elem : 0;
+  a.row = num_rows > 1 ? q->strides[2] * elem : 0;
+  return a;
+}
+
+// A launch over rows x heads x units of 16 columns, a thread each at most.
+dreams_status_t check_units(long long rows, long long heads, long long units) {
+  if (rows > 0 && heads * units > 0x7fffffffLL / rows) return fail(DREAMS_ERR_UNSUPPORTED, "problem too large");
+  return DREAMS_OK;
+}
+
+dreams_status_t check_scales(const dreams_page_scales_t* s, const dreams_page_pool_t* p) {
+  if (!s) return fail(DREAMS_ERR_INVALID_ARG, "scales is NULL");
+  const int64_t page = (int64_t)p->num_kv_heads * (p->page_size / kScaleBlock);
+  if (s->page_stride != 0 && (s->page_stride < page || s->page_stride > ((int64_t)1 << 60) / p->num_pages))
+    return fail(DREAMS_ERR_INVALID_ARG, "scales->page_stride = %lld must hold a page's %lld scales", (long long)s->page_stride,
+                (long long)page);
+  const int64_t stride = s->page_stride ? s->page_stride : page;
+  if (s->layer_stride != 0 && p->num_layers > 1 &&
+      (s->layer_stride < stride * (p->num_pages - 1) + page || s->layer_stride > (int64_t)1 << 60))
+    return fail(DREAMS_ERR_INVALID_ARG, "scales->layer_stride = %lld must hold a layer's scales", (long long)s->layer_stride);
+  return DREAMS_OK;
+}
+
+PagedScaleArgs scale_args(const dreams_page_scales_t* s, const dreams_page_pool_t* p) {
+  PagedScaleArgs a{};
+  a.k = s->k;
+  a.v = s->v;
+  a.page_stride = s->page_stride ? s->page_stride : (int64_t)p->num_kv_heads * (p->page_size / kScaleBlock);
+  a.layer_stride = s->layer_stride ? s->layer_stride : a.page_stride * p->num_pages;
+  return a;
+}
+
+dreams_status_t check_pool8(const dreams_page_pool_t* pool, const dreams_page_scales_t* scales) {
+  int elem = 0;
+  dreams_status_t st = check_pool(pool, &elem, true);
+  return st == DREAMS_OK ? check_scales(scales, pool) : st;
+}
+dreams_status_t check_scale_pointers(const dreams_page_scales_t* scales) {
+  if (!scales->k || !scales->v) return fail(DREAMS_ERR_INVALID_ARG, "scales->k and scales->v must not be NULL");
+  return DREAMS_OK;
+}
+
+}  // namespace
+
+dreams_status_t dreams_rope_frequencies(int32_t rotary_dim, double base, dreams_rope_scaling_t scaling, double factor,
+                                        double trained_len, double low, double high, double* frequencies) {
+  if (rotary_dim < 2 || rotary_dim % 2 != 0)
+    return fail(DREAMS_ERR_INVALID_ARG, "rotary_dim = %d must be even and >= 2", rotary_dim);
+  if (!isfinite(base) || base <= 0.0 || !isfinite(factor) || factor <= 0.0)
+    return fail(DREAMS_ERR_INVALID_ARG, "base = %g and factor = %g must be finite and > 0", base, factor);
+  if (scaling != DREAMS_ROPE_PLAIN && scaling != DREAMS_ROPE_LINEAR && scaling != DREAMS_ROPE_PARTS)
+    return fail(DREAMS_ERR_INVALID_ARG, "scaling = %d is not a dreams_rope_scaling_t", (int)scaling);
+  if (scaling == DREAMS_ROPE_PARTS &&
+      !(isfinite(trained_len) && trained_len > 0.0 && isfinite(high) && low >= 0.0 && low < high))
+    return fail(DREAMS_ERR_INVALID_ARG, "trained_len = %g must be > 0 and 0 <= low = %g < high = %g", trained_len, low, high);
+  if (!frequencies) return fail(DREAMS_ERR_INVALID_ARG, "frequencies is NULL");
+  for (int32_t i = 0; i < rotary_dim / 2; ++i) {
+    double f = pow(base, -2.0 * i / rotary_dim);
+    if (scaling == DREAMS_ROPE_LINEAR) f /= factor;
+    if (scaling == DREAMS_ROPE_PARTS) {
+      const double turns = trained_len * f / 6.283185307179586477;
+      const double keep = std::min(std::max((turns - low) / (high - low), 0.0), 1.0);
+      f *= keep + (1.0 - keep) / factor;
+    }
+    frequencies[i] = f;
+  }
+  return ok();
+}
+
+dreams_status_t dreams_rope(const dreams_rope_t* rope, int32_t batch, int32_t num_heads, int32_t num_rows, int32_t head_dim,
+                            dreams_dtype_t dtype, const void* x, const int64_t* x_strides, const int32_t* kv_len,
+                            void* out, const int64_t* out_strides, hipStream_t stream) {
+  if (batch < 0 || num_rows < 0 || num_heads < 1 || head_dim < 1)
+    return fail(DREAMS_ERR_INVALID_ARG, "batch = %d and num_rows = %d must be >= 0, num_heads = %d and head_dim = %d >= 1",
+                batch, num_rows, num_heads, head_dim);
+  if (dtype != DREAMS_BF16 && dtype != DREAMS_F32)
+    return fail(DREAMS_ERR_INVALID_ARG, "dtype = %d is not DREAMS_BF16 or DREAMS_F32", (int)dtype);
+  const int elem = dtype == DREAMS_BF16 ? 2 : 4;
+  if (head_dim > kRopeMaxDim) return fail(DREAMS_ERR_UNSUPPORTED, "head_dim = %d exceeds %d", head_dim, kRopeMaxDim);
+  dreams_status_t st = check_rope(rope, head_dim, num_rows);
+  if (st != DREAMS_OK) return st;
+  if (!x_strides || !out_strides) return fail(DREAMS_ERR_INVALID_ARG, "x_strides and out_strides must not be NULL");
+  st = check_row_strides("x_strides", x_strides, batch, num_heads, num_rows, elem);
+  if (st == DREAMS_OK) st = check_row_strides("out_strides", out_strides, batch, num_heads, num_rows, elem);
+  if (st == DREAMS_OK) st = check_units(num_rows, num_heads, (head_dim + 15) / 16 + 1);
+  if (st != DREAMS_OK) return st;
+  if (batch > 65535) return fail(DREAMS_ERR_UNSUPPORTED, "problem too large");
+  if (batch == 0 || num_rows == 0) return ok();
+  st = check_rope_pointers(rope, kv_len);
+  if (st != DREAMS_OK) return st;
+  if (!x || !out) return fail(DREAMS_ERR_INVALID_ARG, "x and out must not be NULL");
+  if (!aligned(x, 16) || !aligned(out, 16)) return fail(DREAMS_ERR_INVALID_ARG, "x and out must be 16-byte aligned");
+  RopeCallArgs a{};
+  a.rope = rope_args(rope, kv_len);
+  a.x = (const char*)x;
+  a.out = (char*)out;
+  const int32_t lengths[3] = {batch, num_heads, num_rows};
+  int64_t from[3], to[3];
+  a.in_place = x == out;
+  for (int i = 0; i < 3; ++i) {
+    from[i] = lengths[i] > 1 ? x_strides[i] * elem : 0;
+    to[i] = lengths[i] > 1 ? out_strides[i] * elem : 0;
+    if (lengths[i] > 1 && to[i] == 0) return fail(DREAMS_ERR_INVALID_ARG, "out_strides[%d] is 0: rows share memory", i);
+    if (x == out && from[i] != to[i])
+      return fail(DREAMS_ERR_INVALID_ARG, "x_strides and out_strides differ in a call in place");
+  }
+  a.x_batch = from[0];
+  a.x_head = from[1];
+  a.x_row = from[2];
+  a.out_batch = to[0];
+  a.out_head = to[1];
+  a.out_row = to[2];
+  a.B = batch;
+  a.H = num_heads;
+  a.N = num_rows;
+  a.D = head_dim;
+  a.elem = elem;
+  hipError_t e = launch_rope(a, stream);
+  if (e != hipSuccess) return hip_fail(e, "rope launch");
+  return ok();
+}
+
+dreams_status_t dreams_paged_append_rope(const dreams_page_pool_t* pool, const dreams_rope_t* rope,
+                                         const dreams_rope_queries_t* queries, const void* k_new, const void* v_new,
+                                         int32_t num_rows, const int64_t* strides, const int32_t* page_table,
+                                         const int32_t* kv_len, const int32_t* row_len, void* k_pages, void* v_pages,
+                                         hipStream_t stream) {
+  int elem = 0;
+  dreams_status_t st = check_pool(pool, &elem);
+  if (st == DREAMS_OK) st = check_append(pool, elem, num_rows, strides);
+  if (st == DREAMS_OK) st = check_queries(queries, pool, num_rows, elem);
+  if (st == DREAMS_OK) st = check_rope(rope, pool->head_dim, num_rows);
+  if (st == DREAMS_OK && (pool->batch == 0 || num_rows == 0)) return ok();
+  if (st == DREAMS_OK) st = check_rope_pointers(rope, kv_len);
+  if (st == DREAMS_OK)
+    st = check_units(num_rows, (queries ? queries->num_q_heads : 0) + 2LL * pool->num_kv_heads, (pool->head_dim + 15) / 16 + 1);
+  if (st == DREAMS_OK) st = check_append_pointers(k_new, v_new, page_table, kv_len, row_len, k_pages, v_pages);
+  if (st == DREAMS_OK) st = check_query_pointers(queries);
+  if (st != DREAMS_OK) return st;
+  PagedRowsArgs a = rows_args(pool, elem, k_pages, v_pages, page_table, kv_len);
+  set_new_rows(&a, pool, elem, k_new, v_new, num_rows, strides, row_len);
+  hipError_t e = launch_paged_append_rope(a, rope_args(rope, kv_len), query_args(queries, pool, num_rows, elem), elem,
+                                          pool->head_dim, stream);
+  if (e != hipSuccess) return hip_fail(e, "paged append launch");
+  return ok();
+}
+
+dreams_status_t dreams_paged_append_e4m3(const dreams_page_pool_t* pool, const dreams_page_scales_t* scales,
+                                         const dreams_rope_t* rope, const dreams_rope_queries_t* queries,
+                                         dreams_dtype_t new_dtype, const void* k_new, const void* v_new, int32_t num_rows,
+                                         const int64_t* strides, const int32_t* page_table, const int32_t* kv_len,
+                                         const int32_t* row_len, void* k_pages, void* v_pages, hipStream_t stream) {
+  dreams_status_t st = check_pool8(pool, scales);
+  if (st != DREAMS_OK) return st;
+  if (new_dtype != DREAMS_BF16 && new_dtype != DREAMS_F32)
+    return fail(DREAMS_ERR_INVALID_ARG, "new_dtype = %d is not DREAMS_BF16 or DREAMS_F32", (int)new_dtype);
+  const int elem = new_dtype == DREAMS_BF16 ? 2 : 4;
+  st = check_append(pool, elem, num_rows, strides);
+  if (st == DREAMS_OK) st = check_queries(queries, pool, num_rows, elem);
+  if (st == DREAMS_OK && queries && !rope) return fail(DREAMS_ERR_INVALID_ARG, "queries need rope");
+  if (st == DREAMS_OK && rope) st = check_rope(rope, pool->head_dim, num_rows);
+  if (st == DREAMS_OK && (pool->batch == 0 || num_rows == 0)) return ok();
+  if (st == DREAMS_OK && rope) st = check_rope_pointers(rope, kv_len);
+  if (st == DREAMS_OK)
+    st = check_units(num_rows + 32LL, (queries ? queries->num_q_heads : 0) + 2LL * pool->num_kv_heads, pool->head_dim / 16);
+  if (st == DREAMS_OK) st = check_append_pointers(k_new, v_new, page_table, kv_len, row_len, k_pages, v_pages);
+  if (st == DREAMS_OK) st = check_query_pointers(queries);
+  if (st == DREAMS_OK) st = check_scale_pointers(scales);
+  if (st != DREAMS_OK) return st;
+  PagedRowsArgs a = rows_args(pool, 1, k_pages, v_pages, page_table, kv_len);
+  set_new_rows(&a, pool, elem, k_new, v_new, num_rows, strides, row_len);
+  hipError_t e = launch_paged_append_e4m3(a, scale_args(scales, pool), rope_args(rope, kv_len),
+                                          query_args(queries, pool, num_rows, elem), elem, stream);
+  if (e != hipSuccess) return hip_fail(e, "paged append launch");
+  return ok();
+}
+
+dreams_status_t dreams_paged_kv_commit_e4m3(const dreams_page_pool_t* pool, const dreams_page_scales_t* scales, void* k_pages,
+                                            void* v_pages, const int32_t* page_table, const int32_t* kv_len_in,
+                                            const int32_t* accept_path, const int32_t* accept_len, int32_t path_stride,
+                                            int32_t* kv_len_out, hipStream_t stream) {
+  dreams_status_t st = check_pool8(pool, scales);
+  if (st != DREAMS_OK) return st;
+  if (path_stride < 1) return fail(DREAMS_ERR_INVALID_ARG, "path_stride = %d < 1", path_stride);
+  if (pool->batch == 0) return ok();
+  st = check_commit(pool, k_pages, v_pages, page_table, kv_len_in, accept_path, accept_len, kv_len_out);
+  if (st == DREAMS_OK) st = check_scale_pointers(scales);
+  if (st != DREAMS_OK) return st;
+  if (!fits_grid((long long)pool->num_layers * pool->num_kv_heads * pool->batch, 128))
+    return fail(DREAMS_ERR_UNSUPPORTED, "problem too large");
+  PagedRowsArgs a = rows_args(pool, 1, k_pages, v_pages, page_table, kv_len_in);
+  a.path = accept_path;
+  a.accept_len = accept_len;
+  a.kv_len_out = kv_len_out;
+  a.path_stride = path_stride;
+  hipError_t e = launch_paged_commit_e4m3(a, scale_args(scales, pool), stream);
+  if (e != hipSuccess) return hip_fail(e, "paged commit launch");
+  return ok();
+}
+
+dreams_status_t dreams_paged_read_e4m3(const dreams_page_pool_t* pool, const dreams_page_scales_t* scales,
+                                       const void* k_pages, const void* v_pages, const int32_t* page_table,
+                                       const int32_t* kv_len, int32_t num_slots, void* k_out, void* v_out,
+                                       hipStream_t stream) {
+  dreams_status_t st = check_pool8(pool, scales);
+  if (st != DREAMS_OK) return st;
+  if (num_slots < 0 || num_slots > kPagedMaxSlots)
+    return fail(DREAMS_ERR_INVALID_ARG, "num_slots = %d outside [0, %d]", num_slots, kPagedMaxSlots);
+  if ((long long)pool->batch * pool->num_kv_heads > 65535) return fail(DREAMS_ERR_UNSUPPORTED, "problem too large");
+  st = check_units(num_slots, 1, pool->head_dim / 16);
+  if (st != DREAMS_OK) return st;
+  if (pool->batch == 0 || num_slots == 0) return ok();
+  if (!k_pages || !v_pages || !page_table || !kv_len || !k_out || !v_out)
+    return fail(DREAMS_ERR_INVALID_ARG, "k_pages, v_pages, page_table, kv_len, k_out and v_out must not be NULL");
+  if (!aligned(k_pages, 16) || !aligned(v_pages, 16) || !aligned(k_out, 16) || !aligned(v_out, 16))
+    return fail(DREAMS_ERR_INVALID_ARG, "k_pages, v_pages, k_out and v_out must be 16-byte aligned");
+  if (!aligned(page_table, 4) || !aligned(kv_len, 4))
+    return fail(DREAMS_ERR_INVALID_ARG, "an int32 argument is not 4-byte aligned");
+  st = check_scale_pointers(scales);
+  if (st != DREAMS_OK) return st;
+  PagedRowsArgs a = rows_args(pool, 1, (void*)k_pages, (void*)v_pages, page_table, kv_len);
+  hipError_t e = launch_paged_read_e4m3(a, scale_args(scales, pool), num_slots, (char*)k_out, (char*)v_out, stream);
+  if (e != hipSuccess) return hip_fail(e, "paged read launch");
   return ok();
 }
 
@@ -1705,11 +2040,14 @@ dreams_status_t dreams_pages_reserve(const dreams_page_pool_t* pool, int32_t* pa
   return ok();
 }
 
-dreams_status_t dreams_pages_fork(const dreams_page_pool_t* pool, void* k_pages, void* v_pages, int32_t* page_table,
-                                  int32_t* page_count, int32_t* kv_len, int32_t* refcount, int32_t count,
-                                  const int32_t* src, const int32_t* dst, int32_t* granted, hipStream_t stream) {
+namespace {
+
+dreams_status_t run_fork(const dreams_page_pool_t* pool, const dreams_page_scales_t* scales, void* k_pages, void* v_pages,
+                         int32_t* page_table, int32_t* page_count, int32_t* kv_len, int32_t* refcount, int32_t count,
+                         const int32_t* src, const int32_t* dst, int32_t* granted, hipStream_t stream, bool e4m3) {
   int elem = 0;
-  dreams_status_t st = check_pool(pool, &elem);
+  dreams_status_t st = check_pool(pool, &elem, e4m3);
+  if (st == DREAMS_OK && e4m3) st = check_scales(scales, pool);
   if (st == DREAMS_OK) st = check_tables(pool, page_table, page_count, refcount);
   if (st == DREAMS_OK) st = check_list(count, src, dst);
   if (st != DREAMS_OK) return st;
@@ -1720,6 +2058,8 @@ dreams_status_t dreams_pages_fork(const dreams_page_pool_t* pool, void* k_pages,
     return fail(DREAMS_ERR_INVALID_ARG, "k_pages and v_pages must be 16-byte aligned");
   if (!aligned(kv_len, 4) || !aligned(granted, 4))
     return fail(DREAMS_ERR_INVALID_ARG, "an int32 argument is not 4-byte aligned");
+  if (e4m3) st = check_scale_pointers(scales);
+  if (st != DREAMS_OK) return st;
   PagesArgs a = pages_args(pool, page_table, page_count, kv_len, refcount);
   a.src = src;
   a.dst = dst;
@@ -1732,9 +2072,27 @@ dreams_status_t dreams_pages_fork(const dreams_page_pool_t* pool, void* k_pages,
   a.NL = pool->num_layers;
   a.Hkv = pool->num_kv_heads;
   a.row_bytes = pool->head_dim * elem;
+  if (e4m3) a.scales = scale_args(scales, pool);
   hipError_t e = launch_pages_fork(a, stream);
   if (e != hipSuccess) return hip_fail(e, "page fork launch");
   return ok();
+}
+
+}  // namespace
+
+dreams_status_t dreams_pages_fork(const dreams_page_pool_t* pool, void* k_pages, void* v_pages, int32_t* page_table,
+                                  int32_t* page_count, int32_t* kv_len, int32_t* refcount, int32_t count,
+                                  const int32_t* src, const int32_t* dst, int32_t* granted, hipStream_t stream) {
+  return run_fork(pool, nullptr, k_pages, v_pages, page_table, page_count, kv_len, refcount, count, src, dst, granted, stream,
+                  false);
+}
+
+dreams_status_t dreams_pages_fork_e4m3(const dreams_page_pool_t* pool, const dreams_page_scales_t* scales, void* k_pages,
+                                       void* v_pages, int32_t* page_table, int32_t* page_count, int32_t* kv_len,
+                                       int32_t* refcount, int32_t count, const int32_t* src, const int32_t* dst,
+                                       int32_t* granted, hipStream_t stream) {
+  return run_fork(pool, scales, k_pages, v_pages, page_table, page_count, kv_len, refcount, count, src, dst, granted, stream,
+                  true);
 }
 
 dreams_status_t dreams_pages_release(const dreams_page_pool_t* pool, int32_t* page_table, int32_t* page_count,

@@ -303,6 +303,38 @@ struct CommitArgs {
 
 hipError_t launch_kv_commit(const CommitArgs& a, hipStream_t stream);
 
+// -------------------------------------------------------------------------------------- rotary positions
+// Units of 8 pairs (16 columns): the rotated part of a head's row is R / 16 of them, the rest ceil((D - R) / 16) more.
+struct RopeArgs {
+  const double* freq;        // [R / 2] radians a position; nullptr: nothing is rotated
+  const int32_t* positions;  // [B, N] or nullptr
+  const int32_t* parent;     // [B, N] or nullptr (N <= kMaxNodes)
+  const int32_t* kv_len;     // [B] or nullptr
+  float gain;
+  int R, interleaved;
+};
+constexpr int kRopeThreads = 256;
+constexpr int kRopeMaxDim = 512;
+
+struct RopeCallArgs {        // a tensor by itself
+  RopeArgs rope;
+  const char* x;
+  char* out;
+  int64_t x_batch, x_head, x_row, out_batch, out_head, out_row;   // bytes
+  int B, H, N, D;
+  int elem;                  // 2 or 4 bytes
+  int in_place;              // the columns that are not rotated are there already
+};
+hipError_t launch_rope(const RopeCallArgs& a, hipStream_t stream);
+
+// The queries that go with appended rows: [B, Hq, N, D] at these strides (bytes) to a dense [B, Hq, N, D].
+struct RopeQueryArgs {
+  const char* q;             // nullptr: none
+  char* out;
+  int64_t batch, head, row;
+  int Hq;
+};
+
 // ---------------------------------------------------------------------------------------- paged cache
 // A pool of pages holds the slots of every sequence: page p of KV head g is a [page_size, D] slab at
 // p * page_stride + g * page_size * D.  Slot j of sequence b is row j % page_size of page table[b, j / page_size].  Page
@@ -363,6 +395,24 @@ struct PagedRowsArgs {
 hipError_t launch_paged_append(const PagedRowsArgs& a, hipStream_t stream);
 hipError_t launch_paged_commit(const PagedRowsArgs& a, hipStream_t stream);
 
+// Rows rotated on their way into pages of their own type, and their queries.
+hipError_t launch_paged_append_rope(const PagedRowsArgs& a, const RopeArgs& rope, const RopeQueryArgs& q, int elem, int D,
+                                    hipStream_t stream);
+
+// Pages of 8 bits: PagedRowsArgs with the codes' strides (row_bytes = D), and the scale bytes [NL][pages, Hkv, page_size / 16].
+constexpr int kScaleBlock = 16;              // slots of a scale
+struct PagedScaleArgs {
+  uint8_t* k;
+  uint8_t* v;
+  int64_t layer_stride, page_stride;         // bytes
+};
+hipError_t launch_paged_append_e4m3(const PagedRowsArgs& a, const PagedScaleArgs& sc, const RopeArgs& rope,
+                                    const RopeQueryArgs& q, int elem, hipStream_t stream);
+hipError_t launch_paged_commit_e4m3(const PagedRowsArgs& a, const PagedScaleArgs& sc, hipStream_t stream);
+// slots 0 .. num_slots - 1 of every sequence as bf16 [NL, B, Hkv, num_slots, D]
+hipError_t launch_paged_read_e4m3(const PagedRowsArgs& a, const PagedScaleArgs& sc, int num_slots, char* k_out, char* v_out,
+                                  hipStream_t stream);
+
 struct PagesArgs {
   int32_t* table;            // [B, width]
   int32_t* count;            // [B] pages that a sequence holds
@@ -380,6 +430,7 @@ struct PagesArgs {
   char* v;
   int64_t layer_stride, page_stride;
   int NL, Hkv, row_bytes;
+  PagedScaleArgs scales;     // pages of 8 bits: theirs go with them (else nullptr)
 };
 hipError_t launch_pages_reserve(const PagesArgs& a, hipStream_t stream);
 hipError_t launch_pages_fork(const PagesArgs& a, hipStream_t stream);

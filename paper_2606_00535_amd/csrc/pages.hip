@@ -223,6 +223,14 @@ __global__ __launch_bounds__(kCopyThreads) void fork_copy_kernel(PagesArgs a) {
     *(u32x4*)(a.k + dst + x) = k;
     *(u32x4*)(a.v + dst + x) = v;
   }
+  if (a.scales.k && blockIdx.y == 0) {   // pages of 8 bits: the blocks' scales
+    const int64_t first = layer * a.scales.layer_stride + (((int64_t)g << a.page_shift) / kScaleBlock);
+    const int64_t from_s = first + (int64_t)p * a.scales.page_stride, to_s = first + (int64_t)q * a.scales.page_stride;
+    for (int x = threadIdx.x; x < (tail + kScaleBlock - 1) / kScaleBlock; x += kCopyThreads) {
+      a.scales.k[to_s + x] = a.scales.k[from_s + x];
+      a.scales.v[to_s + x] = a.scales.v[from_s + x];
+    }
+  }
 }
 
 constexpr int kReleaseThreads = 256;

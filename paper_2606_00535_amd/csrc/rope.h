@@ -1,0 +1,113 @@
+// Rotary positions: the angle of a row's pairs, and units of 8 pairs of a row in registers.
+#pragma once
+
+#include "kernels.h"
+
+namespace dreams {
+namespace {
+
+// cos and sin of position * freq radians, times gain.  The angle is reduced in fp64 to a quarter turn (its error grows
+// with the turns, 2^-52 of them), the rest r, |r| <= 1/2 quarter turn, goes through the Taylor polynomials of sine
+// and cosine about 0: the first terms left out are x^11/11! < 2e-9 and x^12/12! < 2e-10 at x = pi/4, below half an ulp of fp32.
+__device__ __forceinline__ void turn(double position, double freq, float gain, float* c, float* s) {
+  const double t = position * (freq * 0.15915494309189533577);
+  const double u = 4.0 * (t - rint(t)), quarter = rint(u);
+  const float x = (float)(u - quarter) * 1.5707963267948966f, y = x * x;
+  const float sn = x * fmaf(y, fmaf(y, fmaf(y, fmaf(y, 1.0f / 362880, -1.0f / 5040), 1.0f / 120), -1.0f / 6), 1.0f);
+  const float cs = fmaf(y, fmaf(y, fmaf(y, fmaf(y, fmaf(y, -1.0f / 3628800, 1.0f / 40320), -1.0f / 720), 1.0f / 24), -0.5f), 1.0f);
+  const int q = (int)quarter;
+  const float a = (q & 1) ? sn : cs, b = (q & 1) ? cs : sn;
+  *c = gain * ((q + 1) & 2 ? -a : a);
+  *s = gain * (q & 2 ? -b : b);
+}
+
+// Depth of tree node i by parents in LDS (an entry that breaks the rules ends the walk).
+__device__ __forceinline__ int depth_of(const int* parent, int i) {
+  int d = 0;
+  for (int j = i;; ++d) {
+    const int p = parent[j];
+    if (p < 0 || p >= j) return d;
+    j = p;
+  }
+}
+
+// 8 columns of a row from column `at` on, as they are in memory, and as fp32.
+template <typename T>
+struct Run {
+  typedef uint32_t words __attribute__((ext_vector_type(4)));
+  typedef T tx8 __attribute__((ext_vector_type(8)));
+  words w[sizeof(T) / 2];
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (auto& x : w) x = words{0u, 0u, 0u, 0u};
+  }
+  __device__ __forceinline__ void load(const char* row, int at) {
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(T) / 2); ++i) w[i] = ((const words*)(row + at * sizeof(T)))[i];
+  }
+  __device__ __forceinline__ void store(char* row, int at) const {
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(T) / 2); ++i) ((words*)(row + at * sizeof(T)))[i] = w[i];
+  }
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t u = sizeof(T) == 2 ? w[0][i / 2] : w[i / 4][i % 4];   // (a bit cast of the element itself takes element 0)
+      x[i] = __builtin_bit_cast(float, sizeof(T) == 4 ? u : i & 1 ? u & 0xffff0000u : u << 16);
+    }
+  }
+  __device__ __forceinline__ void set(const float (&x)[8]) {
+    tx8 y;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = (T)x[i];
+    __builtin_memcpy(&w, &y, sizeof(y));
+  }
+};
+
+// Unit p of a row: where its 16 columns are (two runs of 8), and whether it is rotated.  The columns past R come 16 at a time;
+// the last unit may have 8 (second run: -1).
+struct Unit {
+  int first, second;
+  bool rotated;
+};
+__device__ __forceinline__ Unit unit_of(int p, int R, int D, bool interleaved) {
+  Unit u;
+  u.rotated = p < R / 16;
+  const int at = 16 * p;
+  if (u.rotated && !interleaved) {
+    u.first = 8 * p;
+    u.second = R / 2 + 8 * p;
+  } else {
+    u.first = at;
+    u.second = at + 16 <= D ? at + 8 : -1;
+  }
+  return u;
+}
+// a unit's 16 columns (a: the first run, b: the second), turned by its 8 pairs' cosines and sines
+__device__ __forceinline__ void rotate(float (&a)[8], float (&b)[8], const float (&c)[8], const float (&s)[8],
+                                       bool interleaved) {
+  if (interleaved) {
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+      float x = a[i], y = a[i + 1];
+      a[i] = fmaf(x, c[i / 2], -(y * s[i / 2]));
+      a[i + 1] = fmaf(y, c[i / 2], x * s[i / 2]);
+      x = b[i];
+      y = b[i + 1];
+      b[i] = fmaf(x, c[4 + i / 2], -(y * s[4 + i / 2]));
+      b[i + 1] = fmaf(y, c[4 + i / 2], x * s[4 + i / 2]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float x = a[i], y = b[i];
+      a[i] = fmaf(x, c[i], -(y * s[i]));
+      b[i] = fmaf(y, c[i], x * s[i]);
+    }
+  }
+}
+
+__host__ __device__ inline int rope_units(int R, int D) { return R / 16 + (D - R + 15) / 16; }
+
+}  // namespace
+}  // namespace dreams

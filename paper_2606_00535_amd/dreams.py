@@ -18,7 +18,7 @@ LIBRARY = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libdreams.so
 
 DREAMS_OK, DREAMS_ERR_INVALID_ARG, DREAMS_ERR_UNSUPPORTED, DREAMS_ERR_WORKSPACE, DREAMS_ERR_HIP = 0, -1, -2, -3, -4
 DREAMS_ERR_DEVICE = -5
-DREAMS_F32, DREAMS_BF16 = 0, 1
+DREAMS_F32, DREAMS_BF16, DREAMS_E4M3 = 0, 1, 2
 
 # every symbol include/dreams.h declares
 EXPORTS = (
@@ -33,7 +33,8 @@ EXPORTS = (
     "dreams_prefill_visual_importance", "dreams_prefill_visual_importance_workspace_size",
     "dreams_paged_verify_attn", "dreams_paged_verify_attn_workspace_size", "dreams_paged_prompt_attn",
     "dreams_paged_prompt_attn_workspace_size", "dreams_paged_append", "dreams_paged_kv_commit", "dreams_pages_reserve",
-    "dreams_pages_fork", "dreams_pages_release",
+    "dreams_pages_fork", "dreams_pages_release", "dreams_rope_frequencies", "dreams_rope", "dreams_paged_append_rope",
+    "dreams_paged_append_e4m3", "dreams_paged_kv_commit_e4m3", "dreams_paged_read_e4m3", "dreams_pages_fork_e4m3",
 )
 
 
@@ -66,6 +67,21 @@ class PagePool(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("num_layers", "batch", "num_kv_heads", "head_dim", "num_pages", "page_size",
                                               "table_width")]
     _fields_ += [("dtype", ctypes.c_int), ("layer_stride", ctypes.c_int64), ("page_stride", ctypes.c_int64)]
+
+
+class Rope(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("frequencies", ctypes.c_void_p),
+                ("positions", ctypes.c_void_p), ("parent", ctypes.c_void_p), ("amplitude", ctypes.c_float)]
+
+
+class RopeQueries(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("out", ctypes.c_void_p), ("num_q_heads", ctypes.c_int32),
+                ("strides", ctypes.c_int64 * 3)]
+
+
+class PageScales(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("layer_stride", ctypes.c_int64),
+                ("page_stride", ctypes.c_int64)]
 
 
 _lib = None
@@ -130,6 +146,15 @@ def lib():
                 L.dreams_pages_reserve.argtypes = [PP, P, P, P, P, P, P]
                 L.dreams_pages_fork.argtypes = [PP, P, P, P, P, P, P, I32, P, P, P, P]
                 L.dreams_pages_release.argtypes = [PP, P, P, P, P, I32, P, I32, P]
+                RP, QP, SP, I64P = (ctypes.POINTER(t) for t in (Rope, RopeQueries, PageScales, ctypes.c_int64))
+                F64 = ctypes.c_double
+                L.dreams_rope_frequencies.argtypes = [I32, F64, ctypes.c_int, F64, F64, F64, F64, P]
+                L.dreams_rope.argtypes = [RP, I32, I32, I32, I32, ctypes.c_int, P, I64P, P, P, I64P, P]
+                L.dreams_paged_append_rope.argtypes = [PP, RP, QP, P, P, I32, I64P, P, P, P, P, P, P]
+                L.dreams_paged_append_e4m3.argtypes = [PP, SP, RP, QP, ctypes.c_int, P, P, I32, I64P, P, P, P, P, P, P]
+                L.dreams_paged_kv_commit_e4m3.argtypes = [PP, SP, P, P, P, P, P, P, I32, P, P]
+                L.dreams_paged_read_e4m3.argtypes = [PP, SP, P, P, P, P, I32, P, P, P]
+                L.dreams_pages_fork_e4m3.argtypes = [PP, SP, P, P, P, P, P, P, I32, P, P, P, P]
                 for f in ("dreams_tree_verify_attn_workspace_size", "dreams_tree_verify_attn",
                           "dreams_tree_accept_workspace_size", "dreams_tree_accept", "dreams_kv_commit",
                           "dreams_check_tree_host", "dreams_stream_read", "dreams_tree_verify_attn_entropy",
@@ -797,12 +822,12 @@ def _new(t: torch.Tensor, stream, shape=None, dtype=None) -> torch.Tensor:
         return _new(t, None, shape, dtype)
 
 
-def _code(dtype) -> int:
+def _code(dtype, what: str = "pages") -> int:
     if dtype is torch.bfloat16:
         return DREAMS_BF16
     if dtype is torch.float32:
         return DREAMS_F32
-    raise TypeError("pages must be bfloat16 or float32")
+    raise TypeError("%s must be bfloat16 or float32" % what)
 
 
 def _current(t: torch.Tensor, name: str, dtype=None) -> int:
@@ -856,14 +881,15 @@ def _page_strides(k_pages: torch.Tensor, v_pages: torch.Tensor):
     return shape, st[0] if n == 5 and shape[0] > 1 else 0, st[-4] if P > 1 else H * S * D
 
 
-def _pool(k_pages, v_pages, page_table):
+def _pool(k_pages, v_pages, page_table, code=None):
     """(PagePool, device index)"""
     shape, layer, page = _page_strides(k_pages, v_pages)
     at = _current(k_pages, "k_pages")
     _need_on(page_table, "page_table", torch.int32, at, None, 2)
     P, H, S, D = shape[-4:]
     B, width = page_table.shape
-    return PagePool(shape[0] if len(shape) == 5 else 1, B, H, D, P, S, width, _code(k_pages.dtype), layer, page), at
+    return PagePool(shape[0] if len(shape) == 5 else 1, B, H, D, P, S, width,
+                    _code(k_pages.dtype) if code is None else code, layer, page), at
 
 
 def _table_pool(page_table, page_count, refcount, page_size):
@@ -1024,14 +1050,9 @@ def paged_prompt_attn(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Ten
 _Strides = ctypes.c_int64 * 4
 
 
-def paged_append(k_new: torch.Tensor, v_new: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,
-                 page_table: torch.Tensor, kv_len: torch.Tensor, row_len: Optional[torch.Tensor] = None,
-                 stream=None) -> None:
-    """dreams_paged_append, in place on k_pages / v_pages [NL,num_pages,Hkv,page_size,D] (or one layer's, without NL):
-    rows of k_new / v_new [NL,B,Hkv,N,D] (or without NL), of any strides with dense rows (a transposed view of a
-    projection's [B,N,Hkv,D] serves), go to the slots kv_len[b] .. of every sequence; row_len [B] int32 of them (None: N)."""
-    pool, at = _pool(k_pages, v_pages, page_table)
-    dt, B, n = k_pages.dtype, pool.batch, k_pages.dim()
+def _new_rows(k_new, v_new, k_pages, pool, at, dt, kv_len, row_len):
+    """The strides of new rows of type dt, once they and their lengths are checked against the pool."""
+    B, n = pool.batch, k_pages.dim()
     for t, name in ((k_new, "k_new"), (v_new, "v_new")):
         if not isinstance(t, torch.Tensor):
             raise TypeError("%s must be a torch.Tensor" % name)
@@ -1050,10 +1071,33 @@ def paged_append(k_new: torch.Tensor, v_new: torch.Tensor, k_pages: torch.Tensor
     _need_on(kv_len, "kv_len", torch.int32, at, (B,))
     if row_len is not None:
         _need_on(row_len, "row_len", torch.int32, at, (B,))
-    strides = _Strides(*(st[:4] if n == 5 else (0,) + st[:3]))
-    _check(lib().dreams_paged_append(ctypes.byref(pool), k_new.data_ptr(), v_new.data_ptr(), shape[-2], strides,
+    return _Strides(*(st[:4] if n == 5 else (0,) + st[:3]))
+
+
+def paged_append(k_new: torch.Tensor, v_new: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,
+                 page_table: torch.Tensor, kv_len: torch.Tensor, row_len: Optional[torch.Tensor] = None,
+                 stream=None) -> None:
+    """dreams_paged_append, in place on k_pages / v_pages [NL,num_pages,Hkv,page_size,D] (or one layer's, without NL):
+    rows of k_new / v_new [NL,B,Hkv,N,D] (or without NL), of any strides with dense rows (a transposed view of a
+    projection's [B,N,Hkv,D] serves), go to the slots kv_len[b] .. of every sequence; row_len [B] int32 of them (None: N)."""
+    pool, at = _pool(k_pages, v_pages, page_table)
+    strides = _new_rows(k_new, v_new, k_pages, pool, at, k_pages.dtype, kv_len, row_len)
+    _check(lib().dreams_paged_append(ctypes.byref(pool), k_new.data_ptr(), v_new.data_ptr(), k_new.shape[-2], strides,
                                      page_table.data_ptr(), kv_len.data_ptr(), _ptr(row_len), k_pages.data_ptr(),
                                      v_pages.data_ptr(), _stream_on(stream, at)))
+
+
+def _commit_lengths(B, at, kv_len_in, accept_path, accept_len, kv_len_out, stream):
+    """kv_len_out, the caller's or a new one, once the lengths and the path are checked."""
+    _need_on(kv_len_in, "kv_len_in", torch.int32, at, (B,))
+    _need_on(accept_path, "accept_path", torch.int32, at, None, 2)
+    if accept_path.shape[0] != B:
+        raise ValueError("accept_path must have page_table's batch size")
+    _need_on(accept_len, "accept_len", torch.int32, at, (B,))
+    if kv_len_out is None:
+        return _new(kv_len_in, stream)
+    _need_on(kv_len_out, "kv_len_out", torch.int32, at, (B,))
+    return kv_len_out
 
 
 def paged_kv_commit(k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor, kv_len_in: torch.Tensor,
@@ -1062,16 +1106,7 @@ def paged_kv_commit(k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: to
     """dreams_paged_kv_commit, in place on k_pages / v_pages [NL,num_pages,Hkv,page_size,D] (or one layer's).  Returns
     kv_len_out [B] int32."""
     pool, at = _pool(k_pages, v_pages, page_table)
-    B = pool.batch
-    _need_on(kv_len_in, "kv_len_in", torch.int32, at, (B,))
-    _need_on(accept_path, "accept_path", torch.int32, at, None, 2)
-    if accept_path.shape[0] != B:
-        raise ValueError("accept_path must have page_table's batch size")
-    _need_on(accept_len, "accept_len", torch.int32, at, (B,))
-    if kv_len_out is None:
-        kv_len_out = _new(kv_len_in, stream)
-    else:
-        _need_on(kv_len_out, "kv_len_out", torch.int32, at, (B,))
+    kv_len_out = _commit_lengths(pool.batch, at, kv_len_in, accept_path, accept_len, kv_len_out, stream)
     _check(lib().dreams_paged_kv_commit(ctypes.byref(pool), k_pages.data_ptr(), v_pages.data_ptr(),
                                         page_table.data_ptr(), kv_len_in.data_ptr(), accept_path.data_ptr(),
                                         accept_len.data_ptr(), accept_path.shape[1],
@@ -1095,12 +1130,7 @@ def pages_reserve(page_table: torch.Tensor, page_count: torch.Tensor, refcount: 
     return granted
 
 
-def pages_fork(k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor, page_count: torch.Tensor,
-               kv_len: torch.Tensor, refcount: torch.Tensor, src: torch.Tensor, dst: torch.Tensor,
-               granted: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
-    """dreams_pages_fork, in place: sequence dst[i] (without pages) becomes a copy of sequence src[i]; whole pages are
-    shared, the rows of a partly filled one copied in every layer.  Returns granted [n] int32 (1 or 0)."""
-    pool, at = _pool(k_pages, v_pages, page_table)
+def _fork(call, head, pool, at, k_pages, v_pages, page_table, page_count, kv_len, refcount, src, dst, granted, stream):
     B = pool.batch
     _need_on(page_count, "page_count", torch.int32, at, (B,))
     _need_on(kv_len, "kv_len", torch.int32, at, (B,))
@@ -1112,13 +1142,23 @@ def pages_fork(k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.T
         granted = _new(src, stream)
     else:
         _need_on(granted, "granted", torch.int32, at, (n,))
-    _check(lib().dreams_pages_fork(ctypes.byref(pool), k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(),
-                                   page_count.data_ptr(), kv_len.data_ptr(), refcount.data_ptr(), n, src.data_ptr(),
-                                   dst.data_ptr(), granted.data_ptr(), _stream_on(stream, at)))
+    _check(call(*head, k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(), page_count.data_ptr(),
+                kv_len.data_ptr(), refcount.data_ptr(), n, src.data_ptr(), dst.data_ptr(), granted.data_ptr(),
+                _stream_on(stream, at)))
     if B == 0:      # (no sequence to copy: the library has not written granted)
         with torch.cuda.stream(stream):
             granted.zero_()
     return granted
+
+
+def pages_fork(k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor, page_count: torch.Tensor,
+               kv_len: torch.Tensor, refcount: torch.Tensor, src: torch.Tensor, dst: torch.Tensor,
+               granted: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """dreams_pages_fork, in place: sequence dst[i] (without pages) becomes a copy of sequence src[i]; whole pages are
+    shared, the rows of a partly filled one copied in every layer.  Returns granted [n] int32 (1 or 0)."""
+    pool, at = _pool(k_pages, v_pages, page_table)
+    return _fork(lib().dreams_pages_fork, (ctypes.byref(pool),), pool, at, k_pages, v_pages, page_table, page_count, kv_len,
+                 refcount, src, dst, granted, stream)
 
 
 def pages_release(page_table: torch.Tensor, page_count: torch.Tensor, kv_len: torch.Tensor, refcount: torch.Tensor,
@@ -1131,3 +1171,215 @@ def pages_release(page_table: torch.Tensor, page_count: torch.Tensor, kv_len: to
     _check(lib().dreams_pages_release(ctypes.byref(pool), page_table.data_ptr(), page_count.data_ptr(),
                                       kv_len.data_ptr(), refcount.data_ptr(), seqs.shape[0], seqs.data_ptr(),
                                       1 if trim else 0, _stream_on(stream, at)))
+
+
+# ------------------------------------------------------------------------------------------- rotary positions
+ROPE_SCALINGS = {None: 0, "linear": 1, "parts": 2}
+_Strides3 = ctypes.c_int64 * 3
+
+
+def rope_frequencies(rotary_dim: int, base: float = 10000.0, scaling: Optional[str] = None, factor: float = 1.0,
+                     trained_len: float = 0.0, low: float = 1.0, high: float = 32.0, device=None) -> torch.Tensor:
+    """dreams_rope_frequencies: radians a position of every pair, [rotary_dim / 2] float64 on `device` (None: the current
+    one).  scaling: None, "linear" (all slowed by `factor`) or "parts" (those that make fewer than `low` turns within
+    trained_len positions slowed by it, those that make more than `high` kept, in between in part)."""
+    if scaling not in ROPE_SCALINGS:
+        raise ValueError("scaling must be one of None, 'linear', 'parts'")
+    if not 1 < rotary_dim < 2 ** 31:
+        raise ValueError("rotary_dim must be even and >= 2")
+    f = torch.empty(rotary_dim // 2, dtype=torch.float64)
+    _check(lib().dreams_rope_frequencies(rotary_dim, base, ROPE_SCALINGS[scaling], factor, trained_len, low, high,
+                                         f.data_ptr()))
+    return f.to(torch.device("cuda") if device is None else device)
+
+
+def _rope(frequencies, positions, parent, shape, at, interleaved, amplitude) -> Rope:
+    """The rotation of rows [B, N], checked."""
+    _need_on(frequencies, "frequencies", torch.float64, at, None, 1)
+    if positions is not None:
+        _need_on(positions, "positions", torch.int32, at, shape)
+    if parent is not None:
+        _need_on(parent, "parent", torch.int32, at, shape)
+    return Rope(2 * frequencies.shape[0], 1 if interleaved else 0, frequencies.data_ptr(), _ptr(positions), _ptr(parent),
+                amplitude)
+
+
+def rope(x: torch.Tensor, frequencies: torch.Tensor, kv_len: Optional[torch.Tensor] = None,
+         positions: Optional[torch.Tensor] = None, parent: Optional[torch.Tensor] = None, interleaved: bool = False,
+         amplitude: float = 1.0, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """dreams_rope.  x [B,H,N,D] bf16 or fp32 of any strides with dense rows (a transposed view of a projection's [B,N,H,D]
+    serves); frequencies [R/2] float64 (rope_frequencies, or any others) for its first R columns; the rows' positions are
+    positions [B,N] int32, or kv_len[b] ([B] int32) plus the depth by parent [B,N] int32, or plus 0, 1, ...  out: like x
+    (None: a dense [B,H,N,D]; x itself: in place).  Returns out."""
+    at = _current(x, "x")
+    code = _code(x.dtype, "x")
+    if x.dim() != 4:
+        raise ValueError("x must have 4 dimensions")
+    B, H, N, D = shape = x.shape
+    if D > 1 and x.stride(3) != 1:
+        raise ValueError("the rows of x must be dense")
+    r = _rope(frequencies, positions, parent, (B, N), at, interleaved, amplitude)
+    if kv_len is not None:
+        _need_on(kv_len, "kv_len", torch.int32, at, (B,))
+    if out is None:
+        out = _new(x, stream, shape, x.dtype)
+    else:
+        if not isinstance(out, torch.Tensor):
+            raise TypeError("out must be a torch.Tensor")
+        if out.dtype is not x.dtype or out.get_device() != at or out.shape != shape or (D > 1 and out.stride(3) != 1):
+            raise ValueError("out must be like x, with dense rows")
+    _check(lib().dreams_rope(ctypes.byref(r), B, H, N, D, code, x.data_ptr(), _Strides3(*x.stride()[:3]), _ptr(kv_len),
+                             out.data_ptr(), _Strides3(*out.stride()[:3]), _stream_on(stream, at)))
+    return out
+
+
+def _queries(q, q_out, like, batch, rows, head_dim, at, stream):
+    """(RopeQueries or None, its output)"""
+    if q is None:
+        if q_out is not None:
+            raise ValueError("q_out needs q")
+        return None, None
+    if not isinstance(q, torch.Tensor):
+        raise TypeError("q must be a torch.Tensor")
+    if q.dtype is not like.dtype:
+        raise TypeError("q must be %s, got %s" % (like.dtype, q.dtype))
+    if q.get_device() != at:
+        raise ValueError("q is on %s, expected %s" % (q.device, like.device))
+    if q.dim() != 4 or q.shape[0] != batch or q.shape[2:] != (rows, head_dim):
+        raise ValueError("q must be [B,Hq,N,D] for the new rows")
+    if head_dim > 1 and q.stride(3) != 1:
+        raise ValueError("the rows of q must be dense")
+    if q_out is None:
+        q_out = _new(q, stream, q.shape, q.dtype)
+    else:
+        _need_on(q_out, "q_out", q.dtype, at, q.shape)
+    return RopeQueries(q.data_ptr(), q_out.data_ptr(), q.shape[1], _Strides3(*q.stride()[:3])), q_out
+
+
+def paged_append_rope(k_new: torch.Tensor, v_new: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,
+                      page_table: torch.Tensor, kv_len: torch.Tensor, frequencies: torch.Tensor,
+                      row_len: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None,
+                      positions: Optional[torch.Tensor] = None, parent: Optional[torch.Tensor] = None,
+                      interleaved: bool = False, amplitude: float = 1.0, q_out: Optional[torch.Tensor] = None,
+                      stream=None) -> Optional[torch.Tensor]:
+    """dreams_paged_append_rope: paged_append with the keys rotated (as in rope, from kv_len on) on their way, and, in the
+    same launch, the rows' queries q [B,Hq,N,D] (any strides with dense rows; one layer's rows only).  Returns the rotated
+    queries, dense [B,Hq,N,D] (0 in rows from row_len on), or None."""
+    pool, at = _pool(k_pages, v_pages, page_table)
+    strides = _new_rows(k_new, v_new, k_pages, pool, at, k_pages.dtype, kv_len, row_len)
+    B, N = pool.batch, k_new.shape[-2]
+    r = _rope(frequencies, positions, parent, (B, N), at, interleaved, amplitude)
+    queries, q_out = _queries(q, q_out, k_new, B, N, pool.head_dim, at, stream)
+    _check(lib().dreams_paged_append_rope(ctypes.byref(pool), ctypes.byref(r),
+                                          None if queries is None else ctypes.byref(queries), k_new.data_ptr(),
+                                          v_new.data_ptr(), N, strides, page_table.data_ptr(), kv_len.data_ptr(),
+                                          _ptr(row_len), k_pages.data_ptr(), v_pages.data_ptr(), _stream_on(stream, at)))
+    return q_out
+
+
+# --------------------------------------------------------------------------------------------- pages of 8 bits
+def _scale_strides(k_scales, v_scales, shape, at):
+    """(layer stride, page stride) of the scales [NL, P, Hkv, page_size / 16] of pages of this shape."""
+    want = shape[:-2] + (shape[-2] // 16,)
+    for t, name in ((k_scales, "k_scales"), (v_scales, "v_scales")):
+        if not isinstance(t, torch.Tensor):
+            raise TypeError("%s must be a torch.Tensor" % name)
+        if t.dtype is not torch.float8_e8m0fnu:
+            raise TypeError("%s must be torch.float8_e8m0fnu, got %s" % (name, t.dtype))
+        if t.get_device() != at:
+            raise ValueError("%s is on %s, not with the pages" % (name, t.device))
+        if t.shape != want:
+            raise ValueError("%s must be %s, got %s" % (name, list(want), list(t.shape)))
+    n, st, vst = len(want), k_scales.stride(), v_scales.stride()
+    if any(want[i] > 1 and st[i] != vst[i] for i in range(n)):
+        raise ValueError("k_scales and v_scales differ in layout")
+    P, H, S = want[-3:]
+    if (S > 1 and st[-1] != 1) or (H > 1 and st[-2] != S):
+        raise ValueError("a page's scales must be dense [Hkv, page_size / 16]")
+    if (P > 1 and st[-3] == 0) or (n == 4 and want[0] > 1 and st[0] == 0):
+        raise ValueError("scales of pages or layers share memory (expanded views)")
+    return st[0] if n == 4 and want[0] > 1 else 0, st[-3] if P > 1 else H * S
+
+
+def _pool8(k_pages, v_pages, k_scales, v_scales, page_table):
+    """(PagePool, PageScales, device index) of pages of 8 bits"""
+    if isinstance(k_pages, torch.Tensor) and k_pages.dtype is not torch.float8_e4m3fn:
+        raise TypeError("k_pages must be torch.float8_e4m3fn, got %s" % k_pages.dtype)
+    pool, at = _pool(k_pages, v_pages, page_table, DREAMS_E4M3)
+    layer, page = _scale_strides(k_scales, v_scales, k_pages.shape, at)
+    return pool, PageScales(k_scales.data_ptr(), v_scales.data_ptr(), layer, page), at
+
+
+def paged_append_e4m3(k_new: torch.Tensor, v_new: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,
+                      k_scales: torch.Tensor, v_scales: torch.Tensor, page_table: torch.Tensor, kv_len: torch.Tensor,
+                      row_len: Optional[torch.Tensor] = None, frequencies: Optional[torch.Tensor] = None,
+                      q: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+                      parent: Optional[torch.Tensor] = None, interleaved: bool = False, amplitude: float = 1.0,
+                      q_out: Optional[torch.Tensor] = None, stream=None) -> Optional[torch.Tensor]:
+    """dreams_paged_append_e4m3, in place on k_pages / v_pages [NL,num_pages,Hkv,page_size,D] float8_e4m3fn and k_scales /
+    v_scales [NL,num_pages,Hkv,page_size/16] float8_e8m0fnu (or one layer's): new rows, bf16 or fp32, as in paged_append;
+    with frequencies, keys and queries are rotated as in paged_append_rope.  A block of 16 slots takes the least power of
+    two that holds its rows.  Returns the rotated queries or None."""
+    pool, scales, at = _pool8(k_pages, v_pages, k_scales, v_scales, page_table)
+    code = _code(k_new.dtype if isinstance(k_new, torch.Tensor) else None, "new rows")
+    strides = _new_rows(k_new, v_new, k_pages, pool, at, k_new.dtype, kv_len, row_len)
+    B, N = pool.batch, k_new.shape[-2]
+    if frequencies is None:
+        if q is not None or positions is not None or parent is not None:
+            raise ValueError("q, positions and parent need frequencies")
+        r = None
+    else:
+        r = _rope(frequencies, positions, parent, (B, N), at, interleaved, amplitude)
+    queries, q_out = _queries(q, q_out, k_new, B, N, pool.head_dim, at, stream)
+    _check(lib().dreams_paged_append_e4m3(ctypes.byref(pool), ctypes.byref(scales), None if r is None else ctypes.byref(r),
+                                          None if queries is None else ctypes.byref(queries), code, k_new.data_ptr(),
+                                          v_new.data_ptr(), N, strides, page_table.data_ptr(), kv_len.data_ptr(),
+                                          _ptr(row_len), k_pages.data_ptr(), v_pages.data_ptr(), _stream_on(stream, at)))
+    return q_out
+
+
+def paged_kv_commit_e4m3(k_pages: torch.Tensor, v_pages: torch.Tensor, k_scales: torch.Tensor, v_scales: torch.Tensor,
+                         page_table: torch.Tensor, kv_len_in: torch.Tensor, accept_path: torch.Tensor,
+                         accept_len: torch.Tensor, kv_len_out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """dreams_paged_kv_commit_e4m3, in place on pages and scales (as paged_append_e4m3).  Returns kv_len_out [B] int32."""
+    pool, scales, at = _pool8(k_pages, v_pages, k_scales, v_scales, page_table)
+    kv_len_out = _commit_lengths(pool.batch, at, kv_len_in, accept_path, accept_len, kv_len_out, stream)
+    _check(lib().dreams_paged_kv_commit_e4m3(ctypes.byref(pool), ctypes.byref(scales), k_pages.data_ptr(),
+                                             v_pages.data_ptr(), page_table.data_ptr(), kv_len_in.data_ptr(),
+                                             accept_path.data_ptr(), accept_len.data_ptr(), accept_path.shape[1],
+                                             kv_len_out.data_ptr(), _stream_on(stream, at)))
+    return kv_len_out
+
+
+def paged_read_e4m3(k_pages: torch.Tensor, v_pages: torch.Tensor, k_scales: torch.Tensor, v_scales: torch.Tensor,
+                    page_table: torch.Tensor, kv_len: torch.Tensor, num_slots: int, k_out: Optional[torch.Tensor] = None,
+                    v_out: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """dreams_paged_read_e4m3: the first num_slots slots of every sequence as values, (k_out, v_out) bfloat16
+    [NL,B,Hkv,num_slots,D] (without NL for one layer's pages), 0 from kv_len[b] on."""
+    pool, scales, at = _pool8(k_pages, v_pages, k_scales, v_scales, page_table)
+    _need_on(kv_len, "kv_len", torch.int32, at, (pool.batch,))
+    if not -1 < num_slots < 2 ** 31:
+        raise ValueError("num_slots must be in [0, 2^31)")
+    shape = torch.Size(k_pages.shape[:-4] + (pool.batch, pool.num_kv_heads, num_slots, pool.head_dim))
+    outs = []
+    for t, name in ((k_out, "k_out"), (v_out, "v_out")):
+        if t is None:
+            t = _new(kv_len, stream, shape, torch.bfloat16)
+        else:
+            _need_on(t, name, torch.bfloat16, at, shape)
+        outs.append(t)
+    _check(lib().dreams_paged_read_e4m3(ctypes.byref(pool), ctypes.byref(scales), k_pages.data_ptr(), v_pages.data_ptr(),
+                                        page_table.data_ptr(), kv_len.data_ptr(), num_slots, outs[0].data_ptr(),
+                                        outs[1].data_ptr(), _stream_on(stream, at)))
+    return outs[0], outs[1]
+
+
+def pages_fork_e4m3(k_pages: torch.Tensor, v_pages: torch.Tensor, k_scales: torch.Tensor, v_scales: torch.Tensor,
+                    page_table: torch.Tensor, page_count: torch.Tensor, kv_len: torch.Tensor, refcount: torch.Tensor,
+                    src: torch.Tensor, dst: torch.Tensor, granted: Optional[torch.Tensor] = None,
+                    stream=None) -> torch.Tensor:
+    """dreams_pages_fork_e4m3: pages_fork over pages of 8 bits, whose scales go with the copied rows."""
+    pool, scales, at = _pool8(k_pages, v_pages, k_scales, v_scales, page_table)
+    call, L = (ctypes.byref(pool), ctypes.byref(scales)), lib()
+    return _fork(L.dreams_pages_fork_e4m3, call, pool, at, k_pages, v_pages, page_table, page_count, kv_len, refcount, src,
+                 dst, granted, stream)
