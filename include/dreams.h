@@ -743,6 +743,28 @@ dreams_status_t dreams_paged_read_e4m3(const dreams_page_pool_t* pool, const dre
                                        const int32_t* kv_len, int32_t num_slots, void* k_out, void* v_out,
                                        hipStream_t stream);
 
+/*
+ * dreams_paged_verify_attn_e4m3, dreams_paged_prompt_attn_e4m3 -- dreams_paged_verify_attn and dreams_paged_prompt_attn over
+ * pages of 8 bits: attention of bf16 queries over the values that the codes stand for (exact in bf16; those below its normal
+ * range may be flushed), with the same arithmetic, masks, windows, and rules for slots out of sight.
+ *   desc->dtype        type of q and out, DREAMS_BF16 (DREAMS_F32: DREAMS_ERR_UNSUPPORTED)
+ *   desc->page_stride  codes (bytes) from a page to the next
+ *   scales             of this layer (layer_stride is not read)
+ * The workspace is of the matching size query; splits may differ from those over bf16 pages.
+ */
+dreams_status_t dreams_paged_verify_attn_e4m3_workspace_size(const dreams_paged_desc_t* desc, size_t* bytes);
+dreams_status_t dreams_paged_prompt_attn_e4m3_workspace_size(const dreams_paged_desc_t* desc, size_t* bytes);
+dreams_status_t dreams_paged_verify_attn_e4m3(const dreams_paged_desc_t* desc, const void* q, const void* k_pages,
+                                              const void* v_pages, const dreams_page_scales_t* scales,
+                                              const int32_t* page_table, const int32_t* kv_len, const int32_t* parent,
+                                              const uint64_t* tree_mask, void* out, float* lse, void* workspace,
+                                              size_t workspace_bytes, hipStream_t stream);
+dreams_status_t dreams_paged_prompt_attn_e4m3(const dreams_paged_desc_t* desc, const void* q, const void* k_pages,
+                                              const void* v_pages, const dreams_page_scales_t* scales,
+                                              const int32_t* page_table, const int32_t* kv_len, const int32_t* row_len,
+                                              void* out, float* lse, void* workspace, size_t workspace_bytes,
+                                              hipStream_t stream);
+
 /* dreams_pages_fork_e4m3 -- dreams_pages_fork over pages of 8 bits: the copied rows' scales go with them. */
 dreams_status_t dreams_pages_fork_e4m3(const dreams_page_pool_t* pool, const dreams_page_scales_t* scales, void* k_pages,
                                        void* v_pages, int32_t* page_table, int32_t* page_count, int32_t* kv_len,

@@ -1197,7 +1197,7 @@ dreams_status_t check_page_stride(int64_t stride, int64_t page_elems, int elem, 
   return DREAMS_OK;
 }
 
-dreams_status_t check_paged_desc(const dreams_paged_desc_t* d, bool prompt) {
+dreams_status_t check_paged_desc(const dreams_paged_desc_t* d, bool prompt, bool e4m3) {
   if (!d) return fail(DREAMS_ERR_INVALID_ARG, "desc is NULL");
   if (d->batch < 0) return fail(DREAMS_ERR_INVALID_ARG, "batch = %d < 0", d->batch);
   if (d->num_q_heads < 1 || d->num_kv_heads < 1 || d->num_q_heads % d->num_kv_heads != 0)
@@ -1205,6 +1205,8 @@ dreams_status_t check_paged_desc(const dreams_paged_desc_t* d, bool prompt) {
                 d->num_q_heads, d->num_kv_heads);
   if (d->dtype != DREAMS_BF16 && d->dtype != DREAMS_F32)
     return fail(DREAMS_ERR_INVALID_ARG, "dtype = %d is not DREAMS_BF16 or DREAMS_F32", (int)d->dtype);
+  if (e4m3 && d->dtype != DREAMS_BF16)
+    return fail(DREAMS_ERR_UNSUPPORTED, "pages of 8 bits serve queries of DREAMS_BF16, dtype = %d", (int)d->dtype);
   if (d->head_dim != 64 && d->head_dim != 128)
     return fail(DREAMS_ERR_UNSUPPORTED, "head_dim = %d (supported: 64, 128)", d->head_dim);
   dreams_status_t st = check_pages(d->num_pages, d->page_size, d->table_width);
@@ -1222,7 +1224,7 @@ dreams_status_t check_paged_desc(const dreams_paged_desc_t* d, bool prompt) {
     return fail(DREAMS_ERR_INVALID_ARG, "window = %d and sinks = %d must be >= 0", d->window, d->sinks);
   if (!isfinite(d->scale)) return fail(DREAMS_ERR_INVALID_ARG, "scale is not finite");
   const int64_t page = (int64_t)d->num_kv_heads * d->page_size * d->head_dim;
-  st = check_page_stride(d->page_stride, page, d->dtype == DREAMS_BF16 ? 2 : 4, d->num_pages);
+  st = check_page_stride(d->page_stride, page, e4m3 ? 1 : d->dtype == DREAMS_BF16 ? 2 : 4, d->num_pages);
   if (st != DREAMS_OK) return st;
   const long long rows = (long long)d->batch * d->num_q_heads;
   if (rows > 0x7fffffffLL / d->num_rows ||
@@ -1246,9 +1248,9 @@ dreams_status_t check_paged_tensors(const dreams_paged_desc_t* d, const void* q,
 }
 
 PagedAttnArgs paged_args(const dreams_paged_desc_t* d, const void* q, const void* k_pages, const void* v_pages,
-                         const int32_t* page_table, const int32_t* kv_len, void* out, float* lse) {
+                         const int32_t* page_table, const int32_t* kv_len, void* out, float* lse, bool e4m3) {
   PagedAttnArgs a{};
-  const int elem = d->dtype == DREAMS_BF16 ? 2 : 4;
+  const int elem = e4m3 ? 1 : d->dtype == DREAMS_BF16 ? 2 : 4;
   a.q = q;
   a.k = k_pages;
   a.v = v_pages;
@@ -1304,8 +1306,8 @@ int paged_pieces(int n_keys, long long xcd_wgs, long long xcd_cus, bool level) {
   return pieces;
 }
 
-dreams_status_t plan_paged(const dreams_paged_desc_t* d, bool prompt, PagedPlan* plan) {
-  dreams_status_t st = check_paged_desc(d, prompt);
+dreams_status_t plan_paged(const dreams_paged_desc_t* d, bool prompt, bool e4m3, PagedPlan* plan) {
+  dreams_status_t st = check_paged_desc(d, prompt, e4m3);
   if (st != DREAMS_OK) return st;
   *plan = PagedPlan{};
   AttnPlan& p = plan->p;
@@ -1322,10 +1324,11 @@ dreams_status_t plan_paged(const dreams_paged_desc_t* d, bool prompt, PagedPlan*
   // rows behind 2000 18.8, 22.2; 8 x 16 heads x 48 of 64 columns behind 1500 23.8, 25.8.  Where short keys meet many heads it is
   // the other way round: 16 x 8 heads x 64 rows of 64 columns behind 500 16.0, 13.5; 4 x 32 heads x 40 behind 1000 26.7, 23.1.)
   p.rows_per_wg = tree_attn_bf16_rows_per_wg(p.rows_total);
+  if (e4m3 && p.rows_per_wg > 64) p.rows_per_wg = 64;
   p.row_groups = (p.rows_total + p.rows_per_wg - 1) / p.rows_per_wg;
   p.units = d->batch * d->num_kv_heads;
   int span = T;   // positions that a workgroup's rows can be apart
-  if (prompt && p.row_groups > 1) {
+  if (prompt && p.row_groups > 1 && p.rows_per_wg == 128) {
     // Row groups of one head see only the keys before them; packed ones leave no row of a workgroup empty.  The fewer keys
     // decide (32 heads, 8 KV heads: 2000 rows 69 us packed, 48 by heads; 28 heads, 4 KV heads, 16 x 140 rows behind 1000 keys
     // 45 packed, 63 by heads).
@@ -1398,7 +1401,8 @@ int paged_key_groups(const PagedPlan& plan, int cus) {
 dreams_status_t run_paged(const dreams_paged_desc_t* desc, bool prompt, const PagedAttnArgs& in, void* workspace,
                           size_t workspace_bytes, hipStream_t stream) {
   PagedPlan plan;
-  dreams_status_t st = plan_paged(desc, prompt, &plan);
+  const bool e4m3 = in.k_scale != nullptr;
+  dreams_status_t st = plan_paged(desc, prompt, e4m3, &plan);
   if (st != DREAMS_OK) return st;
   const AttnPlan& p = plan.p;
   if (p.bytes > 0) {
@@ -1457,36 +1461,48 @@ dreams_status_t run_paged(const dreams_paged_desc_t* desc, bool prompt, const Pa
   st = device_cus(&a.cus);
   if (st != DREAMS_OK) return st;
   a.key_groups = paged_key_groups(plan, a.cus);
-  hipError_t e = a.rows_per_wg == 128 ? launch_paged_rows_bf16(a, stream) : launch_paged_attn_bf16(a, stream);
+  a.k_scale = in.k_scale;
+  a.v_scale = in.v_scale;
+  a.scale_stride = in.scale_stride;
+  hipError_t e = e4m3                   ? launch_paged_attn_e4m3(a, stream)
+                 : a.rows_per_wg == 128 ? launch_paged_rows_bf16(a, stream)
+                                        : launch_paged_attn_bf16(a, stream);
   if (e != hipSuccess) return hip_fail(e, "paged attention launch");
   return ok();
 }
 
 }  // namespace
 
-dreams_status_t dreams_paged_verify_attn_workspace_size(const dreams_paged_desc_t* desc, size_t* bytes) {
+namespace {
+
+dreams_status_t paged_workspace(const dreams_paged_desc_t* desc, bool prompt, bool e4m3, size_t* bytes) {
   if (!bytes) return fail(DREAMS_ERR_INVALID_ARG, "bytes is NULL");
   PagedPlan plan;
-  dreams_status_t st = plan_paged(desc, false, &plan);
+  dreams_status_t st = plan_paged(desc, prompt, e4m3, &plan);
   if (st != DREAMS_OK) return st;
   *bytes = plan.p.bytes;
   return ok();
 }
 
-dreams_status_t dreams_paged_prompt_attn_workspace_size(const dreams_paged_desc_t* desc, size_t* bytes) {
-  if (!bytes) return fail(DREAMS_ERR_INVALID_ARG, "bytes is NULL");
-  PagedPlan plan;
-  dreams_status_t st = plan_paged(desc, true, &plan);
-  if (st != DREAMS_OK) return st;
-  *bytes = plan.p.bytes;
-  return ok();
+// scales: of pages of 8 bits (e4m3)
+dreams_status_t set_scales(PagedAttnArgs* a, const dreams_paged_desc_t* d, const dreams_page_scales_t* scales) {
+  if (!scales) return fail(DREAMS_ERR_INVALID_ARG, "scales is NULL");
+  const int64_t page = (int64_t)d->num_kv_heads * (d->page_size / kScaleBlock);
+  if (scales->page_stride != 0 && (scales->page_stride < page || scales->page_stride > ((int64_t)1 << 60) / d->num_pages))
+    return fail(DREAMS_ERR_INVALID_ARG, "scales->page_stride = %lld must hold a page's %lld scales",
+                (long long)scales->page_stride, (long long)page);
+  if (!scales->k || !scales->v) return fail(DREAMS_ERR_INVALID_ARG, "scales->k and scales->v must not be NULL");
+  a->k_scale = scales->k;
+  a->v_scale = scales->v;
+  a->scale_stride = scales->page_stride ? scales->page_stride : page;
+  return DREAMS_OK;
 }
 
-dreams_status_t dreams_paged_verify_attn(const dreams_paged_desc_t* desc, const void* q, const void* k_pages,
-                                         const void* v_pages, const int32_t* page_table, const int32_t* kv_len,
-                                         const int32_t* parent, const uint64_t* tree_mask, void* out, float* lse,
-                                         void* workspace, size_t workspace_bytes, hipStream_t stream) {
-  dreams_status_t st = check_paged_desc(desc, false);
+dreams_status_t paged_verify(const dreams_paged_desc_t* desc, bool e4m3, const void* q, const void* k_pages,
+                             const void* v_pages, const dreams_page_scales_t* scales, const int32_t* page_table,
+                             const int32_t* kv_len, const int32_t* parent, const uint64_t* tree_mask, void* out, float* lse,
+                             void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  dreams_status_t st = check_paged_desc(desc, false, e4m3);
   if (st != DREAMS_OK) return st;
   if (desc->batch == 0) return ok();
   st = check_paged_tensors(desc, q, k_pages, v_pages, page_table, kv_len, out, lse);
@@ -1496,26 +1512,79 @@ dreams_status_t dreams_paged_verify_attn(const dreams_paged_desc_t* desc, const 
     return fail(DREAMS_ERR_INVALID_ARG, "a window needs parent: the nodes' positions follow from their depths");
   if (!aligned(parent, 4) || !aligned(tree_mask, 8))
     return fail(DREAMS_ERR_INVALID_ARG, "parent or tree_mask is misaligned");
-  PagedAttnArgs a = paged_args(desc, q, k_pages, v_pages, page_table, kv_len, out, lse);
+  PagedAttnArgs a = paged_args(desc, q, k_pages, v_pages, page_table, kv_len, out, lse, e4m3);
+  if (e4m3) st = set_scales(&a, desc, scales);
+  if (st != DREAMS_OK) return st;
   a.parent = parent;
   a.mask = tree_mask;
   return run_paged(desc, false, a, workspace, workspace_bytes, stream);
+}
+
+dreams_status_t paged_prompt(const dreams_paged_desc_t* desc, bool e4m3, const void* q, const void* k_pages,
+                             const void* v_pages, const dreams_page_scales_t* scales, const int32_t* page_table,
+                             const int32_t* kv_len, const int32_t* row_len, void* out, float* lse, void* workspace,
+                             size_t workspace_bytes, hipStream_t stream) {
+  dreams_status_t st = check_paged_desc(desc, true, e4m3);
+  if (st != DREAMS_OK) return st;
+  if (desc->batch == 0) return ok();
+  st = check_paged_tensors(desc, q, k_pages, v_pages, page_table, kv_len, out, lse);
+  if (st != DREAMS_OK) return st;
+  if (!aligned(row_len, 4)) return fail(DREAMS_ERR_INVALID_ARG, "row_len is misaligned");
+  PagedAttnArgs a = paged_args(desc, q, k_pages, v_pages, page_table, kv_len, out, lse, e4m3);
+  if (e4m3) st = set_scales(&a, desc, scales);
+  if (st != DREAMS_OK) return st;
+  a.row_len = row_len;
+  a.prompt = 1;
+  return run_paged(desc, true, a, workspace, workspace_bytes, stream);
+}
+
+}  // namespace
+
+dreams_status_t dreams_paged_verify_attn_workspace_size(const dreams_paged_desc_t* desc, size_t* bytes) {
+  return paged_workspace(desc, false, false, bytes);
+}
+dreams_status_t dreams_paged_prompt_attn_workspace_size(const dreams_paged_desc_t* desc, size_t* bytes) {
+  return paged_workspace(desc, true, false, bytes);
+}
+dreams_status_t dreams_paged_verify_attn_e4m3_workspace_size(const dreams_paged_desc_t* desc, size_t* bytes) {
+  return paged_workspace(desc, false, true, bytes);
+}
+dreams_status_t dreams_paged_prompt_attn_e4m3_workspace_size(const dreams_paged_desc_t* desc, size_t* bytes) {
+  return paged_workspace(desc, true, true, bytes);
+}
+
+dreams_status_t dreams_paged_verify_attn(const dreams_paged_desc_t* desc, const void* q, const void* k_pages,
+                                         const void* v_pages, const int32_t* page_table, const int32_t* kv_len,
+                                         const int32_t* parent, const uint64_t* tree_mask, void* out, float* lse,
+                                         void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  return paged_verify(desc, false, q, k_pages, v_pages, nullptr, page_table, kv_len, parent, tree_mask, out, lse, workspace,
+                      workspace_bytes, stream);
+}
+
+dreams_status_t dreams_paged_verify_attn_e4m3(const dreams_paged_desc_t* desc, const void* q, const void* k_pages,
+                                              const void* v_pages, const dreams_page_scales_t* scales,
+                                              const int32_t* page_table, const int32_t* kv_len, const int32_t* parent,
+                                              const uint64_t* tree_mask, void* out, float* lse, void* workspace,
+                                              size_t workspace_bytes, hipStream_t stream) {
+  return paged_verify(desc, true, q, k_pages, v_pages, scales, page_table, kv_len, parent, tree_mask, out, lse, workspace,
+                      workspace_bytes, stream);
 }
 
 dreams_status_t dreams_paged_prompt_attn(const dreams_paged_desc_t* desc, const void* q, const void* k_pages,
                                          const void* v_pages, const int32_t* page_table, const int32_t* kv_len,
                                          const int32_t* row_len, void* out, float* lse, void* workspace,
                                          size_t workspace_bytes, hipStream_t stream) {
-  dreams_status_t st = check_paged_desc(desc, true);
-  if (st != DREAMS_OK) return st;
-  if (desc->batch == 0) return ok();
-  st = check_paged_tensors(desc, q, k_pages, v_pages, page_table, kv_len, out, lse);
-  if (st != DREAMS_OK) return st;
-  if (!aligned(row_len, 4)) return fail(DREAMS_ERR_INVALID_ARG, "row_len is misaligned");
-  PagedAttnArgs a = paged_args(desc, q, k_pages, v_pages, page_table, kv_len, out, lse);
-  a.row_len = row_len;
-  a.prompt = 1;
-  return run_paged(desc, true, a, workspace, workspace_bytes, stream);
+  return paged_prompt(desc, false, q, k_pages, v_pages, nullptr, page_table, kv_len, row_len, out, lse, workspace,
+                      workspace_bytes, stream);
+}
+
+dreams_status_t dreams_paged_prompt_attn_e4m3(const dreams_paged_desc_t* desc, const void* q, const void* k_pages,
+                                              const void* v_pages, const dreams_page_scales_t* scales,
+                                              const int32_t* page_table, const int32_t* kv_len, const int32_t* row_len,
+                                              void* out, float* lse, void* workspace, size_t workspace_bytes,
+                                              hipStream_t stream) {
+  return paged_prompt(desc, true, q, k_pages, v_pages, scales, page_table, kv_len, row_len, out, lse, workspace,
+                      workspace_bytes, stream);
 }
 
 namespace {

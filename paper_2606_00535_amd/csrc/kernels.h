@@ -115,6 +115,10 @@ struct AttnArgs {
   int groups_per_head;    // chain: row groups of a head, or 0: the heads' rows are packed one after another
   int key_groups;         // 128 rows: key groups of 4 waves in a workgroup (1 or 2)
   int unit_parts;         // parts of a unit's row groups, each on one XCD; units * unit_parts is a multiple of 8
+  // Pages of 8 bits: a byte for every 16 slots, [pages, Hkv, page_size / 16], scale_stride bytes a page
+  const uint8_t* k_scale;
+  const uint8_t* v_scale;
+  int64_t scale_stride;
 };
 
 // Query rows per workgroup the bf16 kernel uses for G*T rows per KV head.
@@ -339,6 +343,7 @@ struct RopeQueryArgs {
 // A pool of pages holds the slots of every sequence: page p of KV head g is a [page_size, D] slab at
 // p * page_stride + g * page_size * D.  Slot j of sequence b is row j % page_size of page table[b, j / page_size].  Page
 // sizes are powers of two from 16, so that 16 slots from a multiple of 16 on lie in one page.
+constexpr int kScaleBlock = 16;              // slots of a scale, in pages of 8 bits
 constexpr int kPagedMinPage = 16, kPagedMaxPage = 1 << 15;
 constexpr int kPagedMaxSlots = 1 << 30;      // slots that a table row covers, at most
 constexpr int kPagesMaxPages = 1 << 19;      // pages of a pool that pages are taken from, at most (bits and ranks in LDS)
@@ -363,6 +368,9 @@ struct PagedAttnArgs {       // fp32 (the bf16 kernels' AttnArgs have the same)
   int window, sinks;         // window 0: every key in sight
   float scale_log2;          // scale * log2(e)
   int cus;
+  const uint8_t* k_scale;    // pages of 8 bits (nullptr: they are not): see AttnArgs
+  const uint8_t* v_scale;
+  int64_t scale_stride;
 };
 constexpr int kPagedF32Threads = 1024;
 inline long long paged_attn_f32_workgroups(int units, int G, int T) {   // of a large call: 4 rows each
@@ -371,6 +379,7 @@ inline long long paged_attn_f32_workgroups(int units, int G, int T) {   // of a 
 hipError_t launch_paged_attn_f32(const PagedAttnArgs& a, hipStream_t stream);
 hipError_t launch_paged_attn_bf16(const AttnArgs& a, hipStream_t stream);   // up to 64 rows a KV head
 hipError_t launch_paged_rows_bf16(const AttnArgs& a, hipStream_t stream);   // 128 rows a workgroup
+hipError_t launch_paged_attn_e4m3(const AttnArgs& a, hipStream_t stream);   // pages of 8 bits, up to 64 rows a workgroup
 
 struct PagedRowsArgs {
   char* k;                   // [NL][pages, Hkv, page_size, row bytes]
@@ -400,7 +409,6 @@ hipError_t launch_paged_append_rope(const PagedRowsArgs& a, const RopeArgs& rope
                                     hipStream_t stream);
 
 // Pages of 8 bits: PagedRowsArgs with the codes' strides (row_bytes = D), and the scale bytes [NL][pages, Hkv, page_size / 16].
-constexpr int kScaleBlock = 16;              // slots of a scale
 struct PagedScaleArgs {
   uint8_t* k;
   uint8_t* v;

@@ -1,0 +1,27 @@
+// Attention over a paged cache in 8 bits, up to 64 rows a workgroup: the builds of the kernel in tree_attn_bf16.h that read
+// e4m3 pages and their scales.
+#include "tree_attn_bf16.h"
+
+namespace dreams {
+namespace {
+
+template <int D, int NST>
+hipError_t launch_for_rows(const AttnArgs& a, hipStream_t stream) {
+  switch (a.rows_per_wg) {
+    case 16: return launch_streaming<D, 1, 4, 4, NST, 1, false, true, true>(a, stream);
+    case 32: return launch_streaming<D, 1, 4, 8, NST, 1, false, true, true>(a, stream);
+    case 64: return launch_streaming<D, 2, 2, 4, 1024 / D, 2, false, true, true>(a, stream);
+  }
+  return hipErrorInvalidValue;
+}
+
+}  // namespace
+
+hipError_t launch_paged_attn_e4m3(const AttnArgs& a, hipStream_t stream) {
+  if (a.unit_parts < 1 || a.units * a.unit_parts % 8 != 0) return hipErrorInvalidValue;
+  if (a.D == 128) return launch_for_rows<128, 16>(a, stream);
+  if (a.D == 64) return launch_for_rows<64, 16>(a, stream);
+  return hipErrorInvalidValue;
+}
+
+}  // namespace dreams

@@ -53,6 +53,7 @@
 #include "kernels.h"
 
 #include <math.h>
+#include <type_traits>
 
 namespace dreams {
 namespace {
@@ -63,6 +64,8 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 constexpr float kLn2 = 0.69314718055994530942f;
 constexpr int kStep = 32;          // keys per step
@@ -78,6 +81,21 @@ __device__ __forceinline__ float ent_term(float w, float e, float m, float M, fl
 }
 __device__ __forceinline__ float row_entropy(float l, float e) {
   return l > 0.f ? 0.69314718055994530942f * (__log2f(l) - e / l) : 0.f;
+}
+
+// 8 codes of e4m3 as bf16, the first four times one power of two, the others times another
+__device__ __forceinline__ bf16x8 decode8(uint32_t lo, uint32_t hi, float scale_lo, float scale_hi) {
+  bf16x8 x;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const bf16x2 y = i == 0   ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale_lo, false)
+                     : i == 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale_lo, true)
+                     : i == 2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale_hi, false)
+                              : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale_hi, true);
+    x[2 * i] = y[0];
+    x[2 * i + 1] = y[1];
+  }
+  return x;
 }
 
 typedef __attribute__((address_space(3))) void lds_void;
@@ -149,6 +167,27 @@ struct Rows {
   }
   __device__ static __forceinline__ int off(int r, int c) { return r * ROW + ((c ^ swz(r)) << 4); }
 };
+
+// The same for keys and values in 8 bits (E8): rows of D codes, 16 to a chunk.  A key read takes one chunk of 16 rows, a
+// transposing value read (ds_read_b64_tr_b8) one chunk of 8 rows a quad, in halves of two quads: 16 rows that differ modulo
+// 16 (key_row).  swz is a bijection over the rows of a bank line's parity (D = 64: residue modulo 4) that also keeps rows 0..3
+// and 12..15 at one chunk apart from 4..11 at its neighbour, as a 16-byte read's groups of lanes mix them.
+template <int D>
+struct Rows8 {
+  static constexpr int ROW = D, CPR = D / 16, RPL = 256 / ROW, HALF = kStep * ROW, SLOT = 2 * HALF, C16 = 16 * ROW / 1024;
+  __device__ static __forceinline__ int swz(int r) {
+    if constexpr (D == 128) return (r >> 1) & 7;
+    return (0x78 >> (2 * ((r >> 2) & 3))) & 3;
+  }
+  __device__ static __forceinline__ int off(int r, int c) { return r * ROW + ((c ^ swz(r)) << 4); }
+};
+// The key of a step that operand row m of its block kb holds.
+__device__ __forceinline__ int key_row(int kb, int m) { return kb * 16 + (m ^ (8 * kb)); }
+
+// One byte into LDS (zero-extended to 32 bits) at m0, by the one lane that calls it.
+__device__ __forceinline__ void copy_byte_to_lds(uint32_t m0, const void* src) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_ubyte %1, %2" ::"s"(m0), "v"(0), "s"(src) : "memory");
+}
 
 // Merge of a set's pieces for rows [r0, r0 + nrows) of the set, in piece order (so the result does not
 // depend on which piece finished last): out = sum_s w_s l_s o_s / sum_s w_s l_s, w_s = 2^(m_s - max_s m_s).
@@ -295,39 +334,48 @@ __device__ __forceinline__ void merge_set(const AttnArgs& a, size_t pset, int R,
 
 // LDS of a workgroup: the ring, the query rows when they sit beside it, the ancestor sets and the tree as
 // copied (static), and a few words; WPC workgroups share a compute unit's 160 KB.
-template <int D, int NST, int WPC>
+// (E8: steps of half the bytes, and a word for each of a step's four scales)
+template <int D, int NST, int WPC, bool E8>
 constexpr bool q_beside_ring(int R) {
-  return (size_t)NST * Rows<D>::SLOT + (size_t)R * D * 2 + 4 * kMaxNodes * 8 + 64 <= 160 * 1024 / WPC;
+  return (size_t)NST * (E8 ? Rows8<D>::SLOT + 16 : Rows<D>::SLOT) + (size_t)R * D * 2 + 4 * kMaxNodes * 8 + 64 <=
+         160 * 1024 / WPC;
 }
-template <int D, int NST, int WPC>
+template <int D, int NST, int WPC, bool E8>
 constexpr size_t dynamic_lds(int R) {
-  return (size_t)NST * Rows<D>::SLOT + (q_beside_ring<D, NST, WPC>(R) ? (size_t)R * D * 2 : 0);
+  return (size_t)NST * (E8 ? Rows8<D>::SLOT : Rows<D>::SLOT) + (q_beside_ring<D, NST, WPC, E8>(R) ? (size_t)R * D * 2 : 0);
 }
 
 // WPC: workgroups meant to share a compute unit (their waves share each SIMD, so the register budget is that
 // of WPC * W / 4 waves per SIMD).
-template <int D, int RB, int KW, int W, int NST, bool PIPE, bool ENT, int WPC, bool PAGED>
+// E8 (paged): keys and values in e4m3 with a power-of-two scale for 16 slots of a head.  The ring holds their codes, and
+// they become bf16, exactly, in registers (v_cvt_scalef32_pk_bf16_fp8, the scale's exponent in the same instruction): a
+// step's 64 conversions a wave run beside its 16 RB products.
+template <int D, int RB, int KW, int W, int NST, bool PIPE, bool ENT, int WPC, bool PAGED, bool E8 = false>
 __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(AttnArgs a) {
   constexpr int WR = W / KW;          // waves per key group; each owns a different slice of the rows
   constexpr int RW = 16 * RB;         // query rows per wave
   constexpr int R = WR * RW;          // query rows per workgroup
   constexpr int DS = D / 32;          // k-steps of S^T = K Q^T
   constexpr int DB = D / 16;          // 16-column blocks of O^T
-  using L = Rows<D>;
-  constexpr int C16 = L::C16;         // wave-wide copies per 16 rows
+  using L = Rows<D>;                                      // query rows
+  using V = std::conditional_t<E8, Rows8<D>, Rows<D>>;    // key and value rows
+  static_assert(!E8 || PAGED, "8 bits: paged");
+  constexpr int C16 = V::C16;         // wave-wide copies per 16 rows
   constexpr int NSS = NST / KW;       // ring slots in super-steps (KW consecutive steps, one per key group)
   // The query rows get an LDS region of their own beside the ring where it fits (so the first copies fill the
   // whole ring); otherwise they occupy the ring's last step slots until the prologue has read them.
-  constexpr bool QSEP = q_beside_ring<D, NST, WPC>(R);
-  constexpr int QSLOTS = QSEP ? 0 : (R * L::ROW + L::SLOT - 1) / L::SLOT;   // step slots the query rows occupy
+  constexpr bool QSEP = q_beside_ring<D, NST, WPC, E8>(R);
+  constexpr int QSLOTS = QSEP ? 0 : (R * L::ROW + V::SLOT - 1) / V::SLOT;   // step slots the query rows occupy
   constexpr int QSS = (QSLOTS + KW - 1) / KW;                                // ... in super-steps
   constexpr int CPS = 4 * KW * C16 / W;   // copies per wave per super-step (4*KW blocks of 16 rows)
   constexpr int QB = R / 16;          // 16-row blocks of query rows, dealt to the waves round-robin
   static_assert(W % KW == 0 && (NST & (NST - 1)) == 0 && NSS > QSS && NSS >= 2, "ring layout");
   static_assert(CPS * W == 4 * KW * C16 && CPS >= 1 && (C16 % CPS == 0 || CPS % C16 == 0), "copy split");
-  static_assert(16 * L::ROW == C16 * 1024 && (16 / L::RPL) % L::CPR == 0, "swizzle repeats every 16 rows");
-  static_assert(NSS * CPS + ((QB + W - 1) / W) * C16 + 8 <= 63, "outstanding copies fit the counter");
-  static_assert((size_t)(KW - 1) * R * D * 4 + (size_t)KW * R * 12 <= (size_t)NST * L::SLOT, "group states fit the ring");
+  static_assert(16 * V::ROW == C16 * 1024 && (E8 || (16 / L::RPL) % L::CPR == 0), "swizzle repeats every 16 rows");
+  constexpr int CPT = CPS + (E8 ? (CPS + C16 - 1) / C16 : 0);   // ... with the scales' (one for a block's codes)
+  static_assert(!E8 || CPS % C16 == 0, "whole blocks");
+  static_assert(NSS * CPT + ((QB + W - 1) / W) * L::C16 + 8 <= 63, "outstanding copies fit the counter");
+  static_assert((size_t)(KW - 1) * R * D * 4 + (size_t)KW * R * 12 <= (size_t)NST * V::SLOT, "group states fit the ring");
 
   extern __shared__ __attribute__((aligned(1024))) unsigned char ring[];   // NST step slots (+ the query rows)
   __shared__ uint64_t anc_lds[2 * kMaxNodes];
@@ -336,6 +384,7 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
   __shared__ uint32_t good_lds;                   // 0: a wait gave up (the merged rows are written as NaN)
   __shared__ int par_lds[PAGED ? kMaxNodes : 1];      // paged, mask and window: the parents
   __shared__ int depth_lds[PAGED ? kMaxNodes : 1];    // paged, window: the nodes' depths
+  __shared__ __attribute__((aligned(16))) uint32_t scale_lds[E8 ? NST * 4 : 1];   // a step's scale bytes: 2 K, 2 V
 
   // ---- work item
   const int n = blockIdx.x;
@@ -366,6 +415,7 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
   const int T = a.T;
   const int rows_total = a.G * T;
   const uint32_t ring_lds = __builtin_amdgcn_readfirstlane(lds_addr(ring));
+  const uint32_t scale_base = E8 ? __builtin_amdgcn_readfirstlane(lds_addr(scale_lds)) : 0;
   const int kv_len_b = a.kv_len[b];   // issued before the copies below, ahead of their traffic
 
   // ---- the workgroup's rows: [row_base, row_base + rows_here) of the unit's rows_total
@@ -412,7 +462,7 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
   const int k_end_plan = split == a.splits - 1 ? keys : min(keys, k_begin + piece);
   const int nplan = k_end_plan > k_begin ? (k_end_plan - k_begin + kStep - 1) / kStep : 0;
   const int nsp = (nplan + KW - 1) / KW;
-  const size_t head_off = PAGED ? ((size_t)g << a.page_shift) * L::ROW : (size_t)u * a.S_cap * L::ROW;
+  const size_t head_off = PAGED ? ((size_t)g << a.page_shift) * V::ROW : (size_t)u * a.S_cap * V::ROW;
   const unsigned char* kbase = (const unsigned char*)a.k + head_off;
   const unsigned char* vbase = (const unsigned char*)a.v + head_off;
 
@@ -422,8 +472,8 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
 #pragma unroll
   for (int j = 0; j < C16; ++j) {
     const int e = j * 64 + lane;
-    const int r = e / L::CPR, p = e - r * L::CPR;
-    coff[j] = (uint32_t)(r * L::ROW + ((p ^ L::swz(r)) << 4));
+    const int r = e / V::CPR, p = e - r * V::CPR;
+    coff[j] = (uint32_t)(r * V::ROW + ((p ^ V::swz(r)) << 4));
   }
   // A super-step is KW steps x (32 K rows + 32 V rows) = 4*KW blocks of 16 rows = 4*KW*C16 wave-wide 1 KB
   // copies; wave w issues copies w*CPS .. w*CPS + CPS - 1 (copy ci: block bi = ci / C16 -- step bi/4 of the
@@ -447,20 +497,26 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
     }
   };
   auto issue_group = [&](int jj, int t) {
-    const uint32_t sbase = ring_lds + (jj & (NSS - 1)) * KW * L::SLOT;
+    const uint32_t sbase = ring_lds + (jj & (NSS - 1)) * KW * V::SLOT;
     const int ci0 = wave * CPS + t * GRP;
     const int bi = ci0 / C16, j0 = ci0 - bi * C16;
     const int sis = bi >> 2, part = (bi >> 1) & 1, half = bi & 1;
     const int key0 = k_begin + (jj * KW + sis) * kStep + 16 * half;
     const unsigned char* pbase = part ? vbase : kbase;
-    const uint32_t dst = sbase + sis * L::SLOT + part * L::HALF + half * C16 * 1024;
+    const uint32_t dst = sbase + sis * V::SLOT + part * V::HALF + half * C16 * 1024;
     if constexpr (PAGED) {
       // (a page outside the pool, or past the table: some page of the pool, whose rows no one sees)
       const int page = min(max(next_page[t], 0), a.num_pages - 1);
       const int row = group_slot(jj, t) & ((1 << a.page_shift) - 1);
-      const unsigned char* src = pbase + (int64_t)page * a.page_stride + (int64_t)row * L::ROW;
+      const unsigned char* src = pbase + (int64_t)page * a.page_stride + (int64_t)row * V::ROW;
 #pragma unroll
       for (int j = 0; j < GRP; ++j) copy16_to_lds(dst + (j0 + j) * 1024, src, coff[j0 + j]);
+      if constexpr (E8) {
+        const uint8_t* byte = (part ? a.v_scale : a.k_scale) + (int64_t)page * a.scale_stride +
+                              (int64_t)((((size_t)g << a.page_shift) + row) / kScaleBlock);
+        const uint32_t at = scale_base + ((jj & (NSS - 1)) * KW + sis) * 16 + part * 8 + half * 4;
+        if (lane == 0) copy_byte_to_lds(at, byte);
+      }
     } else if (key0 + 16 <= a.S_cap) {
       const unsigned char* src = pbase + (size_t)key0 * L::ROW;
 #pragma unroll
@@ -482,15 +538,19 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
 
   // ---- first copies: the query rows (into the last step slots), the tree (wave 0), then the ring
   const size_t qrow0 = ((size_t)b * a.Hq + (size_t)g * a.G) * T;   // row 0 of this KV head's query rows
-  const unsigned char* qslab = QSEP ? ring + NST * L::SLOT : ring + (NST - QSLOTS) * L::SLOT;
+  const unsigned char* qslab = QSEP ? ring + NST * V::SLOT : ring + (NST - QSLOTS) * V::SLOT;
 #pragma unroll
   for (int qb = wave; qb < QB; qb += W) {
 #pragma unroll
-    for (int j = 0; j < C16; ++j) {
+    for (int j = 0; j < L::C16; ++j) {
       const int r = (j * 64 + lane) / L::CPR;
       const int row = PAGED ? row_base + min(qb * 16 + r, rows_here - 1) : min(rg * R + qb * 16 + r, rows_total - 1);
-      copy16_to_lds(lds_addr(qslab) + (qb * C16 + j) * 1024,
-                    (const unsigned char*)a.q + (qrow0 + row) * L::ROW + (coff[j] - r * L::ROW));
+      if constexpr (E8)
+        copy16_to_lds(lds_addr(qslab) + (qb * L::C16 + j) * 1024,
+                      (const unsigned char*)a.q + (qrow0 + row) * L::ROW + ((((j * 64 + lane) % L::CPR) ^ L::swz(r)) << 4));
+      else
+        copy16_to_lds(lds_addr(qslab) + (qb * L::C16 + j) * 1024,
+                      (const unsigned char*)a.q + (qrow0 + row) * L::ROW + (coff[j] - r * L::ROW));
     }
   }
   const int Wm = (T + 63) / 64;
@@ -536,7 +596,7 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
   const int nact = k_end > k_begin ? (k_end - k_begin + kStep - 1) / kStep : 0;
   const int nsa = (nact + KW - 1) / KW;
 
-  wait_vm_steps<CPS, NSS - QSS>(fa);   // this wave's query rows and the tree have landed
+  wait_vm_steps<CPT, NSS - QSS>(fa);   // this wave's query rows and the tree have landed
   barrier_lds();
   // Only a piece that reaches the tree slots consults ancestor sets (a step before them has key < L_b
   // everywhere, and a masked step past k_end hides its keys whatever the sets say).
@@ -593,7 +653,11 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
-    for (int ds = 0; ds < DS; ++ds) qf[rb][ds] = *(const bf16x8*)(qslab + L::off(rh * RW + rb * 16 + col, ds * 4 + quad));
+    for (int ds = 0; ds < DS; ++ds) {
+      // (E8: a lane's 16 codes of a key are 16 columns, of two products)
+      const int chunk = E8 ? (ds >> 1) * 8 + quad * 2 + (ds & 1) : ds * 4 + quad;
+      qf[rb][ds] = *(const bf16x8*)(qslab + L::off(rh * RW + rb * 16 + col, chunk));
+    }
   // Scores are scaled by c = |scale| log2(e) > 0 inside the exponent (one fma per score); a negative scale
   // flips the sign of the queries instead (exact in bf16), a zero scale becomes the smallest normal float.
   const float c_scale = fmaxf(fabsf(a.scale_log2), 1.17549435e-38f);
@@ -672,7 +736,7 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
   // them zero them once their own copies have landed, so that no bit pattern (an infinity, a NaN) can reach
   // the products; their scores are then exactly the mask's -inf.
   auto zero_tail = [&](int jj) {
-    unsigned char* sslot = ring + (jj & (NSS - 1)) * KW * L::SLOT;
+    unsigned char* sslot = ring + (jj & (NSS - 1)) * KW * V::SLOT;
 #pragma unroll
     for (int t = 0; t < NGRP; ++t) {
       const int ci0 = wave * CPS + t * GRP;
@@ -683,12 +747,12 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
       const bool before = PAGED && key0 < low && key0 + kStep > sink_end;
       if (key0 + kStep > N || before) {
         // the rows this wave's copies brought: 64*GRP lanes' worth of 16-byte chunks, rows j0*1024/ROW ..
-        constexpr int RPG = GRP * 1024 / L::ROW;   // rows per group of copies
+        constexpr int RPG = GRP * 1024 / V::ROW;   // rows per group of copies
         constexpr int LPR = 64 / RPG;              // lanes per row
-        constexpr int PER = L::CPR / LPR;          // chunks per lane
-        const int r = 16 * half + j0 * 1024 / L::ROW + lane / LPR;
+        constexpr int PER = V::CPR / LPR;          // chunks per lane
+        const int r = 16 * half + j0 * 1024 / V::ROW + lane / LPR;
         if (key0 + r >= N || (before && key0 + r < low && key0 + r >= sink_end)) {
-          unsigned char* vrow = sslot + sis * L::SLOT + part * L::HALF + r * L::ROW;
+          unsigned char* vrow = sslot + sis * V::SLOT + part * V::HALF + r * V::ROW;
 #pragma unroll
           for (int c = 0; c < PER; ++c) *(u32x4*)(vrow + ((lane % LPR) * PER + c) * 16) = u32x4{0u, 0u, 0u, 0u};
         }
@@ -699,11 +763,36 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
   // A step's operands: K fragments (A operand of S^T: A row m holds key kb*16 + (m%4)*4 + m/4) and V^T
   // fragments (A operand of O^T, transposing reads: lo = keys j*4+quad, hi = keys 16+j*4+quad, matching the
   // probabilities' slots).  All are issued together, so their LDS latencies overlap.
-  struct Ops {
+  struct Ops16 {
     bf16x8 kf[2][DS];
     s16x4 vlo[DB], vhi[DB];
   };
+  struct Ops8 {
+    u32x4 k[2][DS / 2];
+    i32x2 v[DB];
+    u32x4 scale;
+  };
+  using Ops = std::conditional_t<E8, Ops8, Ops16>;
+  auto read_ops8 = [&](Ops8& op, int jj) {
+    const unsigned char* tile = ring + ((jj & (NSS - 1)) * KW + kw) * V::SLOT;
+    const unsigned char* vt = tile + V::HALF;
+    op.scale = *(const u32x4*)(scale_lds + ((jj & (NSS - 1)) * KW + kw) * 4);
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int x = 0; x < DS / 2; ++x) op.k[kb][x] = *(const u32x4*)(tile + V::off(key_row(kb, col), x * 4 + quad));
+    const int vrow = key_row((col >> 3) & 1, quad * 4 + ((col >> 1) & 3));    // this lane's row of 8, 8 columns of it
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+      op.v[d] = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+          (__attribute__((address_space(3))) i32x2*)(vt + V::off(vrow, d) + (col & 1) * 8));
+  };
+  // 2^(byte - 127) of a scale byte (a block that no row sees may have any)
+  auto scale_of = [](uint32_t byte) { return __builtin_bit_cast(float, min(byte, 254u) << 23); };
   auto read_ops = [&](Ops& op, int jj) {
+    if constexpr (E8) {
+      read_ops8(op, jj);
+    } else {
     const unsigned char* tile = ring + (jj & (NSS - 1)) * KW * L::SLOT + kw * L::SLOT;
     const unsigned char* vt = tile + L::HALF;
 #pragma unroll
@@ -716,6 +805,36 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
       op.vlo[d] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(vt + L::off(tr_row, c) + tr_half));
       op.vhi[d] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(vt + L::off(16 + tr_row, c) + tr_half));
     }
+    }
+  };
+  // the key fragments of a step, and a block of its values
+  auto keys_of = [&](const Ops& op, bf16x8 (&kf)[2][DS]) {
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      if constexpr (E8) {
+        const uint32_t byte = op.scale[kb];
+#pragma unroll
+        for (int ds = 0; ds < DS; ++ds) kf[kb][ds] = decode8(op.k[kb][ds >> 1][2 * (ds & 1)], op.k[kb][ds >> 1][2 * (ds & 1) + 1], scale_of(byte), scale_of(byte));
+      } else {
+#pragma unroll
+        for (int ds = 0; ds < DS; ++ds) kf[kb][ds] = op.kf[kb][ds];
+      }
+    }
+  };
+  auto values_of = [&](const Ops& op, int d) {
+    bf16x8 va;
+    if constexpr (E8) {
+      const uint32_t b0 = op.scale[2], b1 = op.scale[3];
+      va = decode8((uint32_t)op.v[d][0], (uint32_t)op.v[d][1], scale_of(b0), scale_of(b1));
+    } else {
+      const bf16x4 lo_b = __builtin_bit_cast(bf16x4, op.vlo[d]), hi_b = __builtin_bit_cast(bf16x4, op.vhi[d]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        va[e] = lo_b[e];
+        va[4 + e] = hi_b[e];
+      }
+    }
+    return va;
   };
 
   // One step (32 keys) of this wave's rows: scores, mask, online softmax, value product.
@@ -730,6 +849,8 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
     // another row sees it, or a mask hides it (-inf plus the product of a NaN or an infinity would be NaN).  Only steps that
     // reach the tree slots or the piece end need it.
     f32x4 s[RB][2];
+    bf16x8 kf[2][DS];
+    keys_of(op, kf);
     auto products = [&](bool from_zero) {
       // (the products are issued at a raised wave priority, so that the SIMD's other wave -- in its softmax --
       // does not hold them back: gqa_long 355 -> 339 us)
@@ -741,7 +862,7 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
 #pragma unroll
           for (int rb = 0; rb < RB; ++rb)
             s[rb][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                op.kf[kb][ds], qf[rb][ds], (from_zero && ds == 0) ? f32x4{0.f, 0.f, 0.f, 0.f} : s[rb][kb], 0, 0, 0);
+                kf[kb][ds], qf[rb][ds], (from_zero && ds == 0) ? f32x4{0.f, 0.f, 0.f, 0.f} : s[rb][kb], 0, 0, 0);
       __builtin_amdgcn_s_setprio(0);
     };
     bool edge = key0 + kStep > Lp || key0 + kStep > k_end;
@@ -754,7 +875,7 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
         for (int kb = 0; kb < 2; ++kb) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const int key = key0 + kb * 16 + e * 4 + quad;
+            const int key = key0 + (E8 ? key_row(kb, quad * 4 + e) : kb * 16 + e * 4 + quad);
             const int j = key - Lp;                      // tree node of a key past the prefix
             const uint64_t word = j < 64 ? anc0[rb] : anc1[rb];
             const bool anc = ((word >> (j & 63)) & 1ull) != 0;
@@ -837,13 +958,7 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int d = 0; d < DB; ++d) {
-      bf16x8 va;
-      const bf16x4 lo_b = __builtin_bit_cast(bf16x4, op.vlo[d]), hi_b = __builtin_bit_cast(bf16x4, op.vhi[d]);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        va[e] = lo_b[e];
-        va[4 + e] = hi_b[e];
-      }
+      const bf16x8 va = values_of(op, d);
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) o[rb][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pb[rb], o[rb][d], 0, 0, 0);
     }
@@ -856,7 +971,7 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
     // products and softmax of the previous one on every wave.
     Ops op[2];
     if (nsa > 0) {
-      wait_vm_steps<CPS, NSS - 1>(issued_by(0) - 1);   // this wave's copies of super-step 0 have landed
+      wait_vm_steps<CPT, NSS - 1>(issued_by(0) - 1);   // this wave's copies of super-step 0 have landed
       zero_tail(0);
       barrier_lds();
       if (kw < nact) read_ops(op[0], 0);
@@ -869,7 +984,7 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
       barrier_lds();
       if (js + NSS < nsa) issue_super(js + NSS);
       if (more) {
-        wait_vm_steps<CPS, NSS - 1>(issued_by(js + 1) - 2 - js);   // this wave's copies of super-step js+1
+        wait_vm_steps<CPT, NSS - 1>(issued_by(js + 1) - 2 - js);   // this wave's copies of super-step js+1
         zero_tail(js + 1);
       }
       // super-step js+1 complete in LDS for every wave.  (Also taken after the last super-step, so that on
@@ -891,7 +1006,7 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
       for (int sl = 0; sl < NSS; ++sl) {
         const int js = js0 + sl;
         if (js >= nsa) break;
-        wait_vm_steps<CPS, NSS - 2>(issued_by(js) - 1 - js);   // this wave's copies of super-step js have landed
+        wait_vm_steps<CPT, NSS - 2>(issued_by(js) - 1 - js);   // this wave's copies of super-step js have landed
         zero_tail(js);
         barrier_lds();   // super-step js complete in LDS for every wave; the slots of super-step js-1 are free
         if (js + NSS - 1 < nsa) issue_super(js + NSS - 1);
@@ -1029,7 +1144,7 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
   }
   constexpr int CPR = D / 8;                  // 16-byte pieces per row
   constexpr size_t XBYTES = KW > 1 ? ((size_t)(KW - 1) * R * D * 4 + (size_t)KW * R * 12 + 1023) / 1024 * 1024 : 0;
-  static_assert(XBYTES + (size_t)R * D * 2 + (size_t)R * 12 <= (size_t)NST * L::SLOT, "row staging fits the ring");
+  static_assert(XBYTES + (size_t)R * D * 2 + (size_t)R * 12 <= (size_t)NST * V::SLOT, "row staging fits the ring");
   unsigned char* row_lds = ring + XBYTES;                               // [R][CPR] 16-byte pieces
   float2* ml_lds = (float2*)(row_lds + (size_t)R * D * 2);              // [R]
   float* e_lds = (float*)(ml_lds + R);                                  // [R]
@@ -1085,13 +1200,14 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
   merge_set<D, W, ENT, __bf16>(a, pset, R, split, start_old, qrow0 + (size_t)row_base, rows_valid, &merge_lds, &good_lds);
 }
 
-template <int D, int RB, int KW, int W, int NST, int WPC, bool ENT, bool PAGED>
+template <int D, int RB, int KW, int W, int NST, int WPC, bool ENT, bool PAGED, bool E8 = false>
 hipError_t launch_streaming(const AttnArgs& a, hipStream_t stream) {
-  constexpr size_t lds = dynamic_lds<D, NST, WPC>(16 * RB * (W / KW));
-  static_assert(lds + 2 * kMaxNodes * 8 + 2 * kMaxNodes * 8 + (PAGED ? 2 * kMaxNodes * 4 : 8) + 64 <= 160 * 1024 / WPC,
+  constexpr size_t lds = dynamic_lds<D, NST, WPC, E8>(16 * RB * (W / KW));
+  static_assert(lds + 2 * kMaxNodes * 8 + 2 * kMaxNodes * 8 + (PAGED ? 2 * kMaxNodes * 4 : 8) + (E8 ? NST * 16 : 0) + 64 <=
+                    160 * 1024 / WPC,
                 "LDS budget");
   // two sets of operand registers fit beside one 16-row block's state, not beside two
-  auto kern = tree_attn_bf16_kernel<D, RB, KW, W, NST, RB == 1, ENT, WPC, PAGED>;
+  auto kern = tree_attn_bf16_kernel<D, RB, KW, W, NST, RB == 1, ENT, WPC, PAGED, E8>;
   static bool configured = false;
   if (!configured) {
     hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);

@@ -35,6 +35,8 @@ EXPORTS = (
     "dreams_paged_prompt_attn_workspace_size", "dreams_paged_append", "dreams_paged_kv_commit", "dreams_pages_reserve",
     "dreams_pages_fork", "dreams_pages_release", "dreams_rope_frequencies", "dreams_rope", "dreams_paged_append_rope",
     "dreams_paged_append_e4m3", "dreams_paged_kv_commit_e4m3", "dreams_paged_read_e4m3", "dreams_pages_fork_e4m3",
+    "dreams_paged_verify_attn_e4m3", "dreams_paged_verify_attn_e4m3_workspace_size", "dreams_paged_prompt_attn_e4m3",
+    "dreams_paged_prompt_attn_e4m3_workspace_size",
 )
 
 
@@ -154,6 +156,10 @@ def lib():
                 L.dreams_paged_append_e4m3.argtypes = [PP, SP, RP, QP, ctypes.c_int, P, P, I32, I64P, P, P, P, P, P, P]
                 L.dreams_paged_kv_commit_e4m3.argtypes = [PP, SP, P, P, P, P, P, P, I32, P, P]
                 L.dreams_paged_read_e4m3.argtypes = [PP, SP, P, P, P, P, I32, P, P, P]
+                L.dreams_paged_verify_attn_e4m3_workspace_size.argtypes = [PD, ctypes.POINTER(SZ)]
+                L.dreams_paged_prompt_attn_e4m3_workspace_size.argtypes = [PD, ctypes.POINTER(SZ)]
+                L.dreams_paged_verify_attn_e4m3.argtypes = [PD, P, P, P, SP, P, P, P, P, P, P, P, SZ, P]
+                L.dreams_paged_prompt_attn_e4m3.argtypes = [PD, P, P, P, SP, P, P, P, P, P, P, SZ, P]
                 L.dreams_pages_fork_e4m3.argtypes = [PP, SP, P, P, P, P, P, P, I32, P, P, P, P]
                 for f in ("dreams_tree_verify_attn_workspace_size", "dreams_tree_verify_attn",
                           "dreams_tree_accept_workspace_size", "dreams_tree_accept", "dreams_kv_commit",
@@ -907,10 +913,15 @@ def _table_pool(page_table, page_count, refcount, page_size):
 def paged_desc(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor, window: int = 0,
                sinks: int = 0, max_kv_len: int = 0, num_splits: int = 0, scale: Optional[float] = None) -> PagedDesc:
     """The description of an attention call over pages; checks the tensors' types, devices and shapes."""
+    return _paged_desc(q, k_pages, v_pages, page_table, k_pages.dtype if isinstance(k_pages, torch.Tensor) else None, window,
+                       sinks, max_kv_len, num_splits, scale)
+
+
+def _paged_desc(q, k_pages, v_pages, page_table, dt, window, sinks, max_kv_len, num_splits, scale) -> PagedDesc:
+    """... with queries of type dt."""
     shape, _, page = _page_strides(k_pages, v_pages)
     if len(shape) != 4:
         raise ValueError("attention takes one layer's pages: [num_pages, Hkv, page_size, D]")
-    dt = k_pages.dtype
     code = _code(dt)
     at = _current(q, "q")
     if k_pages.get_device() != at:
@@ -1383,3 +1394,61 @@ def pages_fork_e4m3(k_pages: torch.Tensor, v_pages: torch.Tensor, k_scales: torc
     call, L = (ctypes.byref(pool), ctypes.byref(scales)), lib()
     return _fork(L.dreams_pages_fork_e4m3, call, pool, at, k_pages, v_pages, page_table, page_count, kv_len, refcount, src,
                  dst, granted, stream)
+
+
+def _paged_desc8(q, k_pages, v_pages, k_scales, v_scales, page_table, window, sinks, max_kv_len, num_splits, scale):
+    """(PagedDesc, PageScales) of an attention call over pages of 8 bits"""
+    if isinstance(k_pages, torch.Tensor) and k_pages.dtype is not torch.float8_e4m3fn:
+        raise TypeError("k_pages must be torch.float8_e4m3fn, got %s" % k_pages.dtype)
+    desc = _paged_desc(q, k_pages, v_pages, page_table, torch.bfloat16, window, sinks, max_kv_len, num_splits, scale)
+    _, page = _scale_strides(k_scales, v_scales, k_pages.shape, q.get_device())
+    return desc, PageScales(k_scales.data_ptr(), v_scales.data_ptr(), 0, page)
+
+
+def paged_verify_attn_e4m3(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, k_scales: torch.Tensor,
+                           v_scales: torch.Tensor, page_table: torch.Tensor, kv_len: torch.Tensor,
+                           parent: Optional[torch.Tensor] = None, tree_mask: Optional[torch.Tensor] = None, window: int = 0,
+                           sinks: int = 0, scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                           lse: Optional[torch.Tensor] = None, with_lse: bool = True, max_kv_len: int = 0,
+                           num_splits: int = 0, workspace: Optional[torch.Tensor] = None,
+                           stream=None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """dreams_paged_verify_attn_e4m3: paged_verify_attn with bf16 queries over one layer's pages of 8 bits: k_pages / v_pages
+    [num_pages,Hkv,page_size,D] float8_e4m3fn, k_scales / v_scales [num_pages,Hkv,page_size/16] float8_e8m0fnu, as
+    paged_append_e4m3 writes them.  Returns (out, lse or None)."""
+    desc, scales = _paged_desc8(q, k_pages, v_pages, k_scales, v_scales, page_table, window, sinks, max_kv_len, num_splits,
+                                scale)
+    B, T, at = desc.batch, desc.num_rows, q.get_device()
+    _need_on(kv_len, "kv_len", torch.int32, at, (B,))
+    if parent is not None:
+        _need_on(parent, "parent", torch.int32, at, (B, T))
+    if tree_mask is not None:
+        _need_on(tree_mask, "tree_mask", torch.int64, at, (B, T, (T + 63) // 64))
+    out, lse = _paged_outputs(q, out, lse, with_lse, stream)
+    L = lib()
+    _call_paged(L.dreams_paged_verify_attn_e4m3, L.dreams_paged_verify_attn_e4m3_workspace_size, ctypes.byref(desc),
+                (q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), ctypes.byref(scales), page_table.data_ptr(),
+                 kv_len.data_ptr(), _ptr(parent), _ptr(tree_mask), out.data_ptr(), _ptr(lse)), workspace, at, stream)
+    return out, lse
+
+
+def paged_prompt_attn_e4m3(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, k_scales: torch.Tensor,
+                           v_scales: torch.Tensor, page_table: torch.Tensor, kv_len: torch.Tensor,
+                           row_len: Optional[torch.Tensor] = None, window: int = 0, sinks: int = 0,
+                           scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                           lse: Optional[torch.Tensor] = None, with_lse: bool = True, max_kv_len: int = 0,
+                           num_splits: int = 0, workspace: Optional[torch.Tensor] = None,
+                           stream=None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """dreams_paged_prompt_attn_e4m3: paged_prompt_attn with bf16 queries over one layer's pages of 8 bits (as in
+    paged_verify_attn_e4m3).  Returns (out, lse or None)."""
+    desc, scales = _paged_desc8(q, k_pages, v_pages, k_scales, v_scales, page_table, window, sinks, max_kv_len, num_splits,
+                                scale)
+    B, at = desc.batch, q.get_device()
+    _need_on(kv_len, "kv_len", torch.int32, at, (B,))
+    if row_len is not None:
+        _need_on(row_len, "row_len", torch.int32, at, (B,))
+    out, lse = _paged_outputs(q, out, lse, with_lse, stream)
+    L = lib()
+    _call_paged(L.dreams_paged_prompt_attn_e4m3, L.dreams_paged_prompt_attn_e4m3_workspace_size, ctypes.byref(desc),
+                (q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), ctypes.byref(scales), page_table.data_ptr(),
+                 kv_len.data_ptr(), _ptr(row_len), out.data_ptr(), _ptr(lse)), workspace, at, stream)
+    return out, lse

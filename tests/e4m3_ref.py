@@ -180,3 +180,40 @@ def spread_rows(rng, shape, dev, bf16):
     x[rng.random(shape) < 0.02] = 0
     t = torch.from_numpy(x).to(torch.bfloat16 if bf16 else torch.float32).to(dev)
     return t, t.double().cpu().numpy()
+
+
+class Cache8:
+    """One layer's pool in 8 bits with every sequence's pages at random places, as paged_ref.Cache: k and v are the values in 64
+    bits.  Slots that no sequence fills hold NaN and the largest codes, blocks without a filled slot any scale byte."""
+
+    def __init__(self, rng, dev, fill, Hkv, ps, D, paired=False, width=None, spare=3, scale=1.0):
+        fill = np.asarray(fill)
+        B = len(fill)
+        counts = -(-fill // ps)
+        self.width = max(int(counts.max()), 1) if width is None else width
+        P = int(counts.sum()) + spare
+        ids = rng.permutation(P)
+        self.table = rng.choice(np.array([-1, P, 2 ** 31 - 1, -2 ** 31], np.int64), size=(B, self.width)).astype(np.int32)
+        codes = rng.choice(np.array([0x7f, 0xff, 0x7e, 0xfe], np.uint8), size=(2, P, Hkv, ps, D))
+        scales = rng.integers(0, 256, size=(2, P, Hkv, ps // 16)).astype(np.uint8)
+        at = 0
+        for b in range(B):
+            self.table[b, :counts[b]] = ids[at:at + counts[b]]
+            at += counts[b]
+            for j0 in range(0, fill[b], 16):
+                page, r0, n = self.table[b, j0 // ps], j0 % ps, min(16, fill[b] - j0)
+                for half in range(2):
+                    for g in range(Hkv):
+                        x = (scale if half == 0 else 1.0) * rng.standard_normal((n, D)) * 2.0 ** rng.integers(-2, 2)
+                        byte = scale_byte(np.abs(x).max())
+                        codes[half, page, g, r0:r0 + n] = encode(x / power(byte))
+                        scales[half, page, g, r0 // 16] = byte
+        values = VALUES[codes] * np.repeat(power(scales), 16, axis=3)[..., None]
+        self.k, self.v = values
+        c, s = (torch.from_numpy(x).to(dev) for x in (codes, scales))
+        if paired:
+            c, s = (x.transpose(0, 1).contiguous().transpose(0, 1) for x in (c, s))
+        self.kd, self.vd = (c[i].view(torch.float8_e4m3fn) for i in range(2))
+        self.ksd, self.vsd = (s[i].view(torch.float8_e8m0fnu) for i in range(2))
+        self.tabled = torch.from_numpy(self.table).to(dev)
+        self.pages = (self.kd, self.vd, self.ksd, self.vsd, self.tabled)
