@@ -1324,11 +1324,10 @@ dreams_status_t plan_paged(const dreams_paged_desc_t* d, bool prompt, bool e4m3,
   // rows behind 2000 18.8, 22.2; 8 x 16 heads x 48 of 64 columns behind 1500 23.8, 25.8.  Where short keys meet many heads it is
   // the other way round: 16 x 8 heads x 64 rows of 64 columns behind 500 16.0, 13.5; 4 x 32 heads x 40 behind 1000 26.7, 23.1.)
   p.rows_per_wg = tree_attn_bf16_rows_per_wg(p.rows_total);
-  if (e4m3 && p.rows_per_wg > 64) p.rows_per_wg = 64;
   p.row_groups = (p.rows_total + p.rows_per_wg - 1) / p.rows_per_wg;
   p.units = d->batch * d->num_kv_heads;
   int span = T;   // positions that a workgroup's rows can be apart
-  if (prompt && p.row_groups > 1 && p.rows_per_wg == 128) {
+  if (prompt && p.row_groups > 1) {
     // Row groups of one head see only the keys before them; packed ones leave no row of a workgroup empty.  The fewer keys
     // decide (32 heads, 8 KV heads: 2000 rows 69 us packed, 48 by heads; 28 heads, 4 KV heads, 16 x 140 rows behind 1000 keys
     // 45 packed, 63 by heads).
@@ -1464,9 +1463,9 @@ dreams_status_t run_paged(const dreams_paged_desc_t* desc, bool prompt, const Pa
   a.k_scale = in.k_scale;
   a.v_scale = in.v_scale;
   a.scale_stride = in.scale_stride;
-  hipError_t e = e4m3                   ? launch_paged_attn_e4m3(a, stream)
-                 : a.rows_per_wg == 128 ? launch_paged_rows_bf16(a, stream)
-                                        : launch_paged_attn_bf16(a, stream);
+  hipError_t e;
+  if (a.rows_per_wg == 128) e = e4m3 ? launch_paged_rows_e4m3(a, stream) : launch_paged_rows_bf16(a, stream);
+  else e = e4m3 ? launch_paged_attn_e4m3(a, stream) : launch_paged_attn_bf16(a, stream);
   if (e != hipSuccess) return hip_fail(e, "paged attention launch");
   return ok();
 }

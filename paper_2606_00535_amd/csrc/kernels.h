@@ -379,7 +379,8 @@ inline long long paged_attn_f32_workgroups(int units, int G, int T) {   // of a 
 hipError_t launch_paged_attn_f32(const PagedAttnArgs& a, hipStream_t stream);
 hipError_t launch_paged_attn_bf16(const AttnArgs& a, hipStream_t stream);   // up to 64 rows a KV head
 hipError_t launch_paged_rows_bf16(const AttnArgs& a, hipStream_t stream);   // 128 rows a workgroup
-hipError_t launch_paged_attn_e4m3(const AttnArgs& a, hipStream_t stream);   // pages of 8 bits, up to 64 rows a workgroup
+hipError_t launch_paged_attn_e4m3(const AttnArgs& a, hipStream_t stream);   // pages of 8 bits: up to 64 rows a KV head
+hipError_t launch_paged_rows_e4m3(const AttnArgs& a, hipStream_t stream);   //   128 rows a workgroup
 
 struct PagedRowsArgs {
   char* k;                   // [NL][pages, Hkv, page_size, row bytes]
