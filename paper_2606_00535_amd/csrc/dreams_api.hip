@@ -1280,6 +1280,7 @@ struct PagedPlan {
   AttnPlan p;
   int groups_per_head, unit_parts;
   int longest, shortest;   // keys of a row group, by the host's bound
+  int spread_wgs;          // see AttnArgs
 };
 
 // Pieces of the key axis for workgroups of 128 rows, xcd_wgs on each XCD: the number that takes the least time, in keys that a
@@ -1304,6 +1305,20 @@ int paged_pieces(int n_keys, long long xcd_wgs, long long xcd_cus, bool level) {
     }
   }
   return pieces;
+}
+
+// Whether the keys of all sequences are spread over the workgroups in pieces of one length, with a second launch that merges
+// them (AttnArgs::spread_wgs), instead of as many pieces of every unit as merge on its die.  It costs 2 to 3 us more, 380
+// keys of a compute unit, and pays where units leave dies or compute units idle (a token's rows of 4 KV heads behind 32768:
+// 19.1 us, 24.4 in 32 pieces each; of 3 x 2 heads behind 8192 to 32768 19.7, 34.0; but 15.0 and 15.2 of 4 behind 8000), or
+// where a batch's long sequences may run on behind its short ones (16 x 4 heads behind 100 to 32768: 59, 68; where they
+// are of like lengths, 8 x 8 behind 16384 to 32768, 75.3 and 73.9).
+bool spread_pays(const dreams_paged_desc_t* d, const AttnPlan& p, int parts, int splits, int n_keys, int cus) {
+  if (p.row_groups != 1 || d->batch > kSpreadSeqs || 2 * p.units > cus) return false;
+  const long long even = ((long long)p.units * n_keys + cus - 1) / cus;      // keys of a compute unit, spread
+  if (d->batch > 1 && even >= 4096) return true;
+  const long long dies = 8 / parts, wgs = (p.units + dies - 1) / dies * splits, xcd_cus = std::max(cus / 8, 1);
+  return (wgs + xcd_cus - 1) / xcd_cus * ((n_keys + splits - 1) / splits) >= even + 380;
 }
 
 dreams_status_t plan_paged(const dreams_paged_desc_t* d, bool prompt, bool e4m3, PagedPlan* plan) {
@@ -1356,7 +1371,8 @@ dreams_status_t plan_paged(const dreams_paged_desc_t* d, bool prompt, bool e4m3,
     int cus = 0;
     st = device_cus(&cus);
     if (st != DREAMS_OK) return st;
-    const int wpc = tree_attn_bf16_wgs_per_cu(p.rows_per_wg);
+    const int wpc = e4m3 && p.rows_per_wg < 128 ? paged_attn_e4m3_wgs_per_cu(p.rows_per_wg)
+                                                : tree_attn_bf16_wgs_per_cu(p.rows_per_wg);
     const long long xcd_cus = std::max(cus / 8, 1);
     splits = coarse_splits(8 * xcd_wgs, (long long)cus * wpc, n_keys);
     if (splits > kAttnMaxSplits) splits = kAttnMaxSplits;
@@ -1365,6 +1381,14 @@ dreams_status_t plan_paged(const dreams_paged_desc_t* d, bool prompt, bool e4m3,
     } else if (splits > 1 && xcd_wgs < xcd_cus * wpc) {
       const int fine = fine_splits(xcd_wgs, xcd_cus, wpc, n_keys);
       if (fine < splits || 5 * fine >= 7 * splits) splits = fine;
+    }
+    if (e4m3 && spread_pays(d, p, parts, std::max(splits, 1), n_keys, cus)) {
+      plan->spread_wgs = std::max(p.rows_per_wg == 64 ? 2 * cus : cus, 2 * p.units);
+      const size_t rows = (size_t)plan->spread_wgs * p.rows_per_wg;
+      p.o_off = kCounterBytes;
+      p.ml_off = p.o_off + align_up(rows * d->head_dim * 4, 256);
+      p.bytes = p.ml_off + align_up(rows * 2 * sizeof(float), 256);
+      return DREAMS_OK;
     }
   }
   const int max_splits = (n_keys + kPieceMinKeys - 1) / kPieceMinKeys;
@@ -1463,6 +1487,7 @@ dreams_status_t run_paged(const dreams_paged_desc_t* desc, bool prompt, const Pa
   a.k_scale = in.k_scale;
   a.v_scale = in.v_scale;
   a.scale_stride = in.scale_stride;
+  a.spread_wgs = plan.spread_wgs;
   hipError_t e;
   if (a.rows_per_wg == 128) e = e4m3 ? launch_paged_rows_e4m3(a, stream) : launch_paged_rows_bf16(a, stream);
   else e = e4m3 ? launch_paged_attn_e4m3(a, stream) : launch_paged_attn_bf16(a, stream);

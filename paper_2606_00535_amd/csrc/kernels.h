@@ -119,7 +119,11 @@ struct AttnArgs {
   const uint8_t* k_scale;
   const uint8_t* v_scale;
   int64_t scale_stride;
+  // ... and at most kSpreadSeqs sequences of one row group a unit: workgroups that all of their keys are spread over, in pieces
+  // of one length (spread_plan), whose rows a second launch merges; 0: as above
+  int spread_wgs;
 };
+constexpr int kSpreadSeqs = 64;
 
 // Query rows per workgroup the bf16 kernel uses for G*T rows per KV head.
 int tree_attn_bf16_rows_per_wg(int rows_total);
@@ -380,6 +384,7 @@ hipError_t launch_paged_attn_f32(const PagedAttnArgs& a, hipStream_t stream);
 hipError_t launch_paged_attn_bf16(const AttnArgs& a, hipStream_t stream);   // up to 64 rows a KV head
 hipError_t launch_paged_rows_bf16(const AttnArgs& a, hipStream_t stream);   // 128 rows a workgroup
 hipError_t launch_paged_attn_e4m3(const AttnArgs& a, hipStream_t stream);   // pages of 8 bits: up to 64 rows a KV head
+int paged_attn_e4m3_wgs_per_cu(int rows_per_wg);   // workgroups of that configuration per compute unit
 hipError_t launch_paged_rows_e4m3(const AttnArgs& a, hipStream_t stream);   //   128 rows a workgroup
 
 struct PagedRowsArgs {

@@ -70,6 +70,7 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 constexpr float kLn2 = 0.69314718055994530942f;
 constexpr int kStep = 32;          // keys per step
+constexpr int kSpreadMinSteps = 4; // steps of a piece of spread keys, at least
 constexpr float kLazyLog2 = 8.0f;  // slack of the running maximum, log2 units
 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -333,6 +334,50 @@ __device__ __forceinline__ void merge_set(const AttnArgs& a, size_t pset, int R,
   }
 }
 
+// Pieces of one length over every sequence (spread_wgs), so that a batch's long sequences take no longer than its short
+// ones and the units need not be as many as the dies: lane b holds sequence b's steps and pieces.  The length is the
+// smallest of 64 candidates (from what the workgroups would need without rounding up, 1/24 of it apart) with no more pieces
+// than workgroups.  Every wave that asks computes the same.
+struct SpreadPlan {
+  int steps, pieces;    // of the lane's sequence; pieces of one KV head
+  int piece;            // steps of a piece
+};
+__device__ __forceinline__ int ceil_div(int x, int y, float inv) {   // x >= 1, y >= 1, inv near 1 / y
+  int q = (int)((float)(x - 1) * inv);
+  int r = x - 1 - q * y;
+  q += r >= y ? 1 : 0;
+  q -= r < 0 ? 1 : 0;
+  return q + 1;
+}
+__device__ __forceinline__ SpreadPlan spread_plan(const AttnArgs& a, int lane) {
+  SpreadPlan sp;
+  sp.steps = 0;
+  if (lane < a.B) {
+    int nb = a.T;
+    if (a.chain && a.row_len) nb = min(max(a.row_len[lane], 0), a.T);
+    const int Lp = min(max(a.kv_len[lane], 0), a.S_cap - nb);
+    const int N = nb > 0 ? Lp + nb : 0;
+    int gap = 0;
+    if (a.window > 0 && N > 0) {
+      const int low = max(Lp - a.window + 1, 0);
+      gap = max(low / kStep * kStep - (min(a.sinks, low) + kStep - 1) / kStep * kStep, 0);
+    }
+    sp.steps = max((N - gap + kStep - 1) / kStep, 1);    // (a sequence without keys has its rows' zeros to write)
+  }
+  int total = sp.steps;      // (below 2^31: 64 sequences of 2^25 steps at most)
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) total += __shfl_xor(total, off);
+  const int even = (int)(((long long)total * a.Hkv + a.spread_wgs - 1) / a.spread_wgs);
+  const int base = max(even, kSpreadMinSteps), mine = base + (int)((long long)base * lane / 24);
+  const float inv = 1.0f / (float)mine;
+  long long count = 0;
+  for (int b = 0; b < a.B; ++b) count += ceil_div(__builtin_amdgcn_readlane(sp.steps, b), mine, inv);
+  const uint64_t fits = __ballot(count * a.Hkv <= a.spread_wgs);
+  sp.piece = __builtin_amdgcn_readlane(mine, fits ? __builtin_ctzll(fits) : 63);
+  sp.pieces = sp.steps > 0 ? ceil_div(sp.steps, sp.piece, 1.0f / (float)sp.piece) : 0;
+  return sp;
+}
+
 // LDS of a workgroup: the ring, the query rows when they sit beside it, the ancestor sets and the tree as
 // copied (static), and a few words; WPC workgroups share a compute unit's 160 KB.
 // (E8: steps of half the bytes, and a word for each of a step's four scales)
@@ -391,7 +436,24 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
   const int n = blockIdx.x;
   const int xcd = n & 7, slot = n >> 3;
   int u, split, rg;
-  if constexpr (PAGED) {
+  [[maybe_unused]] int spread_pieces = 0, spread_piece = 0;   // (spread: the unit's pieces, steps of one)
+  bool placed = false;
+  if constexpr (E8) placed = a.spread_wgs > 0;
+  if (placed) {
+    const SpreadPlan sp = spread_plan(a, threadIdx.x & 63);
+    int first = 0, seq = 0, pieces = 0;
+    for (; seq < a.B; ++seq) {
+      pieces = __builtin_amdgcn_readlane(sp.pieces, seq);
+      if (n < first + pieces * a.Hkv) break;
+      first += pieces * a.Hkv;
+    }
+    if (seq == a.B) return;
+    split = (n - first) / a.Hkv;      // (a piece's heads beside one another, as in the pages)
+    u = seq * a.Hkv + (n - first) - split * a.Hkv;
+    rg = 0;
+    spread_pieces = pieces;
+    spread_piece = sp.piece;
+  } else if constexpr (PAGED) {
     // Every unit's row groups are dealt to unit_parts parts (units * unit_parts is a multiple of 8), a part to an XCD.
     // An XCD takes the q-th row group of all of its parts before the next.
     const int here = a.units * a.unit_parts / 8;
@@ -457,10 +519,16 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
   int keys = a.max_keys;
   if constexpr (PAGED) keys = N_paged - gap;
   else if (a.piece_by_len) keys = min(max(kv_len_b, 0), a.S_cap - T) + T;
-  int piece = (keys + a.splits - 1) / a.splits;
+  int piece = (keys + a.splits - 1) / a.splits, last = a.splits - 1;
   piece = (piece + kStep - 1) / kStep * kStep;
+  if constexpr (E8) {
+    if (placed) {
+      piece = spread_piece * kStep;
+      last = spread_pieces - 1;
+    }
+  }
   const int k_begin = split * piece;
-  const int k_end_plan = split == a.splits - 1 ? keys : min(keys, k_begin + piece);
+  const int k_end_plan = split == last ? keys : min(keys, k_begin + piece);
   const int nplan = k_end_plan > k_begin ? (k_end_plan - k_begin + kStep - 1) / kStep : 0;
   const int nsp = (nplan + KW - 1) / KW;
   const size_t head_off = PAGED ? ((size_t)g << a.page_shift) * V::ROW : (size_t)u * a.S_cap * V::ROW;
@@ -593,7 +661,7 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
   if constexpr (PAGED) Lp = Lp_paged;
   const int N = PAGED ? N_paged : Lp + T;
   // the last piece runs to this sequence's true end, whatever the host's bound said
-  const int k_end = split == a.splits - 1 ? N - gap : min(N - gap, k_begin + piece);
+  const int k_end = split == last ? N - gap : min(N - gap, k_begin + piece);
   const int nact = k_end > k_begin ? (k_end - k_begin + kStep - 1) / kStep : 0;
   const int nsa = (nact + KW - 1) / KW;
 
@@ -1126,8 +1194,10 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
   const size_t prow0 = pset * S * R;   // the set's piece 0, row 0
   const int rows_valid = min(R, rows_here);
   if constexpr (PAGED) {
-    if (S > 1) {   // (a piece's rows go to the workspace in fp32, straight from the registers)
-      float* const dst = (float*)a.part_o + (prow0 + (size_t)split * R) * D;
+    if (S > 1 || placed) {   // (a piece's rows go to the workspace in fp32, straight from the registers)
+      size_t prow = prow0 + (size_t)split * R;
+      if (placed) prow = (size_t)n * R;
+      float* const dst = (float*)a.part_o + prow * D;
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
         const int rl = rh * RW + rb * 16 + col;
@@ -1136,8 +1206,9 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
 #pragma unroll
         for (int dd = 0; dd < DBK; ++dd) *(f32x4*)(dst + (size_t)rl * D + c0 + dd * 16) = fin[rb][dd] * inv;
         if (kw == 0 && quad == 0)
-          *(float2*)(a.part_ml + 2 * (prow0 + (size_t)split * R + rl)) = make_float2(m_run[rb], l_run[rb]);
+          *(float2*)(a.part_ml + 2 * (prow + rl)) = make_float2(m_run[rb], l_run[rb]);
       }
+      if (placed) return;
       merge_set<D, W, ENT, float>(a, pset, R, split, start_old, qrow0 + (size_t)row_base, rows_valid, &merge_lds,
                                 &good_lds);
       return;
@@ -1201,6 +1272,61 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
   merge_set<D, W, ENT, __bf16>(a, pset, R, split, start_old, qrow0 + (size_t)row_base, rows_valid, &merge_lds, &good_lds);
 }
 
+// The rows of spread keys: a workgroup per row of a unit, its pieces dealt to groups of D / 8 threads (8 columns each), whose
+// sums meet in LDS in group order.
+template <int D>
+__global__ __launch_bounds__(256) void spread_merge_kernel(AttnArgs a, int R) {
+  constexpr int LANES = D / 8, GROUPS = 256 / LANES, PCH = 4;
+  typedef float f32x8 __attribute__((ext_vector_type(8)));
+  __shared__ f32x8 sums[GROUPS][LANES];
+  __shared__ float2 mls[GROUPS];
+  const int u = blockIdx.x, row = blockIdx.y, seq = u / a.Hkv, g = u - seq * a.Hkv;
+  const SpreadPlan sp = spread_plan(a, threadIdx.x & 63);
+  int first = g;
+  for (int b = 0; b < seq; ++b) first += __builtin_amdgcn_readlane(sp.pieces, b) * a.Hkv;
+  const int S = __builtin_amdgcn_readlane(sp.pieces, seq);
+  const int group = threadIdx.x / LANES, ch = threadIdx.x % LANES;
+  float M = -INFINITY, lsum = 0.f;
+  f32x8 acc;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+  auto join = [&](float m, float l, const f32x8& x, float weight) {   // (m, l) of a state and its rows times `weight`
+    const float Mn = fmaxf(M, m);
+    const float wo = M == -INFINITY ? 0.f : fast_exp2(M - Mn), w = m == -INFINITY ? 0.f : fast_exp2(m - Mn);
+    lsum = lsum * wo + l * w;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] = acc[e] * wo + w * weight * x[e];
+    M = Mn;
+  };
+  for (int s0 = group; s0 < S; s0 += GROUPS * PCH) {
+    f32x8 x[PCH];
+    float2 ml[PCH];
+#pragma unroll
+    for (int k = 0; k < PCH; ++k) {   // (all in flight; those past the last piece repeat it)
+      const size_t at = ((size_t)first + (size_t)min(s0 + k * GROUPS, S - 1) * a.Hkv) * R + row;
+      ml[k] = *(const float2*)(a.part_ml + 2 * at);
+      x[k] = *(const f32x8*)((const float*)a.part_o + at * D + ch * 8);
+    }
+#pragma unroll
+    for (int k = 0; k < PCH; ++k)
+      if (s0 + k * GROUPS < S) join(ml[k].x, ml[k].y, x[k], ml[k].y);
+  }
+  sums[group][ch] = acc;
+  if (ch == 0) mls[group] = make_float2(M, lsum);
+  __syncthreads();
+  if (group > 0) return;
+  const int live = min(S, GROUPS);
+  for (int k = 1; k < live; ++k) join(mls[k].x, mls[k].y, sums[k][ch], 1.f);
+  const size_t orow = ((size_t)seq * a.Hq + (size_t)g * a.G) * a.T + row;
+  const bool some = lsum != 0.f;        // (a NaN sum gives a NaN)
+  const float inv = some ? 1.0f / lsum : 0.f;
+  bf16x8 res;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) res[e] = (__bf16)(acc[e] * inv);
+  *(bf16x8*)((__bf16*)a.out + orow * D + ch * 8) = res;
+  if (ch == 0 && a.lse) a.lse[orow] = some ? (M + __log2f(lsum)) * kLn2 : -INFINITY;
+}
+
 template <int D, int RB, int KW, int W, int NST, int WPC, bool ENT, bool PAGED, bool E8 = false>
 hipError_t launch_streaming(const AttnArgs& a, hipStream_t stream) {
   constexpr size_t lds = dynamic_lds<D, NST, WPC, E8>(16 * RB * (W / KW));
@@ -1220,7 +1346,19 @@ hipError_t launch_streaming(const AttnArgs& a, hipStream_t stream) {
   if (a.splits > 1 && a.ctr_stride < 2) return hipErrorInvalidValue;
   const unsigned units_rounded = PAGED ? a.units * a.unit_parts : (a.units + 7) / 8 * 8;
   const unsigned groups = PAGED ? (a.row_groups + a.unit_parts - 1) / a.unit_parts : a.row_groups;
-  const unsigned grid = units_rounded * (unsigned)a.splits * groups;
+  unsigned grid = units_rounded * (unsigned)a.splits * groups;
+  if constexpr (E8) {
+    if (a.spread_wgs > 0) {
+      if (a.row_groups != 1 || a.splits != 1 || a.B > kSpreadSeqs || a.spread_wgs < 2 * a.units || !a.part_o || !a.part_ml)
+        return hipErrorInvalidValue;
+      hipLaunchKernelGGL(kern, dim3((unsigned)a.spread_wgs), dim3(64 * W), lds, stream, a);
+      hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+      hipLaunchKernelGGL(spread_merge_kernel<D>, dim3((unsigned)a.units, (unsigned)(a.G * a.T)), dim3(256), 0, stream, a,
+                         a.rows_per_wg);
+      return hipGetLastError();
+    }
+  }
   hipLaunchKernelGGL(kern, dim3(grid), dim3(64 * W), lds, stream, a);
   return hipGetLastError();
 }

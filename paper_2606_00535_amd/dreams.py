@@ -852,9 +852,12 @@ def _current(t: torch.Tensor, name: str, dtype=None) -> int:
 
 def _need_on(t: torch.Tensor, name: str, dtype, at: int, shape=None, ndim=None):
     """As _need, for a device index, a whole shape or a number of dimensions."""
-    if (isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == at and t.is_contiguous()
-            and (shape is None or t.shape == shape) and (ndim is None or t.dim() == ndim)):
-        return
+    try:
+        if (t.dtype is dtype and t.get_device() == at and t.is_contiguous() and (shape is None or t.shape == shape)
+                and (ndim is None or t.dim() == ndim)):
+            return
+    except AttributeError:
+        pass
     _need(t, name, dtype, torch.device("cuda", at), ndim)
     raise ValueError("%s must be %s, got %s" % (name, list(shape), list(t.shape)))
 
@@ -865,7 +868,7 @@ def _page_strides(k_pages: torch.Tensor, v_pages: torch.Tensor):
     for t, name in ((k_pages, "k_pages"), (v_pages, "v_pages")):
         if not isinstance(t, torch.Tensor):
             raise TypeError("%s must be a torch.Tensor" % name)
-    shape, st, vst = k_pages.shape, k_pages.stride(), v_pages.stride()
+    shape = k_pages.shape
     if k_pages.dtype is not v_pages.dtype:
         raise TypeError("k_pages and v_pages differ in dtype")
     if k_pages.get_device() != v_pages.get_device():
@@ -876,6 +879,9 @@ def _page_strides(k_pages: torch.Tensor, v_pages: torch.Tensor):
     if n not in (4, 5):
         raise ValueError("k_pages and v_pages must be [NL,] num_pages, Hkv, page_size, D")
     P, H, S, D = shape[-4:]
+    if k_pages.is_contiguous() and v_pages.is_contiguous():      # (most pools: nothing else to look at)
+        return shape, P * H * S * D if n == 5 and shape[0] > 1 else 0, H * S * D
+    st, vst = k_pages.stride(), v_pages.stride()
     # (a stride along an axis of one entry is not used)
     if st != vst and any(shape[i] > 1 and st[i] != vst[i] for i in range(n)):
         raise ValueError("k_pages and v_pages differ in layout")
@@ -1065,7 +1071,7 @@ def _new_rows(k_new, v_new, k_pages, pool, at, dt, kv_len, row_len):
     """The strides of new rows of type dt, once they and their lengths are checked against the pool."""
     B, n = pool.batch, k_pages.dim()
     for t, name in ((k_new, "k_new"), (v_new, "v_new")):
-        if not isinstance(t, torch.Tensor):
+        if type(t) is not torch.Tensor and not isinstance(t, torch.Tensor):
             raise TypeError("%s must be a torch.Tensor" % name)
         if t.dtype is not dt:
             raise TypeError("%s must be %s, got %s" % (name, dt, t.dtype))
@@ -1289,13 +1295,23 @@ def paged_append_rope(k_new: torch.Tensor, v_new: torch.Tensor, k_pages: torch.T
 
 
 # --------------------------------------------------------------------------------------------- pages of 8 bits
+_E4M3, _E8M0 = torch.float8_e4m3fn, torch.float8_e8m0fnu
+
+
 def _scale_strides(k_scales, v_scales, shape, at):
     """(layer stride, page stride) of the scales [NL, P, Hkv, page_size / 16] of pages of this shape."""
-    want = shape[:-2] + (shape[-2] // 16,)
+    P, H, S = shape[-4], shape[-3], shape[-2] // 16
+    want = (P, H, S) if len(shape) == 4 else (shape[0], P, H, S)
+    try:
+        if (k_scales.dtype is _E8M0 and v_scales.dtype is _E8M0 and k_scales.get_device() == at == v_scales.get_device()
+                and k_scales.shape == want == v_scales.shape and k_scales.is_contiguous() and v_scales.is_contiguous()):
+            return P * H * S if len(want) == 4 and want[0] > 1 else 0, H * S
+    except AttributeError:
+        pass
     for t, name in ((k_scales, "k_scales"), (v_scales, "v_scales")):
         if not isinstance(t, torch.Tensor):
             raise TypeError("%s must be a torch.Tensor" % name)
-        if t.dtype is not torch.float8_e8m0fnu:
+        if t.dtype is not _E8M0:
             raise TypeError("%s must be torch.float8_e8m0fnu, got %s" % (name, t.dtype))
         if t.get_device() != at:
             raise ValueError("%s is on %s, not with the pages" % (name, t.device))
@@ -1304,7 +1320,6 @@ def _scale_strides(k_scales, v_scales, shape, at):
     n, st, vst = len(want), k_scales.stride(), v_scales.stride()
     if any(want[i] > 1 and st[i] != vst[i] for i in range(n)):
         raise ValueError("k_scales and v_scales differ in layout")
-    P, H, S = want[-3:]
     if (S > 1 and st[-1] != 1) or (H > 1 and st[-2] != S):
         raise ValueError("a page's scales must be dense [Hkv, page_size / 16]")
     if (P > 1 and st[-3] == 0) or (n == 4 and want[0] > 1 and st[0] == 0):
@@ -1314,7 +1329,7 @@ def _scale_strides(k_scales, v_scales, shape, at):
 
 def _pool8(k_pages, v_pages, k_scales, v_scales, page_table):
     """(PagePool, PageScales, device index) of pages of 8 bits"""
-    if isinstance(k_pages, torch.Tensor) and k_pages.dtype is not torch.float8_e4m3fn:
+    if isinstance(k_pages, torch.Tensor) and k_pages.dtype is not _E4M3:
         raise TypeError("k_pages must be torch.float8_e4m3fn, got %s" % k_pages.dtype)
     pool, at = _pool(k_pages, v_pages, page_table, DREAMS_E4M3)
     layer, page = _scale_strides(k_scales, v_scales, k_pages.shape, at)
@@ -1398,7 +1413,7 @@ def pages_fork_e4m3(k_pages: torch.Tensor, v_pages: torch.Tensor, k_scales: torc
 
 def _paged_desc8(q, k_pages, v_pages, k_scales, v_scales, page_table, window, sinks, max_kv_len, num_splits, scale):
     """(PagedDesc, PageScales) of an attention call over pages of 8 bits"""
-    if isinstance(k_pages, torch.Tensor) and k_pages.dtype is not torch.float8_e4m3fn:
+    if isinstance(k_pages, torch.Tensor) and k_pages.dtype is not _E4M3:
         raise TypeError("k_pages must be torch.float8_e4m3fn, got %s" % k_pages.dtype)
     desc = _paged_desc(q, k_pages, v_pages, page_table, torch.bfloat16, window, sinks, max_kv_len, num_splits, scale)
     _, page = _scale_strides(k_scales, v_scales, k_pages.shape, q.get_device())

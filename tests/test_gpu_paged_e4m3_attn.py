@@ -267,3 +267,82 @@ def test_a_step_as_a_server_runs_it(dev):
             lens[b] += int(taken[b]) + 1
         assert kv.tolist() == lens
         dreams.pages_release(table, count, kv, ref, R.ints([0, 1], dev), ps, trim=True)
+
+
+def spread(q, c, **kw):
+    """Whether the library spreads a call's keys in pieces of one length (its workspace has room for their rows alone)."""
+    import ctypes
+    desc, _ = dreams._paged_desc8(q, *c.pages, kw.get("window", 0), kw.get("sinks", 0), kw.get("max_kv_len", 0), 0, None)
+    n, lib = ctypes.c_size_t(0), dreams.lib()
+    size = lib.dreams_paged_prompt_attn_e4m3_workspace_size if kw.get("prompt") else lib.dreams_paged_verify_attn_e4m3_workspace_size
+    assert size(ctypes.byref(desc), ctypes.byref(n)) == 0
+    rows = desc.num_q_heads // desc.num_kv_heads * desc.num_rows
+    rows = 16 if rows <= 16 else 32 if rows <= 32 else 64
+    cus = torch.cuda.get_device_properties(0).multi_processor_count
+    wgs = max(2 * cus if rows == 64 else cus, 2 * desc.batch * desc.num_kv_heads)
+    return n.value == dreams.WORKSPACE_COUNTER_BYTES + wgs * rows * (desc.head_dim * 4 + 8)
+
+
+# heads, D, lengths, T, window, sinks, mask
+SPREAD = [
+    ((4, 1), 128, [8000, 10, 3333], 1, 0, 0, False),
+    ((7, 1), 128, [6100, 0, 5, 2048, 700], 4, 0, 0, False),
+    ((2, 1), 64, [15000], 1, 0, 0, False),
+    ((3, 1), 64, [6500, 4095, 1], 5, 0, 0, True),
+    ((4, 1), 128, [6200, 4100, 900], 14, 0, 0, False),
+    ((16, 2), 128, [3900, 17, 8000], 2, 0, 0, False),
+    ((2, 1), 128, [9000, 300, 8000], 9, 7000, 40, False),
+]
+
+
+@pytest.mark.parametrize("kind", ["verify", "prompt"])
+@pytest.mark.parametrize("heads,D,lens,T,window,sinks,masked", SPREAD)
+def test_long_keys_of_few_heads(dev, heads, D, lens, T, window, sinks, masked, kind):
+    """Pieces of one length over every sequence and a second launch that merges them; twice the same, bit for bit."""
+    rng = np.random.default_rng(9)
+    B, (Hq, Hkv), ps = len(lens), heads, 64
+    note("spread", heads, D, lens, T, window, sinks, masked, kind)
+    c = E.Cache8(rng, dev, np.array(lens) + T, Hkv, ps, D)
+    q, qh = R.rounded(rng, (B, Hq, T, D), True, dev)
+    kw = dict(window=window, sinks=sinks, max_kv_len=max(lens))
+    assert spread(q, c, prompt=kind == "prompt", **kw)
+    kv = R.ints(lens, dev)
+    if kind == "verify":
+        par = R.tree(rng, B, T)
+        see = R.ancestors(par)
+        if masked:
+            see &= rng.random(see.shape) < 0.5
+        mask = torch.from_numpy(R.mask_bits(see)).to(dev) if masked else None
+        want = R.verify(qh, c.k, c.v, c.table, lens, par, see, window, sinks, 1 / np.sqrt(D))
+        run = lambda: dreams.paged_verify_attn_e4m3(q, *c.pages, kv, parent=R.ints(par, dev), tree_mask=mask, **kw)
+    else:
+        rows = [T if b != 1 else 0 for b in range(B)]       # (a sequence without rows: zeros)
+        rl = R.ints(rows, dev)
+        want = R.prompt(qh, c.k, c.v, c.table, lens, rows, window, sinks, 1 / np.sqrt(D))
+        run = lambda: dreams.paged_prompt_attn_e4m3(q, *c.pages, kv, rl, **kw)
+    out, lse = run()
+    R.check(out, lse, want, True, (heads, lens, kind))
+    again = run()
+    assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
+
+
+def test_long_keys_replayed(dev):
+    """Lengths that change between replays change the pieces."""
+    rng = np.random.default_rng(10)
+    D, ps, B, T = 128, 16, 3, 2
+    c = E.Cache8(rng, dev, [7200, 7200, 7200], 1, ps, D)
+    q, qh = R.rounded(rng, (B, 4, T, D), True, dev)
+    par = R.tree(rng, B, T)
+    kv, pard = R.ints([4000, 4000, 4000], dev), R.ints(par, dev)
+    assert spread(q, c, max_kv_len=7198)
+    run = lambda: dreams.paged_verify_attn_e4m3(q, *c.pages, kv, parent=pard, max_kv_len=7198)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = run()
+    for lens in ([7198, 1, 300], [0, 0, 0], [31, 4100, 2500]):
+        kv.copy_(torch.tensor(lens, dtype=torch.int32))
+        g.replay()
+        torch.cuda.synchronize()
+        got = [x.clone() for x in out]
+        R.check(*got, R.verify(qh, c.k, c.v, c.table, lens, par, R.ancestors(par), 0, 0, 1 / np.sqrt(D)), True, lens)
+        assert all(torch.equal(a, b) for a, b in zip(got, run()))
