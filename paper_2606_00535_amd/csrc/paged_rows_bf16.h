@@ -170,6 +170,9 @@ __global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(At
   const const_table table = (const_table)(uintptr_t)(a.table + (size_t)b * a.width);
   const int ps1 = (1 << a.page_shift) - 1;
   constexpr int ROW = E8 ? D : L::ROW;     // bytes of a row in its page
+  // E8: the next stage is converted between a stage's two tiles (24 heads of 64 columns on 3 x 333 ragged rows 34.7 us, 36.8
+  // ahead of the barrier), where registers allow: at D = 128 it would spill 110 of them.
+  constexpr bool kMidway = E8 && D == 64;
   const size_t head_off = ((size_t)g << a.page_shift) * ROW;
   const unsigned char* kbase = (const unsigned char*)a.k + head_off;
   const unsigned char* vbase = (const unsigned char*)a.v + head_off;
@@ -217,21 +220,35 @@ __global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(At
     before_scale = scale_at;
     page = look_up(key_slot(j + 1));
   };
-  auto write_codes = [&](int j) {   // of stage j; rows that no row of the workgroup sees become zeros
-    unsigned char* stage = ring + (j % L::STAGES) * L::STAGE;
-    const bool whole = j >= whole0 && j < whole1;
+  // Stage j to its slot (a constant in the unrolled loop: offsets are immediate); rows that no row of the workgroup sees
+  // become zeros.
+  typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+  uint32_t write_at[E8 ? L::COPIES : 1];
+  if constexpr (E8) {
+#pragma unroll
+    for (int c = 0; c < L::COPIES; ++c)
+      write_at[c] = ring_lds + wave * L::BLOCK + L::off(c * (64 / L::CPR) + lane / L::CPR, lane % L::CPR);
+  }
+  auto write_codes = [&](int j, int slot) {
+    if (j < whole0 || j >= whole1) {
+#pragma unroll
+      for (int part = 0; part < 2; ++part) {
+        const int s0 = part ? value_slot(j) : key_slot(j);
+#pragma unroll
+        for (int c = 0; c < L::COPIES; ++c) {
+          const int s = s0 + c * (64 / L::CPR) + lane / L::CPR;
+          if (s >= N || (s < low && s >= sink_end)) codes[part][c] = u32x2{0u, 0u};
+        }
+      }
+    }
 #pragma unroll
     for (int part = 0; part < 2; ++part) {
-      unsigned char* at = stage + (part ? value_at : wave * L::BLOCK);
       const float scale = __builtin_bit_cast(float, min(scale_bytes[part], 254u) << 23);
-      const int s0 = part ? value_slot(j) : key_slot(j);
+      const uint32_t to = part ? value_at - wave * L::BLOCK : 0u;
 #pragma unroll
-      for (int c = 0; c < L::COPIES; ++c) {
-        const int r = c * (64 / L::CPR) + lane / L::CPR, s = s0 + r;
-        u32x4 x = __builtin_bit_cast(u32x4, decode8(codes[part][c][0], codes[part][c][1], scale, scale));
-        if (!whole && (s >= N || (s < low && s >= sink_end))) x = u32x4{0u, 0u, 0u, 0u};
-        *(u32x4*)(at + L::off(r, lane % L::CPR)) = x;
-      }
+      for (int c = 0; c < L::COPIES; ++c)
+        *(lds_u32x4*)(uintptr_t)(write_at[c] + to + slot * L::STAGE) =
+            __builtin_bit_cast(u32x4, decode8(codes[part][c][0], codes[part][c][1], scale, scale));
     }
   };
   auto issue = [&](int j) {
@@ -281,6 +298,10 @@ __global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(At
   if constexpr (E8) {
     before_scale = scale_offset(page_before, slot_before);
     if (periods > 0) load_codes(0);
+    if constexpr (kMidway) {
+      if (periods > 0) write_codes(0, 0);
+      if (periods > 1) load_codes(1);
+    }
   } else {
     for (int j = 0; j < AHEAD; ++j)
       if (j < periods) issue(j);
@@ -515,10 +536,13 @@ __global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(At
   };
   constexpr std::true_type yes{};
   constexpr std::false_type no{};
-  auto next_stage = [&](int j) {
+  auto next_stage = [&](int j, int slot) {
     if constexpr (E8) {
-      write_codes(j);      // (its slot is free: every wave was past stage j - STAGES at the last barrier)
-      if (j + 1 < periods) load_codes(j + 1);
+      // (a stage's slot is free: every wave was past stage j - STAGES at the last barrier)
+      if constexpr (!kMidway) {
+        write_codes(j, slot);
+        if (j + 1 < periods) load_codes(j + 1);
+      }
       barrier_lds();
       return;
     }
@@ -560,8 +584,12 @@ __global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(At
     for (int x = 0; x < L::STAGES; ++x) {
       const int j = j0 + x;
       if (j >= periods) break;
-      next_stage(j);
+      next_stage(j, x);
       step(2 * j, s0, s1, x * L::STAGE);
+      if constexpr (kMidway) {
+        if (j + 1 < periods) write_codes(j + 1, (x + 1) % L::STAGES);
+        if (j + 2 < periods) load_codes(j + 2);
+      }
       step(2 * j + 1, s1, s0, x * L::STAGE + kTile * L::ROW);
       if (wave_tiles >> 1 == j) {   // the value product of the wave's last tile
         if (wave_tiles & 1) s1 = s0;
