@@ -2057,7 +2057,7 @@ dreams_status_t dreams_paged_read_e4m3(const dreams_page_pool_t* pool, const dre
   if (num_slots < 0 || num_slots > kPagedMaxSlots)
     return fail(DREAMS_ERR_INVALID_ARG, "num_slots = %d outside [0, %d]", num_slots, kPagedMaxSlots);
   if ((long long)pool->batch * pool->num_kv_heads > 65535) return fail(DREAMS_ERR_UNSUPPORTED, "problem too large");
-  st = check_units(num_slots, 1, pool->head_dim / 16);
+  st = check_units(num_slots, 1, pool->head_dim / 8);
   if (st != DREAMS_OK) return st;
   if (pool->batch == 0 || num_slots == 0) return ok();
   if (!k_pages || !v_pages || !page_table || !kv_len || !k_out || !v_out)

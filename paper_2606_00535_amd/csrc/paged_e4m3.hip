@@ -6,18 +6,22 @@
 //   * commit: a wave per (layer, sequence, KV head) and K or V, which goes through the path's blocks in order: a block's rows are
 //     in registers before one is written.  As in the 16-bit cache a row's source lies at or behind its slot, so that no
 //     block's rows or scale are changed before they are read.
-//   * read: a thread per 16 codes.
+//   * read: a thread per 8 codes.
 // A code times a power of two is exact in bf16, and a scale that grows moves a code's exponent: only codes that fall below
 // e4m3's normal range are rounded again.
 #include "rope.h"
+
+#include <algorithm>
 
 namespace dreams {
 namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kThreads = 256;
+constexpr int kMaxTurns = 4 * kScaleBlock * (kRopeMaxDim / 2);   // of the keys of 4 blocks (the queries': fewer)
 
 // 2^(byte - 127) of bytes 1 .. 254
 __device__ __forceinline__ float power(int byte) { return __builtin_bit_cast(float, (uint32_t)byte << 23); }
@@ -63,28 +67,25 @@ __device__ __forceinline__ int page_of(const PagedRowsArgs& a, const int32_t* ta
   return id < 0 || id >= a.num_pages ? -1 : id;
 }
 
-// A block's row r (16) and unit of 16 columns of a lane, pass by pass: 64 / units rows a pass.
+// Workgroups: query_groups of the queries (a thread per unit of a row), then key_groups of the keys' waves and as many of the
+// values', in the order (block of the sequence, head): the waves of a group are of one block, or of neighbouring ones.  The
+// rows' cosines and sines are computed once a group, in LDS.  A lane holds row t * (64 / units) + lane / units of its wave's
+// block in pass t.  Dynamic LDS: the turns.
 template <typename T, int PASSES>
 __global__ __launch_bounds__(kThreads) void paged_append_e4m3_kernel(PagedRowsArgs a, PagedScaleArgs sc, RopeArgs r,
                                                                     RopeQueryArgs q, int D, int units, int blocks,
-                                                                    unsigned query_groups) {
-  __shared__ int parents[kMaxNodes];
+                                                                    unsigned query_groups, unsigned key_groups) {
+  extern __shared__ __attribute__((aligned(16))) float2 turns[];
+  __shared__ TurnScratch scratch;
   const int b = blockIdx.y, layer = blockIdx.z, tid = threadIdx.x;
-  if (r.parent && !r.positions) {
-    for (int i = tid; i < a.N; i += kThreads) parents[i] = r.parent[(size_t)b * a.N + i];
-    __syncthreads();
-  }
   int n = a.N;
   if (a.row_len) n = min(a.row_len[b], n);
-  const int L = a.kv_len[b];
-  auto position = [&](int i) {
-    if (r.positions) return (double)r.positions[(size_t)b * a.N + i];
-    return (double)L + (double)(r.parent ? depth_of(parents, i) : i);
-  };
-  if (blockIdx.x < query_groups) {   // the queries: a thread per unit of a row
-    const uint32_t item = blockIdx.x * kThreads + tid, rest = item / units;
-    const int p = (int)(item - rest * units), i = (int)(rest / q.Hq), h = (int)(rest - i * (uint32_t)q.Hq);
-    if (i >= a.N) return;
+  if (blockIdx.x < query_groups) {
+    const uint32_t per_row = (uint32_t)units * (uint32_t)q.Hq, base = blockIdx.x * kThreads, item = base + tid;
+    const int i = (int)(item / per_row), first = (int)(base / per_row);
+    const int rows = min((int)((base + kThreads - 1) / per_row) + 1, n) - first;
+    const uint32_t rest = item - i * per_row;
+    const int h = (int)(rest / units), p = (int)(rest - h * (uint32_t)units);
     const Unit u = unit_of(p, r.R, D, r.interleaved != 0);
     Run<T> x, y;
     x.zero();
@@ -93,88 +94,115 @@ __global__ __launch_bounds__(kThreads) void paged_append_e4m3_kernel(PagedRowsAr
       const char* from = q.q + b * q.batch + h * q.head + i * q.row;
       x.load(from, u.first);
       y.load(from, u.second);
-      if (u.rotated) {
-        float c[8], s[8], xf[8], yf[8];
-        const double at = position(i);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) turn(at, r.freq[8 * p + e], r.gain, &c[e], &s[e]);
-        x.get(xf);
-        y.get(yf);
-        rotate(xf, yf, c, s, r.interleaved != 0);
-        x.set(xf);
-        y.set(yf);
-      }
+    }
+    fill_turns<kThreads>(r, scratch, b, first, rows, a.N, turns);
+    if (i >= a.N) return;
+    if (u.rotated && i < n) {
+      float c[8], s[8], xf[8], yf[8];
+      take_turns(turns + (i - first) * (r.R / 2), p, c, s);
+      x.get(xf);
+      y.get(yf);
+      rotate(xf, yf, c, s, r.interleaved != 0);
+      x.set(xf);
+      y.set(yf);
     }
     char* to = q.out + (((size_t)b * q.Hq + h) * a.N + i) * (size_t)(D * sizeof(T));
-    x.store(to, u.first);
-    y.store(to, u.second);
+    x.template store<true>(to, u.first);
+    y.template store<true>(to, u.second);
     return;
   }
   const int lane = tid & 63;
-  const uint32_t task = (blockIdx.x - query_groups) * (kThreads / 64) + __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int half = (int)(task & 1), g = (int)((task >> 1) % (uint32_t)a.Hkv), m = (int)((task >> 1) / (uint32_t)a.Hkv);
-  if (m >= blocks || L < 0 || n <= 0) return;
+  unsigned group = blockIdx.x - query_groups;
+  const int half = group >= key_groups ? 1 : 0;
+  group -= half * key_groups;
+  const uint32_t task0 = group * (kThreads / 64), task = task0 + __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int m = (int)(task / (uint32_t)a.Hkv), g = (int)(task - m * (uint32_t)a.Hkv), m0 = (int)(task0 / (uint32_t)a.Hkv);
+  const int L = a.kv_len[b];
+  if (L < 0 || n <= 0) return;
   const long long slot0 = ((long long)L / kScaleBlock + m) * kScaleBlock;    // the block's first slot
   const int i0 = (int)(slot0 - L);                                           // its row of the new ones (may be < 0)
-  if (i0 >= n) return;
-  const int id = page_of(a, a.table + (size_t)b * a.width, slot0);
+  const bool mine = m < blocks && i0 < n;
+  const int per_pass = 64 / units, sub = lane / units, p = lane - sub * units;
+  const Unit u = unit_of(p, half ? 0 : r.R, D, r.interleaved != 0);     // (a unit of values: 16 columns in a row)
+  // the rows (fresh: a pass's row of this lane is a new one), on their way while the turns are computed
+  Run<T> lo[PASSES], hi[PASSES];
+  uint32_t fresh = 0;
+  if (mine) {
+    const char* rows = (half ? a.v_new : a.k_new) + layer * a.new_layer + b * a.new_batch + g * a.new_head;
+#pragma unroll
+    for (int t = 0; t < PASSES; ++t) {
+      const int row = t * per_pass + sub, i = i0 + row;
+      if (sub < per_pass && row < kScaleBlock && i >= 0 && i < n) {
+        lo[t].load_past(rows + i * a.new_row, u.first);
+        hi[t].load_past(rows + i * a.new_row, u.second);
+        fresh |= 1u << t;
+      }
+    }
+  }
+  const int id = mine ? page_of(a, a.table + (size_t)b * a.width, slot0) : -1;
+  const int first = i0 - (m - m0) * kScaleBlock;     // the row that the turns start with
+  if (r.freq && half == 0) {
+    const int last = (int)((task0 + kThreads / 64 - 1) / (uint32_t)a.Hkv);
+    fill_turns<kThreads>(r, scratch, b, first, min((last - m0 + 1) * kScaleBlock, n - first), a.N, turns);
+  }
   if (id < 0) return;
   const int in_page = (int)slot0 & ((1 << a.page_shift) - 1);
   char* codes = (half ? a.v : a.k) + layer * a.layer_stride + (int64_t)id * a.page_stride +
                 (((int64_t)g << a.page_shift) + in_page) * a.row_bytes;
   uint8_t* scale = (half ? sc.v : sc.k) + layer * sc.layer_stride + (int64_t)id * sc.page_stride +
                    (((int64_t)g << a.page_shift) + in_page) / kScaleBlock;
-  const char* rows = (half ? a.v_new : a.k_new) + layer * a.new_layer + b * a.new_batch + g * a.new_head;
   const int held = i0 < 0 ? *scale : 0;
-  const int per_pass = 64 / units, sub = lane / units, p = lane - sub * units;
-  const Unit u = unit_of(p, r.R, D, r.interleaved != 0);
   float x[PASSES][8], y[PASSES][8];
   uint32_t top = 0;
 #pragma unroll
   for (int t = 0; t < PASSES; ++t) {
-    const int row = t * per_pass + sub, i = i0 + row;
-    if (sub < per_pass && row < kScaleBlock && i >= 0 && i < n) {
-      Run<T> lo, hi;
-      lo.load(rows + i * a.new_row, u.first);
-      hi.load(rows + i * a.new_row, u.second);
-      lo.get(x[t]);
-      hi.get(y[t]);
-      if (u.rotated && half == 0) {
-        float c[8], s[8];
-        const double at = position(i);
+    if (!(fresh >> t & 1u)) continue;
+    lo[t].get(x[t]);
+    hi[t].get(y[t]);
+    if (u.rotated) {
+      float c[8], s[8];
+      take_turns(turns + (i0 + t * per_pass + sub - first) * (r.R / 2), p, c, s);
+      rotate(x[t], y[t], c, s, r.interleaved != 0);
+    }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) turn(at, r.freq[8 * p + e], r.gain, &c[e], &s[e]);
-        rotate(x[t], y[t], c, s, r.interleaved != 0);
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const uint32_t ux = finite_magnitude(x[t][e]), uy = finite_magnitude(y[t][e]);
-        top = top > ux ? top : ux;
-        top = top > uy ? top : uy;
-      }
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t ux = finite_magnitude(x[t][e]), uy = finite_magnitude(y[t][e]);
+      top = top > ux ? top : ux;
+      top = top > uy ? top : uy;
     }
   }
-  const int mine = scale_byte(wave_max(top)), byte = mine > held ? mine : held;
+  const int wanted = scale_byte(wave_max(top)), byte = wanted > held ? wanted : held;
   const float inverse = power(254 - byte);
 #pragma unroll
   for (int t = 0; t < PASSES; ++t) {
-    const int row = t * per_pass + sub, i = i0 + row;
+    const int row = t * per_pass + sub;
     if (sub >= per_pass || row >= kScaleBlock) continue;
-    uint32_t* lo = (uint32_t*)(codes + (int64_t)row * a.row_bytes + u.first);
-    uint32_t* hi = (uint32_t*)(codes + (int64_t)row * a.row_bytes + u.second);
-    if (i >= 0 && i < n) {
+    u32x2* to = (u32x2*)(codes + (int64_t)row * a.row_bytes + u.first);
+    u32x2* to2 = (u32x2*)(codes + (int64_t)row * a.row_bytes + u.second);
+    u32x2 w, w2;
+    if (fresh >> t & 1u) {
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        lo[e] = encode4(x[t][4 * e] * inverse, x[t][4 * e + 1] * inverse, x[t][4 * e + 2] * inverse, x[t][4 * e + 3] * inverse);
-        hi[e] = encode4(y[t][4 * e] * inverse, y[t][4 * e + 1] * inverse, y[t][4 * e + 2] * inverse, y[t][4 * e + 3] * inverse);
+        w[e] = encode4(x[t][4 * e] * inverse, x[t][4 * e + 1] * inverse, x[t][4 * e + 2] * inverse, x[t][4 * e + 3] * inverse);
+        w2[e] = encode4(y[t][4 * e] * inverse, y[t][4 * e + 1] * inverse, y[t][4 * e + 2] * inverse, y[t][4 * e + 3] * inverse);
       }
-    } else if (i < 0 && byte > held) {
+    } else if (i0 + row < 0 && byte > held) {
       const float by = move_by(held, byte);
+      w = *to;
+      w2 = *to2;
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        lo[e] = rescale4(lo[e], by);
-        hi[e] = rescale4(hi[e], by);
+        w[e] = rescale4(w[e], by);
+        w2[e] = rescale4(w2[e], by);
       }
+    } else {
+      continue;
+    }
+    if (half == 1) {
+      *(u32x4*)to = u32x4{w[0], w[1], w2[0], w2[1]};
+    } else {
+      *to = w;
+      *to2 = w2;
     }
   }
   if (lane == 0) *scale = (uint8_t)byte;
@@ -246,6 +274,7 @@ __global__ __launch_bounds__(kThreads) void paged_commit_e4m3_kernel(PagedRowsAr
   }
 }
 
+template <bool PAST>
 __global__ __launch_bounds__(kThreads) void paged_read_e4m3_kernel(PagedRowsArgs a, PagedScaleArgs sc, int num_slots,
                                                                   char* k_out, char* v_out, int units) {
   const int layer = blockIdx.z, bg = blockIdx.y, b = bg / a.Hkv, g = bg - b * a.Hkv;
@@ -255,42 +284,66 @@ __global__ __launch_bounds__(kThreads) void paged_read_e4m3_kernel(PagedRowsArgs
   int id = -1;
   if (slot < a.kv_len[b]) id = page_of(a, a.table + (size_t)b * a.width, slot);
   const int64_t in_head = ((int64_t)g << a.page_shift) + (slot & ((1 << a.page_shift) - 1));
-  const size_t to = (((size_t)layer * a.B * a.Hkv + bg) * num_slots + slot) * a.row_bytes * 2 + p * 32;
+  const size_t to = (((size_t)layer * a.B * a.Hkv + bg) * num_slots + slot) * a.row_bytes * 2 + p * 16;
+  u32x2 x[2] = {};
+  uint32_t byte[2] = {};
+  if (id >= 0) {
+    const int64_t at = layer * a.layer_stride + (int64_t)id * a.page_stride + in_head * a.row_bytes + p * 8;
+    const int64_t scale_at = layer * sc.layer_stride + (int64_t)id * sc.page_stride + in_head / kScaleBlock;
+    x[0] = *(const u32x2*)(a.k + at);
+    x[1] = *(const u32x2*)(a.v + at);
+    byte[0] = sc.k[scale_at];
+    byte[1] = sc.v[scale_at];
+  }
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
-    u32x4 lo{0u, 0u, 0u, 0u}, hi{0u, 0u, 0u, 0u};
+    u32x4 y{0u, 0u, 0u, 0u};
     if (id >= 0) {
-      const u32x4 x = *(const u32x4*)((half ? a.v : a.k) + layer * a.layer_stride + (int64_t)id * a.page_stride +
-                                      in_head * a.row_bytes + p * 16);
-      const float by = power((half ? sc.v : sc.k)[layer * sc.layer_stride + (int64_t)id * sc.page_stride +
-                                                  in_head / kScaleBlock]);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t y0 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[e], by, false));
-        const uint32_t y1 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[e], by, true));
-        (e < 2 ? lo : hi)[2 * (e & 1)] = y0;
-        (e < 2 ? lo : hi)[2 * (e & 1) + 1] = y1;
+      for (int e = 0; e < 2; ++e) {
+        const uint32_t w = x[half][e];
+        y[2 * e] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, power((int)byte[half]), false));
+        y[2 * e + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, power((int)byte[half]), true));
       }
     }
-    char* row = (half ? v_out : k_out) + to;
-    *(u32x4*)row = lo;
-    *(u32x4*)(row + 16) = hi;
+    u32x4* out = (u32x4*)((half ? v_out : k_out) + to);
+    if constexpr (PAST) __builtin_nontemporal_store(y, out);
+    else *out = y;
   }
 }
 
+struct AppendGrid {
+  dim3 grid;
+  size_t lds;
+  int units, blocks;
+  unsigned query_groups, key_groups;
+};
+
 template <typename T, int PASSES>
-void append(const PagedRowsArgs& a, const PagedScaleArgs& sc, const RopeArgs& rope, const RopeQueryArgs& q, dim3 grid,
-            int units, int blocks, unsigned query_groups, hipStream_t stream) {
-  hipLaunchKernelGGL((paged_append_e4m3_kernel<T, PASSES>), grid, dim3(kThreads), 0, stream, a, sc, rope, q, a.row_bytes, units,
-                     blocks, query_groups);
+hipError_t append(const PagedRowsArgs& a, const PagedScaleArgs& sc, const RopeArgs& rope, const RopeQueryArgs& q,
+                  const AppendGrid& s, hipStream_t stream) {
+  auto kern = paged_append_e4m3_kernel<T, PASSES>;
+  static bool configured[64] = {};
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  if (dev < 0 || dev >= 64) return hipErrorInvalidDevice;
+  if (!configured[dev]) {
+    e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kMaxTurns * 8);
+    if (e != hipSuccess) return e;
+    configured[dev] = true;
+  }
+  hipLaunchKernelGGL(kern, s.grid, dim3(kThreads), s.lds, stream, a, sc, rope, q, a.row_bytes, s.units, s.blocks,
+                     s.query_groups, s.key_groups);
+  return hipGetLastError();
 }
 template <typename T>
-void append_passes(int passes, const PagedRowsArgs& a, const PagedScaleArgs& sc, const RopeArgs& rope, const RopeQueryArgs& q,
-                   dim3 grid, int units, int blocks, unsigned query_groups, hipStream_t stream) {
-  if (passes <= 1) append<T, 1>(a, sc, rope, q, grid, units, blocks, query_groups, stream);
-  else if (passes <= 2) append<T, 2>(a, sc, rope, q, grid, units, blocks, query_groups, stream);
-  else if (passes <= 4) append<T, 4>(a, sc, rope, q, grid, units, blocks, query_groups, stream);
-  else append<T, 8>(a, sc, rope, q, grid, units, blocks, query_groups, stream);
+hipError_t append_passes(int passes, const PagedRowsArgs& a, const PagedScaleArgs& sc, const RopeArgs& rope,
+                         const RopeQueryArgs& q, const AppendGrid& s, hipStream_t stream) {
+  if (passes <= 1) return append<T, 1>(a, sc, rope, q, s, stream);
+  if (passes <= 2) return append<T, 2>(a, sc, rope, q, s, stream);
+  if (passes <= 4) return append<T, 4>(a, sc, rope, q, s, stream);
+  return append<T, 8>(a, sc, rope, q, s, stream);
 }
 
 // passes over a block's 16 rows of `units` lanes each (units <= 32: 8 at most)
@@ -301,14 +354,21 @@ int passes_of(int units) { return (kScaleBlock + 64 / units - 1) / (64 / units);
 hipError_t launch_paged_append_e4m3(const PagedRowsArgs& a, const PagedScaleArgs& sc, const RopeArgs& rope,
                                     const RopeQueryArgs& q, int elem, hipStream_t stream) {
   if (a.N == 0 || a.B == 0) return hipSuccess;
-  const int units = a.row_bytes / 16, blocks = (int)(((long long)a.N + 2 * kScaleBlock - 2) / kScaleBlock);
-  const long long waves = 2LL * blocks * a.Hkv, per = kThreads / 64;
-  const unsigned query_groups = (unsigned)(((long long)a.N * q.Hq * units + kThreads - 1) / kThreads);
-  const dim3 grid(query_groups + (unsigned)((waves + per - 1) / per), (unsigned)a.B, (unsigned)a.NL);
-  const int passes = passes_of(units);
-  if (elem == 2) append_passes<__bf16>(passes, a, sc, rope, q, grid, units, blocks, query_groups, stream);
-  else append_passes<float>(passes, a, sc, rope, q, grid, units, blocks, query_groups, stream);
-  return hipGetLastError();
+  const int waves = kThreads / 64, pairs = rope.R / 2;
+  AppendGrid s{};
+  s.units = a.row_bytes / 16;
+  s.blocks = (int)(((long long)a.N + 2 * kScaleBlock - 2) / kScaleBlock);
+  s.query_groups = (unsigned)(((long long)a.N * q.Hq * s.units + kThreads - 1) / kThreads);
+  s.key_groups = (unsigned)(((long long)s.blocks * a.Hkv + waves - 1) / waves);
+  s.grid = dim3(s.query_groups + 2 * s.key_groups, (unsigned)a.B, (unsigned)a.NL);
+  // the turns of a group's rows: of the blocks that 4 waves can be of, of the rows that the queries' items can be of
+  const int key_rows = (a.Hkv % waves == 0 ? 1 : std::min(waves, (waves - 2) / a.Hkv + 2)) * kScaleBlock;
+  const int query_rows = q.Hq > 0 ? (kThreads - 2) / (s.units * q.Hq) + 2 : 0;
+  s.lds = (size_t)std::max(key_rows, query_rows) * pairs * sizeof(float2);
+  if (s.lds > (size_t)kMaxTurns * 8) return hipErrorInvalidValue;
+  const int passes = passes_of(s.units);
+  return elem == 2 ? append_passes<__bf16>(passes, a, sc, rope, q, s, stream)
+                   : append_passes<float>(passes, a, sc, rope, q, s, stream);
 }
 
 hipError_t launch_paged_commit_e4m3(const PagedRowsArgs& a, const PagedScaleArgs& sc, hipStream_t stream) {
@@ -325,11 +385,13 @@ hipError_t launch_paged_commit_e4m3(const PagedRowsArgs& a, const PagedScaleArgs
 
 hipError_t launch_paged_read_e4m3(const PagedRowsArgs& a, const PagedScaleArgs& sc, int num_slots, char* k_out, char* v_out,
                                   hipStream_t stream) {
-  const int units = a.row_bytes / 16;
+  const int units = a.row_bytes / 8;
   const long long items = (long long)num_slots * units;
   if (items == 0 || a.B == 0) return hipSuccess;
   const dim3 grid((unsigned)((items + kThreads - 1) / kThreads), (unsigned)(a.B * a.Hkv), (unsigned)a.NL);
-  hipLaunchKernelGGL(paged_read_e4m3_kernel, grid, dim3(kThreads), 0, stream, a, sc, num_slots, k_out, v_out, units);
+  const bool past = 2LL * a.NL * a.B * a.Hkv * num_slots * a.row_bytes * 2 >= kPastBytes;
+  hipLaunchKernelGGL(past ? paged_read_e4m3_kernel<true> : paged_read_e4m3_kernel<false>, grid, dim3(kThreads), 0, stream, a, sc,
+                     num_slots, k_out, v_out, units);
   return hipGetLastError();
 }
 
