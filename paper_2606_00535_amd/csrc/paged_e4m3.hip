@@ -3,8 +3,8 @@
 //   * append: a wave per block of 16 slots, head, and K or V.  It holds the block's new rows in fp32 (rotated, for K), takes
 //     their largest magnitude across its lanes, hence the scale, and writes their codes.  Rows that the block holds
 //     already move to the new scale where it is larger than theirs.
-//   * commit: a wave per (layer, sequence, KV head) and K or V, which goes through the path's blocks in order: a block's rows are
-//     in registers before one is written.  As in the 16-bit cache a row's source lies at or behind its slot, so that no
+//   * commit: a wave per (layer, sequence, KV head) and K or V, which goes through the path's blocks in order, two at a time:
+//     their rows are in registers before one is written.  As in the 16-bit cache a row's source lies at or behind its slot, so that no
 //     block's rows or scale are changed before they are read.
 //   * read: a thread per 8 codes.
 // A code times a power of two is exact in bf16, and a scale that grows moves a code's exponent: only codes that fall below
@@ -226,50 +226,61 @@ __global__ __launch_bounds__(kThreads) void paged_commit_e4m3_kernel(PagedRowsAr
   uint8_t* scales = (half ? sc.v : sc.k) + layer * sc.layer_stride;
   const int per_pass = 64 / units, sub = lane / units, p = lane - sub * units;
   auto head_slot = [&](long long slot) { return ((int64_t)g << a.page_shift) + ((int)slot & ((1 << a.page_shift) - 1)); };
-  for (long long slot0 = (long long)L / kScaleBlock * kScaleBlock; slot0 <= (long long)L + A; slot0 += kScaleBlock) {
-    const int id = page_of(a, table, slot0);
-    if (id < 0) continue;
-    uint8_t* scale = scales + (int64_t)id * sc.page_stride + head_slot(slot0) / kScaleBlock;
-    const int old = *scale;
-    u32x4 x[PASSES];
-    int from[PASSES];      // the scale byte of a live row (-1: dead)
-    uint32_t moved = 0;    // a bit a pass
-    int top = 0;
+  // (two blocks at a time: a path seldom reaches into a third)
+  constexpr int BLOCKS = 2;
+  for (long long base = (long long)L / kScaleBlock * kScaleBlock; base <= (long long)L + A; base += BLOCKS * kScaleBlock) {
+    u32x4 x[BLOCKS][PASSES];
+    int from[BLOCKS][PASSES];      // the scale byte of a live row (-1: dead)
+    uint32_t moved[BLOCKS] = {};   // a bit a pass
+    int id[BLOCKS], top[BLOCKS] = {};
 #pragma unroll
-    for (int t = 0; t < PASSES; ++t) {
-      const int row = t * per_pass + sub;
-      const long long slot = slot0 + row;
-      const int k = (int)(slot - L);     // < 0: before the rows
-      from[t] = -1;
-      if (sub >= per_pass || row >= kScaleBlock || k > A) continue;
-      int64_t at = (int64_t)id * a.page_stride + head_slot(slot) * a.row_bytes;
-      from[t] = old;
-      if (k >= 0 && path[k] > k) {
-        const long long src = (long long)L + path[k];
-        const int src_id = page_of(a, table, src);
-        if (src_id >= 0) {
-          at = (int64_t)src_id * a.page_stride + head_slot(src) * a.row_bytes;
-          from[t] = scales[(int64_t)src_id * sc.page_stride + head_slot(src) / kScaleBlock];
-          moved |= 1u << t;
+    for (int j = 0; j < BLOCKS; ++j) {
+      const long long slot0 = base + j * kScaleBlock;
+      id[j] = slot0 <= (long long)L + A ? page_of(a, table, slot0) : -1;
+#pragma unroll
+      for (int t = 0; t < PASSES; ++t) {
+        const int row = t * per_pass + sub;
+        const long long slot = slot0 + row;
+        const int k = (int)(slot - L);     // < 0: before the rows
+        from[j][t] = -1;
+        if (id[j] < 0 || sub >= per_pass || row >= kScaleBlock || k > A) continue;
+        int src_id = id[j];
+        long long src = slot;
+        if (k >= 0 && path[k] > k) {
+          const int there = page_of(a, table, (long long)L + path[k]);
+          if (there >= 0) {
+            src_id = there;
+            src = (long long)L + path[k];
+            moved[j] |= 1u << t;
+          }
         }
+        from[j][t] = scales[(int64_t)src_id * sc.page_stride + head_slot(src) / kScaleBlock];
+        x[j][t] = *(const u32x4*)(codes + (int64_t)src_id * a.page_stride + head_slot(src) * a.row_bytes + p * 16);
       }
-      x[t] = *(const u32x4*)(codes + at + p * 16);
-      top = top > from[t] ? top : from[t];
     }
-    const int byte = (int)wave_max((uint32_t)top);
-    if (!__any(moved != 0)) continue;    // (the block's rows stay where they are)
-    wait_vector_memory();                // (every lane's rows are in registers)
 #pragma unroll
-    for (int t = 0; t < PASSES; ++t) {
-      const int row = t * per_pass + sub;
-      if (from[t] < 0 || !((moved >> t & 1u) || from[t] != byte)) continue;
-      const float by = move_by(from[t], byte);
-      u32x4 y;
+    for (int j = 0; j < BLOCKS; ++j) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) y[e] = from[t] == byte ? x[t][e] : rescale4(x[t][e], by);
-      *(u32x4*)(codes + (int64_t)id * a.page_stride + head_slot(slot0 + row) * a.row_bytes + p * 16) = y;
+      for (int t = 0; t < PASSES; ++t) top[j] = top[j] > from[j][t] ? top[j] : from[j][t];
+      top[j] = (int)wave_max((uint32_t)top[j]);
     }
-    if (lane == 0) *scale = (uint8_t)byte;
+    wait_vector_memory();                  // (every lane's rows are in registers)
+#pragma unroll
+    for (int j = 0; j < BLOCKS; ++j) {
+      if (!__any(moved[j] != 0)) continue;     // (the block's rows stay where they are)
+      const long long slot0 = base + j * kScaleBlock;
+#pragma unroll
+      for (int t = 0; t < PASSES; ++t) {
+        const int row = t * per_pass + sub;
+        if (from[j][t] < 0 || !((moved[j] >> t & 1u) || from[j][t] != top[j])) continue;
+        const float by = move_by(from[j][t], top[j]);
+        u32x4 y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = from[j][t] == top[j] ? x[j][t][e] : rescale4(x[j][t][e], by);
+        *(u32x4*)(codes + (int64_t)id[j] * a.page_stride + head_slot(slot0 + row) * a.row_bytes + p * 16) = y;
+      }
+      if (lane == 0) scales[(int64_t)id[j] * sc.page_stride + head_slot(slot0) / kScaleBlock] = (uint8_t)top[j];
+    }
     wait_vector_memory();
   }
 }
