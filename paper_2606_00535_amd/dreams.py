@@ -828,6 +828,13 @@ def _new(t: torch.Tensor, stream, shape=None, dtype=None) -> torch.Tensor:
         return _new(t, None, shape, dtype)
 
 
+def _dense_like(t: torch.Tensor, stream) -> torch.Tensor:
+    """A dense output of t's shape and type (_new)."""
+    if stream is None:
+        return torch.empty_like(t, memory_format=torch.contiguous_format)
+    return _new(t, stream, t.shape, t.dtype)
+
+
 def _code(dtype, what: str = "pages") -> int:
     if dtype is torch.bfloat16:
         return DREAMS_BF16
@@ -1070,8 +1077,26 @@ _Strides = ctypes.c_int64 * 4
 def _new_rows(k_new, v_new, k_pages, pool, at, dt, kv_len, row_len):
     """The strides of new rows of type dt, once they and their lengths are checked against the pool."""
     B, n = pool.batch, k_pages.dim()
+    try:
+        shape, st = k_new.shape, k_new.stride()
+        plain = (k_new.dtype is dt and v_new.dtype is dt and k_new.get_device() == at == v_new.get_device()
+                 and shape == v_new.shape and st == v_new.stride() and len(shape) == n and st[-1] == 1
+                 and shape[-4] == B and shape[-3] == pool.num_kv_heads and shape[-1] == pool.head_dim
+                 and (n == 4 or shape[0] == pool.num_layers))
+    except AttributeError:
+        plain = False
+    if not plain:
+        _check_new_rows(k_new, v_new, k_pages, pool, at, dt, n)
+    _need_on(kv_len, "kv_len", torch.int32, at, (B,))
+    if row_len is not None:
+        _need_on(row_len, "row_len", torch.int32, at, (B,))
+    return _Strides(0, st[0], st[1], st[2]) if n == 4 else _Strides(*st[:4])
+
+
+def _check_new_rows(k_new, v_new, k_pages, pool, at, dt, n):
+    B = pool.batch
     for t, name in ((k_new, "k_new"), (v_new, "v_new")):
-        if type(t) is not torch.Tensor and not isinstance(t, torch.Tensor):
+        if not isinstance(t, torch.Tensor):
             raise TypeError("%s must be a torch.Tensor" % name)
         if t.dtype is not dt:
             raise TypeError("%s must be %s, got %s" % (name, dt, t.dtype))
@@ -1085,10 +1110,6 @@ def _new_rows(k_new, v_new, k_pages, pool, at, dt, kv_len, row_len):
         raise ValueError("k_new and v_new differ in shape or layout")
     if shape[-1] > 1 and st[-1] != 1:
         raise ValueError("the rows of k_new and v_new must be dense")
-    _need_on(kv_len, "kv_len", torch.int32, at, (B,))
-    if row_len is not None:
-        _need_on(row_len, "row_len", torch.int32, at, (B,))
-    return _Strides(*(st[:4] if n == 5 else (0,) + st[:3]))
 
 
 def paged_append(k_new: torch.Tensor, v_new: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,
@@ -1230,23 +1251,28 @@ def rope(x: torch.Tensor, frequencies: torch.Tensor, kv_len: Optional[torch.Tens
     (None: a dense [B,H,N,D]; x itself: in place).  Returns out."""
     at = _current(x, "x")
     code = _code(x.dtype, "x")
-    if x.dim() != 4:
+    shape, st = x.shape, x.stride()
+    if len(shape) != 4:
         raise ValueError("x must have 4 dimensions")
-    B, H, N, D = shape = x.shape
-    if D > 1 and x.stride(3) != 1:
+    B, H, N, D = shape
+    if D > 1 and st[3] != 1:
         raise ValueError("the rows of x must be dense")
     r = _rope(frequencies, positions, parent, (B, N), at, interleaved, amplitude)
     if kv_len is not None:
         _need_on(kv_len, "kv_len", torch.int32, at, (B,))
     if out is None:
-        out = _new(x, stream, shape, x.dtype)
+        out = _dense_like(x, stream)
+        to = _Strides3(H * N * D, N * D, D)
     else:
         if not isinstance(out, torch.Tensor):
             raise TypeError("out must be a torch.Tensor")
         if out.dtype is not x.dtype or out.get_device() != at or out.shape != shape or (D > 1 and out.stride(3) != 1):
             raise ValueError("out must be like x, with dense rows")
-    _check(lib().dreams_rope(ctypes.byref(r), B, H, N, D, code, x.data_ptr(), _Strides3(*x.stride()[:3]), _ptr(kv_len),
-                             out.data_ptr(), _Strides3(*out.stride()[:3]), _stream_on(stream, at)))
+        to = _Strides3(*out.stride()[:3])
+    status = lib().dreams_rope(ctypes.byref(r), B, H, N, D, code, x.data_ptr(), _Strides3(st[0], st[1], st[2]), _ptr(kv_len),
+                               out.data_ptr(), to, _stream_on(stream, at))
+    if status:
+        _check(status)
     return out
 
 
@@ -1262,15 +1288,16 @@ def _queries(q, q_out, like, batch, rows, head_dim, at, stream):
         raise TypeError("q must be %s, got %s" % (like.dtype, q.dtype))
     if q.get_device() != at:
         raise ValueError("q is on %s, expected %s" % (q.device, like.device))
-    if q.dim() != 4 or q.shape[0] != batch or q.shape[2:] != (rows, head_dim):
+    shape, st = q.shape, q.stride()
+    if len(shape) != 4 or shape[0] != batch or shape[2] != rows or shape[3] != head_dim:
         raise ValueError("q must be [B,Hq,N,D] for the new rows")
-    if head_dim > 1 and q.stride(3) != 1:
+    if head_dim > 1 and st[3] != 1:
         raise ValueError("the rows of q must be dense")
     if q_out is None:
-        q_out = _new(q, stream, q.shape, q.dtype)
+        q_out = _dense_like(q, stream)
     else:
-        _need_on(q_out, "q_out", q.dtype, at, q.shape)
-    return RopeQueries(q.data_ptr(), q_out.data_ptr(), q.shape[1], _Strides3(*q.stride()[:3])), q_out
+        _need_on(q_out, "q_out", q.dtype, at, shape)
+    return RopeQueries(q.data_ptr(), q_out.data_ptr(), shape[1], _Strides3(st[0], st[1], st[2])), q_out
 
 
 def paged_append_rope(k_new: torch.Tensor, v_new: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,
@@ -1327,10 +1354,32 @@ def _scale_strides(k_scales, v_scales, shape, at):
     return st[0] if n == 4 and want[0] > 1 else 0, st[-3] if P > 1 else H * S
 
 
+def _dense8(k_pages, v_pages, k_scales, v_scales, page_table, shape, at) -> bool:
+    """Whether a pool of 8 bits is all dense tensors on the current device, as most are: nothing else is to be looked at."""
+    try:
+        scales = shape[:-2] + (shape[-2] // 16,)
+        return (k_pages.dtype is _E4M3 is v_pages.dtype and k_scales.dtype is _E8M0 is v_scales.dtype
+                and page_table.dtype is torch.int32 and len(page_table.shape) == 2 and shape == v_pages.shape
+                and scales == k_scales.shape == v_scales.shape and at >= 0
+                and at == v_pages.get_device() == k_scales.get_device() == v_scales.get_device()
+                == page_table.get_device() == _current_device()
+                and k_pages.is_contiguous() and v_pages.is_contiguous() and k_scales.is_contiguous()
+                and v_scales.is_contiguous() and page_table.is_contiguous())
+    except AttributeError:
+        return False
+
+
 def _pool8(k_pages, v_pages, k_scales, v_scales, page_table):
     """(PagePool, PageScales, device index) of pages of 8 bits"""
-    if isinstance(k_pages, torch.Tensor) and k_pages.dtype is not _E4M3:
-        raise TypeError("k_pages must be torch.float8_e4m3fn, got %s" % k_pages.dtype)
+    if isinstance(k_pages, torch.Tensor):
+        if k_pages.dtype is not _E4M3:
+            raise TypeError("k_pages must be torch.float8_e4m3fn, got %s" % k_pages.dtype)
+        shape, at = k_pages.shape, k_pages.get_device()
+        if len(shape) in (4, 5) and _dense8(k_pages, v_pages, k_scales, v_scales, page_table, shape, at):
+            P, H, S, D = shape[-4:]
+            B, width = page_table.shape
+            return (PagePool(shape[0] if len(shape) == 5 else 1, B, H, D, P, S, width, DREAMS_E4M3, 0, 0),
+                    PageScales(k_scales.data_ptr(), v_scales.data_ptr(), 0, 0), at)
     pool, at = _pool(k_pages, v_pages, page_table, DREAMS_E4M3)
     layer, page = _scale_strides(k_scales, v_scales, k_pages.shape, at)
     return pool, PageScales(k_scales.data_ptr(), v_scales.data_ptr(), layer, page), at
@@ -1386,18 +1435,19 @@ def paged_read_e4m3(k_pages: torch.Tensor, v_pages: torch.Tensor, k_scales: torc
     _need_on(kv_len, "kv_len", torch.int32, at, (pool.batch,))
     if not -1 < num_slots < 2 ** 31:
         raise ValueError("num_slots must be in [0, 2^31)")
-    shape = torch.Size(k_pages.shape[:-4] + (pool.batch, pool.num_kv_heads, num_slots, pool.head_dim))
-    outs = []
-    for t, name in ((k_out, "k_out"), (v_out, "v_out")):
-        if t is None:
-            t = _new(kv_len, stream, shape, torch.bfloat16)
-        else:
-            _need_on(t, name, torch.bfloat16, at, shape)
-        outs.append(t)
+    shape = k_pages.shape[:-4] + (pool.batch, pool.num_kv_heads, num_slots, pool.head_dim)
+    if k_out is None:
+        k_out = kv_len.new_empty(*shape, dtype=torch.bfloat16) if stream is None else _new(kv_len, stream, shape, torch.bfloat16)
+    else:
+        _need_on(k_out, "k_out", torch.bfloat16, at, shape)
+    if v_out is None:
+        v_out = _dense_like(k_out, stream)
+    else:
+        _need_on(v_out, "v_out", torch.bfloat16, at, shape)
     _check(lib().dreams_paged_read_e4m3(ctypes.byref(pool), ctypes.byref(scales), k_pages.data_ptr(), v_pages.data_ptr(),
-                                        page_table.data_ptr(), kv_len.data_ptr(), num_slots, outs[0].data_ptr(),
-                                        outs[1].data_ptr(), _stream_on(stream, at)))
-    return outs[0], outs[1]
+                                        page_table.data_ptr(), kv_len.data_ptr(), num_slots, k_out.data_ptr(),
+                                        v_out.data_ptr(), _stream_on(stream, at)))
+    return k_out, v_out
 
 
 def pages_fork_e4m3(k_pages: torch.Tensor, v_pages: torch.Tensor, k_scales: torch.Tensor, v_scales: torch.Tensor,
@@ -1413,8 +1463,18 @@ def pages_fork_e4m3(k_pages: torch.Tensor, v_pages: torch.Tensor, k_scales: torc
 
 def _paged_desc8(q, k_pages, v_pages, k_scales, v_scales, page_table, window, sinks, max_kv_len, num_splits, scale):
     """(PagedDesc, PageScales) of an attention call over pages of 8 bits"""
-    if isinstance(k_pages, torch.Tensor) and k_pages.dtype is not _E4M3:
-        raise TypeError("k_pages must be torch.float8_e4m3fn, got %s" % k_pages.dtype)
+    if isinstance(k_pages, torch.Tensor):
+        if k_pages.dtype is not _E4M3:
+            raise TypeError("k_pages must be torch.float8_e4m3fn, got %s" % k_pages.dtype)
+        shape, at = k_pages.shape, k_pages.get_device()
+        if (len(shape) == 4 and _dense8(k_pages, v_pages, k_scales, v_scales, page_table, shape, at)
+                and isinstance(q, torch.Tensor) and q.dtype is torch.bfloat16 and q.get_device() == at and q.is_contiguous()
+                and -1 < window < 2 ** 31 and -1 < sinks < 2 ** 31 and -1 < max_kv_len < 2 ** 31 and -1 < num_splits < 2 ** 31):
+            rows, table = q.shape, page_table.shape
+            if len(rows) == 4 and rows[0] == table[0] and rows[3] == shape[3]:
+                return (PagedDesc(rows[0], rows[1], shape[1], rows[3], rows[2], shape[0], shape[2], table[1], max_kv_len,
+                                  num_splits, window, sinks, DREAMS_BF16, 1.0 / math.sqrt(rows[3]) if scale is None else scale,
+                                  0), PageScales(k_scales.data_ptr(), v_scales.data_ptr(), 0, 0))
     desc = _paged_desc(q, k_pages, v_pages, page_table, torch.bfloat16, window, sinks, max_kv_len, num_splits, scale)
     _, page = _scale_strides(k_scales, v_scales, k_pages.shape, q.get_device())
     return desc, PageScales(k_scales.data_ptr(), v_scales.data_ptr(), 0, page)
