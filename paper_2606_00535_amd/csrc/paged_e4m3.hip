@@ -74,7 +74,7 @@ __device__ __forceinline__ int page_of(const PagedRowsArgs& a, const int32_t* ta
 template <typename T, int PASSES>
 __global__ __launch_bounds__(kThreads) void paged_append_e4m3_kernel(PagedRowsArgs a, PagedScaleArgs sc, RopeArgs r,
                                                                     RopeQueryArgs q, int D, int units, int blocks,
-                                                                    unsigned query_groups, unsigned key_groups) {
+                                                                    unsigned query_groups, unsigned key_groups, bool past) {
   extern __shared__ __attribute__((aligned(16))) float2 turns[];
   __shared__ TurnScratch scratch;
   const int b = blockIdx.y, layer = blockIdx.z, tid = threadIdx.x;
@@ -86,29 +86,30 @@ __global__ __launch_bounds__(kThreads) void paged_append_e4m3_kernel(PagedRowsAr
     const int rows = min((int)((base + kThreads - 1) / per_row) + 1, n) - first;
     const uint32_t rest = item - i * per_row;
     const int h = (int)(rest / units), p = (int)(rest - h * (uint32_t)units);
-    const Unit u = unit_of(p, r.R, D, r.interleaved != 0);
-    Run<T> x, y;
+    const Unit u = unit_of<8>(p, r.R, D);
+    Run<T, 8> x, y;
     x.zero();
     y.zero();
     if (i < n) {
       const char* from = q.q + b * q.batch + h * q.head + i * q.row;
       x.load(from, u.first);
-      y.load(from, u.second);
+      if (u.second >= 0) y.load(from, u.second);
     }
     fill_turns<kThreads>(r, scratch, b, first, rows, a.N, turns);
     if (i >= a.N) return;
     if (u.rotated && i < n) {
-      float c[8], s[8], xf[8], yf[8];
-      take_turns(turns + (i - first) * (r.R / 2), p, c, s);
-      x.get(xf);
-      y.get(yf);
-      rotate(xf, yf, c, s, r.interleaved != 0);
-      x.set(xf);
-      y.set(yf);
+      float c[8], s[8];
+      take_turns(turns + (i - first) * (r.R / 2), p, r.R, r.interleaved != 0, c, s);
+      rotate(x, y, c, s, r.interleaved != 0);
     }
     char* to = q.out + (((size_t)b * q.Hq + h) * a.N + i) * (size_t)(D * sizeof(T));
-    x.template store<true>(to, u.first);
-    y.template store<true>(to, u.second);
+    if (past) {
+      x.template store<true>(to, u.first);
+      y.template store<true>(to, u.second);
+    } else {
+      x.store(to, u.first);
+      y.store(to, u.second);
+    }
     return;
   }
   const int lane = tid & 63;
@@ -123,9 +124,10 @@ __global__ __launch_bounds__(kThreads) void paged_append_e4m3_kernel(PagedRowsAr
   const int i0 = (int)(slot0 - L);                                           // its row of the new ones (may be < 0)
   const bool mine = m < blocks && i0 < n;
   const int per_pass = 64 / units, sub = lane / units, p = lane - sub * units;
-  const Unit u = unit_of(p, half ? 0 : r.R, D, r.interleaved != 0);     // (a unit of values: 16 columns in a row)
+  Unit u = unit_of<8>(p, r.R, D);
+  if (half) u = Unit{16 * p, 16 * p + 8, false};     // (a unit of values: 16 columns in a row)
   // the rows (fresh: a pass's row of this lane is a new one), on their way while the turns are computed
-  Run<T> lo[PASSES], hi[PASSES];
+  Run<T, 8> lo[PASSES], hi[PASSES];
   uint32_t fresh = 0;
   if (mine) {
     const char* rows = (half ? a.v_new : a.k_new) + layer * a.new_layer + b * a.new_batch + g * a.new_head;
@@ -133,8 +135,9 @@ __global__ __launch_bounds__(kThreads) void paged_append_e4m3_kernel(PagedRowsAr
     for (int t = 0; t < PASSES; ++t) {
       const int row = t * per_pass + sub, i = i0 + row;
       if (sub < per_pass && row < kScaleBlock && i >= 0 && i < n) {
-        lo[t].load_past(rows + i * a.new_row, u.first);
-        hi[t].load_past(rows + i * a.new_row, u.second);
+        // (rows of two words a run are read in halves of lines, so through the caches)
+        lo[t].template load<sizeof(T) == 2>(rows + i * a.new_row, u.first);
+        hi[t].template load<sizeof(T) == 2>(rows + i * a.new_row, u.second);
         fresh |= 1u << t;
       }
     }
@@ -161,7 +164,7 @@ __global__ __launch_bounds__(kThreads) void paged_append_e4m3_kernel(PagedRowsAr
     hi[t].get(y[t]);
     if (u.rotated) {
       float c[8], s[8];
-      take_turns(turns + (i0 + t * per_pass + sub - first) * (r.R / 2), p, c, s);
+      take_turns(turns + (i0 + t * per_pass + sub - first) * (r.R / 2), p, r.R, r.interleaved != 0, c, s);
       rotate(x[t], y[t], c, s, r.interleaved != 0);
     }
 #pragma unroll
@@ -328,6 +331,7 @@ struct AppendGrid {
   size_t lds;
   int units, blocks;
   unsigned query_groups, key_groups;
+  bool past;       // the queries are stored past the caches
 };
 
 template <typename T, int PASSES>
@@ -345,7 +349,7 @@ hipError_t append(const PagedRowsArgs& a, const PagedScaleArgs& sc, const RopeAr
     configured[dev] = true;
   }
   hipLaunchKernelGGL(kern, s.grid, dim3(kThreads), s.lds, stream, a, sc, rope, q, a.row_bytes, s.units, s.blocks,
-                     s.query_groups, s.key_groups);
+                     s.query_groups, s.key_groups, s.past);
   return hipGetLastError();
 }
 template <typename T>
@@ -377,6 +381,8 @@ hipError_t launch_paged_append_e4m3(const PagedRowsArgs& a, const PagedScaleArgs
   const int query_rows = q.Hq > 0 ? (kThreads - 2) / (s.units * q.Hq) + 2 : 0;
   s.lds = (size_t)std::max(key_rows, query_rows) * pairs * sizeof(float2);
   if (s.lds > (size_t)kMaxTurns * 8) return hipErrorInvalidValue;
+  // (fp32: a run of 8 columns is two words, half lines a store)
+  s.past = elem == 2 && stored_past((long long)a.B * a.N * q.Hq * a.row_bytes * elem, rope.R, a.row_bytes, elem);
   const int passes = passes_of(s.units);
   return elem == 2 ? append_passes<__bf16>(passes, a, sc, rope, q, s, stream)
                    : append_passes<float>(passes, a, sc, rope, q, s, stream);

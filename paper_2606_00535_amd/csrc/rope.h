@@ -31,94 +31,130 @@ __device__ __forceinline__ int depth_of(const int* parent, int i) {
   }
 }
 
-// Bytes of output from which they are stored past the caches (28 heads x 8192 rows 25.1 us in them, 19.7 past them; 2 x 8
-// heads x 437 rows of 64 columns in fp32, 1.8 MB, 4.0 and 4.4).
+// Bytes of output from which they are stored past the caches, where a unit's runs fill 64 bytes at least (28 heads x 8192
+// rows 25.1 us in the caches, 19.7 past them; 2 x 8 heads x 437 rows of 64 columns in fp32, 1.8 MB, 4.0 and 4.4).
 constexpr long long kPastBytes = 4 << 20;
+inline bool stored_past(long long bytes, int R, int D, int elem) {
+  return bytes >= kPastBytes && R / 2 * elem >= 64 && (D == R || (D - R) / 2 * elem >= 64);
+}
 
-// 8 columns of a row from column `at` on, as they are in memory, and as fp32.
-template <typename T>
+// W columns of a row from column `at` on, as they are in memory, and as fp32.
+template <typename T, int W>
 struct Run {
+  static constexpr int WORDS = W * (int)sizeof(T) / 16;    // of 16 bytes
   typedef uint32_t words __attribute__((ext_vector_type(4)));
-  typedef T tx8 __attribute__((ext_vector_type(8)));
-  words w[sizeof(T) / 2];
+  typedef T txw __attribute__((ext_vector_type(W)));
+  words w[WORDS];
   __device__ __forceinline__ void zero() {
 #pragma unroll
     for (auto& x : w) x = words{0u, 0u, 0u, 0u};
   }
+  // (PAST: data that is not kept in the caches)
+  template <bool PAST = false>
   __device__ __forceinline__ void load(const char* row, int at) {
 #pragma unroll
-    for (int i = 0; i < (int)(sizeof(T) / 2); ++i) w[i] = ((const words*)(row + at * sizeof(T)))[i];
+    for (int i = 0; i < WORDS; ++i) {
+      const words* from = (const words*)(row + at * sizeof(T)) + i;
+      if constexpr (PAST) w[i] = __builtin_nontemporal_load(from);
+      else w[i] = *from;
+    }
   }
-  // (past: data that is not kept in the caches)
-  __device__ __forceinline__ void load_past(const char* row, int at) {
-#pragma unroll
-    for (int i = 0; i < (int)(sizeof(T) / 2); ++i) w[i] = __builtin_nontemporal_load((const words*)(row + at * sizeof(T)) + i);
-  }
-  template <bool PAST>
+  template <bool PAST = false>
   __device__ __forceinline__ void store(char* row, int at) const {
 #pragma unroll
-    for (int i = 0; i < (int)(sizeof(T) / 2); ++i) {
+    for (int i = 0; i < WORDS; ++i) {
       words* to = (words*)(row + at * sizeof(T)) + i;
       if constexpr (PAST) __builtin_nontemporal_store(w[i], to);
       else *to = w[i];
     }
   }
-  __device__ __forceinline__ void get(float (&x)[8]) const {
+  __device__ __forceinline__ void get(float (&x)[W]) const {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < W; ++i) {
       const uint32_t u = sizeof(T) == 2 ? w[0][i / 2] : w[i / 4][i % 4];   // (a bit cast of the element itself takes element 0)
       x[i] = __builtin_bit_cast(float, sizeof(T) == 4 ? u : i & 1 ? u & 0xffff0000u : u << 16);
     }
   }
-  __device__ __forceinline__ void set(const float (&x)[8]) {
-    tx8 y;
+  __device__ __forceinline__ void set(const float (&x)[W]) {
+    txw y;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = (T)x[i];
+    for (int i = 0; i < W; ++i) y[i] = (T)x[i];
     __builtin_memcpy(&w, &y, sizeof(y));
   }
 };
 
-// Unit p of a row: where its 16 columns are (two runs of 8), and whether it is rotated.  The columns past R come 16 at a time;
-// the last unit may have 8 (second run: -1).
+// Unit p of a row is two runs of W columns: 8 p (W = 8) and half of the rotated columns behind it, so that the lanes of a wave
+// read and write whole lines, run by run.  In the half layout they are W pairs, in the interleaved one W / 2 each.  The
+// columns past R are halved likewise (an odd run is the first of a unit whose second is -1).
 struct Unit {
   int first, second;
   bool rotated;
 };
-__device__ __forceinline__ Unit unit_of(int p, int R, int D, bool interleaved) {
+template <int W>
+__device__ __forceinline__ Unit unit_of(int p, int R, int D) {
   Unit u;
-  u.rotated = p < R / 16;
-  const int at = 16 * p;
-  if (u.rotated && !interleaved) {
-    u.first = 8 * p;
-    u.second = R / 2 + 8 * p;
+  const int turned = R / (2 * W);
+  u.rotated = p < turned;
+  if (u.rotated) {
+    u.first = W * p;
+    u.second = R / 2 + W * p;
   } else {
-    u.first = at;
-    u.second = at + 16 <= D ? at + 8 : -1;
+    const int runs = (D - R) / W, half = (runs + 1) / 2, t = p - turned;
+    u.first = R + W * t;
+    u.second = t + half < runs ? R + W * (t + half) : -1;
   }
   return u;
 }
-// a unit's 16 columns (a: the first run, b: the second), turned by its 8 pairs' cosines and sines
-__device__ __forceinline__ void rotate(float (&a)[8], float (&b)[8], const float (&c)[8], const float (&s)[8],
+template <int W>
+__host__ __device__ inline int rope_units(int R, int D) { return R / (2 * W) + (D - R + 2 * W - 1) / (2 * W); }
+
+// The cosines and sines of a unit's W pairs, of a row's R / 2: half layout W in a row, interleaved W / 2 for each run.
+template <int W>
+__device__ __forceinline__ void take_turns(const float2* row, int p, int R, bool interleaved, float (&c)[W], float (&s)[W]) {
+  typedef float f32x4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+  for (int i = 0; i < W / 2; ++i) {
+    const int at = !interleaved ? W * p + 2 * i : i < W / 4 ? W / 2 * p + 2 * i : R / 4 + W / 2 * p + 2 * (i - W / 4);
+    const f32x4 x = *(const f32x4*)(row + at);
+    c[2 * i] = x[0];
+    s[2 * i] = x[1];
+    c[2 * i + 1] = x[2];
+    s[2 * i + 1] = x[3];
+  }
+}
+// a unit's two runs, turned
+template <int W>
+__device__ __forceinline__ void rotate(float (&a)[W], float (&b)[W], const float (&c)[W], const float (&s)[W],
                                        bool interleaved) {
   if (interleaved) {
 #pragma unroll
-    for (int i = 0; i < 8; i += 2) {
+    for (int i = 0; i < W; i += 2) {
       float x = a[i], y = a[i + 1];
       a[i] = fmaf(x, c[i / 2], -(y * s[i / 2]));
       a[i + 1] = fmaf(y, c[i / 2], x * s[i / 2]);
       x = b[i];
       y = b[i + 1];
-      b[i] = fmaf(x, c[4 + i / 2], -(y * s[4 + i / 2]));
-      b[i + 1] = fmaf(y, c[4 + i / 2], x * s[4 + i / 2]);
+      b[i] = fmaf(x, c[W / 2 + i / 2], -(y * s[W / 2 + i / 2]));
+      b[i + 1] = fmaf(y, c[W / 2 + i / 2], x * s[W / 2 + i / 2]);
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < W; ++i) {
       const float x = a[i], y = b[i];
       a[i] = fmaf(x, c[i], -(y * s[i]));
       b[i] = fmaf(y, c[i], x * s[i]);
     }
   }
+}
+template <typename T, int W>
+__device__ __forceinline__ void rotate(Run<T, W>& x, Run<T, W>& y, const float (&c)[W], const float (&s)[W],
+                                       bool interleaved) {
+  float a[W], b[W];
+  x.get(a);
+  y.get(b);
+  rotate(a, b, c, s, interleaved);
+  x.set(a);
+  y.set(b);
 }
 
 // A row's position, by a table, by a tree (parents in LDS) or in order.
@@ -165,20 +201,6 @@ __device__ __forceinline__ void fill_turns(const RopeArgs& r, TurnScratch& scrat
   }
   __syncthreads();
 }
-// unit p's 8 pairs of such a row
-__device__ __forceinline__ void take_turns(const float2* row, int p, float (&c)[8], float (&s)[8]) {
-  typedef float f32x4 __attribute__((ext_vector_type(4)));
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const f32x4 x = *(const f32x4*)(row + 8 * p + 2 * i);
-    c[2 * i] = x[0];
-    s[2 * i] = x[1];
-    c[2 * i + 1] = x[2];
-    s[2 * i + 1] = x[3];
-  }
-}
-
-__host__ __device__ inline int rope_units(int R, int D) { return R / 16 + (D - R + 15) / 16; }
 
 }  // namespace
 }  // namespace dreams

@@ -1,25 +1,16 @@
 // Rotary positions: queries or keys rotated by themselves, and rows rotated on their way into the pages of a cache (their
 // queries in the same launch, their values copied).
 //
-// A thread takes a unit of 8 pairs (16 columns) of a row of a head, the heads of a row after one another; the rows' cosines and
+// A thread takes a unit (two 16-byte runs) of a row of a head, the heads of a row after one another; the rows' cosines and
 // sines are computed once a workgroup, in LDS.
 #include "rope.h"
 
 namespace dreams {
 namespace {
 
-// Cosines and sines of the rows that a workgroup's items are of: k = R / 16 items a row at least, so (254 / k + 2) rows of 8 k.
+// Cosines and sines of the rows that a workgroup's items are of: k >= R / (2 W) items a row, so at most 254 / k + 2 rows of
+// R / 2 <= W k.
 constexpr int kTurns = 8 * kRopeThreads + kRopeMaxDim;
-
-template <typename T>
-__device__ __forceinline__ void rotate(Run<T>& x, Run<T>& y, const float (&c)[8], const float (&s)[8], bool interleaved) {
-  float a[8], b[8];
-  x.get(a);
-  y.get(b);
-  rotate(a, b, c, s, interleaved);
-  x.set(a);
-  y.set(b);
-}
 
 // What a workgroup's items are of: item = (row * heads + head) * units + unit.
 struct Item {
@@ -38,15 +29,15 @@ __device__ __forceinline__ Item item_of(int units, int heads, int N) {
   return x;
 }
 
-template <typename T, bool PAST>
+template <typename T, int W, bool PAST>
 __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeCallArgs a, int units) {
   __shared__ TurnScratch scratch;
   __shared__ __attribute__((aligned(16))) float2 turns[kTurns];
   const int b = blockIdx.y;
   const Item it = item_of(units, a.H, a.N);
-  const Unit u = unit_of(it.unit, a.rope.R, a.D, a.rope.interleaved != 0);
+  const Unit u = unit_of<W>(it.unit, a.rope.R, a.D);
   const bool mine = it.row < a.N && !(a.in_place && !u.rotated);
-  Run<T> x, y;
+  Run<T, W> x, y;
   if (mine) {      // (on their way while the turns are computed)
     const char* row = a.x + b * a.x_batch + it.head * a.x_head + it.row * a.x_row;
     x.load(row, u.first);
@@ -55,8 +46,8 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeCallArgs a, int 
   fill_turns<kRopeThreads>(a.rope, scratch, b, it.first, it.rows, a.N, turns);
   if (!mine) return;
   if (u.rotated) {
-    float c[8], s[8];
-    take_turns(turns + (it.row - it.first) * (a.rope.R / 2), it.unit, c, s);
+    float c[W], s[W];
+    take_turns(turns + (it.row - it.first) * (a.rope.R / 2), it.unit, a.rope.R, a.rope.interleaved != 0, c, s);
     rotate(x, y, c, s, a.rope.interleaved != 0);
   }
   char* to = a.out + b * a.out_batch + it.head * a.out_head + it.row * a.out_row;
@@ -65,7 +56,7 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeCallArgs a, int 
 }
 
 // Heads 0 .. Hq - 1 are the queries', then Hkv of keys, then Hkv of values.
-template <typename T, bool PAST>
+template <typename T, int W, bool PAST>
 __global__ __launch_bounds__(kRopeThreads) void paged_append_rope_kernel(PagedRowsArgs a, RopeArgs r, RopeQueryArgs q, int D,
                                                                         int units) {
   __shared__ TurnScratch scratch;
@@ -78,8 +69,8 @@ __global__ __launch_bounds__(kRopeThreads) void paged_append_rope_kernel(PagedRo
   const bool mine = i < a.N, live = i < n;
   const bool query = h < q.Hq, value = h >= q.Hq + a.Hkv;
   const int g = query ? h : h - q.Hq - (value ? a.Hkv : 0);
-  const Unit u = unit_of(it.unit, r.R, D, r.interleaved != 0);
-  Run<T> x, y;
+  const Unit u = unit_of<W>(it.unit, r.R, D);
+  Run<T, W> x, y;
   x.zero();
   y.zero();
   if (mine && live) {      // (on their way while the turns are computed)
@@ -103,8 +94,8 @@ __global__ __launch_bounds__(kRopeThreads) void paged_append_rope_kernel(PagedRo
          (((int64_t)g << a.page_shift) + ((int)slot & ((1 << a.page_shift) - 1))) * a.row_bytes;
   }
   if (u.rotated && !value && live) {
-    float c[8], s[8];
-    take_turns(turns + (i - it.first) * (r.R / 2), it.unit, c, s);
+    float c[W], s[W];
+    take_turns(turns + (i - it.first) * (r.R / 2), it.unit, r.R, r.interleaved != 0, c, s);
     rotate(x, y, c, s, r.interleaved != 0);
   }
   x.template store<PAST>(to, u.first);
@@ -114,26 +105,26 @@ __global__ __launch_bounds__(kRopeThreads) void paged_append_rope_kernel(PagedRo
 }  // namespace
 
 hipError_t launch_rope(const RopeCallArgs& a, hipStream_t stream) {
-  const int units = rope_units(a.rope.R, a.D);
+  const int units = a.elem == 2 ? rope_units<8>(a.rope.R, a.D) : rope_units<4>(a.rope.R, a.D);
   const long long items = (long long)a.N * units * a.H;
   if (items == 0 || a.B == 0) return hipSuccess;
   const dim3 grid((unsigned)((items + kRopeThreads - 1) / kRopeThreads), (unsigned)a.B);
-  const bool past = (long long)a.B * a.H * a.N * a.D * a.elem >= kPastBytes;
-  auto kern = a.elem == 2 ? (past ? rope_kernel<__bf16, true> : rope_kernel<__bf16, false>)
-                          : (past ? rope_kernel<float, true> : rope_kernel<float, false>);
+  const bool past = stored_past((long long)a.B * a.H * a.N * a.D * a.elem, a.rope.R, a.D, a.elem);
+  auto kern = a.elem == 2 ? (past ? rope_kernel<__bf16, 8, true> : rope_kernel<__bf16, 8, false>)
+                          : (past ? rope_kernel<float, 4, true> : rope_kernel<float, 4, false>);
   hipLaunchKernelGGL(kern, grid, dim3(kRopeThreads), 0, stream, a, units);
   return hipGetLastError();
 }
 
 hipError_t launch_paged_append_rope(const PagedRowsArgs& a, const RopeArgs& rope, const RopeQueryArgs& q, int elem, int D,
                                     hipStream_t stream) {
-  const int units = rope_units(rope.R, D);
+  const int units = elem == 2 ? rope_units<8>(rope.R, D) : rope_units<4>(rope.R, D);
   const long long heads = q.Hq + 2LL * a.Hkv, items = (long long)a.N * units * heads;
   if (items == 0 || a.B == 0) return hipSuccess;
   const dim3 grid((unsigned)((items + kRopeThreads - 1) / kRopeThreads), (unsigned)a.B, (unsigned)a.NL);
-  const bool past = a.NL * a.B * heads * a.N * a.row_bytes >= kPastBytes;
-  auto kern = elem == 2 ? (past ? paged_append_rope_kernel<__bf16, true> : paged_append_rope_kernel<__bf16, false>)
-                        : (past ? paged_append_rope_kernel<float, true> : paged_append_rope_kernel<float, false>);
+  const bool past = stored_past(a.NL * a.B * heads * a.N * a.row_bytes, rope.R, D, elem);
+  auto kern = elem == 2 ? (past ? paged_append_rope_kernel<__bf16, 8, true> : paged_append_rope_kernel<__bf16, 8, false>)
+                        : (past ? paged_append_rope_kernel<float, 4, true> : paged_append_rope_kernel<float, 4, false>);
   hipLaunchKernelGGL(kern, grid, dim3(kRopeThreads), 0, stream, a, rope, q, D, units);
   return hipGetLastError();
 }
