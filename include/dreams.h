@@ -702,7 +702,8 @@ dreams_status_t dreams_paged_append_rope(const dreams_page_pool_t* pool, const d
  * A block takes the least scale (s >= 1) at which the largest finite magnitude in it is at most 448 times it.  Powers of two
  * lose nothing here: codes have an exponent of their own, and rows that move to a larger scale change only where they
  * fall below the codes' normal range (2^-14 of the block's largest value and less).  The bytes that these calls write are 1 ..
- * 247; 0 and 255 give unspecified values.  An infinity or NaN becomes NaN.
+ * 247; 0 and 255 give unspecified values.  An infinity or NaN becomes NaN; a magnitude from 1.9375 * 2^127 on rounds to 2^128,
+ * an infinity as it is read.
  *   k, v           device uint8 [NL][num_pages, Hkv, page_size / 16]
  *   layer_stride, page_stride   bytes, 0 means dense (page_stride Hkv * page_size / 16)
  */

@@ -1314,7 +1314,7 @@ int paged_pieces(int n_keys, long long xcd_wgs, long long xcd_cus, bool level) {
 // where a batch's long sequences may run on behind its short ones (16 x 4 heads behind 100 to 32768: 59, 68; where they
 // are of like lengths, 8 x 8 behind 16384 to 32768, 75.3 and 73.9).
 bool spread_pays(const dreams_paged_desc_t* d, const AttnPlan& p, int parts, int splits, int n_keys, int cus) {
-  if (p.row_groups != 1 || d->batch > kSpreadSeqs || 2 * p.units > cus) return false;
+  if (p.row_groups != 1 || d->batch > kSpreadSeqs || p.units > cus / 2) return false;
   const long long even = ((long long)p.units * n_keys + cus - 1) / cus;      // keys of a compute unit, spread
   if (d->batch > 1 && even >= 4096) return true;
   const long long dies = 8 / parts, wgs = (p.units + dies - 1) / dies * splits, xcd_cus = std::max(cus / 8, 1);
@@ -1852,11 +1852,14 @@ RopeQueryArgs query_args(const dreams_rope_queries_t* q, const dreams_page_pool_
   return a;
 }
 
-// A launch over rows x heads x units of 16 columns, a thread each at most.
+// A launch over rows x heads x units, a thread each at most.
 dreams_status_t check_units(long long rows, long long heads, long long units) {
   if (rows > 0 && heads * units > 0x7fffffffLL / rows) return fail(DREAMS_ERR_UNSUPPORTED, "problem too large");
   return DREAMS_OK;
 }
+
+// Units of a row of D columns in a rotation (two runs of 16 bytes), at most.
+long long row_units(int32_t head_dim, int elem) { return elem == 2 ? (head_dim + 15) / 16 + 1 : (head_dim + 7) / 8 + 1; }
 
 dreams_status_t check_scales(const dreams_page_scales_t* s, const dreams_page_pool_t* p) {
   if (!s) return fail(DREAMS_ERR_INVALID_ARG, "scales is NULL");
@@ -1932,7 +1935,7 @@ dreams_status_t dreams_rope(const dreams_rope_t* rope, int32_t batch, int32_t nu
   if (!x_strides || !out_strides) return fail(DREAMS_ERR_INVALID_ARG, "x_strides and out_strides must not be NULL");
   st = check_row_strides("x_strides", x_strides, batch, num_heads, num_rows, elem);
   if (st == DREAMS_OK) st = check_row_strides("out_strides", out_strides, batch, num_heads, num_rows, elem);
-  if (st == DREAMS_OK) st = check_units(num_rows, num_heads, (head_dim + 15) / 16 + 1);
+  if (st == DREAMS_OK) st = check_units(num_rows, num_heads, row_units(head_dim, elem));
   if (st != DREAMS_OK) return st;
   if (batch > 65535) return fail(DREAMS_ERR_UNSUPPORTED, "problem too large");
   if (batch == 0 || num_rows == 0) return ok();
@@ -1983,7 +1986,7 @@ dreams_status_t dreams_paged_append_rope(const dreams_page_pool_t* pool, const d
   if (st == DREAMS_OK && (pool->batch == 0 || num_rows == 0)) return ok();
   if (st == DREAMS_OK) st = check_rope_pointers(rope, kv_len);
   if (st == DREAMS_OK)
-    st = check_units(num_rows, (queries ? queries->num_q_heads : 0) + 2LL * pool->num_kv_heads, (pool->head_dim + 15) / 16 + 1);
+    st = check_units(num_rows, (queries ? queries->num_q_heads : 0) + 2LL * pool->num_kv_heads, row_units(pool->head_dim, elem));
   if (st == DREAMS_OK) st = check_append_pointers(k_new, v_new, page_table, kv_len, row_len, k_pages, v_pages);
   if (st == DREAMS_OK) st = check_query_pointers(queries);
   if (st != DREAMS_OK) return st;
@@ -2011,8 +2014,9 @@ dreams_status_t dreams_paged_append_e4m3(const dreams_page_pool_t* pool, const d
   if (st == DREAMS_OK && rope) st = check_rope(rope, pool->head_dim, num_rows);
   if (st == DREAMS_OK && (pool->batch == 0 || num_rows == 0)) return ok();
   if (st == DREAMS_OK && rope) st = check_rope_pointers(rope, kv_len);
-  if (st == DREAMS_OK)
-    st = check_units(num_rows + 32LL, (queries ? queries->num_q_heads : 0) + 2LL * pool->num_kv_heads, pool->head_dim / 16);
+  if (st == DREAMS_OK)      // (a wave, so 4 lanes a row at least, for every block of 16 rows of a head)
+    st = check_units(num_rows + 32LL, (queries ? queries->num_q_heads : 0) + 2LL * pool->num_kv_heads,
+                     std::max(pool->head_dim / 16, 4));
   if (st == DREAMS_OK) st = check_append_pointers(k_new, v_new, page_table, kv_len, row_len, k_pages, v_pages);
   if (st == DREAMS_OK) st = check_query_pointers(queries);
   if (st == DREAMS_OK) st = check_scale_pointers(scales);

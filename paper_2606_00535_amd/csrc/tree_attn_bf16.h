@@ -364,9 +364,9 @@ __device__ __forceinline__ SpreadPlan spread_plan(const AttnArgs& a, int lane) {
     }
     sp.steps = max((N - gap + kStep - 1) / kStep, 1);    // (a sequence without keys has its rows' zeros to write)
   }
-  int total = sp.steps;      // (below 2^31: 64 sequences of 2^25 steps at most)
+  uint32_t total = (uint32_t)sp.steps;      // (64 sequences of 2^25 steps at most)
 #pragma unroll
-  for (int off = 1; off < 64; off <<= 1) total += __shfl_xor(total, off);
+  for (int off = 1; off < 64; off <<= 1) total += (uint32_t)__shfl_xor((int)total, off);
   const int even = (int)(((long long)total * a.Hkv + a.spread_wgs - 1) / a.spread_wgs);
   const int base = max(even, kSpreadMinSteps), mine = base + (int)((long long)base * lane / 24);
   const float inv = 1.0f / (float)mine;
@@ -862,18 +862,18 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
     if constexpr (E8) {
       read_ops8(op, jj);
     } else {
-    const unsigned char* tile = ring + (jj & (NSS - 1)) * KW * L::SLOT + kw * L::SLOT;
-    const unsigned char* vt = tile + L::HALF;
+      const unsigned char* tile = ring + (jj & (NSS - 1)) * KW * L::SLOT + kw * L::SLOT;
+      const unsigned char* vt = tile + L::HALF;
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
+      for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-      for (int ds = 0; ds < DS; ++ds) op.kf[kb][ds] = *(const bf16x8*)(tile + L::off(kb * 16 + ka_row, ds * 4 + quad));
+        for (int ds = 0; ds < DS; ++ds) op.kf[kb][ds] = *(const bf16x8*)(tile + L::off(kb * 16 + ka_row, ds * 4 + quad));
 #pragma unroll
-    for (int d = 0; d < DB; ++d) {
-      const int c = d * 2 + tr_c;
-      op.vlo[d] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(vt + L::off(tr_row, c) + tr_half));
-      op.vhi[d] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(vt + L::off(16 + tr_row, c) + tr_half));
-    }
+      for (int d = 0; d < DB; ++d) {
+        const int c = d * 2 + tr_c;
+        op.vlo[d] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(vt + L::off(tr_row, c) + tr_half));
+        op.vhi[d] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(vt + L::off(16 + tr_row, c) + tr_half));
+      }
     }
   };
   // the key fragments of a step, and a block of its values

@@ -46,6 +46,8 @@ def test_rope(D):
     assert call(rope(D, parent=0x100000), N=129) == -1 and b"tree nodes" in lib.dreams_last_error_message()
     assert call(rope(D), B=0) == 0 and call(rope(D), N=0) == 0
     assert call(rope(D), dt=0, dim=68) == -2 and call(rope(D), dt=0, dim=520) == -2
+    # (fp32 rows have twice the units: more than 2^31 of them, fewer in bf16 -- which the null pointer then refuses)
+    assert call(rope(D), N=1 << 25, dt=0, x=None, B=1) == -2 and call(rope(D), N=1 << 25, x=None, B=1) == -1
 
 
 def test_frequencies(D):
@@ -116,6 +118,8 @@ def test_appends(D):
     assert eight(pool(D, num_layers=1), q=queries()) == -1 and b"need rope" in lib.dreams_last_error_message()
     assert eight(pool(D, dtype=D.DREAMS_F32)) == -1 and eight(pool(D), dt=2) == -1
     assert eight(pool(D, head_dim=520)) == -2 and eight(pool(D, head_dim=72)) == -2
+    # (a wave a block of 16 rows of a head: 2^32 threads and more, however short the rows)
+    assert eight(pool(D, head_dim=16), n=1 << 27) == -2 and eight(pool(D, head_dim=16), n=1 << 25, k=None) == -1
     for s in (D.PageScales(None, 0x100000, 0, 0), D.PageScales(0x100000, None, 0, 0), D.PageScales(0x100000, 0x100000, 0, 1),
               D.PageScales(0x100000, 0x100000, 0, -4), D.PageScales(0x100000, 0x100000, 100, 0),
               D.PageScales(0x100000, 0x100000, 0, 1 << 60), D.PageScales(0x100000, 0x100000, -1, 0)):
