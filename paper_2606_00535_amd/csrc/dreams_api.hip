@@ -1307,6 +1307,24 @@ int paged_pieces(int n_keys, long long xcd_wgs, long long xcd_cus, bool level) {
   return pieces;
 }
 
+// Pieces of the key axis for 16 rows over pages of 8 bits, up to `splits`: the number that takes the least time, in keys that
+// a compute unit's workgroups go through one after another (two that run together share its copies: one alone is about as
+// fast).  Pieces cost 500 keys' time for their merge; with several sequences their lengths differ, and pieces even that out
+// (a quarter less).  8 x 32 heads, one row: behind 1000 each 16.6 us whole, 20.9 in 2 pieces; 100 to 1000 15.9, 19.1; 3000 each
+// 35.2, 40.6; 100 to 3000 33.5, 30.2; 4 x 32 behind 3000 33.2, 26.0.
+int token_pieces(long long xcd_wgs, long long xcd_cus, int n_keys, int splits, bool several) {
+  int pieces = 1;
+  long long best = 0;
+  for (int s = 1; s <= splits; ++s) {
+    const long long deep = (xcd_wgs * s + xcd_cus - 1) / xcd_cus, keys = deep * ((n_keys + s - 1) / s);
+    const long long cost = s == 1 ? keys : (several ? keys * 3 / 4 : keys) + 500;
+    if (s > 1 && cost >= best) continue;
+    best = cost;
+    pieces = s;
+  }
+  return pieces;
+}
+
 // Whether the keys of all sequences are spread over the workgroups in pieces of one length, with a second launch that merges
 // them (AttnArgs::spread_wgs), instead of as many pieces of every unit as merge on its die.  It costs 2 to 3 us more, 380
 // keys of a compute unit, and pays where units leave dies or compute units idle (a token's rows of 4 KV heads behind 32768:
@@ -1382,6 +1400,7 @@ dreams_status_t plan_paged(const dreams_paged_desc_t* d, bool prompt, bool e4m3,
       const int fine = fine_splits(xcd_wgs, xcd_cus, wpc, n_keys);
       if (fine < splits || 5 * fine >= 7 * splits) splits = fine;
     }
+    if (e4m3 && p.rows_per_wg == 16) splits = token_pieces(xcd_wgs, xcd_cus, n_keys, splits, d->batch > 1);
     if (e4m3 && spread_pays(d, p, parts, std::max(splits, 1), n_keys, cus)) {
       plan->spread_wgs = std::max(p.rows_per_wg == 64 ? 2 * cus : cus, 2 * p.units);
       const size_t rows = (size_t)plan->spread_wgs * p.rows_per_wg;
