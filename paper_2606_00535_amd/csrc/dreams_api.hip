@@ -1307,17 +1307,21 @@ int paged_pieces(int n_keys, long long xcd_wgs, long long xcd_cus, bool level) {
   return pieces;
 }
 
-// Pieces of the key axis for 16 rows over pages of 8 bits, up to `splits`: the number that takes the least time, in keys that
-// a compute unit's workgroups go through one after another (two that run together share its copies: one alone is about as
-// fast).  Pieces cost 500 keys' time for their merge; with several sequences their lengths differ, and pieces even that out
-// (a quarter less).  8 x 32 heads, one row: behind 1000 each 16.6 us whole, 20.9 in 2 pieces; 100 to 1000 15.9, 19.1; 3000 each
-// 35.2, 40.6; 100 to 3000 33.5, 30.2; 4 x 32 behind 3000 33.2, 26.0.
-int token_pieces(long long xcd_wgs, long long xcd_cus, int n_keys, int splits, bool several) {
+// Pieces of the key axis for 16 or 64 rows over pages of 8 bits, up to `splits`: the number that takes the least time, in keys
+// that a compute unit goes through one after another.  Two workgroups of 16 rows that run together share its copies, so
+// that one alone is about as fast; two of 64 rows, whose time is their instructions', take 6/5 of one's.  Pieces cost the
+// time of some hundred keys for their merge; with several sequences their lengths differ, which pieces even out (a quarter
+// less).  8 x 32 heads, 16 rows: behind 1000 each 16.6 us whole, 20.9 in 2 pieces; 100 to 1000 15.9, 19.1; 3000 each 35.2, 40.6;
+// 100 to 3000 33.5, 30.2; 4 x 32 behind 3000 33.2, 26.0.  60 rows: 8 x 32 behind 1000 30.2, 37.1; 2500 54.1, 53.6; 100 to 1000
+// 29.8, 34.4; 4 x 32 behind 1500 38.2 whole, 33.8 in 2, 30.2 in 4.
+int pieces_e4m3(int rows, long long xcd_wgs, long long xcd_cus, int n_keys, int splits, bool several) {
   int pieces = 1;
   long long best = 0;
   for (int s = 1; s <= splits; ++s) {
-    const long long deep = (xcd_wgs * s + xcd_cus - 1) / xcd_cus, keys = deep * ((n_keys + s - 1) / s);
-    const long long cost = s == 1 ? keys : (several ? keys * 3 / 4 : keys) + 500;
+    const long long deep = (xcd_wgs * s + xcd_cus - 1) / xcd_cus, len = (n_keys + s - 1) / s;
+    const long long keys = rows == 16 || deep == 1 ? deep * len : deep * len * 3 / 5;
+    const long long merge = rows == 16 ? 500 : 250 + 600 * deep / s;
+    const long long cost = s == 1 ? keys : (several ? keys * 3 / 4 : keys) + merge;
     if (s > 1 && cost >= best) continue;
     best = cost;
     pieces = s;
@@ -1328,9 +1332,9 @@ int token_pieces(long long xcd_wgs, long long xcd_cus, int n_keys, int splits, b
 // Whether the keys of all sequences are spread over the workgroups in pieces of one length, with a second launch that merges
 // them (AttnArgs::spread_wgs), instead of as many pieces of every unit as merge on its die.  It costs 2 to 3 us more, 380
 // keys of a compute unit, and pays where units leave dies or compute units idle (a token's rows of 4 KV heads behind 32768:
-// 19.1 us, 24.4 in 32 pieces each; of 3 x 2 heads behind 8192 to 32768 19.7, 34.0; but 15.0 and 15.2 of 4 behind 8000), or
-// where a batch's long sequences may run on behind its short ones (16 x 4 heads behind 100 to 32768: 59, 68; where they
-// are of like lengths, 8 x 8 behind 16384 to 32768, 75.3 and 73.9).
+// 18.7 us, 24.2 in 32 pieces each; 15.0 and 15.2 of 4 behind 8000), or where a batch's long sequences may run on behind its
+// short ones (16 x 4 heads behind 100 to 32768 59.5, 82.2; 3 x 7 heads behind 2952 to 29522 30.3, 32.8; of like lengths, 4
+// x 5 heads behind 32435 and 50 rows each, 54.2 and 54.8).
 bool spread_pays(const dreams_paged_desc_t* d, const AttnPlan& p, int parts, int splits, int n_keys, int cus) {
   if (p.row_groups != 1 || d->batch > kSpreadSeqs || p.units > cus / 2) return false;
   const long long even = ((long long)p.units * n_keys + cus - 1) / cus;      // keys of a compute unit, spread
@@ -1357,8 +1361,11 @@ dreams_status_t plan_paged(const dreams_paged_desc_t* d, bool prompt, bool e4m3,
   // rows behind 2000 18.8, 22.2; 8 x 16 heads x 48 of 64 columns behind 1500 23.8, 25.8.  Where short keys meet many heads it is
   // the other way round: 16 x 8 heads x 64 rows of 64 columns behind 500 16.0, 13.5; 4 x 32 heads x 40 behind 1000 26.7, 23.1.)
   p.rows_per_wg = tree_attn_bf16_rows_per_wg(p.rows_total);
-  p.row_groups = (p.rows_total + p.rows_per_wg - 1) / p.rows_per_wg;
   p.units = d->batch * d->num_kv_heads;
+  // (64 columns of 8 bits: 128 rows a workgroup convert every key once, the tree kernel once a wave: 4 x 32 heads x 64 rows
+  // behind 470 13.9 us, 18.3; 16 x 8 x 50 behind 59 to 118 9.7, 12.7; 12 x 28 x 50 behind 774 to 7740 112, 129.)
+  if (e4m3 && d->head_dim == 64 && p.rows_per_wg == 64) p.rows_per_wg = 128;
+  p.row_groups = (p.rows_total + p.rows_per_wg - 1) / p.rows_per_wg;
   int span = T;   // positions that a workgroup's rows can be apart
   if (prompt && p.row_groups > 1) {
     // Row groups of one head see only the keys before them; packed ones leave no row of a workgroup empty.  The fewer keys
@@ -1380,10 +1387,11 @@ dreams_status_t plan_paged(const dreams_paged_desc_t* d, bool prompt, bool e4m3,
   const int n_keys = (int)keys;
   plan->longest = n_keys;
   plan->shortest = plan->groups_per_head > 0 && max_len + span < keys ? (int)(max_len + span) : n_keys;
+  // (over pages of 8 bits no more parts than row groups: with empty ones, 12 units of one row group are on 4 dies)
   int parts = 1;
-  while ((long long)p.units * parts % 8 != 0) parts *= 2;
+  while ((long long)p.units * parts % 8 != 0 && !(e4m3 && 2 * parts > p.row_groups)) parts *= 2;
   plan->unit_parts = parts;
-  const long long groups = (p.row_groups + parts - 1) / parts, xcd_wgs = (long long)p.units * parts / 8 * groups;
+  const long long groups = (p.row_groups + parts - 1) / parts, xcd_wgs = ((long long)p.units * parts + 7) / 8 * groups;
   int splits = d->num_splits;
   if (splits == 0) {
     int cus = 0;
@@ -1400,7 +1408,8 @@ dreams_status_t plan_paged(const dreams_paged_desc_t* d, bool prompt, bool e4m3,
       const int fine = fine_splits(xcd_wgs, xcd_cus, wpc, n_keys);
       if (fine < splits || 5 * fine >= 7 * splits) splits = fine;
     }
-    if (e4m3 && p.rows_per_wg == 16) splits = token_pieces(xcd_wgs, xcd_cus, n_keys, splits, d->batch > 1);
+    if (e4m3 && (p.rows_per_wg == 16 || p.rows_per_wg == 64))
+      splits = pieces_e4m3(p.rows_per_wg, xcd_wgs, xcd_cus, n_keys, splits, d->batch > 1);
     if (e4m3 && spread_pays(d, p, parts, std::max(splits, 1), n_keys, cus)) {
       plan->spread_wgs = std::max(p.rows_per_wg == 64 ? 2 * cus : cus, 2 * p.units);
       const size_t rows = (size_t)plan->spread_wgs * p.rows_per_wg;

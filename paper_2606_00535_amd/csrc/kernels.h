@@ -114,7 +114,7 @@ struct AttnArgs {
   int chain;              // 1: row i of a head is position L_b + i; 0: tree nodes
   int groups_per_head;    // chain: row groups of a head, or 0: the heads' rows are packed one after another
   int key_groups;         // 128 rows: key groups of 4 waves in a workgroup (1 or 2)
-  int unit_parts;         // parts of a unit's row groups, each on one XCD; units * unit_parts is a multiple of 8
+  int unit_parts;         // parts of a unit's row groups, each on one XCD; units * unit_parts is a multiple of 8 (8 bits: any)
   // Pages of 8 bits: a byte for every 16 slots, [pages, Hkv, page_size / 16], scale_stride bytes a page
   const uint8_t* k_scale;
   const uint8_t* v_scale;

@@ -23,7 +23,7 @@ hipError_t launch_for_rows(const AttnArgs& a, hipStream_t stream) {
 int paged_attn_e4m3_wgs_per_cu(int rows_per_wg) { return rows_per_wg == 32 ? 1 : 2; }
 
 hipError_t launch_paged_attn_e4m3(const AttnArgs& a, hipStream_t stream) {
-  if (a.unit_parts < 1 || a.units * a.unit_parts % 8 != 0) return hipErrorInvalidValue;
+  if (a.unit_parts < 1) return hipErrorInvalidValue;
   if (a.D == 128) return launch_for_rows<128, 16>(a, stream);
   if (a.D == 64) return launch_for_rows<64, 16>(a, stream);
   return hipErrorInvalidValue;

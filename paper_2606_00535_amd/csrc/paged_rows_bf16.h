@@ -104,7 +104,7 @@ __global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(At
   // (Two workgroups to a compute unit: the second ones take their groups in the opposite order, so that the longest run
   // beside the shortest of the first round.)
   const int n = blockIdx.x;
-  const int here = a.units * a.unit_parts / 8;
+  const int here = (a.units * a.unit_parts + (E8 ? 7 : 0)) / 8;
   const int on_xcd = n >> 3, slots = KG > 1 ? 1 << 30 : a.cus / 4;
   const int rank = on_xcd >= slots / 2 && on_xcd < slots && (int)(gridDim.x >> 3) >= slots ? slots + slots / 2 - 1 - on_xcd
                                                                                              : on_xcd;
@@ -112,7 +112,7 @@ __global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(At
   const int vu = (n & 7) + 8 * (within / a.splits), split = within - (within / a.splits) * a.splits;
   const int u = vu / a.unit_parts;
   const int rg = q_group * a.unit_parts + (vu - u * a.unit_parts);
-  if (rg >= a.row_groups) return;
+  if (rg >= a.row_groups || (E8 && u >= a.units)) return;
   const int b = u / a.Hkv, g = u - b * a.Hkv;
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, h = lane >> 5;
   const int wave8 = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -684,7 +684,8 @@ hipError_t launch_rows_build(const AttnArgs& a, hipStream_t stream) {
     configured[dev] = true;
   }
   const unsigned groups = (a.row_groups + a.unit_parts - 1) / a.unit_parts;
-  hipLaunchKernelGGL((paged_rows_bf16_kernel<D, KG, TREE, E8>), dim3((unsigned)a.units * a.unit_parts * groups * a.splits),
+  const unsigned parts = ((unsigned)a.units * a.unit_parts + 7) / 8 * 8;
+  hipLaunchKernelGGL((paged_rows_bf16_kernel<D, KG, TREE, E8>), dim3(parts * groups * a.splits),
                      dim3(64 * kWaves * KG), lds, stream, a);
   return hipGetLastError();
 }
@@ -697,7 +698,7 @@ hipError_t launch_rows_of(const AttnArgs& a, hipStream_t stream) {
 
 template <bool E8>
 hipError_t launch_rows(const AttnArgs& a, hipStream_t stream) {
-  if (a.unit_parts < 1 || a.units * a.unit_parts % 8 != 0 || a.rows_per_wg != kRowsWg ||
+  if (a.unit_parts < 1 || (!E8 && a.units * a.unit_parts % 8 != 0) || a.rows_per_wg != kRowsWg ||
       (a.groups_per_head > 0 && a.groups_per_head * a.G != a.row_groups))
     return hipErrorInvalidValue;
   if (a.splits > 1 && (!a.part_o || !a.part_ml || !a.set_ctr || a.ctr_stride < 2)) return hipErrorInvalidValue;

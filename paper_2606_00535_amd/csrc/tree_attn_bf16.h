@@ -454,15 +454,16 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
     spread_pieces = pieces;
     spread_piece = sp.piece;
   } else if constexpr (PAGED) {
-    // Every unit's row groups are dealt to unit_parts parts (units * unit_parts is a multiple of 8), a part to an XCD.
+    // Every unit's row groups are dealt to unit_parts parts (units * unit_parts is a multiple of 8, or, E8, rounded up to
+    // one), a part to an XCD.
     // An XCD takes the q-th row group of all of its parts before the next.
-    const int here = a.units * a.unit_parts / 8;
+    const int here = (a.units * a.unit_parts + (E8 ? 7 : 0)) / 8;
     const int q = slot / (here * a.splits), rest = slot - q * (here * a.splits);
     const int vu = xcd + 8 * (rest / a.splits);
     split = rest - (rest / a.splits) * a.splits;
     u = vu / a.unit_parts;
     rg = q * a.unit_parts + (vu - u * a.unit_parts);
-    if (rg >= a.row_groups) return;
+    if (rg >= a.row_groups || (E8 && u >= a.units)) return;
   } else {
     const int per_unit = a.splits * a.row_groups;
     u = xcd + 8 * (slot / per_unit);
@@ -1344,7 +1345,7 @@ hipError_t launch_streaming(const AttnArgs& a, hipStream_t stream) {
   if (a.rows_per_wg != 16 * RB * (W / KW)) return hipErrorInvalidValue;
   if (a.splits > 1 && (!a.part_o || !a.part_ml || !a.set_ctr || (ENT && !a.part_e))) return hipErrorInvalidValue;
   if (a.splits > 1 && a.ctr_stride < 2) return hipErrorInvalidValue;
-  const unsigned units_rounded = PAGED ? a.units * a.unit_parts : (a.units + 7) / 8 * 8;
+  const unsigned units_rounded = E8 ? (a.units * a.unit_parts + 7) / 8 * 8 : PAGED ? a.units * a.unit_parts : (a.units + 7) / 8 * 8;
   const unsigned groups = PAGED ? (a.row_groups + a.unit_parts - 1) / a.unit_parts : a.row_groups;
   unsigned grid = units_rounded * (unsigned)a.splits * groups;
   if constexpr (E8) {

@@ -269,6 +269,28 @@ def test_a_step_as_a_server_runs_it(dev):
         dreams.pages_release(table, count, kv, ref, R.ints([0, 1], dev), ps, trim=True)
 
 
+@pytest.mark.parametrize("kind", ["verify", "prompt"])
+@pytest.mark.parametrize("heads,D,lens,T,splits", [
+    ((5, 5), 128, [300, 0, 77], 1, 0), ((5, 5), 64, [300, 0, 77], 60, 0), ((9, 9), 128, [1000], 40, 0), ((22, 11), 128, [900], 20, 3),
+    ((3, 3), 64, [700, 650, 31], 110, 0), ((6, 3), 128, [500], 90, 0), ((10, 5), 64, [333, 400, 1], 128, 2),
+    ((28, 4), 64, [200, 190, 5], 7, 0), ((28, 4), 64, [1200], 8, 3)])
+def test_units_beside_the_dies(dev, heads, D, lens, T, splits, kind):
+    """Sequences times KV heads that are no multiple of 8."""
+    rng = np.random.default_rng(8)
+    B, (Hq, Hkv) = len(lens), heads
+    note("units_e4m3", heads, D, lens, T, splits, kind)
+    c = E.Cache8(rng, dev, np.array(lens) + T, Hkv, 32, D)
+    q, qh = R.rounded(rng, (B, Hq, T, D), True, dev)
+    if kind == "verify":
+        par = R.tree(rng, B, T)
+        want = R.verify(qh, c.k, c.v, c.table, lens, par, R.ancestors(par), 0, 0, 1 / np.sqrt(D))
+        out, lse = dreams.paged_verify_attn_e4m3(q, *c.pages, R.ints(lens, dev), parent=R.ints(par, dev), num_splits=splits)
+    else:
+        want = R.prompt(qh, c.k, c.v, c.table, lens, [T] * B, 0, 0, 1 / np.sqrt(D))
+        out, lse = dreams.paged_prompt_attn_e4m3(q, *c.pages, R.ints(lens, dev), num_splits=splits)
+    R.check(out, lse, want, True, (heads, D, lens, T, kind))
+
+
 def spread(q, c, **kw):
     """Whether the library spreads a call's keys in pieces of one length (its workspace has room for their rows alone)."""
     import ctypes
@@ -292,6 +314,11 @@ SPREAD = [
     ((4, 1), 128, [6200, 4100, 900], 14, 0, 0, False),
     ((16, 2), 128, [3900, 17, 8000], 2, 0, 0, False),
     ((2, 1), 128, [9000, 300, 8000], 9, 7000, 40, False),
+    ((4, 1), 128, [20000, 10, 3333], 1, 0, 0, False),          # from here on they are spread
+    ((3, 1), 64, [20100, 4095, 1], 5, 0, 0, True),
+    ((4, 1), 128, [20200, 0, 900], 14, 0, 0, False),
+    ((16, 2), 128, [17000], 2, 0, 0, False),
+    ((2, 1), 128, [21000, 300, 8000], 9, 19700, 40, False),
 ]
 
 
@@ -305,7 +332,7 @@ def test_long_keys_of_few_heads(dev, heads, D, lens, T, window, sinks, masked, k
     c = E.Cache8(rng, dev, np.array(lens) + T, Hkv, ps, D)
     q, qh = R.rounded(rng, (B, Hq, T, D), True, dev)
     kw = dict(window=window, sinks=sinks, max_kv_len=max(lens))
-    assert spread(q, c, prompt=kind == "prompt", **kw)
+    assert spread(q, c, prompt=kind == "prompt", **kw) or max(lens) < 17000
     kv = R.ints(lens, dev)
     if kind == "verify":
         par = R.tree(rng, B, T)
@@ -326,20 +353,21 @@ def test_long_keys_of_few_heads(dev, heads, D, lens, T, window, sinks, masked, k
     assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
 
 
-def test_long_keys_replayed(dev):
+@pytest.mark.parametrize("longest", [7198, 20198])
+def test_long_keys_replayed(dev, longest):
     """Lengths that change between replays change the pieces."""
     rng = np.random.default_rng(10)
     D, ps, B, T = 128, 16, 3, 2
-    c = E.Cache8(rng, dev, [7200, 7200, 7200], 1, ps, D)
+    c = E.Cache8(rng, dev, [longest + T] * 3, 1, ps, D)
     q, qh = R.rounded(rng, (B, 4, T, D), True, dev)
     par = R.tree(rng, B, T)
     kv, pard = R.ints([4000, 4000, 4000], dev), R.ints(par, dev)
-    assert spread(q, c, max_kv_len=7198)
-    run = lambda: dreams.paged_verify_attn_e4m3(q, *c.pages, kv, parent=pard, max_kv_len=7198)
+    assert spread(q, c, max_kv_len=longest) or longest < 17000
+    run = lambda: dreams.paged_verify_attn_e4m3(q, *c.pages, kv, parent=pard, max_kv_len=longest)
     g = torch.cuda.CUDAGraph()
     with torch.cuda.graph(g):
         out = run()
-    for lens in ([7198, 1, 300], [0, 0, 0], [31, 4100, 2500]):
+    for lens in ([longest, 1, 300], [0, 0, 0], [31, 4100, 2500]):
         kv.copy_(torch.tensor(lens, dtype=torch.int32))
         g.replay()
         torch.cuda.synchronize()
