@@ -6,19 +6,20 @@
 namespace dreams {
 namespace {
 
-// cos and sin of position * freq radians, times gain.  The angle is reduced in fp64 to a quarter turn (its error grows
-// with the turns, 2^-52 of them), the rest r, |r| <= 1/2 quarter turn, goes through the Taylor polynomials of sine
-// and cosine about 0: the first terms left out are x^11/11! < 2e-9 and x^12/12! < 2e-10 at x = pi/4, below half an ulp of fp32.
+// cos and sin of position * freq radians, times gain.  In fp64 and rounded once, so that the rotated columns are as near as
+// fp32 products can be: rows that go into 8 bits fall on another code where an error reaches its border.  The angle is reduced
+// to a quarter turn (its error grows with the turns, 2^-52 of them); the rest x, |x| <= pi/4, goes through the Taylor
+// polynomials of sine and cosine about 0, whose first terms left out are x^13/13! < 7e-12 and x^12/12! < 2e-10.
 __device__ __forceinline__ void turn(double position, double freq, float gain, float* c, float* s) {
   const double t = position * (freq * 0.15915494309189533577);
   const double u = 4.0 * (t - rint(t)), quarter = rint(u);
-  const float x = (float)(u - quarter) * 1.5707963267948966f, y = x * x;
-  const float sn = x * fmaf(y, fmaf(y, fmaf(y, fmaf(y, 1.0f / 362880, -1.0f / 5040), 1.0f / 120), -1.0f / 6), 1.0f);
-  const float cs = fmaf(y, fmaf(y, fmaf(y, fmaf(y, fmaf(y, -1.0f / 3628800, 1.0f / 40320), -1.0f / 720), 1.0f / 24), -0.5f), 1.0f);
+  const double x = (u - quarter) * 1.57079632679489661923, y = x * x;
+  const double sn = x * fma(y, fma(y, fma(y, fma(y, fma(y, -1.0 / 39916800, 1.0 / 362880), -1.0 / 5040), 1.0 / 120), -1.0 / 6), 1.0);
+  const double cs = fma(y, fma(y, fma(y, fma(y, fma(y, -1.0 / 3628800, 1.0 / 40320), -1.0 / 720), 1.0 / 24), -0.5), 1.0);
   const int q = (int)quarter;
-  const float a = (q & 1) ? sn : cs, b = (q & 1) ? cs : sn;
-  *c = gain * ((q + 1) & 2 ? -a : a);
-  *s = gain * (q & 2 ? -b : b);
+  const double a = (q & 1) ? sn : cs, b = (q & 1) ? cs : sn, g = (double)gain;
+  *c = (float)(g * ((q + 1) & 2 ? -a : a));
+  *s = (float)(g * (q & 2 ? -b : b));
 }
 
 // Depth of tree node i by parents in LDS (an entry that breaks the rules ends the walk).

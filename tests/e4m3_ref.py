@@ -1,10 +1,9 @@
 """Plain definitions of rotary positions and of pages in 8 bits (numpy), for their tests.
 
-Rotation tolerances.  The angle's quarter turns, r (|r| <= 1/2), come from 64 bits with 2^-51 of the turns at most (two
-products' and one constant's roundings), r itself, its product with pi/2 and that constant are rounded to fp32 (3 half steps of
-2^-24 at most pi/4), the polynomials leave out 2e-9 and round their last steps: under 4 * 2^-24 on a cosine or sine.  The
-gain and the two products' roundings add 3 half steps: |got - (a cos - b sin)| <= gain (|a| + |b|) (8 * 2^-24 + 2 pi 2^-51 turns).
-bf16 adds half a step of 2^-8 of the result."""
+Rotation tolerances.  Angles, sines and cosines are computed in 64 bits -- 2^-51 of the turns at most (two products' and one
+constant's roundings), polynomials off by 2e-10 = 2^-32 -- and rounded to fp32 with the gain, half a step of 2^-24.  One product
+and the sum add a half step each: |got - (a cos - b sin)| <= gain (|a| + |b|) (4 * 2^-24 + 2 pi 2^-51 turns).  bf16 adds half a
+step of 2^-8 of the result."""
 import numpy as np
 import torch
 
@@ -32,7 +31,7 @@ def rotate(x, position, freq, gain, interleaved):
 
 def check_rotation(got, want, size, far, bf16, label):
     got = np.asarray(got, np.float64)
-    tol = size * (8 * 2.0 ** -24 + 2 * np.pi * 2.0 ** -51 * far)
+    tol = size * (4 * 2.0 ** -24 + 2 * np.pi * 2.0 ** -51 * far)
     if bf16:
         tol = np.where(size > 0, tol * (1 + 2.0 ** -8) + 2.0 ** -8 * np.abs(want), 0.0)   # (other columns: bit for bit)
     err = np.abs(got - want)
