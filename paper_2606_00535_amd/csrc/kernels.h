@@ -312,7 +312,7 @@ struct CommitArgs {
 hipError_t launch_kv_commit(const CommitArgs& a, hipStream_t stream);
 
 // -------------------------------------------------------------------------------------- rotary positions
-// Units of 8 pairs (16 columns): the rotated part of a head's row is R / 16 of them, the rest ceil((D - R) / 16) more.
+// A row of a head in units of two 16-byte runs (rope.h): R columns that are rotated, then D - R that are not.
 struct RopeArgs {
   const double* freq;        // [R / 2] radians a position; nullptr: nothing is rotated
   const int32_t* positions;  // [B, N] or nullptr

@@ -7,8 +7,13 @@
 //     their rows are in registers before one is written.  As in the 16-bit cache a row's source lies at or behind its slot, so that no
 //     block's rows or scale are changed before they are read.
 //   * read: a thread per 8 codes.
-// A code times a power of two is exact in bf16, and a scale that grows moves a code's exponent: only codes that fall below
-// e4m3's normal range are rounded again.
+// A value x becomes the code nearest to x 2^(127 - s), where s is the least byte at which the block's largest magnitude is at
+// most 448 2^(s - 127); the byte follows from that magnitude's bits.  A code times a power of two is exact in bf16, and a scale
+// that grows moves a code's exponent: only codes that fall below e4m3's normal range are rounded again.  A scale for 16 slots
+// makes the wave's own lanes enough to find it, and a block's rows lie in one page.
+// What bounds them: append, the memory and the chain of load, wave maximum and store (32 heads x 3136 rows with their queries,
+// 128 MB, 29.4 us, 4.4 TB/s; without the queries 20.8, unrotated 17.5; 8 x 60 nodes of 8 heads 7.5).  Commit, the chain of path,
+// table, rows (8 sequences 4.7).  Read, the memory (32 x 3136 slots, 77 MB, 13.9 us, 5.5 TB/s).
 #include "rope.h"
 
 #include <algorithm>

@@ -1,4 +1,4 @@
-// Rotary positions: the angle of a row's pairs, and units of 8 pairs of a row in registers.
+// Rotary positions: the angles of a row's pairs, and units (two runs of columns) of a row in registers.
 #pragma once
 
 #include "kernels.h"

@@ -48,6 +48,10 @@
 //     token of 32 heads on 4 sequences with 1028 keys in sight 13.0 us from HBM, nearly all of it latency: lengths, table,
 //     ring, exchange, merge.  10 to 42 scalar registers spill to lanes of vector registers, with up to
 //     16 accesses in the loop over steps.)
+//   * Over pages of 8 bits (E8) the ring holds codes and, beside it, a step's four scale bytes; they become bf16 on the way from
+//     LDS into the products, so that a ring of the same size is twice as deep.  Keys in other rows than the bf16 build's (key_row) let
+//     the 8-bit transposing reads deliver values in the order of the probabilities.  The keys of a batch may also be spread
+//     over all workgroups in pieces of one length, merged by a second launch (SpreadPlan).
 #pragma once
 
 #include "kernels.h"
