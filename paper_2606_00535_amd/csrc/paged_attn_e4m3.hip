@@ -1,12 +1,12 @@
 // Attention over a paged cache in 8 bits, up to 64 rows a workgroup: the builds of the kernel in tree_attn_bf16.h that read
 // e4m3 pages and their scales.
 //
-// Tokens of long contexts are bound by the memory (8 sequences x 8 KV heads behind 16384 to 32768 slots, 403 MB, 76.5 us with
-// the launch that merges: 5.3 TB/s; 8 x 32 heads behind 6000 each 62 us, 6.3 TB/s), those of short ones by the chain of
+// Tokens of long contexts are bound by the memory (8 sequences x 8 KV heads behind 16384 to 32768 slots, 403 MB, 74.8 us with
+// the launch that merges: 5.4 TB/s; 8 x 32 heads behind 6000 each 62 us, 6.3 TB/s), those of short ones by the chain of
 // lengths, table, first copies and merge (4 sequences with 1028 keys in sight 13.7).  64 rows are bound by instructions: a
-// step of a wave (32 rows, 32 keys) is 32 products, 64 conversions, 16 exponentials, 110 other vector and 180 scalar
+// step of a wave (32 rows, 32 keys) is 32 products, 64 conversions, 16 exponentials, 110 other vector and 120 scalar
 // instructions, about half of its time, a third is waits for barriers and counts (32 heads x 60 nodes behind 3136 slots
-// 22.2 us; bf16 pages, twice the bytes: 22.3).
+// 22.0 us; bf16 pages, twice the bytes: 22.3).
 // Tried there: two steps' operands in registers (24.7), reads ahead of the copies' addresses and look-ups behind the score
 // product (registers spill at 128 columns, 20.3 instead of 19.5 us at 64).
 #include "tree_attn_bf16.h"
@@ -17,14 +17,20 @@ namespace {
 // (16 rows: two workgroups of half a ring each to a compute unit: 8 x 8 KV heads of 16384 to 32768 tokens, one row of 4 heads
 // each, 85.5 us with one of a whole ring, 73.9 with two.  64 rows: 8 waves in 4 key groups, one workgroup to a unit, would be
 // 22.6 us instead of 22.0 for 32 heads x 60 nodes behind 3136.)
-template <int D, int NST>
+// (64 rows of 64 columns are on the 128-row kernel.)
+template <int D, bool WIDE>
 hipError_t launch_for_rows(const AttnArgs& a, hipStream_t stream) {
   switch (a.rows_per_wg) {
-    case 16: return launch_streaming<D, 1, 4, 4, 1024 / D, 2, false, true, true>(a, stream);
-    case 32: return launch_streaming<D, 1, 4, 8, NST, 1, false, true, true>(a, stream);
-    case 64: return launch_streaming<D, 2, 2, 4, 1024 / D, 2, false, true, true>(a, stream);
+    case 16: return launch_streaming<D, 1, 4, 4, 1024 / D, 2, false, true, true, WIDE>(a, stream);
+    case 32: return launch_streaming<D, 1, 4, 8, 16, 1, false, true, true, WIDE>(a, stream);
+    case 64:
+      if constexpr (D == 128) return launch_streaming<D, 2, 2, 4, 1024 / D, 2, false, true, true, WIDE>(a, stream);
   }
   return hipErrorInvalidValue;
+}
+template <int D>
+hipError_t launch_for_pages(const AttnArgs& a, hipStream_t stream) {
+  return 1 << a.page_shift >= kStep ? launch_for_rows<D, true>(a, stream) : launch_for_rows<D, false>(a, stream);
 }
 
 }  // namespace
@@ -33,8 +39,8 @@ int paged_attn_e4m3_wgs_per_cu(int rows_per_wg) { return rows_per_wg == 32 ? 1 :
 
 hipError_t launch_paged_attn_e4m3(const AttnArgs& a, hipStream_t stream) {
   if (a.unit_parts < 1) return hipErrorInvalidValue;
-  if (a.D == 128) return launch_for_rows<128, 16>(a, stream);
-  if (a.D == 64) return launch_for_rows<64, 16>(a, stream);
+  if (a.D == 128) return launch_for_pages<128>(a, stream);
+  if (a.D == 64) return launch_for_pages<64>(a, stream);
   return hipErrorInvalidValue;
 }
 

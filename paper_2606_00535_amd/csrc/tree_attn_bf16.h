@@ -121,6 +121,19 @@ __device__ __forceinline__ void copy16_to_lds(uint32_t m0, const void* sbase, ui
 __device__ __forceinline__ void copy4_to_lds(uint32_t m0, const void* src) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(m0), "v"(src) : "memory");
 }
+// N copies to consecutive KB from m0 on, from one base: the instructions' offsets count on both sides, so voff[j % 2] are those
+// of rows that lie as in the first (two) KB.
+template <int N>
+__device__ __forceinline__ void copy_run_to_lds(uint32_t m0, const void* sbase, const uint32_t (&voff)[2]) {
+  static_assert(N == 2 || N == 4);
+  if constexpr (N == 2)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3 nt\n\t"
+                 "global_load_lds_dwordx4 %2, %3 offset:1024 nt" ::"s"(m0), "v"(voff[0]), "v"(voff[1]), "s"(sbase) : "memory");
+  else
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3 nt\n\t"
+                 "global_load_lds_dwordx4 %2, %3 offset:1024 nt\n\tglobal_load_lds_dwordx4 %1, %3 offset:2048 nt\n\t"
+                 "global_load_lds_dwordx4 %2, %3 offset:3072 nt" ::"s"(m0), "v"(voff[0]), "v"(voff[1]), "s"(sbase) : "memory");
+}
 // At most N of this wave's vector-memory operations still outstanding (they complete in issue order).
 template <int N>
 __device__ __forceinline__ void wait_vm() {
@@ -190,9 +203,9 @@ struct Rows8 {
 // The key of a step that operand row m of its block kb holds.
 __device__ __forceinline__ int key_row(int kb, int m) { return kb * 16 + (m ^ (8 * kb)); }
 
-// One byte into LDS (zero-extended to 32 bits) at m0, by the one lane that calls it.
-__device__ __forceinline__ void copy_byte_to_lds(uint32_t m0, const void* src) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_ubyte %1, %2" ::"s"(m0), "v"(0), "s"(src) : "memory");
+// Bytes into LDS (zero-extended to 32 bits), lane l's from src + voff to m0 + 4 l, by the lanes that call it.
+__device__ __forceinline__ void copy_byte_to_lds(uint32_t m0, const void* src, uint32_t voff) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_ubyte %1, %2" ::"s"(m0), "v"(voff), "s"(src) : "memory");
 }
 
 // Merge of a set's pieces for rows [r0, r0 + nrows) of the set, in piece order (so the result does not
@@ -400,7 +413,8 @@ constexpr size_t dynamic_lds(int R) {
 // E8 (paged): keys and values in e4m3 with a power-of-two scale for 16 slots of a head.  The ring holds their codes, and
 // they become bf16, exactly, in registers (v_cvt_scalef32_pk_bf16_fp8, the scale's exponent in the same instruction): a
 // step's 64 conversions a wave run beside its 16 RB products.
-template <int D, int RB, int KW, int W, int NST, bool PIPE, bool ENT, int WPC, bool PAGED, bool E8 = false>
+// WIDE (E8): pages of 32 slots or more, so that a step's keys lie in one.
+template <int D, int RB, int KW, int W, int NST, bool PIPE, bool ENT, int WPC, bool PAGED, bool E8 = false, bool WIDE = false>
 __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(AttnArgs a) {
   constexpr int WR = W / KW;          // waves per key group; each owns a different slice of the rows
   constexpr int RW = 16 * RB;         // query rows per wave
@@ -422,8 +436,10 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
   static_assert(W % KW == 0 && (NST & (NST - 1)) == 0 && NSS > QSS && NSS >= 2, "ring layout");
   static_assert(CPS * W == 4 * KW * C16 && CPS >= 1 && (C16 % CPS == 0 || CPS % C16 == 0), "copy split");
   static_assert(16 * V::ROW == C16 * 1024 && (E8 || (16 / L::RPL) % L::CPR == 0), "swizzle repeats every 16 rows");
-  constexpr int CPT = CPS + (E8 ? (CPS + C16 - 1) / C16 : 0);   // ... with the scales' (one for a block's codes)
+  // ... with the scales' (one for a block's codes, or (WIDE) two blocks')
+  constexpr int CPT = CPS + (WIDE ? CPS / (2 * C16) : E8 ? (CPS + C16 - 1) / C16 : 0);
   static_assert(!E8 || CPS % C16 == 0, "whole blocks");
+  static_assert(!WIDE || (E8 && (CPS == 2 * C16 || CPS == 4 * C16)), "a wave's copies are of one step");
   static_assert(NSS * CPT + ((QB + W - 1) / W) * L::C16 + 8 <= 63, "outstanding copies fit the counter");
   static_assert((size_t)(KW - 1) * R * D * 4 + (size_t)KW * R * 12 <= (size_t)NST * V::SLOT, "group states fit the ring");
 
@@ -558,7 +574,7 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
   // Paged: the pages of this wave's next super-step to copy, looked up a super-step ahead (scalar loads: the constant
   // address space, so that no vector load and no wait for one comes between the copies).
   typedef const __attribute__((address_space(4))) int32_t* const_table;
-  int next_page[PAGED ? NGRP : 1];
+  int next_page[PAGED && !WIDE ? NGRP : 1];
   auto group_slot = [&](int jj, int t) {
     const int bi = (wave * CPS + t * GRP) / C16;
     return slot_of(k_begin + (jj * KW + (bi >> 2)) * kStep) + 16 * (bi & 1);
@@ -567,7 +583,7 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
     if constexpr (PAGED) {
       const const_table table = (const_table)(uintptr_t)(a.table + (size_t)b * a.width);
 #pragma unroll
-      for (int t = 0; t < NGRP; ++t) next_page[t] = table[min(group_slot(jj, t) >> a.page_shift, a.width - 1)];
+      for (int t = 0; t < (WIDE ? 1 : NGRP); ++t) next_page[t] = table[min(group_slot(jj, t) >> a.page_shift, a.width - 1)];
     }
   };
   auto issue_group = [&](int jj, int t) {
@@ -589,7 +605,7 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
         const uint8_t* byte = (part ? a.v_scale : a.k_scale) + (int64_t)page * a.scale_stride +
                               (int64_t)((((size_t)g << a.page_shift) + row) / kScaleBlock);
         const uint32_t at = scale_base + ((jj & (NSS - 1)) * KW + sis) * 16 + part * 8 + half * 4;
-        if (lane == 0) copy_byte_to_lds(at, byte);
+        if (lane == 0) copy_byte_to_lds(at, byte, 0u);
       }
     } else if (key0 + 16 <= a.S_cap) {
       const unsigned char* src = pbase + (size_t)key0 * L::ROW;
@@ -604,9 +620,34 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
       }
     }
   };
-  auto issue_super = [&](int jj) {
+  // WIDE: the 32 key rows or value rows (or both) of a step that are this wave's are one run of their page, and so are
+  // their two scales: one look-up, one offset.  (With those for every 16 rows, 12 sequences x 28 heads of 64 columns behind 774
+  // to 7740 slots 72 us instead of 59, 8 x 8 of 128 behind 16384 to 32768 76.9 instead of 74.8, 8 x 32 heads x 60 nodes behind
+  // 2000 47.5 instead of 43.7.)
+  auto issue_run = [&]([[maybe_unused]] int jj) {
+    if constexpr (WIDE) {
+      const uint32_t slot_at = (jj & (NSS - 1)) * KW;
+      const int sis = wave * CPS / C16 >> 2;
+      const int page = min(max(next_page[0], 0), a.num_pages - 1);
+      const int row = group_slot(jj, 0) & ((1 << a.page_shift) - 1);
+      const int64_t off = (int64_t)page * a.page_stride + (int64_t)row * V::ROW;
+      const int64_t scale_off = (int64_t)page * a.scale_stride + (((int64_t)g << a.page_shift) + row) / kScaleBlock;
+      const uint32_t voff[2] = {coff[0], C16 == 2 ? coff[C16 - 1] - 1024 : coff[0]};
 #pragma unroll
-    for (int t = 0; t < NGRP; ++t) issue_group(jj, t);
+      for (int t = 0; t < CPS / (2 * C16); ++t) {
+        const int part = (wave * CPS / C16 >> 1 & 1) + t;
+        copy_run_to_lds<2 * C16>(ring_lds + (slot_at + sis) * V::SLOT + part * V::HALF, (part ? vbase : kbase) + off, voff);
+        if (lane < 2) copy_byte_to_lds(scale_base + (slot_at + sis) * 16 + part * 8, (part ? a.v_scale : a.k_scale) + scale_off, lane);
+      }
+    }
+  };
+  auto issue_super = [&](int jj) {
+    if constexpr (WIDE) {
+      issue_run(jj);
+    } else {
+#pragma unroll
+      for (int t = 0; t < NGRP; ++t) issue_group(jj, t);
+    }
     look_up(jj + 1);
   };
 
@@ -1058,7 +1099,9 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
       barrier_lds();
       if (js + NSS < nsa) issue_super(js + NSS);
       if (more) {
-        wait_vm_steps<CPT, NSS - 1>(issued_by(js + 1) - 2 - js);   // this wave's copies of super-step js+1
+        // this wave's copies of super-step js+1
+        if (E8 && js + 1 + NSS <= nsa) wait_vm<(NSS - 1) * CPT>();
+        else wait_vm_steps<CPT, NSS - 1>(issued_by(js + 1) - 2 - js);
         zero_tail(js + 1);
       }
       // super-step js+1 complete in LDS for every wave.  (Also taken after the last super-step, so that on
@@ -1080,7 +1123,9 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
       for (int sl = 0; sl < NSS; ++sl) {
         const int js = js0 + sl;
         if (js >= nsa) break;
-        wait_vm_steps<CPT, NSS - 2>(issued_by(js) - 1 - js);   // this wave's copies of super-step js have landed
+        // this wave's copies of super-step js have landed
+        if (E8 && js + NSS - 1 <= nsa) wait_vm<(NSS - 2) * CPT>();
+        else wait_vm_steps<CPT, NSS - 2>(issued_by(js) - 1 - js);
         zero_tail(js);
         barrier_lds();   // super-step js complete in LDS for every wave; the slots of super-step js-1 are free
         if (js + NSS - 1 < nsa) issue_super(js + NSS - 1);
@@ -1332,14 +1377,14 @@ __global__ __launch_bounds__(256) void spread_merge_kernel(AttnArgs a, int R) {
   if (ch == 0 && a.lse) a.lse[orow] = some ? (M + __log2f(lsum)) * kLn2 : -INFINITY;
 }
 
-template <int D, int RB, int KW, int W, int NST, int WPC, bool ENT, bool PAGED, bool E8 = false>
+template <int D, int RB, int KW, int W, int NST, int WPC, bool ENT, bool PAGED, bool E8 = false, bool WIDE = false>
 hipError_t launch_streaming(const AttnArgs& a, hipStream_t stream) {
   constexpr size_t lds = dynamic_lds<D, NST, WPC, E8>(16 * RB * (W / KW));
   static_assert(lds + 2 * kMaxNodes * 8 + 2 * kMaxNodes * 8 + (PAGED ? 2 * kMaxNodes * 4 : 8) + (E8 ? NST * 16 : 0) + 64 <=
                     160 * 1024 / WPC,
                 "LDS budget");
   // two sets of operand registers fit beside one 16-row block's state, not beside two
-  auto kern = tree_attn_bf16_kernel<D, RB, KW, W, NST, RB == 1, ENT, WPC, PAGED, E8>;
+  auto kern = tree_attn_bf16_kernel<D, RB, KW, W, NST, RB == 1, ENT, WPC, PAGED, E8, WIDE>;
   static bool configured = false;
   if (!configured) {
     hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);

@@ -926,8 +926,8 @@ def _table_pool(page_table, page_count, refcount, page_size):
 def paged_desc(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor, window: int = 0,
                sinks: int = 0, max_kv_len: int = 0, num_splits: int = 0, scale: Optional[float] = None) -> PagedDesc:
     """The description of an attention call over pages; checks the tensors' types, devices and shapes."""
-    return _paged_desc(q, k_pages, v_pages, page_table, k_pages.dtype if isinstance(k_pages, torch.Tensor) else None, window,
-                       sinks, max_kv_len, num_splits, scale)
+    return _paged_desc(q, k_pages, v_pages, page_table, getattr(k_pages, "dtype", None), window, sinks, max_kv_len, num_splits,
+                       scale)
 
 
 def _paged_desc(q, k_pages, v_pages, page_table, dt, window, sinks, max_kv_len, num_splits, scale) -> PagedDesc:
@@ -1034,7 +1034,8 @@ def paged_verify_attn(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Ten
     out of its sight, but for the first `sinks` (window 0: none is).  max_kv_len bounds kv_len for the plan (0: the table's
     width; max(1, longest) where it is known, 1 without a prefix).  A row's own slots hold finite values.  Returns (out, lse
     [B,Hq,T] float32 or None); what a call over pages allocates belongs to the stream it runs on."""
-    desc = paged_desc(q, k_pages, v_pages, page_table, window, sinks, max_kv_len, num_splits, scale)
+    desc = _paged_desc(q, k_pages, v_pages, page_table, getattr(k_pages, "dtype", None), window, sinks, max_kv_len, num_splits,
+                       scale)
     B, T, at = desc.batch, desc.num_rows, q.get_device()
     _need_on(kv_len, "kv_len", torch.int32, at, (B,))
     if parent is not None:
@@ -1058,7 +1059,8 @@ def paged_prompt_attn(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Ten
     """dreams_paged_prompt_attn: causal attention of prompt rows at positions kv_len[b] + i, whose K/V the pages hold
     already.  q [B,Hq,N,D]; row_len [B] int32 live rows (None: N each; the others give 0 and -inf); the rest as for
     paged_verify_attn.  Returns (out, lse [B,Hq,N] float32 or None)."""
-    desc = paged_desc(q, k_pages, v_pages, page_table, window, sinks, max_kv_len, num_splits, scale)
+    desc = _paged_desc(q, k_pages, v_pages, page_table, getattr(k_pages, "dtype", None), window, sinks, max_kv_len, num_splits,
+                       scale)
     B, at = desc.batch, q.get_device()
     _need_on(kv_len, "kv_len", torch.int32, at, (B,))
     if row_len is not None:
