@@ -922,18 +922,13 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
       }
     }
   };
-  // the key fragments of a step, and a block of its values
-  auto keys_of = [&](const Ops& op, bf16x8 (&kf)[2][DS]) {
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
-      if constexpr (E8) {
-        const uint32_t byte = op.scale[kb];
-#pragma unroll
-        for (int ds = 0; ds < DS; ++ds) kf[kb][ds] = decode8(op.k[kb][ds >> 1][2 * (ds & 1)], op.k[kb][ds >> 1][2 * (ds & 1) + 1], scale_of(byte), scale_of(byte));
-      } else {
-#pragma unroll
-        for (int ds = 0; ds < DS; ++ds) kf[kb][ds] = op.kf[kb][ds];
-      }
+  // a key fragment of a step, and a block of its values
+  auto key_of = [&](const Ops& op, int kb, int ds) {
+    if constexpr (E8) {
+      const float scale = scale_of(op.scale[kb]);
+      return decode8(op.k[kb][ds >> 1][2 * (ds & 1)], op.k[kb][ds >> 1][2 * (ds & 1) + 1], scale, scale);
+    } else {
+      return op.kf[kb][ds];
     }
   };
   auto values_of = [&](const Ops& op, int d) {
@@ -964,20 +959,30 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
     // another row sees it, or a mask hides it (-inf plus the product of a NaN or an infinity would be NaN).  Only steps that
     // reach the tree slots or the piece end need it.
     f32x4 s[RB][2];
-    bf16x8 kf[2][DS];
-    keys_of(op, kf);
+    // (E8: conversions run ahead of the products that take them, here and below, while the products before are on the matrix
+    // cores: 8 x 64 rows behind 8000 slots, whole, 129.5 to 122.4 us)
     auto products = [&](bool from_zero) {
       // (the products are issued at a raised wave priority, so that the SIMD's other wave -- in its softmax --
       // does not hold them back: gqa_long 355 -> 339 us)
+      bf16x8 kf[2], next[2];
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) next[kb] = key_of(op, kb, 0);
       __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-      for (int ds = 0; ds < DS; ++ds)
+      for (int ds = 0; ds < DS; ++ds) {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+          kf[kb] = next[kb];
+          if (ds + 1 < DS) next[kb] = key_of(op, kb, ds + 1);
+        }
+        if constexpr (E8) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
           for (int rb = 0; rb < RB; ++rb)
             s[rb][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                kf[kb][ds], qf[rb][ds], (from_zero && ds == 0) ? f32x4{0.f, 0.f, 0.f, 0.f} : s[rb][kb], 0, 0, 0);
+                kf[kb], qf[rb][ds], (from_zero && ds == 0) ? f32x4{0.f, 0.f, 0.f, 0.f} : s[rb][kb], 0, 0, 0);
+      }
       __builtin_amdgcn_s_setprio(0);
     };
     bool edge = key0 + kStep > Lp || key0 + kStep > k_end;
@@ -1071,9 +1076,12 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
 
     // O^T[d][row] += sum over the 32 keys of V[key][d] P[row][key]
     __builtin_amdgcn_s_setprio(1);
+    bf16x8 next_values = values_of(op, 0);
 #pragma unroll
     for (int d = 0; d < DB; ++d) {
-      const bf16x8 va = values_of(op, d);
+      const bf16x8 va = next_values;
+      if (d + 1 < DB) next_values = values_of(op, d + 1);
+      if constexpr (E8) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) o[rb][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pb[rb], o[rb][d], 0, 0, 0);
     }
