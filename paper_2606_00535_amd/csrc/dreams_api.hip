@@ -1280,7 +1280,7 @@ struct PagedPlan {
   AttnPlan p;
   int groups_per_head, unit_parts;
   int longest, shortest;   // keys of a row group, by the host's bound
-  int spread_wgs;          // see AttnArgs
+  int spread_wgs;          // see AttnArgs8
 };
 
 // Pieces of the key axis for workgroups of 128 rows, xcd_wgs on each XCD: the number that takes the least time, in keys that a
@@ -1330,7 +1330,7 @@ int pieces_e4m3(int rows, long long xcd_wgs, long long xcd_cus, int n_keys, int 
 }
 
 // Whether the keys of all sequences are spread over the workgroups in pieces of one length, with a second launch that merges
-// them (AttnArgs::spread_wgs), instead of as many pieces of every unit as merge on its die.  It costs 2 to 3 us more, 380
+// them (AttnArgs8::spread_wgs), instead of as many pieces of every unit as merge on its die.  It costs 2 to 3 us more, 380
 // keys of a compute unit, and pays where units leave dies or compute units idle (a token's rows of 4 KV heads behind 32768:
 // 18.7 us, 24.2 in 32 pieces each; 15.0 and 15.2 of 4 behind 8000), or where a batch's long sequences may run on behind its
 // short ones (16 x 4 heads behind 100 to 32768 59.5, 82.2; 3 x 7 heads behind 2952 to 29522 30.3, 32.8; of like lengths, 4
@@ -1449,10 +1449,11 @@ int paged_key_groups(const PagedPlan& plan, int cus) {
   return 2.0 * second <= 1.3 * plan.longest ? 2 : 1;
 }
 
-dreams_status_t run_paged(const dreams_paged_desc_t* desc, bool prompt, const PagedAttnArgs& in, void* workspace,
-                          size_t workspace_bytes, hipStream_t stream) {
+// (scales: of pages of 8 bits, else nullptr)
+dreams_status_t run_paged(const dreams_paged_desc_t* desc, bool prompt, const PagedAttnArgs& in, const PagedScaleArgs* scales,
+                          void* workspace, size_t workspace_bytes, hipStream_t stream) {
   PagedPlan plan;
-  const bool e4m3 = in.k_scale != nullptr;
+  const bool e4m3 = scales != nullptr;
   dreams_status_t st = plan_paged(desc, prompt, e4m3, &plan);
   if (st != DREAMS_OK) return st;
   const AttnPlan& p = plan.p;
@@ -1470,7 +1471,7 @@ dreams_status_t run_paged(const dreams_paged_desc_t* desc, bool prompt, const Pa
     if (e != hipSuccess) return hip_fail(e, "paged attention launch");
     return ok();
   }
-  AttnArgs a{};
+  AttnArgs8 a{};
   a.q = in.q;
   a.k = in.k;
   a.v = in.v;
@@ -1512,10 +1513,12 @@ dreams_status_t run_paged(const dreams_paged_desc_t* desc, bool prompt, const Pa
   st = device_cus(&a.cus);
   if (st != DREAMS_OK) return st;
   a.key_groups = paged_key_groups(plan, a.cus);
-  a.k_scale = in.k_scale;
-  a.v_scale = in.v_scale;
-  a.scale_stride = in.scale_stride;
-  a.spread_wgs = plan.spread_wgs;
+  if (e4m3) {
+    a.k_scale = scales->k;
+    a.v_scale = scales->v;
+    a.scale_stride = scales->page_stride;
+    a.spread_wgs = plan.spread_wgs;
+  }
   hipError_t e;
   if (a.rows_per_wg == 128) e = e4m3 ? launch_paged_rows_e4m3(a, stream) : launch_paged_rows_bf16(a, stream);
   else e = e4m3 ? launch_paged_attn_e4m3(a, stream) : launch_paged_attn_bf16(a, stream);
@@ -1537,16 +1540,16 @@ dreams_status_t paged_workspace(const dreams_paged_desc_t* desc, bool prompt, bo
 }
 
 // scales: of pages of 8 bits (e4m3)
-dreams_status_t set_scales(PagedAttnArgs* a, const dreams_paged_desc_t* d, const dreams_page_scales_t* scales) {
+dreams_status_t set_scales(PagedScaleArgs* a, const dreams_paged_desc_t* d, const dreams_page_scales_t* scales) {
   if (!scales) return fail(DREAMS_ERR_INVALID_ARG, "scales is NULL");
   const int64_t page = (int64_t)d->num_kv_heads * (d->page_size / kScaleBlock);
   if (scales->page_stride != 0 && (scales->page_stride < page || scales->page_stride > ((int64_t)1 << 60) / d->num_pages))
     return fail(DREAMS_ERR_INVALID_ARG, "scales->page_stride = %lld must hold a page's %lld scales",
                 (long long)scales->page_stride, (long long)page);
   if (!scales->k || !scales->v) return fail(DREAMS_ERR_INVALID_ARG, "scales->k and scales->v must not be NULL");
-  a->k_scale = scales->k;
-  a->v_scale = scales->v;
-  a->scale_stride = scales->page_stride ? scales->page_stride : page;
+  a->k = scales->k;
+  a->v = scales->v;
+  a->page_stride = scales->page_stride ? scales->page_stride : page;
   return DREAMS_OK;
 }
 
@@ -1565,11 +1568,12 @@ dreams_status_t paged_verify(const dreams_paged_desc_t* desc, bool e4m3, const v
   if (!aligned(parent, 4) || !aligned(tree_mask, 8))
     return fail(DREAMS_ERR_INVALID_ARG, "parent or tree_mask is misaligned");
   PagedAttnArgs a = paged_args(desc, q, k_pages, v_pages, page_table, kv_len, out, lse, e4m3);
-  if (e4m3) st = set_scales(&a, desc, scales);
+  PagedScaleArgs s{};
+  if (e4m3) st = set_scales(&s, desc, scales);
   if (st != DREAMS_OK) return st;
   a.parent = parent;
   a.mask = tree_mask;
-  return run_paged(desc, false, a, workspace, workspace_bytes, stream);
+  return run_paged(desc, false, a, e4m3 ? &s : nullptr, workspace, workspace_bytes, stream);
 }
 
 dreams_status_t paged_prompt(const dreams_paged_desc_t* desc, bool e4m3, const void* q, const void* k_pages,
@@ -1583,11 +1587,12 @@ dreams_status_t paged_prompt(const dreams_paged_desc_t* desc, bool e4m3, const v
   if (st != DREAMS_OK) return st;
   if (!aligned(row_len, 4)) return fail(DREAMS_ERR_INVALID_ARG, "row_len is misaligned");
   PagedAttnArgs a = paged_args(desc, q, k_pages, v_pages, page_table, kv_len, out, lse, e4m3);
-  if (e4m3) st = set_scales(&a, desc, scales);
+  PagedScaleArgs s{};
+  if (e4m3) st = set_scales(&s, desc, scales);
   if (st != DREAMS_OK) return st;
   a.row_len = row_len;
   a.prompt = 1;
-  return run_paged(desc, true, a, workspace, workspace_bytes, stream);
+  return run_paged(desc, true, a, e4m3 ? &s : nullptr, workspace, workspace_bytes, stream);
 }
 
 }  // namespace
@@ -2197,8 +2202,9 @@ dreams_status_t run_fork(const dreams_page_pool_t* pool, const dreams_page_scale
   a.NL = pool->num_layers;
   a.Hkv = pool->num_kv_heads;
   a.row_bytes = pool->head_dim * elem;
-  if (e4m3) a.scales = scale_args(scales, pool);
-  hipError_t e = launch_pages_fork(a, stream);
+  hipError_t e;
+  if (e4m3) e = launch_pages_fork_e4m3(PagesArgs8{a, scale_args(scales, pool)}, stream);
+  else e = launch_pages_fork(a, stream);
   if (e != hipSuccess) return hip_fail(e, "page fork launch");
   return ok();
 }

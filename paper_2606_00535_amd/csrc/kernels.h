@@ -115,11 +115,13 @@ struct AttnArgs {
   int groups_per_head;    // chain: row groups of a head, or 0: the heads' rows are packed one after another
   int key_groups;         // 128 rows: key groups of 4 waves in a workgroup (1 or 2)
   int unit_parts;         // parts of a unit's row groups, each on one XCD; units * unit_parts is a multiple of 8 (8 bits: any)
-  // Pages of 8 bits: a byte for every 16 slots, [pages, Hkv, page_size / 16], scale_stride bytes a page
-  const uint8_t* k_scale;
+};
+// Over pages of 8 bits (what the other kernels take stays as small as it is: 32 bytes more of arguments would be 0.15 us a call)
+struct AttnArgs8 : AttnArgs {
+  const uint8_t* k_scale;    // a byte for every 16 slots, [pages, Hkv, page_size / 16], scale_stride bytes a page
   const uint8_t* v_scale;
   int64_t scale_stride;
-  // ... and at most kSpreadSeqs sequences of one row group a unit: workgroups that all of their keys are spread over, in pieces
+  // At most kSpreadSeqs sequences of one row group a unit: workgroups that all of their keys are spread over, in pieces
   // of one length (spread_plan), whose rows a second launch merges; 0: as above
   int spread_wgs;
 };
@@ -372,9 +374,6 @@ struct PagedAttnArgs {       // fp32 (the bf16 kernels' AttnArgs have the same)
   int window, sinks;         // window 0: every key in sight
   float scale_log2;          // scale * log2(e)
   int cus;
-  const uint8_t* k_scale;    // pages of 8 bits (nullptr: they are not): see AttnArgs
-  const uint8_t* v_scale;
-  int64_t scale_stride;
 };
 constexpr int kPagedF32Threads = 1024;
 inline long long paged_attn_f32_workgroups(int units, int G, int T) {   // of a large call: 4 rows each
@@ -383,9 +382,9 @@ inline long long paged_attn_f32_workgroups(int units, int G, int T) {   // of a 
 hipError_t launch_paged_attn_f32(const PagedAttnArgs& a, hipStream_t stream);
 hipError_t launch_paged_attn_bf16(const AttnArgs& a, hipStream_t stream);   // up to 64 rows a KV head
 hipError_t launch_paged_rows_bf16(const AttnArgs& a, hipStream_t stream);   // 128 rows a workgroup
-hipError_t launch_paged_attn_e4m3(const AttnArgs& a, hipStream_t stream);   // pages of 8 bits: up to 64 rows a KV head
+hipError_t launch_paged_attn_e4m3(const AttnArgs8& a, hipStream_t stream);   // pages of 8 bits: up to 64 rows a KV head
 int paged_attn_e4m3_wgs_per_cu(int rows_per_wg);   // workgroups of that configuration per compute unit
-hipError_t launch_paged_rows_e4m3(const AttnArgs& a, hipStream_t stream);   //   128 rows a workgroup
+hipError_t launch_paged_rows_e4m3(const AttnArgs8& a, hipStream_t stream);   //   128 rows a workgroup
 
 struct PagedRowsArgs {
   char* k;                   // [NL][pages, Hkv, page_size, row bytes]
@@ -444,10 +443,13 @@ struct PagesArgs {
   char* v;
   int64_t layer_stride, page_stride;
   int NL, Hkv, row_bytes;
-  PagedScaleArgs scales;     // pages of 8 bits: theirs go with them (else nullptr)
+};
+struct PagesArgs8 : PagesArgs {
+  PagedScaleArgs scales;     // pages of 8 bits: theirs go with them
 };
 hipError_t launch_pages_reserve(const PagesArgs& a, hipStream_t stream);
 hipError_t launch_pages_fork(const PagesArgs& a, hipStream_t stream);
+hipError_t launch_pages_fork_e4m3(const PagesArgs8& a, hipStream_t stream);
 hipError_t launch_pages_release(const PagesArgs& a, hipStream_t stream);
 
 // ------------------------------------------------------------------------------- stream read (measurement)

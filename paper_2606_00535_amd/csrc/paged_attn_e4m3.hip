@@ -19,7 +19,7 @@ namespace {
 // 22.6 us instead of 22.0 for 32 heads x 60 nodes behind 3136.)
 // (64 rows of 64 columns are on the 128-row kernel.)
 template <int D, bool WIDE>
-hipError_t launch_for_rows(const AttnArgs& a, hipStream_t stream) {
+hipError_t launch_for_rows(const AttnArgs8& a, hipStream_t stream) {
   switch (a.rows_per_wg) {
     case 16: return launch_streaming<D, 1, 4, 4, 1024 / D, 2, false, true, true, WIDE>(a, stream);
     case 32: return launch_streaming<D, 1, 4, 8, 16, 1, false, true, true, WIDE>(a, stream);
@@ -29,7 +29,7 @@ hipError_t launch_for_rows(const AttnArgs& a, hipStream_t stream) {
   return hipErrorInvalidValue;
 }
 template <int D>
-hipError_t launch_for_pages(const AttnArgs& a, hipStream_t stream) {
+hipError_t launch_for_pages(const AttnArgs8& a, hipStream_t stream) {
   return 1 << a.page_shift >= kStep ? launch_for_rows<D, true>(a, stream) : launch_for_rows<D, false>(a, stream);
 }
 
@@ -37,7 +37,7 @@ hipError_t launch_for_pages(const AttnArgs& a, hipStream_t stream) {
 
 int paged_attn_e4m3_wgs_per_cu(int rows_per_wg) { return rows_per_wg == 32 ? 1 : 2; }
 
-hipError_t launch_paged_attn_e4m3(const AttnArgs& a, hipStream_t stream) {
+hipError_t launch_paged_attn_e4m3(const AttnArgs8& a, hipStream_t stream) {
   if (a.unit_parts < 1) return hipErrorInvalidValue;
   if (a.D == 128) return launch_for_pages<128>(a, stream);
   if (a.D == 64) return launch_for_pages<64>(a, stream);

@@ -92,7 +92,7 @@ struct TileRows {
 // registers while it works on this one, and writes them to the ring as bf16 (exact: the scale is a power of two): a
 // conversion for every row that the four waves read, where conversions behind the ring would be one for each wave.
 template <int D, int KG, bool TREE, bool E8 = false>
-__global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(AttnArgs a) {
+__global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(Args<E8> a) {
   using L = TileRows<D>;
   constexpr int KS = D / 16;        // products of a tile's scores
   constexpr int DB = D / 32;        // 32-column blocks of the output
@@ -190,9 +190,16 @@ __global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(At
     const uint32_t p = min(max(page, 0), a.num_pages - 1);
     return (uint64_t)p * (uint64_t)a.page_stride + (uint32_t)(slot & ps1) * (uint32_t)ROW;
   };
+  [[maybe_unused]] const uint8_t *k_scale = nullptr, *v_scale = nullptr;
+  [[maybe_unused]] int64_t scale_stride = 0;
+  if constexpr (E8) {
+    k_scale = a.k_scale;
+    v_scale = a.v_scale;
+    scale_stride = a.scale_stride;
+  }
   auto scale_offset = [&](int page, int slot) {
     const uint32_t p = min(max(page, 0), a.num_pages - 1);
-    return (uint64_t)p * (uint64_t)a.scale_stride + ((((uint64_t)g << a.page_shift) + (uint32_t)(slot & ps1)) / kScaleBlock);
+    return (uint64_t)p * (uint64_t)scale_stride + ((((uint64_t)g << a.page_shift) + (uint32_t)(slot & ps1)) / kScaleBlock);
   };
   // (lane's offset of copy 0; copy c is 1 KB on, its rows' swizzle differs by swz(first row of c))
   const uint32_t coff0 = (uint32_t)((lane / L::CPR) * L::ROW + (((lane % L::CPR) ^ L::swz(lane / L::CPR)) << 4));
@@ -213,7 +220,7 @@ __global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(At
   auto load_codes = [&](int j) {
     const uint64_t at = offset(page, key_slot(j)), scale_at = scale_offset(page, key_slot(j));
     const unsigned char* rows[2] = {kbase + at, vbase + (wave < 2 ? at : before)};
-    const uint8_t* bytes[2] = {a.k_scale + scale_at, a.v_scale + (wave < 2 ? scale_at : before_scale)};
+    const uint8_t* bytes[2] = {k_scale + scale_at, v_scale + (wave < 2 ? scale_at : before_scale)};
 #pragma unroll
     for (int part = 0; part < 2; ++part) {
       scale_bytes[part] = *bytes[part];
@@ -674,7 +681,7 @@ __global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(At
 }
 
 template <int D, int KG, bool TREE, bool E8>
-hipError_t launch_rows_build(const AttnArgs& a, hipStream_t stream) {
+hipError_t launch_rows_build(const Args<E8>& a, hipStream_t stream) {
   constexpr int lds = KG * 65536;
   static bool configured[64] = {};
   int dev = 0;
@@ -695,13 +702,13 @@ hipError_t launch_rows_build(const AttnArgs& a, hipStream_t stream) {
 }
 
 template <int D, bool E8>
-hipError_t launch_rows_of(const AttnArgs& a, hipStream_t stream) {
+hipError_t launch_rows_of(const Args<E8>& a, hipStream_t stream) {
   if (!a.chain) return a.key_groups == 2 ? launch_rows_build<D, 2, true, E8>(a, stream) : launch_rows_build<D, 1, true, E8>(a, stream);
   return a.key_groups == 2 ? launch_rows_build<D, 2, false, E8>(a, stream) : launch_rows_build<D, 1, false, E8>(a, stream);
 }
 
 template <bool E8>
-hipError_t launch_rows(const AttnArgs& a, hipStream_t stream) {
+hipError_t launch_rows(const Args<E8>& a, hipStream_t stream) {
   if (a.unit_parts < 1 || (!E8 && a.units * a.unit_parts % 8 != 0) || a.rows_per_wg != kRowsWg ||
       (a.groups_per_head > 0 && a.groups_per_head * a.G != a.row_groups))
     return hipErrorInvalidValue;

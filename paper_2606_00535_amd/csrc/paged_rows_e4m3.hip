@@ -4,6 +4,6 @@
 
 namespace dreams {
 
-hipError_t launch_paged_rows_e4m3(const AttnArgs& a, hipStream_t stream) { return launch_rows<true>(a, stream); }
+hipError_t launch_paged_rows_e4m3(const AttnArgs8& a, hipStream_t stream) { return launch_rows<true>(a, stream); }
 
 }  // namespace dreams

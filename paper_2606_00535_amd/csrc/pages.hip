@@ -18,6 +18,8 @@
 // and 147); a release does not.
 #include "kernels.h"
 
+#include <type_traits>
+
 namespace dreams {
 namespace {
 
@@ -203,7 +205,8 @@ constexpr int kCopyThreads = 256;
 constexpr int kCopyBytes = 65536;   // bytes of a page's head that a workgroup copies
 
 // A workgroup per (layer and KV head, piece of its slab, pair): the filled rows of the source's last page.
-__global__ __launch_bounds__(kCopyThreads) void fork_copy_kernel(PagesArgs a) {
+template <typename Args>
+__global__ __launch_bounds__(kCopyThreads) void fork_copy_kernel(Args a) {
   const int i = blockIdx.z;
   if (!a.granted[i]) return;
   const int from = a.src[i], to = a.dst[i];
@@ -223,7 +226,8 @@ __global__ __launch_bounds__(kCopyThreads) void fork_copy_kernel(PagesArgs a) {
     *(u32x4*)(a.k + dst + x) = k;
     *(u32x4*)(a.v + dst + x) = v;
   }
-  if (a.scales.k && blockIdx.y == 0) {   // pages of 8 bits: the blocks' scales
+  if constexpr (std::is_same_v<Args, PagesArgs8>) {   // the blocks' scales
+    if (blockIdx.y > 0) return;
     const int64_t first = layer * a.scales.layer_stride + (((int64_t)g << a.page_shift) / kScaleBlock);
     const int64_t from_s = first + (int64_t)p * a.scales.page_stride, to_s = first + (int64_t)q * a.scales.page_stride;
     for (int x = threadIdx.x; x < (tail + kScaleBlock - 1) / kScaleBlock; x += kCopyThreads) {
@@ -285,14 +289,22 @@ hipError_t launch_take(const PagesArgs& a, hipStream_t stream) {
 
 hipError_t launch_pages_reserve(const PagesArgs& a, hipStream_t stream) { return launch_take<false>(a, stream); }
 
-hipError_t launch_pages_fork(const PagesArgs& a, hipStream_t stream) {
+namespace {
+
+template <typename Args>
+hipError_t launch_fork(const Args& a, hipStream_t stream) {
   hipError_t e = launch_take<true>(a, stream);
   if (e != hipSuccess) return e;
   const int64_t slab = ((int64_t)a.row_bytes << a.page_shift);
   const dim3 grid((unsigned)(a.NL * a.Hkv), (unsigned)((slab + kCopyBytes - 1) / kCopyBytes), (unsigned)a.n);
-  hipLaunchKernelGGL(fork_copy_kernel, grid, dim3(kCopyThreads), 0, stream, a);
+  hipLaunchKernelGGL(fork_copy_kernel<Args>, grid, dim3(kCopyThreads), 0, stream, a);
   return hipGetLastError();
 }
+
+}  // namespace
+
+hipError_t launch_pages_fork(const PagesArgs& a, hipStream_t stream) { return launch_fork(a, stream); }
+hipError_t launch_pages_fork_e4m3(const PagesArgs8& a, hipStream_t stream) { return launch_fork(a, stream); }
 
 hipError_t launch_pages_release(const PagesArgs& a, hipStream_t stream) {
   hipLaunchKernelGGL(pages_release_kernel, dim3((unsigned)a.n), dim3(kReleaseThreads), 0, stream, a);

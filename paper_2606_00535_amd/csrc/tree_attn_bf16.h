@@ -72,6 +72,9 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef int i32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
+template <bool E8>
+using Args = std::conditional_t<E8, AttnArgs8, AttnArgs>;
+
 constexpr float kLn2 = 0.69314718055994530942f;
 constexpr int kStep = 32;          // keys per step
 constexpr int kSpreadMinSteps = 4; // steps of a piece of spread keys, at least
@@ -366,7 +369,7 @@ __device__ __forceinline__ int ceil_div(int x, int y, float inv) {   // x >= 1, 
   q -= r < 0 ? 1 : 0;
   return q + 1;
 }
-__device__ __forceinline__ SpreadPlan spread_plan(const AttnArgs& a, int lane) {
+__device__ __forceinline__ SpreadPlan spread_plan(const AttnArgs8& a, int lane) {
   SpreadPlan sp;
   sp.steps = 0;
   if (lane < a.B) {
@@ -415,7 +418,7 @@ constexpr size_t dynamic_lds(int R) {
 // step's 64 conversions a wave run beside its 16 RB products.
 // WIDE (E8): pages of 32 slots or more, so that a step's keys lie in one.
 template <int D, int RB, int KW, int W, int NST, bool PIPE, bool ENT, int WPC, bool PAGED, bool E8 = false, bool WIDE = false>
-__global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(AttnArgs a) {
+__global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Args<E8> a) {
   constexpr int WR = W / KW;          // waves per key group; each owns a different slice of the rows
   constexpr int RW = 16 * RB;         // query rows per wave
   constexpr int R = WR * RW;          // query rows per workgroup
@@ -458,21 +461,25 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
   int u, split, rg;
   [[maybe_unused]] int spread_pieces = 0, spread_piece = 0;   // (spread: the unit's pieces, steps of one)
   bool placed = false;
-  if constexpr (E8) placed = a.spread_wgs > 0;
-  if (placed) {
-    const SpreadPlan sp = spread_plan(a, threadIdx.x & 63);
-    int first = 0, seq = 0, pieces = 0;
-    for (; seq < a.B; ++seq) {
-      pieces = __builtin_amdgcn_readlane(sp.pieces, seq);
-      if (n < first + pieces * a.Hkv) break;
-      first += pieces * a.Hkv;
+  if constexpr (E8) {
+    placed = a.spread_wgs > 0;
+    if (placed) {
+      const SpreadPlan sp = spread_plan(a, threadIdx.x & 63);
+      int first = 0, seq = 0, pieces = 0;
+      for (; seq < a.B; ++seq) {
+        pieces = __builtin_amdgcn_readlane(sp.pieces, seq);
+        if (n < first + pieces * a.Hkv) break;
+        first += pieces * a.Hkv;
+      }
+      if (seq == a.B) return;
+      split = (n - first) / a.Hkv;      // (a piece's heads beside one another, as in the pages)
+      u = seq * a.Hkv + (n - first) - split * a.Hkv;
+      rg = 0;
+      spread_pieces = pieces;
+      spread_piece = sp.piece;
     }
-    if (seq == a.B) return;
-    split = (n - first) / a.Hkv;      // (a piece's heads beside one another, as in the pages)
-    u = seq * a.Hkv + (n - first) - split * a.Hkv;
-    rg = 0;
-    spread_pieces = pieces;
-    spread_piece = sp.piece;
+  }
+  if (placed) {
   } else if constexpr (PAGED) {
     // Every unit's row groups are dealt to unit_parts parts (units * unit_parts is a multiple of 8, or, E8, rounded up to
     // one), a part to an XCD.
@@ -1333,7 +1340,7 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Att
 // The rows of spread keys: a workgroup per row of a unit, its pieces dealt to groups of D / 8 threads (8 columns each), whose
 // sums meet in LDS in group order.
 template <int D>
-__global__ __launch_bounds__(256) void spread_merge_kernel(AttnArgs a, int R) {
+__global__ __launch_bounds__(256) void spread_merge_kernel(AttnArgs8 a, int R) {
   constexpr int LANES = D / 8, GROUPS = 256 / LANES, PCH = 4;
   typedef float f32x8 __attribute__((ext_vector_type(8)));
   __shared__ f32x8 sums[GROUPS][LANES];
@@ -1386,7 +1393,7 @@ __global__ __launch_bounds__(256) void spread_merge_kernel(AttnArgs a, int R) {
 }
 
 template <int D, int RB, int KW, int W, int NST, int WPC, bool ENT, bool PAGED, bool E8 = false, bool WIDE = false>
-hipError_t launch_streaming(const AttnArgs& a, hipStream_t stream) {
+hipError_t launch_streaming(const Args<E8>& a, hipStream_t stream) {
   constexpr size_t lds = dynamic_lds<D, NST, WPC, E8>(16 * RB * (W / KW));
   static_assert(lds + 2 * kMaxNodes * 8 + 2 * kMaxNodes * 8 + (PAGED ? 2 * kMaxNodes * 4 : 8) + (E8 ? NST * 16 : 0) + 64 <=
                     160 * 1024 / WPC,
