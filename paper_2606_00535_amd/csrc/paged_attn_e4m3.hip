@@ -2,7 +2,7 @@
 // e4m3 pages and their scales.
 //
 // Tokens of long contexts are bound by the memory (8 sequences x 8 KV heads behind 16384 to 32768 slots, 403 MB, 74.8 us with
-// the launch that merges: 5.4 TB/s; 8 x 32 heads behind 6000 each 62 us, 6.3 TB/s), those of short ones by the chain of
+// the launch that merges: 5.4 TB/s; 8 x 32 heads behind 6000 each 62 us in one piece, 6.3 TB/s), those of short ones by the chain of
 // lengths, table, first copies and merge (4 sequences with 1028 keys in sight 13.7).  64 rows are bound by instructions: a
 // step of a wave (32 rows, 32 keys) is 32 products, 64 conversions, 16 exponentials, 110 other vector and 120 scalar
 // instructions, about half of its time, a third is waits for barriers and counts (32 heads x 60 nodes behind 3136 slots
