@@ -1859,6 +1859,15 @@ dreams_status_t check_row_strides(const char* name, const int64_t* strides, int3
   return DREAMS_OK;
 }
 
+// Bytes from the first to the last element of such rows.
+int64_t row_extent(const int64_t* strides, int32_t batch, int32_t heads, int32_t rows, int32_t head_dim, int elem) {
+  const int32_t lengths[3] = {batch, heads, rows};
+  int64_t last = head_dim;
+  for (int i = 0; i < 3; ++i)
+    if (lengths[i] > 1) last += (lengths[i] - 1) * std::min<int64_t>(strides[i], ((int64_t)1 << 60) / lengths[i] / 8);
+  return last * elem;
+}
+
 dreams_status_t check_queries(const dreams_rope_queries_t* q, const dreams_page_pool_t* pool, int32_t num_rows, int elem) {
   if (!q) return DREAMS_OK;
   if (pool->num_layers != 1)
@@ -1866,11 +1875,14 @@ dreams_status_t check_queries(const dreams_rope_queries_t* q, const dreams_page_
   if (q->num_q_heads < 1) return fail(DREAMS_ERR_INVALID_ARG, "num_q_heads = %d < 1", q->num_q_heads);
   return check_row_strides("queries->strides", q->strides, pool->batch, q->num_q_heads, num_rows, elem);
 }
-dreams_status_t check_query_pointers(const dreams_rope_queries_t* q) {
+dreams_status_t check_query_pointers(const dreams_rope_queries_t* q, const dreams_page_pool_t* pool, int32_t num_rows, int elem) {
   if (!q) return DREAMS_OK;
   if (!q->q || !q->out) return fail(DREAMS_ERR_INVALID_ARG, "queries->q and queries->out must not be NULL");
   if (!aligned(q->q, 16) || !aligned(q->out, 16))
     return fail(DREAMS_ERR_INVALID_ARG, "queries->q and queries->out must be 16-byte aligned");
+  if (overlap(q->out, (size_t)pool->batch * q->num_q_heads * num_rows * pool->head_dim * elem, q->q,
+              (size_t)row_extent(q->strides, pool->batch, q->num_q_heads, num_rows, pool->head_dim, elem)))
+    return fail(DREAMS_ERR_INVALID_ARG, "queries->out must not overlap queries->q");
   return DREAMS_OK;
 }
 RopeQueryArgs query_args(const dreams_rope_queries_t* q, const dreams_page_pool_t* pool, int32_t num_rows, int elem) {
@@ -1990,6 +2002,13 @@ dreams_status_t dreams_rope(const dreams_rope_t* rope, int32_t batch, int32_t nu
     if (x == out && from[i] != to[i])
       return fail(DREAMS_ERR_INVALID_ARG, "x_strides and out_strides differ in a call in place");
   }
+  if (x != out) {      // (rows that lie between one another's may share a range, where neither side is dense)
+    const int64_t dense = (int64_t)batch * num_heads * num_rows * head_dim * elem;
+    const int64_t ex = row_extent(x_strides, batch, num_heads, num_rows, head_dim, elem);
+    const int64_t eo = row_extent(out_strides, batch, num_heads, num_rows, head_dim, elem);
+    if ((ex <= dense || eo <= dense) && overlap(out, (size_t)eo, x, (size_t)ex))
+      return fail(DREAMS_ERR_INVALID_ARG, "out must not overlap x, or be x");
+  }
   a.x_batch = from[0];
   a.x_head = from[1];
   a.x_row = from[2];
@@ -2021,7 +2040,7 @@ dreams_status_t dreams_paged_append_rope(const dreams_page_pool_t* pool, const d
   if (st == DREAMS_OK)
     st = check_units(num_rows, (queries ? queries->num_q_heads : 0) + 2LL * pool->num_kv_heads, row_units(pool->head_dim, elem));
   if (st == DREAMS_OK) st = check_append_pointers(k_new, v_new, page_table, kv_len, row_len, k_pages, v_pages);
-  if (st == DREAMS_OK) st = check_query_pointers(queries);
+  if (st == DREAMS_OK) st = check_query_pointers(queries, pool, num_rows, elem);
   if (st != DREAMS_OK) return st;
   PagedRowsArgs a = rows_args(pool, elem, k_pages, v_pages, page_table, kv_len);
   set_new_rows(&a, pool, elem, k_new, v_new, num_rows, strides, row_len);
@@ -2051,7 +2070,7 @@ dreams_status_t dreams_paged_append_e4m3(const dreams_page_pool_t* pool, const d
     st = check_units(num_rows + 32LL, (queries ? queries->num_q_heads : 0) + 2LL * pool->num_kv_heads,
                      std::max(pool->head_dim / 16, 4));
   if (st == DREAMS_OK) st = check_append_pointers(k_new, v_new, page_table, kv_len, row_len, k_pages, v_pages);
-  if (st == DREAMS_OK) st = check_query_pointers(queries);
+  if (st == DREAMS_OK) st = check_query_pointers(queries, pool, num_rows, elem);
   if (st == DREAMS_OK) st = check_scale_pointers(scales);
   if (st != DREAMS_OK) return st;
   PagedRowsArgs a = rows_args(pool, 1, k_pages, v_pages, page_table, kv_len);

@@ -46,6 +46,12 @@ def test_rope(D):
     assert call(rope(D, parent=0x100000), N=129) == -1 and b"tree nodes" in lib.dreams_last_error_message()
     assert call(rope(D), B=0) == 0 and call(rope(D), N=0) == 0
     assert call(rope(D), dt=0, dim=68) == -2 and call(rope(D), dt=0, dim=520) == -2
+    at = lambda x: ctypes.c_void_p(0x100000 + x)
+    dense = (4 * 5 * 128, 5 * 128, 128)
+    for kw in (dict(out=at(256)), dict(out=at(-256)), dict(xs=dense, out=at(2 * 4 * 5 * 128 * 2 - 16), os=dense),
+               dict(xs=(0, 0, 0), out=at(-256), os=dense), dict(xs=(4096, 512, 2048), os=dense, out=at(1024))):
+        kw = dict(dict(xs=dense, os=dense), **kw)
+        assert call(rope(D), **kw) == -1 and b"overlap" in lib.dreams_last_error_message(), kw
     # (fp32 rows have twice the units: more than 2^31 of them, fewer in bf16 -- which the null pointer then refuses)
     assert call(rope(D), N=1 << 25, dt=0, x=None, B=1) == -2 and call(rope(D), N=1 << 25, x=None, B=1) == -1
 
@@ -112,6 +118,9 @@ def test_appends(D):
         for kw in (dict(num_q_heads=0), dict(q=None), dict(out=None), dict(q=0x100002), dict(out=0x100008),
                    dict(strides=(ctypes.c_int64 * 3)(8192, 129, 1024)), dict(strides=(ctypes.c_int64 * 3)(8192, 128, -1024))):
             assert f(pool(D, num_layers=1), r=rope(D), q=queries(**kw)) == -1, kw
+        for kw in (dict(out=0x100000), dict(out=0x100000 + 2 * 8192), dict(q=0x300000 + 2 * 2 * 8 * 5 * 128 - 16)):
+            assert f(pool(D, num_layers=1), r=rope(D), q=queries(**kw)) == -1, kw
+            assert b"overlap" in lib.dreams_last_error_message()
     assert plain(pool(D, dtype=D.DREAMS_E4M3)) == -1
     assert lib.dreams_paged_append_rope(ctypes.byref(pool(D)), None, None, FAKE, FAKE, 5, st4((4096, 1024, 512, 128)), FAKE, FAKE,
                                         None, FAKE, FAKE, None) == -1
