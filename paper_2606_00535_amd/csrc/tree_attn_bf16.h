@@ -1400,11 +1400,17 @@ hipError_t launch_streaming(const Args<E8>& a, hipStream_t stream) {
                 "LDS budget");
   // two sets of operand registers fit beside one 16-row block's state, not beside two
   auto kern = tree_attn_bf16_kernel<D, RB, KW, W, NST, RB == 1, ENT, WPC, PAGED, E8, WIDE>;
-  static bool configured = false;
-  if (!configured) {
+  static bool configured[E8 ? 64 : 1] = {};
+  int dev = 0;
+  if constexpr (E8) {      // (on each device)
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return e;
+    if (dev < 0 || dev >= 64) return hipErrorInvalidDevice;
+  }
+  if (!configured[dev]) {
     hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
-    configured = true;
+    configured[dev] = true;
   }
   if (a.rows_per_wg != 16 * RB * (W / KW)) return hipErrorInvalidValue;
   if (a.splits > 1 && (!a.part_o || !a.part_ml || !a.set_ctr || (ENT && !a.part_e))) return hipErrorInvalidValue;
