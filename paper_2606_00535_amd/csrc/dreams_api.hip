@@ -1281,6 +1281,7 @@ struct PagedPlan {
   int groups_per_head, unit_parts;
   int longest, shortest;   // keys of a row group, by the host's bound
   int spread_wgs;          // see AttnArgs8
+  bool half_ring;
 };
 
 // Pieces of the key axis for workgroups of 128 rows, xcd_wgs on each XCD: the number that takes the least time, in keys that a
@@ -1307,11 +1308,17 @@ int paged_pieces(int n_keys, long long xcd_wgs, long long xcd_cus, bool level) {
   return pieces;
 }
 
-// Pieces of the key axis for 16 or 64 rows over pages of 8 bits, up to `splits`: the number that takes the least time, in keys
-// that a compute unit goes through one after another.  Two workgroups of 16 rows that run together share its copies, so
+// Whether 32 rows over pages of 8 bits take workgroups of 4 waves, two to a compute unit, instead of 8 waves: where there are more of
+// them than units, or where their pieces are long, since more pieces leave fewer units idle and even lengths out (32 heads x
+// 24 rows: 12 sequences behind 1000 slots 25.6 us, 36.5 of 8 waves; 6 x 16 heads x 29 rows of 64 columns behind 5295 24.8 and
+// 36.5).  8 waves are up to 1 us faster on short pieces (4 x 32 heads x 29 behind 20 to 205 10.7, 11.6).
+bool half_ring_pays(int n_keys, int splits, bool more_than_units) { return more_than_units || n_keys / splits >= 1000; }
+
+// Pieces of the key axis for 16, 32 or 64 rows over pages of 8 bits, up to `splits`: the number that takes the least time, in keys
+// that a compute unit goes through one after another.  Two workgroups of 16 or 32 rows that run together share its copies, so
 // that one alone is about as fast; two of 64 rows, whose time is their instructions', take 6/5 of one's.  Pieces cost the
-// time of some hundred keys for their merge; with several sequences their lengths differ, which pieces even out (a quarter
-// less).  8 x 32 heads, 16 rows: behind 1000 each 16.6 us whole, 20.9 in 2 pieces; 100 to 1000 15.9, 19.1; 3000 each 35.2, 40.6;
+// time of some hundred keys for their merge; with several sequences their lengths differ, which pieces even out (for lengths
+// from nothing on, to 1/2 + 1/2s of the longest).  8 x 32 heads, 16 rows: behind 1000 each 16.6 us whole, 20.9 in 2 pieces; 100 to 1000 15.9, 19.1; 3000 each 35.2, 40.6;
 // 100 to 3000 33.5, 30.2; 4 x 32 behind 3000 33.2, 26.0.  60 rows: 8 x 32 behind 1000 30.2, 37.1; 2500 54.1, 53.6; 100 to 1000
 // 29.8, 34.4; 4 x 32 behind 1500 38.2 whole, 33.8 in 2, 30.2 in 4.
 int pieces_e4m3(int rows, long long xcd_wgs, long long xcd_cus, int n_keys, int splits, bool several) {
@@ -1319,9 +1326,9 @@ int pieces_e4m3(int rows, long long xcd_wgs, long long xcd_cus, int n_keys, int 
   long long best = 0;
   for (int s = 1; s <= splits; ++s) {
     const long long deep = (xcd_wgs * s + xcd_cus - 1) / xcd_cus, len = (n_keys + s - 1) / s;
-    const long long keys = rows == 16 || deep == 1 ? deep * len : deep * len * 3 / 5;
-    const long long merge = rows == 16 ? 500 : 250 + 600 * deep / s;
-    const long long cost = s == 1 ? keys : (several ? keys * 3 / 4 : keys) + merge;
+    const long long keys = rows != 64 || deep == 1 ? deep * len : deep * len * 3 / 5;
+    const long long merge = rows == 16 ? 500 : rows == 32 ? 800 : 250 + 600 * deep / s;
+    const long long cost = s == 1 ? keys : (several ? keys * (s + 1) / (2 * s) : keys) + merge;
     if (s > 1 && cost >= best) continue;
     best = cost;
     pieces = s;
@@ -1397,20 +1404,26 @@ dreams_status_t plan_paged(const dreams_paged_desc_t* d, bool prompt, bool e4m3,
     int cus = 0;
     st = device_cus(&cus);
     if (st != DREAMS_OK) return st;
-    const int wpc = e4m3 && p.rows_per_wg < 128 ? paged_attn_e4m3_wgs_per_cu(p.rows_per_wg)
-                                                : tree_attn_bf16_wgs_per_cu(p.rows_per_wg);
     const long long xcd_cus = std::max(cus / 8, 1);
-    splits = coarse_splits(8 * xcd_wgs, (long long)cus * wpc, n_keys);
-    if (splits > kAttnMaxSplits) splits = kAttnMaxSplits;
-    if (p.rows_per_wg == 128) {
-      splits = paged_pieces(n_keys, xcd_wgs, xcd_cus, 10LL * plan->shortest >= 6LL * plan->longest);
-    } else if (splits > 1 && xcd_wgs < xcd_cus * wpc) {
-      const int fine = fine_splits(xcd_wgs, xcd_cus, wpc, n_keys);
-      if (fine < splits || 5 * fine >= 7 * splits) splits = fine;
+    auto pieces = [&](int wpc) {
+      if (p.rows_per_wg == 128) return paged_pieces(n_keys, xcd_wgs, xcd_cus, 10LL * plan->shortest >= 6LL * plan->longest);
+      int s = std::min(coarse_splits(8 * xcd_wgs, (long long)cus * wpc, n_keys), kAttnMaxSplits);
+      if (s > 1 && xcd_wgs < xcd_cus * wpc) {
+        const int fine = fine_splits(xcd_wgs, xcd_cus, wpc, n_keys);
+        if (fine < s || 5 * fine >= 7 * s) s = fine;
+      }
+      return s;
+    };
+    const bool tree_e4m3 = e4m3 && p.rows_per_wg < 128;
+    splits = pieces(tree_e4m3 && p.rows_per_wg != 32 ? 2 : tree_attn_bf16_wgs_per_cu(p.rows_per_wg));
+    if (tree_e4m3 && p.rows_per_wg == 32 && half_ring_pays(n_keys, std::max(splits, 1), xcd_wgs > xcd_cus)) {
+      plan->half_ring = true;
+      splits = pieces(2);
     }
-    if (e4m3 && (p.rows_per_wg == 16 || p.rows_per_wg == 64))
+    if (tree_e4m3 && (p.rows_per_wg != 32 || plan->half_ring))
       splits = pieces_e4m3(p.rows_per_wg, xcd_wgs, xcd_cus, n_keys, splits, d->batch > 1);
     if (e4m3 && spread_pays(d, p, parts, std::max(splits, 1), n_keys, cus)) {
+      plan->half_ring = false;
       plan->spread_wgs = std::max(p.rows_per_wg == 64 ? 2 * cus : cus, 2 * p.units);
       const size_t rows = (size_t)plan->spread_wgs * p.rows_per_wg;
       p.o_off = kCounterBytes;
@@ -1425,6 +1438,7 @@ dreams_status_t plan_paged(const dreams_paged_desc_t* d, bool prompt, bool e4m3,
   const long long sets = (long long)p.units * p.row_groups;
   if (2 * sets > kMaxSetCounters || splits < 1) splits = 1;
   p.splits = splits;
+  if (d->num_splits > 0) plan->half_ring = e4m3 && p.rows_per_wg == 32 && half_ring_pays(n_keys, splits, false);
   if (!fits_grid(8 * xcd_wgs * splits, 512)) return fail(DREAMS_ERR_UNSUPPORTED, "problem too large");
   if (splits > 1) {
     int stride = 16;
@@ -1518,6 +1532,7 @@ dreams_status_t run_paged(const dreams_paged_desc_t* desc, bool prompt, const Pa
     a.v_scale = scales->v;
     a.scale_stride = scales->page_stride;
     a.spread_wgs = plan.spread_wgs;
+    a.half_ring = plan.half_ring;
   }
   hipError_t e;
   if (a.rows_per_wg == 128) e = e4m3 ? launch_paged_rows_e4m3(a, stream) : launch_paged_rows_bf16(a, stream);

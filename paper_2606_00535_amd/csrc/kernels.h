@@ -124,6 +124,7 @@ struct AttnArgs8 : AttnArgs {
   // At most kSpreadSeqs sequences of one row group a unit: workgroups that all of their keys are spread over, in pieces
   // of one length (spread_plan), whose rows a second launch merges; 0: as above
   int spread_wgs;
+  int half_ring;             // 32 rows: two workgroups of 4 waves to a compute unit, not one of 8
 };
 constexpr int kSpreadSeqs = 64;
 
@@ -383,7 +384,6 @@ hipError_t launch_paged_attn_f32(const PagedAttnArgs& a, hipStream_t stream);
 hipError_t launch_paged_attn_bf16(const AttnArgs& a, hipStream_t stream);   // up to 64 rows a KV head
 hipError_t launch_paged_rows_bf16(const AttnArgs& a, hipStream_t stream);   // 128 rows a workgroup
 hipError_t launch_paged_attn_e4m3(const AttnArgs8& a, hipStream_t stream);   // pages of 8 bits: up to 64 rows a KV head
-int paged_attn_e4m3_wgs_per_cu(int rows_per_wg);   // workgroups of that configuration per compute unit
 hipError_t launch_paged_rows_e4m3(const AttnArgs8& a, hipStream_t stream);   //   128 rows a workgroup
 
 struct PagedRowsArgs {

@@ -17,12 +17,14 @@ namespace {
 // (16 rows: two workgroups of half a ring each to a compute unit: 8 x 8 KV heads of 16384 to 32768 tokens, one row of 4 heads
 // each, 85.5 us with one of a whole ring, 73.9 with two.  64 rows: 8 waves in 4 key groups, one workgroup to a unit, would be
 // 22.6 us instead of 22.0 for 32 heads x 60 nodes behind 3136.)
-// (64 rows of 64 columns are on the 128-row kernel.)
+// (32 rows: 8 waves on a whole ring, or 4 on half of one; 64 rows of 64 columns are on the 128-row kernel.)
 template <int D, bool WIDE>
 hipError_t launch_for_rows(const AttnArgs8& a, hipStream_t stream) {
   switch (a.rows_per_wg) {
     case 16: return launch_streaming<D, 1, 4, 4, 1024 / D, 2, false, true, true, WIDE>(a, stream);
-    case 32: return launch_streaming<D, 1, 4, 8, 16, 1, false, true, true, WIDE>(a, stream);
+    case 32:
+      if (a.half_ring) return launch_streaming<D, 2, 4, 4, 1024 / D, 2, false, true, true, WIDE>(a, stream);
+      return launch_streaming<D, 1, 4, 8, 16, 1, false, true, true, WIDE>(a, stream);
     case 64:
       if constexpr (D == 128) return launch_streaming<D, 2, 2, 4, 1024 / D, 2, false, true, true, WIDE>(a, stream);
   }
@@ -34,8 +36,6 @@ hipError_t launch_for_pages(const AttnArgs8& a, hipStream_t stream) {
 }
 
 }  // namespace
-
-int paged_attn_e4m3_wgs_per_cu(int rows_per_wg) { return rows_per_wg == 32 ? 1 : 2; }
 
 hipError_t launch_paged_attn_e4m3(const AttnArgs8& a, hipStream_t stream) {
   if (a.unit_parts < 1) return hipErrorInvalidValue;

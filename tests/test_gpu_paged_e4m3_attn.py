@@ -291,6 +291,35 @@ def test_units_beside_the_dies(dev, heads, D, lens, T, splits, kind):
     R.check(out, lse, want, True, (heads, D, lens, T, kind))
 
 
+@pytest.mark.parametrize("kind", ["verify", "prompt"])
+@pytest.mark.parametrize("heads,D,ps,lens,T,window,sinks,masked,splits", [
+    ((8, 2), 128, 16, [2100, 300], 6, 0, 0, False, 1), ((8, 2), 64, 64, [2100, 3], 8, 0, 0, True, 2), ((3, 3), 128, 64, [1500], 17, 0, 0, False, 1),
+    ((1, 1), 64, 16, [2500, 1100, 0], 32, 0, 0, False, 1), ((4, 1), 128, 32, [4100, 900], 7, 3000, 33, False, 1),
+    ((4, 1), 128, 16, [4100, 30], 5, 1200, 2, True, 1), ((40, 40), 128, 64, [70, 40, 0, 12, 9, 31, 64], 19, 0, 0, False, 0),
+    ((290, 290), 64, 16, [50], 30, 0, 0, True, 0)])
+def test_two_rings_to_a_compute_unit(dev, heads, D, ps, lens, T, window, sinks, masked, splits, kind):
+    """17 to 32 rows in long pieces, or of more heads than there are compute units: workgroups of 4 waves."""
+    rng = np.random.default_rng(11)
+    B, (Hq, Hkv) = len(lens), heads
+    note("rings", heads, D, ps, lens, T, window, sinks, masked, splits, kind)
+    c = E.Cache8(rng, dev, np.array(lens) + T, Hkv, ps, D)
+    q, qh = R.rounded(rng, (B, Hq, T, D), True, dev)
+    kw = dict(window=window, sinks=sinks, num_splits=splits)
+    if kind == "verify":
+        par = R.tree(rng, B, T)
+        see = R.ancestors(par)
+        if masked:
+            see &= rng.random(see.shape) < 0.5
+        mask = torch.from_numpy(R.mask_bits(see)).to(dev) if masked else None
+        want = R.verify(qh, c.k, c.v, c.table, lens, par, see, window, sinks, 1 / np.sqrt(D))
+        out, lse = dreams.paged_verify_attn_e4m3(q, *c.pages, R.ints(lens, dev), parent=R.ints(par, dev), tree_mask=mask, **kw)
+    else:
+        rows = [T if b != 1 else T // 2 for b in range(B)]
+        want = R.prompt(qh, c.k, c.v, c.table, lens, rows, window, sinks, 1 / np.sqrt(D))
+        out, lse = dreams.paged_prompt_attn_e4m3(q, *c.pages, R.ints(lens, dev), R.ints(rows, dev), **kw)
+    R.check(out, lse, want, True, (heads, D, lens, T, kind))
+
+
 def spread(q, c, **kw):
     """Whether the library spreads a call's keys in pieces of one length (its workspace has room for their rows alone)."""
     import ctypes
