@@ -1318,9 +1318,9 @@ bool half_ring_pays(int n_keys, int splits, bool more_than_units) { return more_
 // that a compute unit goes through one after another.  Two workgroups of 16 or 32 rows that run together share its copies, so
 // that one alone is about as fast; two of 64 rows, whose time is their instructions', take 6/5 of one's.  Pieces cost the
 // time of some hundred keys for their merge; with several sequences their lengths differ, which pieces even out (for lengths
-// from nothing on, to 1/2 + 1/2s of the longest).  8 x 32 heads, 16 rows: behind 1000 each 16.6 us whole, 20.9 in 2 pieces; 100 to 1000 15.9, 19.1; 3000 each 35.2, 40.6;
-// 100 to 3000 33.5, 30.2; 4 x 32 behind 3000 33.2, 26.0.  60 rows: 8 x 32 behind 1000 30.2, 37.1; 2500 54.1, 53.6; 100 to 1000
-// 29.8, 34.4; 4 x 32 behind 1500 38.2 whole, 33.8 in 2, 30.2 in 4.
+// from nothing on, to 1/2 + 1/2s of the longest).  8 x 32 heads, a token: behind 1000 each 16.2 us whole, 20.7 in 2 pieces; 100 to
+// 1000 14.8, 18.7; 3000 each 35.0, 40.1; 100 to 3000 30.1, 29.1; 4 x 32 behind 3000 29.5, 25.7, 24.0 in 4.  60 rows: 8 x 32
+// behind 1000 27.2, 36.5; 2500 46.5, 49.5; 100 to 1000 26.7, 33.9; 4 x 32 behind 1500 33.8, 32.0, 30.3 in 4.
 int pieces_e4m3(int rows, long long xcd_wgs, long long xcd_cus, int n_keys, int splits, bool several) {
   int pieces = 1;
   long long best = 0;
@@ -1337,17 +1337,18 @@ int pieces_e4m3(int rows, long long xcd_wgs, long long xcd_cus, int n_keys, int 
 }
 
 // Whether the keys of all sequences are spread over the workgroups in pieces of one length, with a second launch that merges
-// them (AttnArgs8::spread_wgs), instead of as many pieces of every unit as merge on its die.  It costs 2 to 3 us more, 380
-// keys of a compute unit, and pays where units leave dies or compute units idle (a token's rows of 4 KV heads behind 32768:
-// 18.7 us, 24.2 in 32 pieces each; 15.0 and 15.2 of 4 behind 8000), or where a batch's long sequences may run on behind its
-// short ones (16 x 4 heads behind 100 to 32768 59.5, 82.2; 3 x 7 heads behind 2952 to 29522 30.3, 32.8; of like lengths, 4
-// x 5 heads behind 32435 and 50 rows each, 54.2 and 54.8).
+// them (AttnArgs8::spread_wgs), instead of as many pieces of every unit as merge on its die.  It costs 2 to 3 us more, 380 keys
+// of a compute unit, or, where units are whole, so that nothing merges, 4 to 7 (12 x 8 heads of 64 columns behind 662 18.0 us,
+// 10.9 whole).  It pays where units leave dies or compute units idle (a token's rows of 4 KV heads behind 32768: 18.7 us, 24.2
+// in 32 pieces each; 15.0 and 15.2 of 4 behind 8000), or where a batch's long sequences may run on behind its short ones (16 x 4
+// heads behind 100 to 32768 59.5, 82.2; 3 x 7 heads behind 2952 to 29522 30.3, 32.8; of like lengths, 4 x 5 heads behind 32435
+// and 50 rows each, 54.2 and 54.8).
 bool spread_pays(const dreams_paged_desc_t* d, const AttnPlan& p, int parts, int splits, int n_keys, int cus) {
   if (p.row_groups != 1 || d->batch > kSpreadSeqs || p.units > cus / 2) return false;
   const long long even = ((long long)p.units * n_keys + cus - 1) / cus;      // keys of a compute unit, spread
   if (d->batch > 1 && even >= 4096) return true;
   const long long dies = 8 / parts, wgs = (p.units + dies - 1) / dies * splits, xcd_cus = std::max(cus / 8, 1);
-  return (wgs + xcd_cus - 1) / xcd_cus * ((n_keys + splits - 1) / splits) >= even + 380;
+  return (wgs + xcd_cus - 1) / xcd_cus * ((n_keys + splits - 1) / splits) >= even + (splits > 1 ? 380 : 1200);
 }
 
 dreams_status_t plan_paged(const dreams_paged_desc_t* d, bool prompt, bool e4m3, PagedPlan* plan) {
