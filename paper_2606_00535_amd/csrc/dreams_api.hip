@@ -1342,7 +1342,7 @@ int pieces_e4m3(int rows, long long xcd_wgs, long long xcd_cus, int n_keys, int 
 // 10.9 whole).  It pays where units leave dies or compute units idle (a token's rows of 4 KV heads behind 32768: 18.7 us, 24.2
 // in 32 pieces each; 15.0 and 15.2 of 4 behind 8000), or where a batch's long sequences may run on behind its short ones (16 x 4
 // heads behind 100 to 32768 59.5, 82.2; 3 x 7 heads behind 2952 to 29522 30.3, 32.8; of like lengths, 4 x 5 heads behind 32435
-// and 50 rows each, 54.2 and 54.8).
+// and 50 rows each, 54.2 and 54.8).  For up to 64 rows a unit: the kernel of 128 rows takes pieces alone.
 bool spread_pays(const dreams_paged_desc_t* d, const AttnPlan& p, int parts, int splits, int n_keys, int cus) {
   if (p.row_groups != 1 || d->batch > kSpreadSeqs || p.units > cus / 2) return false;
   const long long even = ((long long)p.units * n_keys + cus - 1) / cus;      // keys of a compute unit, spread
@@ -1423,7 +1423,7 @@ dreams_status_t plan_paged(const dreams_paged_desc_t* d, bool prompt, bool e4m3,
     }
     if (tree_e4m3 && (p.rows_per_wg != 32 || plan->half_ring))
       splits = pieces_e4m3(p.rows_per_wg, xcd_wgs, xcd_cus, n_keys, splits, d->batch > 1);
-    if (e4m3 && spread_pays(d, p, parts, std::max(splits, 1), n_keys, cus)) {
+    if (tree_e4m3 && spread_pays(d, p, parts, std::max(splits, 1), n_keys, cus)) {
       plan->half_ring = false;
       plan->spread_wgs = std::max(p.rows_per_wg == 64 ? 2 * cus : cus, 2 * p.units);
       const size_t rows = (size_t)plan->spread_wgs * p.rows_per_wg;

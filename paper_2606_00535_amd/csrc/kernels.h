@@ -121,8 +121,8 @@ struct AttnArgs8 : AttnArgs {
   const uint8_t* k_scale;    // a byte for every 16 slots, [pages, Hkv, page_size / 16], scale_stride bytes a page
   const uint8_t* v_scale;
   int64_t scale_stride;
-  // At most kSpreadSeqs sequences of one row group a unit: workgroups that all of their keys are spread over, in pieces
-  // of one length (spread_plan), whose rows a second launch merges; 0: as above
+  // At most kSpreadSeqs sequences of one row group a unit, up to 64 rows: workgroups that all of their keys are spread over,
+  // in pieces of one length (spread_plan), whose rows a second launch merges; 0: as above
   int spread_wgs;
   int half_ring;             // 32 rows: two workgroups of 4 waves to a compute unit, not one of 8
 };

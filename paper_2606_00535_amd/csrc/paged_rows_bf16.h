@@ -712,6 +712,9 @@ hipError_t launch_rows(const Args<E8>& a, hipStream_t stream) {
   if (a.unit_parts < 1 || (!E8 && a.units * a.unit_parts % 8 != 0) || a.rows_per_wg != kRowsWg ||
       (a.groups_per_head > 0 && a.groups_per_head * a.G != a.row_groups))
     return hipErrorInvalidValue;
+  if constexpr (E8) {
+    if (a.spread_wgs > 0) return hipErrorInvalidValue;
+  }
   if (a.splits > 1 && (!a.part_o || !a.part_ml || !a.set_ctr || a.ctr_stride < 2)) return hipErrorInvalidValue;
   if (a.D == 128) return launch_rows_of<128, E8>(a, stream);
   if (a.D == 64) return launch_rows_of<64, E8>(a, stream);
