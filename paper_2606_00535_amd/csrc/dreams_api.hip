@@ -1321,14 +1321,23 @@ bool half_ring_pays(int n_keys, int splits, bool more_than_units) { return more_
 // from nothing on, to 1/2 + 1/2s of the longest).  8 x 32 heads, a token: behind 1000 each 16.2 us whole, 20.7 in 2 pieces; 100 to
 // 1000 14.8, 18.7; 3000 each 35.0, 40.1; 100 to 3000 30.1, 29.1; 4 x 32 behind 3000 29.5, 25.7, 24.0 in 4.  60 rows: 8 x 32
 // behind 1000 27.2, 36.5; 2500 46.5, 49.5; 100 to 1000 26.7, 33.9; 4 x 32 behind 1500 33.8, 32.0, 30.3 in 4.
+// Units that fill the chip more than once (`full`) even out by themselves, nearly, and every piece costs its start and its part of
+// a merge, 0.1 us of its die: a token of 16 x 40 heads behind 500 23.2 us whole, 39.9 in 2 pieces, 53.1 in 4; 27 x 40 behind 1000 55.1,
+// 76.6, 104.9, 60 rows of them 89.0, 149.6, 187.5; 14 x 37 behind 3000 83.6, 87.7, 91.3, behind 8000 214, 196, 192.
 int pieces_e4m3(int rows, long long xcd_wgs, long long xcd_cus, int n_keys, int splits, bool several) {
+  const bool full = xcd_wgs > 2 * xcd_cus;
   int pieces = 1;
   long long best = 0;
   for (int s = 1; s <= splits; ++s) {
     const long long deep = (xcd_wgs * s + xcd_cus - 1) / xcd_cus, len = (n_keys + s - 1) / s;
     const long long keys = rows != 64 || deep == 1 ? deep * len : deep * len * 3 / 5;
-    const long long merge = rows == 16 ? 500 : rows == 32 ? 800 : 250 + 600 * deep / s;
-    const long long cost = s == 1 ? keys : (several ? keys * (s + 1) / (2 * s) : keys) + merge;
+    long long cost = keys;
+    if (s > 1) {
+      const int part = !full ? 1 : rows == 64 ? 3 : 7;     // (pieces even out 1 / (part + 1) of the time at most)
+      if (several) cost = keys * (part * s + 1) / ((part + 1) * s);
+      cost += rows == 16 ? 500 : rows == 32 ? 800 : 250 + 600 * deep / s;
+      if (full) cost += (rows == 16 ? 10 : 14) * xcd_wgs * s;
+    }
     if (s > 1 && cost >= best) continue;
     best = cost;
     pieces = s;
@@ -1342,13 +1351,17 @@ int pieces_e4m3(int rows, long long xcd_wgs, long long xcd_cus, int n_keys, int 
 // 10.9 whole).  It pays where units leave dies or compute units idle (a token's rows of 4 KV heads behind 32768: 18.7 us, 24.2
 // in 32 pieces each; 15.0 and 15.2 of 4 behind 8000), or where a batch's long sequences may run on behind its short ones (16 x 4
 // heads behind 100 to 32768 59.5, 82.2; 3 x 7 heads behind 2952 to 29522 30.3, 32.8; of like lengths, 4 x 5 heads behind 32435
-// and 50 rows each, 54.2 and 54.8).  For up to 64 rows a unit: the kernel of 128 rows takes pieces alone.
+// and 50 rows each, 54.2 and 54.8).  32 pieces of 64 rows, as many as there can be, leave a compute unit one workgroup where two
+// would run: 290 keys there (2 heads x 36 rows behind 15776 21.1 us, 27.4 in pieces; 4 x 3 x 52 behind 22211 39.1, 41.6; 3 x 3 x
+// 63 behind 13533 32.5, 30.3; 72 drawn calls 0.91 in the mean).  For up to 64 rows a unit: the kernel of 128 rows takes pieces
+// alone.
 bool spread_pays(const dreams_paged_desc_t* d, const AttnPlan& p, int parts, int splits, int n_keys, int cus) {
   if (p.row_groups != 1 || d->batch > kSpreadSeqs || p.units > cus / 2) return false;
   const long long even = ((long long)p.units * n_keys + cus - 1) / cus;      // keys of a compute unit, spread
   if (d->batch > 1 && even >= 4096) return true;
   const long long dies = 8 / parts, wgs = (p.units + dies - 1) / dies * splits, xcd_cus = std::max(cus / 8, 1);
-  return (wgs + xcd_cus - 1) / xcd_cus * ((n_keys + splits - 1) / splits) >= even + (splits > 1 ? 380 : 1200);
+  const int more = splits == 1 ? 1200 : p.rows_per_wg == 64 && splits == kAttnMaxSplits ? 290 : 380;
+  return (wgs + xcd_cus - 1) / xcd_cus * ((n_keys + splits - 1) / splits) >= even + more;
 }
 
 dreams_status_t plan_paged(const dreams_paged_desc_t* d, bool prompt, bool e4m3, PagedPlan* plan) {
@@ -1406,6 +1419,7 @@ dreams_status_t plan_paged(const dreams_paged_desc_t* d, bool prompt, bool e4m3,
     st = device_cus(&cus);
     if (st != DREAMS_OK) return st;
     const long long xcd_cus = std::max(cus / 8, 1);
+    const int most = std::min(kAttnMaxSplits, (n_keys + kPieceMinKeys - 1) / kPieceMinKeys);
     auto pieces = [&](int wpc) {
       if (p.rows_per_wg == 128) return paged_pieces(n_keys, xcd_wgs, xcd_cus, 10LL * plan->shortest >= 6LL * plan->longest);
       int s = std::min(coarse_splits(8 * xcd_wgs, (long long)cus * wpc, n_keys), kAttnMaxSplits);
@@ -1413,7 +1427,7 @@ dreams_status_t plan_paged(const dreams_paged_desc_t* d, bool prompt, bool e4m3,
         const int fine = fine_splits(xcd_wgs, xcd_cus, wpc, n_keys);
         if (fine < s || 5 * fine >= 7 * s) s = fine;
       }
-      return s;
+      return std::min(s, most);
     };
     const bool tree_e4m3 = e4m3 && p.rows_per_wg < 128;
     splits = pieces(tree_e4m3 && p.rows_per_wg != 32 ? 2 : tree_attn_bf16_wgs_per_cu(p.rows_per_wg));

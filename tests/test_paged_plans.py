@@ -68,6 +68,29 @@ def test_keys_of_128_rows_come_in_pieces(plans, batch, heads, dim, rows, longest
     assert p.workgroups >= p.units * pieces
 
 
+# batch, heads, D, rows, longest prefix, window: more (sequence, KV head)s than twice the compute units
+FULL = [(14, (37, 37), 128, 5, 16598, 260), (16, (40, 40), 128, 1, 500, 0), (16, (40, 40), 64, 5, 1000, 0), (27, (40, 40), 128, 1, 2000, 0),
+        (27, (40, 40), 128, 20, 2000, 0), (27, (40, 40), 128, 60, 2000, 0), (40, (40, 40), 128, 60, 3000, 0), (14, (74, 37), 128, 8, 1000, 0)]
+
+
+@pytest.mark.parametrize("kind", ["verify", "prompt"])
+@pytest.mark.parametrize("batch,heads,dim,rows,longest,window", FULL)
+def test_units_that_fill_the_chip_stay_whole(plans, batch, heads, dim, rows, longest, window, kind):
+    """Pieces would cost their starts and merges and gain nothing."""
+    p, = plans([call(True, kind, batch, heads, dim, rows, longest, window=window, sinks=4)])
+    assert p.status == 0 and p.units > 2 * CUS and p.rows_per_wg <= 64
+    assert p.splits == 1 and p.bytes == 0
+
+
+@pytest.mark.parametrize("batch,heads,rows,longest", [(1, (20, 4), 11, 22364), (4, (3, 1), 12, 22285), (3, (2, 1), 22, 17733), (1, (2, 2), 36, 15776)])
+def test_spread_rather_than_as_many_pieces_as_there_can_be(plans, batch, heads, rows, longest):
+    """64 rows of few heads: 32 pieces leave each compute unit one workgroup, spread keys two."""
+    p, = plans([call(True, "verify", batch, heads, 128, rows, longest)])
+    assert p.rows_per_wg == 64 and p.spread == 2 * CUS
+    forced, = plans([call(True, "verify", batch, heads, 128, rows, longest, splits=60)])
+    assert forced.spread == 0 and forced.splits == 32
+
+
 def test_plans_are_carried_out(plans):
     """Spread keys: two launches, of as many workgroups as planned, up to 64 rows a KV head.  Else one launch of every unit's
     pieces.  The workspace is the launch's."""
