@@ -630,7 +630,8 @@ dreams_status_t dreams_pages_release(const dreams_page_pool_t* pool, int32_t* pa
  * Rotary positions.  A head's first rotary_dim columns are rotary_dim / 2 pairs, of which pair i of a row at position p is
  * turned by the angle p * frequencies[i] (radians):
  *     (x, y)  becomes  (amplitude * (x cos - y sin), amplitude * (y cos + x sin))
- * The other columns stay as they are.  Angles are reduced in 64 bits, sines and products are 32-bit, the result is rounded
+ * The other columns stay as they are.  Cosines and sines, times the amplitude, are computed in 64 bits and rounded once to 32;
+ * two products and their sum in 32 bits follow (one of the products unrounded), and the result is rounded
  * once to the type of the output.
  *   rotary_dim    R, a multiple of 16, 16 .. head_dim
  *   interleaved   0: pair i is columns i and i + R/2;  1: columns 2i and 2i + 1
@@ -747,7 +748,8 @@ dreams_status_t dreams_paged_read_e4m3(const dreams_page_pool_t* pool, const dre
 /*
  * dreams_paged_verify_attn_e4m3, dreams_paged_prompt_attn_e4m3 -- dreams_paged_verify_attn and dreams_paged_prompt_attn over
  * pages of 8 bits: attention of bf16 queries over the values that the codes stand for (exact in bf16; those below its normal
- * range may be flushed), with the same arithmetic, masks, windows, and rules for slots out of sight.
+ * range may be flushed), with the same arithmetic (scores and sums in fp32, the probabilities rounded to bf16 once before the
+ * value product), masks, windows, and rules for slots out of sight.
  *   desc->dtype        type of q and out, DREAMS_BF16 (DREAMS_F32: DREAMS_ERR_UNSUPPORTED)
  *   desc->page_stride  codes (bytes) from a page to the next
  *   scales             of this layer (layer_stride is not read)

@@ -3,10 +3,12 @@
 //
 // Tokens of long contexts are bound by the memory (8 sequences x 8 KV heads behind 16384 to 32768 slots, 403 MB, 74.8 us with
 // the launch that merges: 5.4 TB/s; 8 x 32 heads behind 6000 each 62 us in one piece, 6.3 TB/s), those of short ones by the chain of
-// lengths, table, first copies and merge (4 sequences with 1028 keys in sight 13.7).  64 rows are bound by instructions: a
-// step of a wave (32 rows, 32 keys) is 32 products, 64 conversions, 16 exponentials, 110 other vector and 120 scalar
-// instructions, about half of its time, a third is waits for barriers and counts (32 heads x 60 nodes behind 3136 slots
-// 22.0 us; bf16 pages, twice the bytes: 22.3).
+// lengths, table, first copies and merge (4 sequences with 1028 keys in sight 13.7).  64 rows of contexts like 32 heads x 60 nodes
+// behind 3136 slots, 22.3 us (bf16 pages, twice the bytes: 23.2), are bound by that chain too: 12 until the first step and from
+// the last one on (11.7 behind 40 slots), 4 to 5 for the pieces' exchange and merge, 5.8 for the keys, 1.8 for each 1000.  So over the
+// whole call waves wait for counts and barriers 58 % of the time, for issue 11 %, and matrix cores work 4 %.  In the loop over
+// steps instructions are about half of the time (a wave's 32 rows and 32 keys: 32 products, 64 conversions, 16 exponentials, 110
+// other vector and 120 scalar instructions), a third waits for barriers and counts.
 // Tried there: two steps' operands in registers (24.7), reads ahead of the copies' addresses and look-ups behind the score
 // product (registers spill at 128 columns, 20.3 instead of 19.5 us at 64).
 #include "tree_attn_bf16.h"

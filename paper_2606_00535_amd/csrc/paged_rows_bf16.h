@@ -34,8 +34,8 @@
 // last value products put off to the next tile (2-3 % slower), the copies' addresses beside the products (level).
 //
 // Over pages of 8 bits (E8): as above, in bf16 from the ring on.  A wave loads the codes of its two blocks of the next stage into
-// registers, converts them (exactly) and writes them to the ring.  28 heads x 8192 rows 493 us (975 TFLOP/s), 3 to 10 % above
-// bf16 pages: the conversions and LDS writes, 88 instead of 67 M vector instructions.
+// registers, converts them (exactly) and writes them to the ring.  28 heads x 8192 rows 490 to 530 us by the device (910 to 980 TFLOP/s),
+// 3 to 10 % above bf16 pages: the conversions and LDS writes, 88 instead of 67 M vector instructions.
 #pragma once
 
 #include "tree_attn_bf16.h"
@@ -499,7 +499,7 @@ __global__ __launch_bounds__(64 * kWaves * KG, 2) void paged_rows_bf16_kernel(Ar
         sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ds], qf[ds], z, 0, 0, 0);
       }
     };
-    auto weight = [&](int i) {
+    auto weight = [&](int i) {     // (rounded to bf16 for the value product, half a step of 2^-8; summed as they are)
       e[i & 1] = __builtin_amdgcn_exp2f(fmaf(sc[i], c_scale, -m));
       sum[i & 1] = i < 2 ? e[i & 1] : sum[i & 1] + e[i & 1];
       if (i & 1) {

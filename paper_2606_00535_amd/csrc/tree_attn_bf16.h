@@ -1060,6 +1060,9 @@ __global__ __launch_bounds__(64 * W, WPC * W / 4) void tree_attn_bf16_kernel(Arg
         }
       }
     }
+    // (probabilities are rounded to bf16 for the value product, half a step of 2^-8 of each: in fp32 the product would take a
+    // second, of the remainders; their sum is of the unrounded ones.  32 heads x 60 nodes behind 3136 slots: outputs off 64-bit
+    // ones by 0.0021 of their norm, 0.0017 with fp32 probabilities, which is the outputs' own rounding)
     bf16x8 pb[RB];
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
